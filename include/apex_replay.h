@@ -55,7 +55,8 @@ typedef enum apex_status {
   APEX_ERR_EMPTY = -4,       /* sample: nothing stored                                               */
   APEX_ERR_HIP = -5,         /* a HIP call failed; see apex_last_hip_error()                         */
   APEX_ERR_TOO_LARGE = -6    /* sample: more than APEX_MAX_SAMPLES_PER_CALL samples or
-                                APEX_MAX_BATCHES_PER_CALL batches; update: m >= 2^32                 */
+                                APEX_MAX_BATCHES_PER_CALL batches; update: m >= 2^32; operators: a size above
+                                its limit                                                            */
 } apex_status;
 
 #define APEX_MAX_SAMPLES_PER_CALL 65536u
@@ -553,6 +554,118 @@ int apex_pe_sample_update(apex_pe_replay_t *r, uint32_t k, float beta, const uin
                           uint64_t *key_out, uint32_t *slot_out, float *weight_out, void *obs_out, void *act_out,
                           float *ret_out, float *gacc_out, void *hip_stream);
 int apex_pe_stats(apex_pe_replay_t *r, apex_pe_stats_t *out /*host*/, void *hip_stream);
+
+/* ----------------------------------------------------------------------------------------
+ * Operators of a recurrent draft model around the memory.
+ *
+ * Where the transitions are what a target model answered and the learner trains a small model that drafts those answers
+ * ahead of it, actors and learner need three operators beside the replay verbs: the recurrence that is the draft model's
+ * memory (apex_gated_scan; a sequence's start state and its discounts come out of the replay memory), the loss against the
+ * target's stored top logits with its gradient (apex_distill_topk: the importance weights enter it, the new priorities
+ * leave it), and the verification of what the draft proposed (apex_verify_draft).
+ *
+ * Conventions, beyond those above
+ *   - Stateless.  Arrays are device, strides are counted in elements, the last index is contiguous, and a pointer is
+ *     aligned to its element type, no further.  Outputs do not overlap inputs or one another except where said.
+ *   - Element types: apex_dtype.  Sums, maxima, states and logarithms are held in 32 bits whatever the type of the arrays,
+ *     and outputs in fewer bits are rounded once, to nearest even.
+ *   - A workspace is device memory of the caller's, of at least the size that the operator's _workspace_bytes call reports
+ *     for these or larger sizes, 256-byte aligned and filled with zeros before its first use.  Every call leaves it ready
+ *     for the next one, of the same operator and whatever sizes it is large enough for.  Calls that share a workspace must
+ *     be ordered (one stream, or events); calls that may overlap take one each.
+ *   - Results do not depend on the order in which workgroups run: the same inputs give the same bits.
+ * ---------------------------------------------------------------------------------------- */
+typedef enum apex_dtype { APEX_F32 = 0, APEX_BF16 = 1, APEX_F16 = 2 } apex_dtype;
+typedef enum apex_gate {
+  APEX_GATE_GIVEN = 0,  /* a = g, b = x                          */
+  APEX_GATE_SIGMOID = 1 /* a = sigma(g), b = (1 - sigma(g)) x    */
+} apex_gate;
+
+#define APEX_SCAN_CHUNK 64u           /* steps per stored state of apex_gated_scan's carry           */
+#define APEX_MAX_VOCABULARY 1048576u  /* V of apex_distill_topk and apex_verify_draft                */
+#define APEX_MAX_TOP 1024u            /* K of apex_distill_topk                                      */
+#define APEX_MAX_DRAFT 64u            /* G of apex_verify_draft                                      */
+
+/*
+ * A gated linear recurrence over S sequences of T steps of D independent channels.  For t in [0, len_s), per channel:
+ *     h_t = a_t * k_{t-1} h_{t-1} + b_t,     a and b from g and x by `gate`,
+ *     k_t = 1 if discount[s,t] != 0, else 0 (the episode ended on that step: nothing of its state, NaN included, passes);
+ *     k_{-1} h_{-1} = h0[s].
+ * g, x: element (s, t, d) at s * seq_stride + t * time_stride + d, of type dtype, each with strides of its own (halves of
+ * one projection, time-major arrays).  discount [S,T] as of apex_nstep_priorities (NULL: no episode ends); length [S]
+ * (NULL: T everywhere; values are taken into [0, T]).  h0 [S,D] fp32 (NULL: zeros).
+ * Outputs: h [S,T,D] of dtype, 0 for steps past a sequence's length, whose inputs are not looked at; h_last [S,D] fp32 =
+ * k_{len-1} h_{len-1}, what the sequence's next step would start from, or h0 where len = 0 (may be NULL; may be h0);
+ * carry [S, ceil(T / APEX_SCAN_CHUNK), D] fp32 (may be NULL): what passes into step t = c * APEX_SCAN_CHUNK, for those t
+ * below the length; the others are unspecified.  The gradient asks for it.
+ * With T = 1 this is the step of an actor: state in, state out.
+ * Workspace: may be NULL if the reported size is 0.
+ */
+int apex_gated_scan_workspace_bytes(uint32_t S, uint32_t T, uint32_t D, size_t *bytes /*host*/);
+int apex_gated_scan(uint32_t S, uint32_t T, uint32_t D, int dtype, int gate, const void *g, uint64_t g_seq_stride,
+                    uint64_t g_time_stride, const void *x, uint64_t x_seq_stride, uint64_t x_time_stride,
+                    const float *discount, const int32_t *length, const float *h0, void *h, float *h_last, float *carry,
+                    void *workspace, void *hip_stream);
+/*
+ * Its gradient.  dh [S,T,D] of dtype and dh_last [S,D] fp32 (NULL: zeros) are the gradients of h and h_last:
+ *     lambda_t = dh_t + k_t a_{t+1} lambda_{t+1},     lambda_{len-1} = dh_{len-1} + k_{len-1} dh_last,
+ *     da_t = lambda_t k_{t-1} h_{t-1},  db_t = lambda_t,  dh0 = a_0 lambda_0 (dh_last where len = 0).
+ * The states are computed again, in 32 bits, from `carry` as apex_gated_scan left it.  dg, dx: strided
+ * arrays of dtype whose rows do not overlap (an input broadcast by a stride of 0 has its gradient in full), 0 for steps
+ * past the length; dh0 [S,D] fp32 (may be NULL).  dg and dx may be g and x, strides included.
+ */
+int apex_gated_scan_backward(uint32_t S, uint32_t T, uint32_t D, int dtype, int gate, const void *g, uint64_t g_seq_stride,
+                             uint64_t g_time_stride, const void *x, uint64_t x_seq_stride, uint64_t x_time_stride,
+                             const float *discount, const int32_t *length, const float *carry, const void *dh,
+                             const float *dh_last, void *dg, uint64_t dg_seq_stride, uint64_t dg_time_stride, void *dx,
+                             uint64_t dx_seq_stride, uint64_t dx_time_stride, float *dh0, void *workspace, void *hip_stream);
+
+/*
+ * Distillation from a teacher's top logits, with the gradient.  For each of N rows, of logits z [V] (row i at i *
+ * row_stride, of type dtype) and a teacher's K largest logits: top_index [N,K] int32 and top_value [N,K] of value_dtype.
+ * A place whose index is not in [0, V), or stands in an earlier place of the row already, is empty: its value is not
+ * looked at.  With temperature tau > 0:
+ *     p_j = exp(z_j / tau - lse),  lse = log sum_j exp(z_j / tau);
+ *     without top_lse: q_k = the softmax of top_value / tau over the row's places, r = 0;
+ *     with top_lse [N] (the teacher's log-sum-exp of all its logits / tau): q_k = exp(top_value_k / tau - top_lse),
+ *         r = max(0, 1 - sum_k q_k): what the teacher gives to the tokens not named, taken as one class (0 if all are named);
+ *     loss = sum_k q_k (log q_k - log p_k) + r (log r - log s),  s = sum of p_j over the tokens not named;
+ *     grad_j = weight / tau * ((sum_k q_k + r) p_j - q_j - r exp(z_j / tau - lse_rest)),  the last term for j not named only,
+ *         lse_rest = the log-sum-exp of z / tau over these.
+ * weight [N] (NULL: 1) are the importance weights, divided by the batch as the caller has it; loss [N] fp32 is without
+ * them: what apex_replay_update_priorities takes.  (The customary factor tau^2 belongs into the weights.)
+ * A row that names nothing has loss 0 and gradient 0; a row of weight 0 has gradient 0 whatever it holds.  A logit of -inf
+ * has p = 0.  A row with a NaN, a logit of +inf or no finite logit has a NaN loss and, unless its weight is 0, a NaN gradient.
+ * lse [N] fp32 may be NULL.  grad (row i at i * grad_stride, of dtype) may be NULL (the loss alone), and may be logits with
+ * the same stride.
+ */
+int apex_distill_topk_workspace_bytes(uint32_t N, uint32_t V, size_t *bytes /*host*/);
+int apex_distill_topk(uint32_t N, uint32_t V, uint32_t K, int dtype, const void *logits, uint64_t row_stride,
+                      const int32_t *top_index, int value_dtype, const void *top_value, const float *top_lse,
+                      const float *weight, float temperature, float *loss, float *lse, void *grad, uint64_t grad_stride,
+                      void *workspace, void *hip_stream);
+
+/*
+ * Verification of drafted tokens.  For each of B sequences: token [B,G] int32 drafted one after the other, token i from the
+ * probabilities draft [B,G,V] (row (b, i) at b * draft_seq_stride + i * draft_row_stride), and the target's probabilities
+ * target [B,G+1,V] at the same places and the one behind them (strides likewise), both of dtype; length [B] tokens of a
+ * sequence are drafted (NULL: G; values are taken into [0, G]); rnd [B,G+1] uniform 64-bit integers.
+ * A probability x counts as the integer mass m(x) = floor(min(x, 1) * 2^40), 0 where x is not above 0 (NaN included), so
+ * that sums are exact and the outcome is the same on any machine.  In order, token i stands if
+ *     floor(rnd[b,i] * m(q_i) / 2^64) < m(p_i),   p_i = target[b,i,token_i], q_i = draft[b,i,token_i]:
+ * with probability min(1, p_i / q_i).  A token outside [0, V) does not stand.  accepted[b] = n = how many stand before the
+ * first that does not.  One token follows them, drawn from
+ *     max(0, m(target[b,n,v]) - m(draft[b,n,v]))      if n < length (from m(target[b,n,v]) if that is 0 for every v),
+ *     m(target[b,n,v])                                if n = length:
+ * the lowest v whose cumulative mass exceeds floor(rnd[b,G] * total / 2^64).  So every token is distributed as the target's.
+ * token_out [B,G+1] int32: the n tokens, the one that follows (-1 if the target's row has no mass), then -1.  accepted [B].
+ * G = 0 draws a token (draft, token and length may be NULL then).
+ */
+int apex_verify_draft_workspace_bytes(uint32_t B, uint32_t V, size_t *bytes /*host*/);
+int apex_verify_draft(uint32_t B, uint32_t G, uint32_t V, int dtype, const void *target, uint64_t target_seq_stride,
+                      uint64_t target_row_stride, const void *draft, uint64_t draft_seq_stride, uint64_t draft_row_stride,
+                      const int32_t *token, const uint64_t *rnd, const int32_t *length, int32_t *accepted,
+                      int32_t *token_out, void *workspace, void *hip_stream);
 
 /* hipError_t of the last failed HIP call of the calling thread (0 if none). */
 int apex_last_hip_error(void);

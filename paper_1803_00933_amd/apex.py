@@ -20,6 +20,9 @@ STATUS_NAMES = {0: "APEX_OK", -1: "APEX_ERR_INVALID_ARG", -2: "APEX_ERR_FULL", -
 MAX_SAMPLES_PER_CALL = 65536
 MAX_BATCHES_PER_CALL = 1024
 NOALLOC_MAX_SAMPLES = 16384
+F32, BF16, F16 = 0, 1, 2
+GATES = {"given": 0, "sigmoid": 1}
+SCAN_CHUNK, MAX_VOCABULARY, MAX_TOP, MAX_DRAFT = 64, 1 << 20, 1024, 64
 TREE_MAX_LEVELS = 8
 
 EXPORTS = ["apex_replay_workspace_bytes", "apex_replay_create", "apex_replay_destroy", "apex_replay_layout",
@@ -34,7 +37,10 @@ EXPORTS = ["apex_replay_workspace_bytes", "apex_replay_create", "apex_replay_des
            "apex_pe_sample", "apex_pe_update_priorities", "apex_pe_evict", "apex_pe_stats",
            "apex_pe_evict_enqueue", "apex_pe_add_round", "apex_pe_sample_update",
            "apex_codec_row_bytes", "apex_replay_add_payload_encoded", "apex_replay_gather_decoded",
-           "apex_pipeline_set_codec"]
+           "apex_pipeline_set_codec",
+           "apex_gated_scan_workspace_bytes", "apex_gated_scan", "apex_gated_scan_backward",
+           "apex_distill_topk_workspace_bytes", "apex_distill_topk", "apex_verify_draft_workspace_bytes",
+           "apex_verify_draft"]
 
 
 class Config(C.Structure):
@@ -135,6 +141,15 @@ lib.apex_pe_stats.argtypes = [_vp, C.POINTER(PeStats), _vp]
 lib.apex_pe_evict_enqueue.argtypes = [_vp, _u32, _vp, C.POINTER(_u64), _vp]
 lib.apex_pe_add_round.argtypes = [_vp, _u32, _u32, _u32, _u32] + [_vp] * 8
 lib.apex_pe_sample_update.argtypes = [_vp, _u32, _f32] + [_vp] * 10
+_size = C.POINTER(C.c_size_t)
+lib.apex_gated_scan_workspace_bytes.argtypes = [_u32, _u32, _u32, _size]
+lib.apex_gated_scan.argtypes = [_u32, _u32, _u32, C.c_int, C.c_int, _vp, _u64, _u64, _vp, _u64, _u64] + [_vp] * 8
+lib.apex_gated_scan_backward.argtypes = [_u32, _u32, _u32, C.c_int, C.c_int, _vp, _u64, _u64, _vp, _u64, _u64] + [_vp] * 5 + [_vp, _u64, _u64] * 2 + [_vp] * 3
+lib.apex_distill_topk_workspace_bytes.argtypes = [_u32, _u32, _size]
+lib.apex_distill_topk.argtypes = [_u32, _u32, _u32, C.c_int, _vp, _u64, _vp, C.c_int, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _u64,
+                                  _vp, _vp]
+lib.apex_verify_draft_workspace_bytes.argtypes = [_u32, _u32, _size]
+lib.apex_verify_draft.argtypes = [_u32, _u32, _u32, C.c_int, _vp, _u64, _u64, _vp, _u64, _u64] + [_vp] * 7
 for _name in EXPORTS:
     getattr(lib, _name).restype = C.c_int
 
@@ -189,6 +204,98 @@ def nstep_priorities(q_online, q_target, action, reward, discount, n, alpha, eps
     rc = _call.nstep_priorities(S, T, n, A, q_online, q_target, action, reward, discount, alpha, eps, frac_bits, max_slots,
                                 prio, ret, gacc, fx, stream)
     return rc, prio, ret, gacc, fx
+
+
+# -- operators of a recurrent draft model around the memory (see the header) -------------------------------------------
+# Each takes its outputs in `out` (a dict, as it returns) or makes them, and a workspace that the caller keeps (one per stream;
+# without one the call makes its own, at the price of an allocation and a fill).
+
+def _workspace(entry, device, *sizes):
+    n = C.c_size_t(0)
+    rc = entry(*sizes, C.byref(n))
+    if rc != OK:
+        raise ValueError("%s%r rejected: %s" % (entry.__name__, sizes, STATUS_NAMES.get(rc, rc)))
+    return torch.zeros(n.value, dtype=torch.uint8, device=device) if n.value else None
+
+
+def gated_scan_carry_shape(S, T, D):
+    return S, -(-T // SCAN_CHUNK), D
+
+
+def gated_scan_workspace(S, T, D, device="cuda:0"):
+    """Workspace of gated_scan and gated_scan_backward for these sizes, or None where they need none."""
+    return _workspace(lib.apex_gated_scan_workspace_bytes, device, S, T, D)
+
+
+def gated_scan(g, x, gate="sigmoid", discount=None, length=None, h0=None, carry=False, out=None, workspace=None, stream=None):
+    """h_t = a_t h_{t-1} + b_t over device tensors g, x [S,T,D] (any strides but the channels'), a and b by `gate`: "given"
+    or "sigmoid".  discount fp32 [S,T] (0: nothing passes on), length int32 [S], h0 fp32 [S,D].
+    Returns (rc, out): h [S,T,D], h_last fp32 [S,D], and with carry=True what gated_scan_backward needs."""
+    if out is None:
+        S, T, D = g.shape
+        out = dict(h=torch.empty((S, T, D), dtype=g.dtype, device=g.device),
+                   h_last=torch.empty((S, D), dtype=torch.float32, device=g.device))
+        if carry:
+            out["carry"] = torch.empty(gated_scan_carry_shape(S, T, D), dtype=torch.float32, device=g.device)
+    if workspace is None:
+        workspace = gated_scan_workspace(*g.shape, device=g.device)
+    get = out.get
+    return _call.gated_scan(g, x, GATES[gate], discount, length, h0, out["h"], get("h_last"), get("carry"), workspace, stream), out
+
+
+def gated_scan_backward(g, x, dh, carry, gate="sigmoid", discount=None, length=None, dh_last=None, out=None, workspace=None,
+                        stream=None):
+    """Gradients of gated_scan from dh [S,T,D] and dh_last fp32 [S,D], with the carry it left.
+    Returns (rc, out): dg and dx [S,T,D] (of any strides where `out` brings them), dh0 fp32 [S,D]."""
+    if out is None:
+        S, T, D = g.shape
+        out = dict(dg=torch.empty(g.shape, dtype=g.dtype, device=g.device), dx=torch.empty(x.shape, dtype=x.dtype, device=x.device))
+        out["dh0"] = torch.empty((S, D), dtype=torch.float32, device=g.device)
+    if workspace is None:
+        workspace = gated_scan_workspace(*g.shape, device=g.device)
+    return _call.gated_scan_backward(g, x, GATES[gate], discount, length, carry, dh, dh_last, out["dg"], out["dx"], out.get("dh0"),
+                                     workspace, stream), out
+
+
+def distill_topk_workspace(N, V, device="cuda:0"):
+    """Workspace of distill_topk for these sizes, or None where it needs none."""
+    return _workspace(lib.apex_distill_topk_workspace_bytes, device, N, V)
+
+
+def distill_topk(logits, top_index, top_value, weight=None, top_lse=None, temperature=1.0, grad=True, out=None, workspace=None,
+                 stream=None):
+    """Loss of logits [N,V] (rows of any stride) against a teacher's top logits: top_index int32 [N,K] (-1: empty place),
+    top_value [N,K], and with top_lse fp32 [N] the tokens that are not named as a class of their own.
+    Returns (rc, out): loss and lse fp32 [N] and, unless grad=False, grad [N,V], the gradient of sum(weight * loss)."""
+    if out is None:
+        N = logits.shape[0]
+        out = dict(loss=torch.empty(N, dtype=torch.float32, device=logits.device),
+                   lse=torch.empty(N, dtype=torch.float32, device=logits.device))
+        if grad:
+            out["grad"] = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    if workspace is None:
+        workspace = distill_topk_workspace(*logits.shape, device=logits.device)
+    get = out.get
+    return _call.distill_topk(logits, top_index, top_value, top_lse, weight, temperature, out["loss"], get("lse"), get("grad"),
+                              workspace, stream), out
+
+
+def verify_draft_workspace(B, V, device="cuda:0"):
+    """Workspace of verify_draft for these sizes."""
+    return _workspace(lib.apex_verify_draft_workspace_bytes, device, B, V)
+
+
+def verify_draft(target, draft, token, rnd, length=None, out=None, workspace=None, stream=None):
+    """Which of the drafted tokens int32 [B,G] stand, given the target's probabilities [B,G+1,V], the draft's [B,G,V] and
+    uniform 64-bit integers [B,G+1]; length int32 [B].
+    Returns (rc, out): accepted int32 [B], and token int32 [B,G+1]: those that stand, the one that follows, -1."""
+    B, places, V = target.shape
+    if out is None:
+        out = dict(accepted=torch.empty(B, dtype=torch.int32, device=target.device),
+                   token=torch.empty((B, places), dtype=torch.int32, device=target.device))
+    if workspace is None:
+        workspace = verify_draft_workspace(B, V, device=target.device)
+    return _call.verify_draft(target, draft, token, rnd, length, out["accepted"], out["token"], workspace, stream), out
 
 
 class Replay:

@@ -122,6 +122,78 @@ struct From<float> {
   }
 };
 
+// What a call is given does not fit it: an AssertionError, raised where the interpreter's lock is held.
+struct Refused {
+  const char *why;
+};
+
+void require(bool holds, const char *why)
+{
+  if (!holds) throw Refused{why};
+}
+
+// A tensor on the GPU as the operators take theirs: sizes, strides in elements, type.
+struct View {
+  void *p = nullptr;
+  int64_t n[3] = {0, 0, 0}, stride[3] = {0, 0, 0}, count = 0;
+  int dim = 0, dtype = -1;  // apex_dtype, or -1
+  bool contiguous = false, is_int = false, is_long = false;
+  bool fits(int64_t a, int64_t b) const { return dim == 2 && n[0] == a && n[1] == b; }
+  bool fits(int64_t a, int64_t b, int64_t c) const { return dim == 3 && n[0] == a && n[1] == b && n[2] == c; }
+  // the last index is contiguous (where there is anything to step over), the others step forward
+  bool rows() const
+  {
+    bool forward = n[dim - 1] < 2 || stride[dim - 1] == 1;
+    for (int i = 0; i + 1 < dim; ++i) forward = forward && stride[i] >= 0;
+    return forward;
+  }
+};
+template <>
+struct From<View> {
+  static View get(PyObject *o)
+  {
+    View v;
+    if (o == Py_None) return v;
+    if (!THPVariable_Check(o)) {
+      PyErr_Format(PyExc_TypeError, "a tensor is required, not %.80s", Py_TYPE(o)->tp_name);
+      throw Failed{};
+    }
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.dim() < 1 || t.dim() > 3) {
+      PyErr_SetString(PyExc_AssertionError, "device tensors of one to three dimensions only");
+      throw Failed{};
+    }
+    v.p = t.data_ptr();
+    v.dim = (int)t.dim();
+    for (int i = 0; i < v.dim; ++i) {
+      v.n[i] = t.size(i), v.stride[i] = t.stride(i);
+      if (v.n[i] > INT32_MAX) {
+        PyErr_SetString(PyExc_AssertionError, "sizes of 31 bits only");
+        throw Failed{};
+      }
+    }
+    v.count = t.numel();
+    const at::ScalarType s = t.scalar_type();
+    v.dtype = s == at::kFloat ? APEX_F32 : s == at::kBFloat16 ? APEX_BF16 : s == at::kHalf ? APEX_F16 : -1;
+    v.is_int = s == at::kInt;
+    v.is_long = s == at::kLong;
+    v.contiguous = t.is_contiguous();
+    return v;
+  }
+};
+
+// The address of a contiguous fp32 array of `count` elements, or null where there is none.
+float *floats(const View &v, int64_t count, const char *why)
+{
+  require(!v.p || (v.dtype == APEX_F32 && v.contiguous && v.count == count), why);
+  return static_cast<float *>(v.p);
+}
+int32_t *ints(const View &v, int64_t count, const char *why)
+{
+  require(!v.p || (v.is_int && v.contiguous && v.count == count), why);
+  return static_cast<int32_t *>(v.p);
+}
+
 // The last argument of the verbs that take a stream.
 struct Stream {
   void *h;
@@ -172,6 +244,8 @@ PyObject *call(R (*f)(A...), PyObject *const *args, Py_ssize_t n)
   try {
     return invoke(f, args, std::index_sequence_for<A...>{});
   } catch (const Failed &) {
+  } catch (const Refused &r) {
+    PyErr_SetString(PyExc_AssertionError, r.why);
   } catch (const std::exception &e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
   }
@@ -184,7 +258,8 @@ PyObject *call(R (*f)(A...), PyObject *const *args, Py_ssize_t n)
   X(apex_replay_add_payload_encoded) X(apex_replay_sample) X(apex_replay_sample_noalloc)                            \
   X(apex_replay_update_priorities) X(apex_replay_update_from_q) X(apex_replay_evict) X(apex_pipeline_fork)          \
   X(apex_pipeline_join) X(apex_pipeline_steps) X(apex_pipeline_add_begin) X(apex_pipeline_add_end) X(apex_pe_add)   \
-  X(apex_pe_sample) X(apex_pe_update_priorities) X(apex_pe_evict_enqueue) X(apex_pe_add_round) X(apex_pe_sample_update)
+  X(apex_pe_sample) X(apex_pe_update_priorities) X(apex_pe_evict_enqueue) X(apex_pe_add_round) X(apex_pe_sample_update) \
+  X(apex_gated_scan) X(apex_gated_scan_backward) X(apex_distill_topk) X(apex_verify_draft)
 #define X(name) decltype(&::name) p_##name = nullptr;
 APEX_ENTRIES(X)
 #undef X
@@ -281,6 +356,62 @@ VERB(pe_sample_update, [](Pe r, uint32_t k, float beta, U64 rnd, F new_prio, uin
   return p_apex_pe_sample_update(r, k, beta, rnd, new_prio, key, slot, weight, obs, act, ret, gacc, s);
 })
 
+// The two strided arrays of a scan, and the shape that everything else of it follows.
+void scan_inputs(const View &g, const View &x)
+{
+  require(g.p && x.p && g.dim == 3 && x.fits(g.n[0], g.n[1], g.n[2]) && g.dtype >= 0 && x.dtype == g.dtype,
+          "g and x: [S,T,D] of one floating type");
+  require(g.rows() && x.rows(), "g and x: contiguous channels");
+}
+
+VERB(gated_scan, [](View g, View x, int gate, View discount, View length, View h0, View h, View h_last, View carry, V workspace, Stream s) {
+  scan_inputs(g, x);
+  const int64_t S = g.n[0], T = g.n[1], D = g.n[2], chunks = (T + APEX_SCAN_CHUNK - 1) / APEX_SCAN_CHUNK;
+  require(h.p && h.fits(S, T, D) && h.contiguous && h.dtype == g.dtype, "h: [S,T,D], contiguous, of g's type");
+  return p_apex_gated_scan(S, T, D, g.dtype, gate, g.p, g.stride[0], g.stride[1], x.p, x.stride[0], x.stride[1],
+                           floats(discount, S * T, "discount: fp32 [S,T]"), ints(length, S, "length: int32 [S]"),
+                           floats(h0, S * D, "h0: fp32 [S,D]"), h.p, floats(h_last, S * D, "h_last: fp32 [S,D]"),
+                           floats(carry, S * chunks * D, "carry: fp32 [S,chunks,D]"), const_cast<void *>(workspace), s);
+})
+VERB(gated_scan_backward, [](View g, View x, int gate, View discount, View length, View carry, View dh, View dh_last, View dg, View dx,
+                             View dh0, V workspace, Stream s) {
+  scan_inputs(g, x);
+  const int64_t S = g.n[0], T = g.n[1], D = g.n[2], chunks = (T + APEX_SCAN_CHUNK - 1) / APEX_SCAN_CHUNK;
+  require(dh.p && dh.fits(S, T, D) && dh.contiguous && dh.dtype == g.dtype, "dh: [S,T,D], contiguous, of g's type");
+  const auto gradient = [&](const View &v) { return v.p && v.fits(S, T, D) && v.dtype == g.dtype && v.rows(); };
+  require(gradient(dg) && gradient(dx), "dg and dx: [S,T,D] of g's type, contiguous channels");
+  return p_apex_gated_scan_backward(S, T, D, g.dtype, gate, g.p, g.stride[0], g.stride[1], x.p, x.stride[0], x.stride[1],
+                                    floats(discount, S * T, "discount: fp32 [S,T]"), ints(length, S, "length: int32 [S]"),
+                                    floats(carry, S * chunks * D, "carry: fp32 [S,chunks,D]"), dh.p,
+                                    floats(dh_last, S * D, "dh_last: fp32 [S,D]"), dg.p, dg.stride[0], dg.stride[1], dx.p,
+                                    dx.stride[0], dx.stride[1], floats(dh0, S * D, "dh0: fp32 [S,D]"), const_cast<void *>(workspace), s);
+})
+VERB(distill_topk, [](View logits, View index, View value, View top_lse, View weight, float temperature, View loss, View lse, View grad,
+                      V workspace, Stream s) {
+  require(logits.p && logits.dim == 2 && logits.dtype >= 0 && logits.rows(), "logits: [N,V] of a floating type, contiguous rows");
+  const int64_t N = logits.n[0], vocabulary = logits.n[1];
+  require(index.p && index.dim == 2 && index.n[0] == N, "top_index: int32 [N,K]");
+  const int64_t K = index.n[1];
+  require(value.p && value.fits(N, K) && value.contiguous && value.dtype >= 0, "top_value: [N,K] of a floating type");
+  require(!grad.p || (grad.fits(N, vocabulary) && grad.dtype == logits.dtype && grad.rows()), "grad: [N,V] of the logits' type");
+  return p_apex_distill_topk(N, vocabulary, K, logits.dtype, logits.p, logits.stride[0], ints(index, N * K, "top_index: int32 [N,K]"),
+                             value.dtype, value.p, floats(top_lse, N, "top_lse: fp32 [N]"), floats(weight, N, "weight: fp32 [N]"),
+                             temperature, floats(loss, N, "loss: fp32 [N]"), floats(lse, N, "lse: fp32 [N]"), grad.p, grad.stride[0],
+                             const_cast<void *>(workspace), s);
+})
+VERB(verify_draft, [](View target, View draft, View token, View rnd, View length, View accepted, View token_out, V workspace, Stream s) {
+  require(target.p && target.dim == 3 && target.dtype >= 0 && target.rows() && target.n[1] > 0,
+          "target: [B,G+1,V] of a floating type, contiguous rows");
+  const int64_t B = target.n[0], G = target.n[1] - 1, vocabulary = target.n[2];
+  require(!G || (draft.p && draft.fits(B, G, vocabulary) && draft.dtype == target.dtype && draft.rows()),
+          "draft: [B,G,V] of the target's type, contiguous rows");
+  require(rnd.is_long && rnd.contiguous && rnd.count == B * (G + 1), "rnd: int64 [B,G+1]");
+  return p_apex_verify_draft(B, G, vocabulary, target.dtype, target.p, target.stride[0], target.stride[1], draft.p, draft.stride[0],
+                             draft.stride[1], ints(token, B * G, "token: int32 [B,G]"), static_cast<const uint64_t *>(rnd.p),
+                             ints(length, B, "length: int32 [B]"), ints(accepted, B, "accepted: int32 [B]"),
+                             ints(token_out, B * (G + 1), "token_out: int32 [B,G+1]"), const_cast<void *>(workspace), s);
+})
+
 // load(path of the library, _ptr, _plain, current device, current raw stream)
 PyObject *load(PyObject *, PyObject *args)
 {
@@ -309,6 +440,7 @@ PyMethodDef methods[] = {
     FAST(sample_noalloc), FAST(update_priorities), FAST(update_from_q), FAST(evict), FAST(pipeline_fork), FAST(pipeline_join),
     FAST(pipeline_steps), FAST(pipeline_add_begin), FAST(pipeline_add_end), FAST(pe_add), FAST(pe_sample),
     FAST(pe_update_priorities), FAST(pe_evict_enqueue), FAST(pe_add_round), FAST(pe_sample_update),
+    FAST(gated_scan), FAST(gated_scan_backward), FAST(distill_topk), FAST(verify_draft),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "apex_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,70 @@
+// Elements of 32 and 16 bits in runs that are aligned to the element only, and reductions over a wave, for the operators.
+#pragma once
+#include "wave.hpp"
+
+namespace apex {
+
+// N neighbouring elements as one load or store.  The target takes global accesses of 16 bytes at any address, so that rows
+// of odd lengths and strides need no path of their own.
+template <typename T, int N>
+struct RunOf {
+  typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
+template <typename T>
+struct RunOf<T, 1> {
+  typedef T type;
+};
+template <typename T, int N>
+using Run = typename RunOf<T, N>::type;
+
+template <typename T, int N>
+__device__ __forceinline__ Run<T, N> load_run(const T *p)
+{
+  return *reinterpret_cast<const Run<T, N> *>(p);
+}
+
+template <int N, typename T>
+__device__ __forceinline__ float element(const Run<T, N> &r, int i)
+{
+  if constexpr (N == 1)
+    return (float)r;
+  else
+    return (float)r[i];
+}
+
+// One step of a reduction with data-parallel primitives: a lane to which the control routes no value takes `none`.
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ float dpp_from(float v, float none)
+{
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp((int)__float_as_uint(none), (int)__float_as_uint(v), kCtrl, kRowMask,
+                                                               0xf, false));
+}
+
+// f over the 64 lanes in a fixed order, the same in every lane.  `none` is f's neutral element.
+template <typename F>
+__device__ __forceinline__ float wave_reduce(float v, float none, F f)
+{
+  v = f(v, dpp_from<0x111, 0xf>(v, none));  // row_shr:1, the steps of wave_inclusive_scan
+  v = f(v, dpp_from<0x112, 0xf>(v, none));
+  v = f(v, dpp_from<0x114, 0xf>(v, none));
+  v = f(v, dpp_from<0x118, 0xf>(v, none));
+  v = f(v, dpp_from<0x142, 0xa>(v, none));
+  v = f(v, dpp_from<0x143, 0xc>(v, none));
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), kWave - 1));
+}
+__device__ __forceinline__ float wave_sum(float v)
+{
+  return wave_reduce(v, 0.0f, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float wave_max(float v)
+{
+  return wave_reduce(v, -__builtin_inff(), [](float a, float b) { return fmaxf(a, b); });
+}
+
+// 2^x and log2 x as the hardware has them: within 1 ulp; results of 2^x below the normal range are 0.
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
+
+constexpr float kLog2e = 0x1.715476p+0f, kLn2 = 0x1.62e430p-1f;
+
+}  // namespace apex
