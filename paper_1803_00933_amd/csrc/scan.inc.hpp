@@ -73,6 +73,324 @@ __device__ __forceinline__ void scan_gate_back(float g, float x, float prev, flo
   }
 }
 
+// ---- tiles ----
+//
+// A tile is a stretch of steps of 16 runs of channels (16 bytes each), held in the registers of one workgroup: a thread has a
+// run of channels in kTileRows steps.  h -> A h + B composes: every thread composes its own steps, the compositions go through
+// LDS (segments of N groups of steps, then the segments), and with the state that enters the tile every thread goes through
+// its steps once more.  Reads every input once.
+//
+// A sequence longer than a tile is a chain of tiles, whose states are handed on while they run: a tile publishes its
+// composition as soon as it has it, looks back for the nearest tile whose outgoing state is there, applies the compositions
+// in between one after the other, and publishes its own.  However far it looks back, the operations on a state are the same, so
+// the bits are.  Only words of 64 bits cross between workgroups, a number and a tag in one, written and read at agent scope.
+// Tiles are taken by tickets, earlier steps first, so that whatever a tile waits for is held by a workgroup that runs, and the
+// tile with the smallest ticket waits for nobody.
+constexpr uint32_t kTileRows = 4, kTileLanes = 16, kTileMaxThreads = 1024;
+constexpr uint32_t kTileMaxSteps = kTileMaxThreads / kTileLanes * kTileRows;
+
+// Shared by all tiles of a call.  Zero before the first call; a call leaves ticket and done at 0 and has moved epoch on, so that
+// no word of an earlier call carries the tag of a later one.
+struct ScanSpace {
+  uint32_t ticket, pad0[31], done, pad1[31], epoch, pad2[63];
+  uint64_t word[1];  // [tile][3][channels of a tile]
+};
+constexpr size_t kScanSpaceHead = offsetof(ScanSpace, word);
+
+struct Chain {
+  ScanSpace *space;
+  uint32_t columns, tiles;  // of a call: `columns` pieces of channels of a sequence, `tiles` tiles each
+};
+
+__device__ __forceinline__ uint64_t tagged(float v, uint32_t tag) { return ((uint64_t)tag << 32) | __float_as_uint(v); }
+__device__ __forceinline__ void publish(uint64_t *word, uint64_t v)
+{
+  __hip_atomic_store(word, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t seen(const uint64_t *word)
+{
+  return __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+constexpr uint32_t kCutTag = 0x80000000u;  // of a composition: the state that enters does not get through
+__device__ __forceinline__ uint32_t next_tag(uint32_t epoch)  // never that of memory filled with zeros
+{
+  const uint32_t tag = (epoch + 1) & ~kCutTag;
+  return tag ? tag : 1;
+}
+constexpr uint32_t kMostPolls = 1u << 20;  // a wait gives up (and hands on NaN) where the workspace was not as required
+
+// The words of one tile: compositions A and B, state.
+struct TileWords {
+  uint64_t *a, *b, *state;
+  __device__ __forceinline__ TileWords(ScanSpace *space, uint64_t tile, uint32_t width)
+      : a(space->word + tile * 3 * width), b(a + width), state(b + width) {}
+};
+
+// The state that enters a tile from the one `behind` it, for the channel of this lane; called by a wave, whose first lane's
+// channel exists.  word_of(i): the words of the tile i places away, i < reach.
+template <typename F>
+__device__ __forceinline__ float look_back(F word_of, uint32_t channel, bool exists, uint32_t reach, uint32_t tag)
+{
+  const uint32_t lane = lane_id();
+  const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane((int)channel);
+  uint64_t there = 0;
+  uint32_t polls = 0;
+  for (;;) {
+    uint64_t w = 0;
+    if (lane < reach) w = seen(word_of(lane).state + first);
+    there = __ballot((uint32_t)(w >> 32) == tag);
+    if (there || ++polls == kMostPolls) break;
+    __builtin_amdgcn_s_sleep(1);
+  }
+  if (!there) return __builtin_nanf("");
+  const uint32_t nearest = (uint32_t)__builtin_ctzll(there);
+  if (!exists) return 0.0f;
+  uint64_t w = seen(word_of(nearest).state + channel);
+  while ((uint32_t)(w >> 32) != tag && ++polls < kMostPolls) w = seen(word_of(nearest).state + channel);
+  float state = __uint_as_float((uint32_t)w);
+  constexpr uint32_t kBatch = 2;
+  for (uint32_t i = nearest; i > 0;) {
+    uint64_t wa[kBatch], wb[kBatch];
+#pragma unroll
+    for (uint32_t j = 0; j < kBatch; ++j) {
+      const TileWords t = word_of(i > j ? i - 1 - j : 0);
+      wa[j] = seen(t.a + channel);
+      wb[j] = seen(t.b + channel);
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < kBatch; ++j) {
+      if (i == 0) break;
+      const TileWords t = word_of(i - 1);
+      while (((uint32_t)(wb[j] >> 32) != tag || ((uint32_t)(wa[j] >> 32) & ~kCutTag) != tag) && ++polls < kMostPolls)
+        wa[j] = seen(t.a + channel), wb[j] = seen(t.b + channel);
+      const float A = __uint_as_float((uint32_t)wa[j]), B = __uint_as_float((uint32_t)wb[j]);
+      state = (uint32_t)(wa[j] >> 32) & kCutTag ? B : __builtin_fmaf(A, state, B);
+      --i;
+    }
+  }
+  return polls >= kMostPolls ? __builtin_nanf("") : state;
+}
+
+// Bits of a tile's rows, in LDS.
+struct RowBits {
+  uint64_t word[kTileMaxSteps / kWave];
+  __device__ __forceinline__ uint32_t of_group(uint32_t g) const { return (uint32_t)(word[g / 16] >> (g % 16 * 4)) & 15u; }
+  template <int kGroups>
+  __device__ __forceinline__ bool all(uint32_t g) const  // of kGroups (4 or 8) groups, from a multiple of theirs on
+  {
+    const uint32_t mask = kGroups == 8 ? 0xffffffffu : 0xffffu;
+    return ((uint32_t)(word[g / 16] >> (g % 16 * 4)) & mask) == mask;
+  }
+};
+
+// Elements [d, d + N) of a row, 0 beyond D.
+template <typename T, int N>
+__device__ __forceinline__ Run<T, N> run_of(const T *row, uint32_t d, uint32_t D)
+{
+  if (d + N <= D) return load_run<T, N>(row + d);
+  Run<T, N> r;
+#pragma unroll
+  for (int e = 0; e < N; ++e) r[e] = d + e < D ? row[d + e] : (T)0.0f;
+  return r;
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_run_of(T *row, uint32_t d, uint32_t D, const Run<T, N> &r)
+{
+  if (d + N <= D) {
+    *reinterpret_cast<Run<T, N> *>(row + d) = r;
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (d + e < D) row[d + e] = r[e];
+  }
+}
+
+template <int N>
+constexpr uint32_t tile_lds(uint32_t threads)  // bytes: compositions of the groups, of the segments, states that enter segments
+{
+  return threads * N * 8 + threads * 12;
+}
+
+// kChained: tiles of a sequence wait for one another; else a sequence has one tile.
+template <typename T, int kGate, bool kChained>
+__global__ __launch_bounds__(kTileMaxThreads) void scan_tile_kernel(ScanArgs a, Chain chain)
+{
+  constexpr uint32_t N = 16 / sizeof(T), kWidth = kTileLanes * N, kSegment = N;  // channels of a tile, groups of a segment
+  extern __shared__ uint64_t lds[];
+  __shared__ RowBits into;  // whether the state passes into a row
+  __shared__ uint32_t sh_first, sh_next;  // tickets
+  const uint32_t threads = blockDim.x, thread = threadIdx.x, lane = lane_id(), wave = thread / kWave;
+  const uint32_t groups = threads / kTileLanes, segments = threads / kWidth, steps = groups * kTileRows;
+  float2 *const group_ab = reinterpret_cast<float2 *>(lds);                    // [groups][kWidth]; .x later: the state that enters
+  float2 *const segment_ab = group_ab + groups * kWidth;                       // [segments][kWidth]
+  float *const segment_in = reinterpret_cast<float *>(segment_ab + segments * kWidth);
+  const uint32_t pieces = (a.D + kWidth - 1) / kWidth;  // of a row
+  const uint32_t group = thread / kTileLanes, run = thread % kTileLanes * N;
+  const uint32_t segment = thread / kWidth, channel = thread % kWidth;  // the same threads, when they go through compositions
+  const uint32_t chunks = (a.T + APEX_SCAN_CHUNK - 1) / APEX_SCAN_CHUNK;
+  uint32_t tag = 0, ticket = blockIdx.x;
+  if (kChained) {
+    tag = next_tag(chain.space->epoch);
+    if (thread == 0) sh_first = __hip_atomic_fetch_add(&chain.space->ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    ticket = sh_first;
+  }
+  for (;;) {
+    if (kChained && ticket >= chain.columns * chain.tiles) break;
+    const uint32_t tile = kChained ? ticket / chain.columns : 0, column = kChained ? ticket % chain.columns : ticket;
+    const uint32_t s = column / pieces, d0 = column % pieces * kWidth, t0 = tile * steps;
+    const uint32_t len = scan_length(a.length, s, a.T);
+    const uint32_t t_group = t0 + group * kTileRows, d = d0 + run;
+    const bool exists = d < a.D;
+    // the rows of this thread
+    const T *const g = static_cast<const T *>(a.g) + s * a.g_seq, *const x = static_cast<const T *>(a.x) + s * a.x_seq;
+    Run<T, N> gr[kTileRows], xr[kTileRows];
+#pragma unroll
+    for (uint32_t l = 0; l < kTileRows; ++l) {
+      const uint32_t t = t_group + l;
+      if (exists && t < len) gr[l] = run_of<T, N>(g + t * a.g_time, d, a.D), xr[l] = run_of<T, N>(x + t * a.x_time, d, a.D);
+    }
+    if (thread < steps) {
+      const uint32_t t = t0 + thread;
+      const bool passes = !a.discount || t == 0 || t >= len || a.discount[(uint64_t)s * a.T + t - 1] != 0.0f;
+      const uint64_t bits = __ballot(passes);
+      if (lane == 0) into.word[wave] = bits;
+    }
+    if (kChained && thread == 0)
+      sh_next = __hip_atomic_fetch_add(&chain.space->ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    const uint32_t bits = into.of_group(group);
+    float fa[kTileRows][N], fb[kTileRows][N];
+    {
+      float A[N], B[N];
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) A[e] = 1.0f, B[e] = 0.0f;
+#pragma unroll
+      for (uint32_t l = 0; l < kTileRows; ++l) {
+        const bool inside = exists && t_group + l < len, passes = bits >> l & 1;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+          float f = 1.0f, b = 0.0f;
+          if (inside) scan_gate<kGate>(element<N, T>(gr[l], e), element<N, T>(xr[l], e), &f, &b);
+          fa[l][e] = f;
+          fb[l][e] = b;
+          A[e] = passes ? A[e] * f : 0.0f;
+          B[e] = passes ? __builtin_fmaf(f, B[e], b) : b;
+        }
+      }
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) group_ab[group * kWidth + run + e] = make_float2(A[e], B[e]);
+    }
+    __syncthreads();
+    if (segments > 1) {
+      float A = 1.0f, B = 0.0f;
+#pragma unroll
+      for (uint32_t i = 0; i < kSegment; ++i) {
+        const float2 c = group_ab[(segment * kSegment + i) * kWidth + channel];
+        const bool passes = into.of_group(segment * kSegment + i) == 15u;
+        A = passes ? A * c.x : 0.0f;
+        B = passes ? __builtin_fmaf(c.x, B, c.y) : c.y;
+      }
+      segment_ab[segment * kWidth + channel] = make_float2(A, B);
+      __syncthreads();
+    }
+    const uint32_t next = kChained ? sh_next : 0;
+    if (thread < kWidth) {
+      const bool is = d0 + channel < a.D;
+      const uint64_t at = (uint64_t)s * a.D + d0 + channel;
+      float state = 0.0f;
+      if (kChained && t0 < len && __ballot(is)) {
+        float A = 1.0f, B = 0.0f;
+        bool cut = false;
+        for (uint32_t i = 0; i < segments; ++i) {
+          const float2 c = segment_ab[i * kWidth + channel];
+          const bool passes = into.all<kSegment>(i * kSegment);
+          cut = cut || !passes;
+          A = passes ? A * c.x : 0.0f;
+          B = passes ? __builtin_fmaf(c.x, B, c.y) : c.y;
+        }
+        const auto words = [&](uint32_t behind) { return TileWords(chain.space, (uint64_t)column * chain.tiles + tile - 1 - behind, kWidth); };
+        const TileWords own(chain.space, (uint64_t)column * chain.tiles + tile, kWidth);
+        if (is && tile > 0) {
+          publish(own.a + channel, tagged(A, cut ? tag | kCutTag : tag));
+          publish(own.b + channel, tagged(B, tag));
+        }
+        if (is && cut) publish(own.state + channel, tagged(B, tag));
+        if (tile == 0)
+          state = a.h0 && is ? a.h0[at] : 0.0f;
+        else
+          state = look_back(words, channel, is, min(tile, kWave), tag);
+        if (is && !cut) publish(own.state + channel, tagged(__builtin_fmaf(A, state, B), tag));
+      } else if (!kChained && is) {
+        state = a.h0 ? a.h0[at] : 0.0f;
+      }
+      if (t0 == 0 && len == 0 && is && a.h_last) a.h_last[at] = a.h0 ? a.h0[at] : 0.0f;
+      segment_in[channel] = state;
+      for (uint32_t i = 0; i + 1 < segments; ++i) {
+        const float2 c = segment_ab[i * kWidth + channel];
+        state = into.all<kSegment>(i * kSegment) ? __builtin_fmaf(c.x, state, c.y) : c.y;
+        segment_in[(i + 1) * kWidth + channel] = state;
+      }
+    }
+    __syncthreads();
+    {
+      float state = segment_in[segment * kWidth + channel];
+#pragma unroll
+      for (uint32_t i = 0; i < kSegment; ++i) {
+        float2 *const at = group_ab + (segment * kSegment + i) * kWidth + channel;
+        const float2 c = *at;
+        at->x = state;
+        state = into.of_group(segment * kSegment + i) == 15u ? __builtin_fmaf(c.x, state, c.y) : c.y;
+      }
+    }
+    __syncthreads();
+    if (exists) {
+      float state[N];
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) state[e] = group_ab[group * kWidth + run + e].x;
+      if (a.carry && t_group % APEX_SCAN_CHUNK == 0 && t_group < len) {
+        float *const c = a.carry + ((uint64_t)s * chunks + t_group / APEX_SCAN_CHUNK) * a.D;
+        Run<float, N> r;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) r[e] = bits & 1 ? state[e] : 0.0f;
+        store_run_of<float, N>(c, d, a.D, r);
+      }
+      T *const h = static_cast<T *>(a.h) + (uint64_t)s * a.T * a.D;
+#pragma unroll
+      for (uint32_t l = 0; l < kTileRows; ++l) {
+        const uint32_t t = t_group + l;
+        const bool passes = bits >> l & 1;
+        Run<T, N> r;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+          state[e] = passes ? __builtin_fmaf(fa[l][e], state[e], fb[l][e]) : fb[l][e];
+          r[e] = t < len ? (T)state[e] : (T)0.0f;
+        }
+        if (t < a.T) store_run_of<T, N>(h + (uint64_t)t * a.D, d, a.D, r);
+        if (a.h_last && t + 1 == len) {
+          const bool on = !a.discount || a.discount[(uint64_t)s * a.T + t] != 0.0f;
+          Run<float, N> last;
+#pragma unroll
+          for (uint32_t e = 0; e < N; ++e) last[e] = on ? state[e] : 0.0f;
+          store_run_of<float, N>(a.h_last + (uint64_t)s * a.D, d, a.D, last);
+        }
+      }
+    }
+    if (!kChained) break;
+    __syncthreads();  // LDS is free
+    ticket = next;
+  }
+  if (kChained && thread == 0) {
+    // the last workgroup of the call leaves the counters as it found them
+    if (__hip_atomic_fetch_add(&chain.space->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1) {
+      __hip_atomic_store(&chain.space->ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(&chain.space->done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(&chain.space->epoch, tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  }
+}
+
 constexpr uint32_t kChannelThreads = 64;
 
 // A thread per channel, step after step.
@@ -189,6 +507,48 @@ int scan_check(uint32_t S, uint32_t T, uint32_t D, int dtype, int gate, const vo
   return APEX_OK;
 }
 
+template <typename F>
+void with_gate(int gate, F f)
+{
+  if (gate == APEX_GATE_SIGMOID)
+    f(std::integral_constant<int, APEX_GATE_SIGMOID>());
+  else
+    f(std::integral_constant<int, APEX_GATE_GIVEN>());
+}
+
+constexpr uint32_t kTileMinSteps = 16;  // shorter sequences: a thread per channel
+constexpr uint32_t kChainThreads = 512, kChainSteps = kChainThreads / kTileLanes * kTileRows;
+
+struct ScanLaunch {
+  bool by_channel;
+  uint32_t grid, threads, lds;
+  Chain chain;
+};
+
+int scan_launch(uint32_t S, uint32_t T, uint32_t D, int dtype, void *workspace, ScanLaunch *l)
+{
+  if (T < kTileMinSteps) {
+    *l = ScanLaunch{true, S * blocks_for(D, kChannelThreads), kChannelThreads, 0, {}};
+    return APEX_OK;
+  }
+  const uint32_t run = 16 / element_size(dtype), width = kTileLanes * run;
+  l->by_channel = false;
+  l->chain = Chain{static_cast<ScanSpace *>(workspace), S * blocks_for(D, width), 1};
+  if (T <= kTileMaxSteps) {
+    l->threads = (uint32_t)round_up(blocks_for(T, kTileRows) * kTileLanes, width);
+    l->grid = l->chain.columns;
+  } else {
+    if (!workspace || (uintptr_t)workspace % 256) return APEX_ERR_INVALID_ARG;
+    l->threads = kChainThreads;
+    l->chain.tiles = blocks_for(T, kChainSteps);
+    const uint64_t tiles = (uint64_t)l->chain.columns * l->chain.tiles;
+    if (tiles > 0xf0000000ull) return APEX_ERR_TOO_LARGE;
+    l->grid = (uint32_t)std::min<uint64_t>(tiles, 2 * kChipCus);
+  }
+  l->lds = run == 8 ? tile_lds<8>(l->threads) : tile_lds<4>(l->threads);
+  return APEX_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -196,7 +556,12 @@ extern "C" {
 int apex_gated_scan_workspace_bytes(uint32_t S, uint32_t T, uint32_t D, size_t *bytes)
 {
   if (!S || !T || !D || !bytes) return APEX_ERR_INVALID_ARG;
-  *bytes = 0;
+  size_t n = 0, words;
+  if (T > kTileMaxSteps &&
+      (__builtin_mul_overflow((uint64_t)S * blocks_for(T, kChainSteps), round_up(D, 128) * 3 * 8, &words) ||
+       __builtin_add_overflow(words, kScanSpaceHead, &n)))
+    return APEX_ERR_TOO_LARGE;
+  *bytes = n;
   return APEX_OK;
 }
 
@@ -209,14 +574,20 @@ int apex_gated_scan(uint32_t S, uint32_t T, uint32_t D, int dtype, int gate, con
     return rc;
   if (!h || (uintptr_t)h % element_size(dtype) || ((uintptr_t)h0 | (uintptr_t)h_last | (uintptr_t)carry) % 4) return APEX_ERR_INVALID_ARG;
   const ScanArgs a{S, T, D, g_seq_stride, g_time_stride, x_seq_stride, x_time_stride, g, x, discount, length, h0, h, h_last, carry};
-  const dim3 grid(S * ((D - 1) / kChannelThreads + 1)), block(kChannelThreads);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  ScanLaunch l;
+  if (const int rc = scan_launch(S, T, D, dtype, workspace, &l)) return rc;
   with_type(dtype, [&](auto t) {
     typedef decltype(t) E;
-    if (gate == APEX_GATE_SIGMOID)
-      scan_channel_kernel<E, APEX_GATE_SIGMOID><<<grid, block, 0, stream>>>(a);
-    else
-      scan_channel_kernel<E, APEX_GATE_GIVEN><<<grid, block, 0, stream>>>(a);
+    with_gate(gate, [&](auto gate_of) {
+      constexpr int kGate = decltype(gate_of)::value;
+      if (l.by_channel)
+        scan_channel_kernel<E, kGate><<<l.grid, l.threads, 0, stream>>>(a);
+      else if (l.chain.tiles > 1)
+        scan_tile_kernel<E, kGate, true><<<l.grid, l.threads, l.lds, stream>>>(a, l.chain);
+      else
+        scan_tile_kernel<E, kGate, false><<<l.grid, l.threads, l.lds, stream>>>(a, l.chain);
+    });
   });
   APEX_HIP(hipGetLastError());
   return APEX_OK;
