@@ -86,7 +86,7 @@ __device__ __forceinline__ void scan_gate_back(float g, float x, float prev, flo
 // the bits are.  Only words of 64 bits cross between workgroups, a number and a tag in one, written and read at agent scope.
 // Tiles are taken by tickets, earlier steps first, so that whatever a tile waits for is held by a workgroup that runs, and the
 // tile with the smallest ticket waits for nobody.
-constexpr uint32_t kTileRows = 4, kTileLanes = 16, kTileMaxThreads = 1024;
+constexpr uint32_t kTileRows = 4, kTileLanes = 16, kTileMaxThreads = 1024, kTileBackMaxThreads = 512;
 constexpr uint32_t kTileMaxSteps = kTileMaxThreads / kTileLanes * kTileRows;
 
 // Shared by all tiles of a call.  Zero before the first call; a call leaves ticket and done at 0 and has moved epoch on, so that
@@ -170,6 +170,16 @@ __device__ __forceinline__ float look_back(F word_of, uint32_t channel, bool exi
     }
   }
   return polls >= kMostPolls ? __builtin_nanf("") : state;
+}
+
+// The last workgroup of a call leaves the counters as the next one has to find them.
+__device__ __forceinline__ void leave(const Chain &chain, uint32_t tag)
+{
+  if (threadIdx.x != 0) return;
+  if (__hip_atomic_fetch_add(&chain.space->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != gridDim.x - 1) return;
+  __hip_atomic_store(&chain.space->ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(&chain.space->done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(&chain.space->epoch, tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // Bits of a tile's rows, in LDS.
@@ -381,14 +391,242 @@ __global__ __launch_bounds__(kTileMaxThreads) void scan_tile_kernel(ScanArgs a, 
     __syncthreads();  // LDS is free
     ticket = next;
   }
-  if (kChained && thread == 0) {
-    // the last workgroup of the call leaves the counters as it found them
-    if (__hip_atomic_fetch_add(&chain.space->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1) {
-      __hip_atomic_store(&chain.space->ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_store(&chain.space->done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_store(&chain.space->epoch, tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
+  if (kChained) leave(chain, tag);
+}
+
+// The gradient in tiles: the states from `carry`, which begins anew every APEX_SCAN_CHUNK steps, and lambda by a chain from the
+// last step to the first.  A row's bit says whether its state passes on; the rows of a chunk take each other's, and what enters
+// a chunk's first row has been through its bit already.
+template <int N>
+constexpr uint32_t tile_back_lds(uint32_t threads)  // both kinds of compositions of the groups, segments' compositions, what enters
+{
+  return threads * N * 16 + threads * 12;
+}
+
+template <typename T, int kGate, bool kChained>
+__global__ __launch_bounds__(kTileBackMaxThreads) void scan_tile_back_kernel(ScanBackArgs a, Chain chain)
+{
+  constexpr uint32_t N = 16 / sizeof(T), kWidth = kTileLanes * N, kSegment = N;
+  constexpr uint32_t kChunkGroups = APEX_SCAN_CHUNK / kTileRows, kChunkSegments = kChunkGroups / kSegment;
+  static_assert(APEX_SCAN_CHUNK == kWave);  // a word of RowBits is a chunk
+  extern __shared__ uint64_t lds[];
+  __shared__ RowBits on;  // whether a row's state passes on
+  __shared__ uint32_t sh_first, sh_next;
+  const uint32_t threads = blockDim.x, thread = threadIdx.x, lane = lane_id(), wave = thread / kWave;
+  const uint32_t groups = threads / kTileLanes, segments = threads / kWidth, steps = groups * kTileRows;
+  float2 *const group_ab = reinterpret_cast<float2 *>(lds);  // [groups][kWidth]; .x later: the state that enters
+  float2 *const group_pq = group_ab + groups * kWidth;       // [groups][kWidth]; .x later: the gradient that enters from behind
+  float2 *const segment_pq = group_pq + groups * kWidth;     // [segments][kWidth]
+  float *const segment_in = reinterpret_cast<float *>(segment_pq + segments * kWidth);
+  const uint32_t pieces = (a.D + kWidth - 1) / kWidth;
+  const uint32_t group = thread / kTileLanes, run = thread % kTileLanes * N;
+  const uint32_t segment = thread / kWidth, channel = thread % kWidth;
+  const uint32_t chunks = (a.T + APEX_SCAN_CHUNK - 1) / APEX_SCAN_CHUNK;
+  uint32_t tag = 0, ticket = blockIdx.x;
+  if (kChained) {
+    tag = next_tag(chain.space->epoch);
+    if (thread == 0) sh_first = __hip_atomic_fetch_add(&chain.space->ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    ticket = sh_first;
   }
+  for (;;) {
+    if (kChained && ticket >= chain.columns * chain.tiles) break;
+    const uint32_t tile = kChained ? chain.tiles - 1 - ticket / chain.columns : 0, column = kChained ? ticket % chain.columns : ticket;
+    const uint32_t s = column / pieces, d0 = column % pieces * kWidth, t0 = tile * steps;
+    const uint32_t len = scan_length(a.length, s, a.T);
+    const uint32_t t_group = t0 + group * kTileRows, d = d0 + run;
+    const bool exists = d < a.D;
+    const T *const g = static_cast<const T *>(a.g) + s * a.g_seq, *const x = static_cast<const T *>(a.x) + s * a.x_seq;
+    const T *const dh = static_cast<const T *>(a.dh) + (uint64_t)s * a.T * a.D;
+    Run<T, N> gr[kTileRows], xr[kTileRows], hr[kTileRows];
+#pragma unroll
+    for (uint32_t l = 0; l < kTileRows; ++l) {
+      const uint32_t t = t_group + l;
+      if (exists && t < len) {
+        gr[l] = run_of<T, N>(g + t * a.g_time, d, a.D);
+        xr[l] = run_of<T, N>(x + t * a.x_time, d, a.D);
+        hr[l] = run_of<T, N>(dh + (uint64_t)t * a.D, d, a.D);
+      }
+    }
+    // the state that enters the chunk of this thread's segment
+    const bool is = d0 + channel < a.D;
+    const uint32_t chunk = t0 / APEX_SCAN_CHUNK + segment / kChunkSegments;
+    float state = 0.0f;
+    if (is && chunk * APEX_SCAN_CHUNK < len) state = a.carry[((uint64_t)s * chunks + chunk) * a.D + d0 + channel];
+    if (thread < steps) {
+      const uint32_t t = t0 + thread;
+      const uint64_t bits = __ballot(!a.discount || t >= len || a.discount[(uint64_t)s * a.T + t] != 0.0f);
+      if (lane == 0) on.word[wave] = bits;
+    }
+    if (kChained && thread == 0)
+      sh_next = __hip_atomic_fetch_add(&chain.space->ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    const uint32_t bits = on.of_group(group);
+    const uint32_t into = (uint32_t)((on.word[group / kChunkGroups] << 1 | 1) >> (group % kChunkGroups * kTileRows)) & 15u;
+    {
+      float A[N], B[N], P[N], Q[N];
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) A[e] = P[e] = 1.0f, B[e] = Q[e] = 0.0f;
+      float f[kTileRows][N];
+#pragma unroll
+      for (uint32_t l = 0; l < kTileRows; ++l) {
+        const bool inside = exists && t_group + l < len, passes = into >> l & 1;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+          float b = 0.0f;
+          f[l][e] = 1.0f;
+          if (inside) scan_gate<kGate>(element<N, T>(gr[l], e), element<N, T>(xr[l], e), &f[l][e], &b);
+          A[e] = passes ? A[e] * f[l][e] : 0.0f;
+          B[e] = passes ? __builtin_fmaf(f[l][e], B[e], b) : b;
+        }
+      }
+#pragma unroll
+      for (uint32_t l = kTileRows; l-- > 0;) {
+        const bool inside = exists && t_group + l < len, passes = bits >> l & 1;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+          const float dht = inside ? element<N, T>(hr[l], e) : 0.0f;
+          P[e] = passes ? P[e] * f[l][e] : 0.0f;
+          Q[e] = f[l][e] * (passes ? Q[e] + dht : dht);
+        }
+      }
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) {
+        group_ab[group * kWidth + run + e] = make_float2(A[e], B[e]);
+        group_pq[group * kWidth + run + e] = make_float2(P[e], Q[e]);
+      }
+    }
+    __syncthreads();
+    // the states that enter the groups of a segment, from the chunk's; the segment's composition, from its last group
+    float states[kSegment];
+    {
+      const uint32_t first = segment / kChunkSegments * kChunkGroups;
+      const uint64_t chunk_bits = on.word[first / kChunkGroups] << 1 | 1;
+      const auto through = [&](uint32_t i) {
+        const float2 c = group_ab[i * kWidth + channel];
+        state = ((uint32_t)(chunk_bits >> (i - first) * kTileRows) & 15u) == 15u ? __builtin_fmaf(c.x, state, c.y) : c.y;
+      };
+      for (uint32_t i = first; i < segment * kSegment; ++i) through(i);
+#pragma unroll
+      for (uint32_t i = 0; i < kSegment; ++i) {
+        states[i] = state;
+        through(segment * kSegment + i);
+      }
+      float P = 1.0f, Q = 0.0f;
+#pragma unroll
+      for (uint32_t i = kSegment; i-- > 0;) {
+        const float2 c = group_pq[(segment * kSegment + i) * kWidth + channel];
+        const bool passes = on.of_group(segment * kSegment + i) == 15u;
+        P = passes ? P * c.x : 0.0f;
+        Q = passes ? __builtin_fmaf(c.x, Q, c.y) : c.y;
+      }
+      segment_pq[segment * kWidth + channel] = make_float2(P, Q);
+    }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t i = 0; i < kSegment; ++i) group_ab[(segment * kSegment + i) * kWidth + channel].x = states[i];
+    const uint32_t next = kChained ? sh_next : 0;
+    if (thread < kWidth) {
+      const uint64_t at = (uint64_t)s * a.D + d0 + channel;
+      const uint32_t last = len ? (len - 1) / steps : 0;
+      float back = 0.0f;  // what enters the tile from behind
+      if (is && a.dh_last && tile == last) back = a.dh_last[at];
+      if (len == 0 && tile == 0 && is && a.dh0) a.dh0[at] = back;
+      if (kChained && t0 < len && __ballot(is)) {
+        float P = 1.0f, Q = 0.0f;
+        bool cut = false;
+        for (uint32_t i = segments; i-- > 0;) {
+          const float2 c = segment_pq[i * kWidth + channel];
+          const bool passes = on.all<kSegment>(i * kSegment);
+          cut = cut || !passes;
+          P = passes ? P * c.x : 0.0f;
+          Q = passes ? __builtin_fmaf(c.x, Q, c.y) : c.y;
+        }
+        const auto words = [&](uint32_t behind) { return TileWords(chain.space, (uint64_t)column * chain.tiles + tile + 1 + behind, kWidth); };
+        const TileWords own(chain.space, (uint64_t)column * chain.tiles + tile, kWidth);
+        if (is && tile < last) {
+          publish(own.a + channel, tagged(P, cut ? tag | kCutTag : tag));
+          publish(own.b + channel, tagged(Q, tag));
+        }
+        if (is && cut) publish(own.state + channel, tagged(Q, tag));
+        if (tile < last) back = look_back(words, channel, is, min(last - tile, kWave), tag);
+        if (is && !cut) publish(own.state + channel, tagged(__builtin_fmaf(P, back, Q), tag));
+      }
+      for (uint32_t i = segments; i-- > 0;) {
+        segment_in[i * kWidth + channel] = back;
+        const float2 c = segment_pq[i * kWidth + channel];
+        back = on.all<kSegment>(i * kSegment) ? __builtin_fmaf(c.x, back, c.y) : c.y;
+      }
+    }
+    __syncthreads();
+    {
+      float back = segment_in[segment * kWidth + channel];
+#pragma unroll
+      for (uint32_t i = kSegment; i-- > 0;) {
+        float2 *const at = group_pq + (segment * kSegment + i) * kWidth + channel;
+        const float2 c = *at;
+        at->x = back;
+        back = on.of_group(segment * kSegment + i) == 15u ? __builtin_fmaf(c.x, back, c.y) : c.y;
+      }
+    }
+    __syncthreads();
+    if (exists) {
+      float prev[kTileRows][N], back[N];
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) {
+        prev[0][e] = group_ab[group * kWidth + run + e].x;
+        back[e] = group_pq[group * kWidth + run + e].x;
+      }
+#pragma unroll
+      for (uint32_t l = 0; l < kTileRows; ++l) {
+        const bool inside = t_group + l < len, passes = into >> l & 1;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+          if (!passes) prev[l][e] = 0.0f;
+          if (l + 1 < kTileRows) {
+            float f = 1.0f, b = 0.0f;
+            if (inside) scan_gate<kGate>(element<N, T>(gr[l], e), element<N, T>(xr[l], e), &f, &b);
+            prev[(l + 1) % kTileRows][e] = __builtin_fmaf(f, prev[l][e], b);
+          }
+        }
+      }
+      T *const dg = static_cast<T *>(a.dg) + s * a.dg_seq, *const dx = static_cast<T *>(a.dx) + s * a.dx_seq;
+#pragma unroll
+      for (uint32_t l = kTileRows; l-- > 0;) {
+        const uint32_t t = t_group + l;
+        const bool inside = t < len, passes = bits >> l & 1;
+        Run<T, N> dgr, dxr;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+          float dgt = 0.0f, dxt = 0.0f;
+          if (inside) {
+            const float gt = element<N, T>(gr[l], e), xt = element<N, T>(xr[l], e);
+            float f, b;
+            scan_gate<kGate>(gt, xt, &f, &b);
+            const float lambda = element<N, T>(hr[l], e) + (passes ? back[e] : 0.0f);
+            scan_gate_back<kGate>(gt, xt, prev[l][e], lambda, &dgt, &dxt);
+            back[e] = f * lambda;
+          }
+          dgr[e] = (T)dgt;
+          dxr[e] = (T)dxt;
+        }
+        if (t < a.T) {
+          store_run_of<T, N>(dg + t * a.dg_time, d, a.D, dgr);
+          store_run_of<T, N>(dx + t * a.dx_time, d, a.D, dxr);
+        }
+      }
+      if (a.dh0 && t_group == 0 && len > 0) {
+        Run<float, N> r;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) r[e] = back[e];
+        store_run_of<float, N>(a.dh0 + (uint64_t)s * a.D, d, a.D, r);
+      }
+    }
+    if (!kChained) break;
+    __syncthreads();  // LDS is free
+    ticket = next;
+  }
+  if (kChained) leave(chain, tag);
 }
 
 constexpr uint32_t kChannelThreads = 64;
@@ -525,7 +763,7 @@ struct ScanLaunch {
   Chain chain;
 };
 
-int scan_launch(uint32_t S, uint32_t T, uint32_t D, int dtype, void *workspace, ScanLaunch *l)
+int scan_launch(uint32_t S, uint32_t T, uint32_t D, int dtype, bool back, void *workspace, ScanLaunch *l)
 {
   if (T < kTileMinSteps) {
     *l = ScanLaunch{true, S * blocks_for(D, kChannelThreads), kChannelThreads, 0, {}};
@@ -534,7 +772,7 @@ int scan_launch(uint32_t S, uint32_t T, uint32_t D, int dtype, void *workspace, 
   const uint32_t run = 16 / element_size(dtype), width = kTileLanes * run;
   l->by_channel = false;
   l->chain = Chain{static_cast<ScanSpace *>(workspace), S * blocks_for(D, width), 1};
-  if (T <= kTileMaxSteps) {
+  if (T <= (back ? kChainSteps : kTileMaxSteps)) {
     l->threads = (uint32_t)round_up(blocks_for(T, kTileRows) * kTileLanes, width);
     l->grid = l->chain.columns;
   } else {
@@ -545,7 +783,10 @@ int scan_launch(uint32_t S, uint32_t T, uint32_t D, int dtype, void *workspace, 
     if (tiles > 0xf0000000ull) return APEX_ERR_TOO_LARGE;
     l->grid = (uint32_t)std::min<uint64_t>(tiles, 2 * kChipCus);
   }
-  l->lds = run == 8 ? tile_lds<8>(l->threads) : tile_lds<4>(l->threads);
+  if (back)
+    l->lds = run == 8 ? tile_back_lds<8>(l->threads) : tile_back_lds<4>(l->threads);
+  else
+    l->lds = run == 8 ? tile_lds<8>(l->threads) : tile_lds<4>(l->threads);
   return APEX_OK;
 }
 
@@ -557,7 +798,7 @@ int apex_gated_scan_workspace_bytes(uint32_t S, uint32_t T, uint32_t D, size_t *
 {
   if (!S || !T || !D || !bytes) return APEX_ERR_INVALID_ARG;
   size_t n = 0, words;
-  if (T > kTileMaxSteps &&
+  if (T > kChainSteps &&
       (__builtin_mul_overflow((uint64_t)S * blocks_for(T, kChainSteps), round_up(D, 128) * 3 * 8, &words) ||
        __builtin_add_overflow(words, kScanSpaceHead, &n)))
     return APEX_ERR_TOO_LARGE;
@@ -576,7 +817,7 @@ int apex_gated_scan(uint32_t S, uint32_t T, uint32_t D, int dtype, int gate, con
   const ScanArgs a{S, T, D, g_seq_stride, g_time_stride, x_seq_stride, x_time_stride, g, x, discount, length, h0, h, h_last, carry};
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   ScanLaunch l;
-  if (const int rc = scan_launch(S, T, D, dtype, workspace, &l)) return rc;
+  if (const int rc = scan_launch(S, T, D, dtype, false, workspace, &l)) return rc;
   with_type(dtype, [&](auto t) {
     typedef decltype(t) E;
     with_gate(gate, [&](auto gate_of) {
@@ -607,14 +848,20 @@ int apex_gated_scan_backward(uint32_t S, uint32_t T, uint32_t D, int dtype, int 
     return APEX_ERR_INVALID_ARG;
   const ScanBackArgs a{S, T, D, g_seq_stride, g_time_stride, x_seq_stride, x_time_stride, g, x, discount, length, carry, dh, dh_last,
                        dg_seq_stride, dg_time_stride, dx_seq_stride, dx_time_stride, dg, dx, dh0};
-  const dim3 grid(S * ((D - 1) / kChannelThreads + 1)), block(kChannelThreads);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  ScanLaunch l;
+  if (const int rc = scan_launch(S, T, D, dtype, true, workspace, &l)) return rc;
   with_type(dtype, [&](auto t) {
     typedef decltype(t) E;
-    if (gate == APEX_GATE_SIGMOID)
-      scan_channel_back_kernel<E, APEX_GATE_SIGMOID><<<grid, block, 0, stream>>>(a);
-    else
-      scan_channel_back_kernel<E, APEX_GATE_GIVEN><<<grid, block, 0, stream>>>(a);
+    with_gate(gate, [&](auto gate_of) {
+      constexpr int kGate = decltype(gate_of)::value;
+      if (l.by_channel)
+        scan_channel_back_kernel<E, kGate><<<l.grid, l.threads, 0, stream>>>(a);
+      else if (l.chain.tiles > 1)
+        scan_tile_back_kernel<E, kGate, true><<<l.grid, l.threads, l.lds, stream>>>(a, l.chain);
+      else
+        scan_tile_back_kernel<E, kGate, false><<<l.grid, l.threads, l.lds, stream>>>(a, l.chain);
+    });
   });
   APEX_HIP(hipGetLastError());
   return APEX_OK;
