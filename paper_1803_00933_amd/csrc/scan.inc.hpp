@@ -79,9 +79,9 @@ __device__ __forceinline__ void scan_gate_back(float a, float rest, float x, flo
 // its steps once more.  Reads every input once.
 //
 // A sequence longer than a tile is a chain of tiles, whose states are handed on while they run: a tile publishes its
-// composition as soon as it has it, looks back for the nearest tile whose outgoing state is there, applies the compositions
-// in between one after the other, and publishes its own.  However far it looks back, the operations on a state are the same, so
-// the bits are.  Only words of 64 bits cross between workgroups, a number and a tag in one, written and read at agent scope.
+// composition as soon as it has it and goes back to the nearest place whose state is there.  However far it goes back, the
+// operations on a state are the same, so the bits are.  Only words of 64 bits cross between workgroups, a number and a tag in
+// one, written and read at agent scope.
 // The tiles of a column of channels are taken by tickets, earlier ones first, so that whatever a tile waits for is held by a
 // workgroup that runs, and the first one waits for nobody.  (A counter per column: atomics on one address take turns of some
 // 14 ns.)
@@ -134,58 +134,139 @@ __device__ __forceinline__ uint32_t next_tag(uint32_t epoch)  // never that of m
   const uint32_t tag = (epoch + 1) & ~kCutTag;
   return tag ? tag : 1;
 }
+constexpr uint32_t kMostTiles = 1u << 22;  // of a chain: its words are counted in 32 bits
 constexpr uint32_t kMostPolls = 1u << 20;  // a wait gives up (and hands on NaN) where the workspace was not as required
 
-// The words of one tile: compositions A and B, state.
-struct TileWords {
-  uint64_t *a, *b, *state;
-  __device__ __forceinline__ TileWords(ScanSpace *space, uint64_t tile, uint32_t width)
-      : a(space->word + tile * 3 * width), b(a + width), state(b + width) {}
+constexpr uint32_t kStretch = 8;  // tiles of a stretch
+constexpr uint32_t kWindow = 16;  // compositions that a workgroup fetches at once
+
+__device__ __forceinline__ bool carries(uint64_t word, uint32_t tag) { return ((uint32_t)(word >> 32) & ~kCutTag) == tag; }
+__device__ __forceinline__ float number(uint64_t word) { return __uint_as_float((uint32_t)word); }
+// The word once it carries the tag (w: what it was just now); NaN if it never does.
+__device__ __forceinline__ uint64_t waited_for(uint64_t w, const uint64_t *word, uint32_t tag)
+{
+  for (uint32_t polls = 0; !carries(w, tag); w = seen(word))
+    if (++polls == kMostPolls) return tagged(__builtin_nanf(""), tag);
+  return w;
+}
+
+// Compositions fetched by a workgroup, in LDS.
+template <uint32_t kCount>
+struct Fetched {
+  float a[kCount][kTileWidth], b[kCount][kTileWidth];
+  uint32_t cut[kCount];
+
+  // `count` compositions at word + offset(i, 0), + offset(i, 1); by all threads, behind a barrier and before the next.
+  template <typename F>
+  __device__ __forceinline__ void fetch(const uint64_t *word, uint32_t count, bool is, uint32_t tag, F offset)
+  {
+    constexpr uint32_t kSlots = kChainThreads / kTileWidth, kEach = (kCount + kSlots - 1) / kSlots;
+    const uint32_t channel = threadIdx.x % kTileWidth, slot = threadIdx.x / kTileWidth;
+    uint64_t wa[kEach], wb[kEach];
+#pragma unroll
+    for (uint32_t u = 0; u < kEach; ++u) {
+      const uint32_t i = slot + u * kSlots;
+      if (i < count && is) wa[u] = seen(word + (offset(i, 0) + channel)), wb[u] = seen(word + (offset(i, 1) + channel));
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < kEach; ++u) {
+      const uint32_t i = slot + u * kSlots;
+      if (i < count && is) {
+        wa[u] = waited_for(wa[u], word + (offset(i, 0) + channel), tag);
+        wb[u] = waited_for(wb[u], word + (offset(i, 1) + channel), tag);
+        a[i][channel] = number(wa[u]);
+        b[i][channel] = number(wb[u]);
+        if (channel == 0) cut[i] = (uint32_t)(wa[u] >> 32) & kCutTag;
+      }
+    }
+  }
+  __device__ __forceinline__ float through(uint32_t i, uint32_t channel, float state) const
+  {
+    return cut[i] ? b[i][channel] : __builtin_fmaf(a[i][channel], state, b[i][channel]);
+  }
 };
 
-// The state that enters a tile from the one `behind` it, for the channel of this lane; called by a wave, whose first lane's
-// channel exists.  word_of(i): the words of the tile i places away, i < reach.
-template <typename F>
-__device__ __forceinline__ float look_back(F word_of, uint32_t channel, bool exists, uint32_t reach, uint32_t tag)
+struct ChainSpace {
+  Fetched<kStretch - 1> tiles;
+  Fetched<kWindow> stretches;
+  uint32_t nearest;
+};
+
+// The state that enters the tile at position q of a chain, for thread < kTileWidth and its channel (`is`: there is one), from
+// the composition (A, B) of the tile (`cut`: B is its outgoing state whatever enters) and the state that enters the chain.  By
+// the whole workgroup.  Publishes what the tiles behind ask for.
+//
+// kStretch tiles are a stretch: a tile publishes its composition, the last one of a stretch the stretch's and the state behind
+// it.  A tile goes back to the nearest stretch whose state is there (the first wave looks at 64 at once), through the
+// compositions of the stretches from there on, and through those of the tiles of its own stretch before it, which all threads
+// fetch, up to kWindow with one round trip.
+// Words of position p: word + p * 3 * kTileWidth: A, B, and a third row that the last three tiles of a stretch lend to the
+// stretch: its A, its B, and the state behind it.
+__device__ __forceinline__ float chain_state(uint64_t *word, uint32_t q, bool is, float A, float B, bool cut, float start, uint32_t tag,
+                                             ChainSpace &w)
 {
-  const uint32_t lane = lane_id();
-  const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane((int)channel);
-  uint64_t there = 0;
-  uint32_t polls = 0;
-  for (;;) {
-    uint64_t w = 0;
-    if (lane < reach) w = seen(word_of(lane).state + first);
-    there = __ballot((uint32_t)(w >> 32) == tag);
-    if (there || ++polls == kMostPolls) break;
-    __builtin_amdgcn_s_sleep(1);
+  const uint32_t thread = threadIdx.x, channel = thread % kTileWidth, stretch = q / kStretch, place = q % kStretch;
+  const bool speaks = thread < kTileWidth && is;
+  const auto row = [&](uint32_t position, uint32_t i) { return (position * 3 + i) * kTileWidth; };  // (kMostTiles)
+  const auto stretch_row = [&](uint32_t k, uint32_t i) { return row(k * kStretch + kStretch - 3 + i, 2); };
+  const auto say = [&](uint32_t at, uint64_t v) { publish(word + (at + channel), v); };
+  if (speaks && place < kStretch - 1) {
+    say(row(q, 0), tagged(A, cut ? tag | kCutTag : tag));
+    say(row(q, 1), tagged(B, tag));
   }
-  if (!there) return __builtin_nanf("");
-  const uint32_t nearest = (uint32_t)__builtin_ctzll(there);
-  if (!exists) return 0.0f;
-  uint64_t w = seen(word_of(nearest).state + channel);
-  while ((uint32_t)(w >> 32) != tag && ++polls < kMostPolls) w = seen(word_of(nearest).state + channel);
-  float state = __uint_as_float((uint32_t)w);
-  constexpr uint32_t kBatch = 2;
-  for (uint32_t i = nearest; i > 0;) {
-    uint64_t wa[kBatch], wb[kBatch];
-#pragma unroll
-    for (uint32_t j = 0; j < kBatch; ++j) {
-      const TileWords t = word_of(i > j ? i - 1 - j : 0);
-      wa[j] = seen(t.a + channel);
-      wb[j] = seen(t.b + channel);
+  if (q == 0) return start;
+  w.tiles.fetch(word, place, is, tag, [&](uint32_t i, uint32_t r) { return row(q - place + i, r); });
+  if (thread >= kChainThreads - kWave && stretch > 0) {
+    const uint32_t lane = lane_id(), reach = min(stretch, (uint32_t)kWave);
+    uint64_t there = 0;
+    for (uint32_t polls = 0; polls < kMostPolls; ++polls) {
+      const uint64_t v = lane < reach ? seen(word + stretch_row(stretch - 1 - lane, 2)) : 0;
+      there = __ballot(lane < reach && carries(v, tag));
+      if (there) break;
+      __builtin_amdgcn_s_sleep(1);
     }
-#pragma unroll
-    for (uint32_t j = 0; j < kBatch; ++j) {
-      if (i == 0) break;
-      const TileWords t = word_of(i - 1);
-      while (((uint32_t)(wb[j] >> 32) != tag || ((uint32_t)(wa[j] >> 32) & ~kCutTag) != tag) && ++polls < kMostPolls)
-        wa[j] = seen(t.a + channel), wb[j] = seen(t.b + channel);
-      const float A = __uint_as_float((uint32_t)wa[j]), B = __uint_as_float((uint32_t)wb[j]);
-      state = (uint32_t)(wa[j] >> 32) & kCutTag ? B : __builtin_fmaf(A, state, B);
-      --i;
+    if (lane == 0) w.nearest = there ? (uint32_t)__builtin_ctzll(there) : 0;
+  }
+  __syncthreads();
+  float SA = 1.0f, SB = 0.0f;
+  bool stretch_cut = cut;
+  const bool last = place == kStretch - 1;
+  if (last && thread < kTileWidth) {
+    for (uint32_t i = 0; i < kStretch - 1; ++i) {
+      stretch_cut = stretch_cut || w.tiles.cut[i];
+      SB = w.tiles.through(i, channel, SB);
+      SA *= w.tiles.a[i][channel];
+    }
+    SB = cut ? B : __builtin_fmaf(A, SB, B);
+    SA = A * SA;
+    if (is) {
+      say(stretch_row(stretch, 0), tagged(SA, stretch_cut ? tag | kCutTag : tag));
+      say(stretch_row(stretch, 1), tagged(SB, tag));
+      if (stretch_cut) say(stretch_row(stretch, 2), tagged(SB, tag));
     }
   }
-  return polls >= kMostPolls ? __builtin_nanf("") : state;
+  float state = start;
+  if (stretch > 0) {
+    const uint32_t nearest = w.nearest;
+    const uint64_t *const from = word + (stretch_row(stretch - 1 - nearest, 2) + channel);
+    uint64_t v = 0;
+    if (speaks) v = seen(from);
+    for (uint32_t left = nearest; left > 0;) {
+      const uint32_t count = min(left, kWindow), first = stretch - left;
+      w.stretches.fetch(word, count, is, tag, [&](uint32_t i, uint32_t r) { return stretch_row(first + i, r); });
+      if (left == nearest && speaks) state = number(waited_for(v, from, tag));
+      __syncthreads();
+      if (thread < kTileWidth)
+        for (uint32_t i = 0; i < count; ++i) state = w.stretches.through(i, channel, state);
+      left -= count;
+      if (left) __syncthreads();
+    }
+    if (nearest == 0 && speaks) state = number(waited_for(v, from, tag));
+  }
+  if (speaks && last && !stretch_cut) say(stretch_row(stretch, 2), tagged(__builtin_fmaf(SA, state, SB), tag));
+  if (thread < kTileWidth)
+    for (uint32_t i = 0; i < place; ++i) state = w.tiles.through(i, channel, state);
+  return state;
 }
 
 // A workgroup that waits for nothing any more: the last one of a counter, and of them the last of the call, leave the counters as
@@ -240,168 +321,210 @@ constexpr uint32_t tile_lds(uint32_t threads)  // bytes: compositions of the gro
   return threads * kTileRun * 8 + threads * 12;
 }
 
+// What a workgroup's threads are to its tile.
+struct TileShape {
+  uint32_t threads, thread, groups, segments, steps;
+  uint32_t group, run;        // a thread's steps and channels ...
+  uint32_t segment, channel;  // ... and what it does when the compositions are gone through
+  __device__ __forceinline__ TileShape()
+  {
+    threads = blockDim.x, thread = threadIdx.x;
+    groups = threads / kTileLanes, segments = threads / kTileWidth, steps = groups * kTileRows;
+    group = thread / kTileLanes, run = thread % kTileLanes * kTileRun;
+    segment = thread / kTileWidth, channel = thread % kTileWidth;
+  }
+};
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+static_assert(kTileRun == 4);
+
+// Whether every row of the tile passes on; behind the barrier that the bits were written before.
+__device__ __forceinline__ bool uncut(const RowBits &bits, uint32_t steps)
+{
+  uint64_t missing = 0;
+  for (uint32_t i = 0; i * kWave < steps; ++i)
+    missing |= ~bits.word[i] & (steps - i * kWave >= kWave ? ~0ull : (1ull << (steps - i * kWave)) - 1);
+  return missing == 0;
+}
+
+// f(integral_constant<bool>): the common case apart, in which no element has to be asked whether it counts.
+template <typename F>
+__device__ __forceinline__ void plainly(bool plain, F f)
+{
+  if (plain)
+    f(std::integral_constant<bool, true>());
+  else
+    f(std::integral_constant<bool, false>());
+}
+
 // kChained: tiles of a sequence wait for one another; else a sequence has one tile.
 template <typename T, int kGate, bool kChained>
-__global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, 4) void scan_tile_kernel(ScanArgs a, Chain chain)
+__global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChained ? 6 : 4) void scan_tile_kernel(ScanArgs a, Chain chain)
 {
   constexpr uint32_t N = kTileRun, kWidth = kTileWidth;
-  extern __shared__ uint64_t lds[];
+  extern __shared__ __align__(16) float scan_lds[];
   __shared__ RowBits into;  // whether the state passes into a row
   __shared__ uint2 sh_tile;
-  const uint32_t threads = blockDim.x, thread = threadIdx.x, lane = lane_id(), wave = thread / kWave;
-  const uint32_t groups = threads / kTileLanes, segments = threads / kWidth, steps = groups * kTileRows;
-  float2 *const group_ab = reinterpret_cast<float2 *>(lds);                    // [groups][kWidth]; .x later: the state that enters
-  float2 *const segment_ab = group_ab + groups * kWidth;                       // [segments][kWidth]
-  float *const segment_in = reinterpret_cast<float *>(segment_ab + segments * kWidth);
+  __shared__ typename std::conditional<kChained, ChainSpace, uint32_t>::type sh_chain;
+  const TileShape w;
+  float *const group_a = scan_lds, *const group_b = group_a + w.groups * kWidth;  // [groups][kWidth]; group_a later: the state that enters
+  float *const segment_a = group_b + w.groups * kWidth, *const segment_b = segment_a + w.threads;  // [segments][kWidth]
+  float *const segment_in = segment_b + w.threads;
   const uint32_t pieces = (a.D + kWidth - 1) / kWidth;  // of a row
-  const uint32_t group = thread / kTileLanes, run = thread % kTileLanes * N;
-  const uint32_t segment = thread / kWidth, channel = thread % kWidth;  // the same threads, when they go through compositions
   const uint32_t chunks = (a.T + APEX_SCAN_CHUNK - 1) / APEX_SCAN_CHUNK;
   uint32_t tag = 0, tile = 0, column = blockIdx.x;
   if (kChained) {
     tag = next_tag(chain.space->epoch);
-    if (thread == 0) sh_tile = take_tile(chain);
+    if (w.thread == 0) sh_tile = take_tile(chain);
     __syncthreads();
     tile = sh_tile.x, column = sh_tile.y;
   }
-  const uint32_t s = column / pieces, d0 = column % pieces * kWidth, t0 = tile * steps;
+  const uint32_t s = column / pieces, d0 = column % pieces * kWidth, t0 = tile * w.steps;
   const uint32_t len = scan_length(a.length, s, a.T);
-  const uint32_t t_group = t0 + group * kTileRows, d = d0 + run;
-  const bool exists = d < a.D;
+  const uint32_t t_group = t0 + w.group * kTileRows, d = d0 + w.run;
+  const bool exists = d < a.D, whole = t0 + w.steps <= len && d0 + kWidth <= a.D;
   // the rows of this thread
-  const T *const g = static_cast<const T *>(a.g) + s * a.g_seq, *const x = static_cast<const T *>(a.x) + s * a.x_seq;
   Run<T, N> gr[kTileRows], xr[kTileRows];
+  {
+    const T *const g = static_cast<const T *>(a.g) + s * a.g_seq + t_group * a.g_time;
+    const T *const x = static_cast<const T *>(a.x) + s * a.x_seq + t_group * a.x_time;
+    if (whole) {
 #pragma unroll
-  for (uint32_t l = 0; l < kTileRows; ++l) {
-    const uint32_t t = t_group + l;
-    if (exists && t < len) gr[l] = run_of<T, N>(g + t * a.g_time, d, a.D), xr[l] = run_of<T, N>(x + t * a.x_time, d, a.D);
+      for (uint32_t l = 0; l < kTileRows; ++l) gr[l] = load_run<T, N>(g + l * a.g_time + d), xr[l] = load_run<T, N>(x + l * a.x_time + d);
+    } else {
+#pragma unroll
+      for (uint32_t l = 0; l < kTileRows; ++l)
+        if (exists && t_group + l < len) gr[l] = run_of<T, N>(g + l * a.g_time, d, a.D), xr[l] = run_of<T, N>(x + l * a.x_time, d, a.D);
+    }
   }
-  if (thread < steps) {
-    const uint32_t t = t0 + thread;
-    const bool passes = !a.discount || t == 0 || t >= len || a.discount[(uint64_t)s * a.T + t - 1] != 0.0f;
-    const uint64_t bits = __ballot(passes);
-    if (lane == 0) into.word[wave] = bits;
+  if (w.thread < w.steps) {
+    const uint32_t t = t0 + w.thread;
+    const uint64_t bits = __ballot(!a.discount || t == 0 || t >= len || a.discount[(uint64_t)s * a.T + t - 1] != 0.0f);
+    if (lane_id() == 0) into.word[w.thread / kWave] = bits;
   }
   __syncthreads();
-  const uint32_t bits = into.of_group(group);
+  const uint32_t bits = into.of_group(w.group);
+  const bool no_cut = uncut(into, w.steps), plain = whole && no_cut;
   float fa[kTileRows][N], fb[kTileRows][N];
-  {
-    float A[N], B[N];
+  plainly(plain, [&](auto is_plain) {
+    constexpr bool kPlain = decltype(is_plain)::value;
+    f32x4 A, B;
 #pragma unroll
     for (uint32_t e = 0; e < N; ++e) A[e] = 1.0f, B[e] = 0.0f;
 #pragma unroll
     for (uint32_t l = 0; l < kTileRows; ++l) {
-      const bool inside = exists && t_group + l < len, passes = bits >> l & 1;
+      const bool inside = kPlain || (exists && t_group + l < len), passes = kPlain || (bits >> l & 1);
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) {
         float f = 1.0f, b = 0.0f, rest;
         if (inside) scan_gate<kGate>(element<N, T>(gr[l], e), element<N, T>(xr[l], e), &f, &rest, &b);
         fa[l][e] = f;
         fb[l][e] = b;
-        A[e] = passes ? A[e] * f : 0.0f;
-        B[e] = passes ? __builtin_fmaf(f, B[e], b) : b;
+        if (l == 0) {
+          A[e] = passes ? f : 0.0f;
+          B[e] = b;
+        } else {
+          A[e] = passes ? A[e] * f : 0.0f;
+          B[e] = passes ? __builtin_fmaf(f, B[e], b) : b;
+        }
       }
     }
-#pragma unroll
-    for (uint32_t e = 0; e < N; ++e) group_ab[group * kWidth + run + e] = make_float2(A[e], B[e]);
-  }
+    *reinterpret_cast<f32x4 *>(group_a + w.group * kWidth + w.run) = A;
+    *reinterpret_cast<f32x4 *>(group_b + w.group * kWidth + w.run) = B;
+  });
   __syncthreads();
-  if (segments > 1) {
+  if (w.segments > 1) {
     float A = 1.0f, B = 0.0f;
 #pragma unroll
     for (uint32_t i = 0; i < kSegment; ++i) {
-      const float2 c = group_ab[(segment * kSegment + i) * kWidth + channel];
-      const bool passes = into.of_group(segment * kSegment + i) == 15u;
-      A = passes ? A * c.x : 0.0f;
-      B = passes ? __builtin_fmaf(c.x, B, c.y) : c.y;
+      const uint32_t at = (w.segment * kSegment + i) * kWidth + w.channel;
+      const float ga = group_a[at], gb = group_b[at];
+      const bool passes = no_cut || into.of_group(w.segment * kSegment + i) == 15u;
+      A = passes ? A * ga : 0.0f;
+      B = passes ? __builtin_fmaf(ga, B, gb) : gb;
     }
-    segment_ab[segment * kWidth + channel] = make_float2(A, B);
+    segment_a[w.thread] = A;
+    segment_b[w.thread] = B;
     __syncthreads();
   }
-  if (thread < kWidth) {
-    const bool is = d0 + channel < a.D;
-    const uint64_t at = (uint64_t)s * a.D + d0 + channel;
-    float state = 0.0f;
-    if (kChained && t0 < len && __ballot(is)) {
+  const bool speaks = w.thread < kWidth && d0 + w.channel < a.D;
+  float state_in = 0.0f;  // what enters the chain; then what enters the tile
+  if (speaks && a.h0 && tile < kStretch) state_in = a.h0[(uint64_t)s * a.D + d0 + w.channel];
+  if (speaks && a.h_last && tile == 0 && len == 0) a.h_last[(uint64_t)s * a.D + d0 + w.channel] = state_in;
+  if constexpr (kChained) {
+    if (t0 < len) {
       float A = 1.0f, B = 0.0f;
-      bool cut = false;
-      for (uint32_t i = 0; i < segments; ++i) {
-        const float2 c = segment_ab[i * kWidth + channel];
-        const bool passes = into.all_of_segment(i);
-        cut = cut || !passes;
-        A = passes ? A * c.x : 0.0f;
-        B = passes ? __builtin_fmaf(c.x, B, c.y) : c.y;
-      }
-      const auto words = [&](uint32_t behind) { return TileWords(chain.space, (uint64_t)column * chain.tiles + tile - 1 - behind, kWidth); };
-      const TileWords own(chain.space, (uint64_t)column * chain.tiles + tile, kWidth);
-      if (is && tile > 0) {
-        publish(own.a + channel, tagged(A, cut ? tag | kCutTag : tag));
-        publish(own.b + channel, tagged(B, tag));
-      }
-      if (is && cut) publish(own.state + channel, tagged(B, tag));
-      if (tile == 0)
-        state = a.h0 && is ? a.h0[at] : 0.0f;
-      else
-        state = look_back(words, channel, is, min(tile, kWave), tag);
-      if (is && !cut) publish(own.state + channel, tagged(__builtin_fmaf(A, state, B), tag));
-    } else if (!kChained && is) {
-      state = a.h0 ? a.h0[at] : 0.0f;
+      if (w.thread < kWidth)
+        for (uint32_t i = 0; i < w.segments; ++i) {
+          const float sa = segment_a[i * kWidth + w.channel], sb = segment_b[i * kWidth + w.channel];
+          const bool passes = into.all_of_segment(i);
+          A = passes ? A * sa : 0.0f;
+          B = passes ? __builtin_fmaf(sa, B, sb) : sb;
+        }
+      state_in = chain_state(chain.space->word + (uint64_t)column * chain.tiles * 3 * kWidth, tile, d0 + w.channel < a.D, A, B, !no_cut,
+                             state_in, tag, sh_chain);
     }
-    if (t0 == 0 && len == 0 && is && a.h_last) a.h_last[at] = a.h0 ? a.h0[at] : 0.0f;
-    segment_in[channel] = state;
-    for (uint32_t i = 0; i + 1 < segments; ++i) {
-      const float2 c = segment_ab[i * kWidth + channel];
-      state = into.all_of_segment(i) ? __builtin_fmaf(c.x, state, c.y) : c.y;
-      segment_in[(i + 1) * kWidth + channel] = state;
+  }
+  if (w.thread < kWidth) {
+    segment_in[w.channel] = state_in;
+    for (uint32_t i = 0; i + 1 < w.segments; ++i) {
+      const float sa = segment_a[i * kWidth + w.channel], sb = segment_b[i * kWidth + w.channel];
+      state_in = into.all_of_segment(i) ? __builtin_fmaf(sa, state_in, sb) : sb;
+      segment_in[(i + 1) * kWidth + w.channel] = state_in;
     }
   }
   __syncthreads();
   uint32_t before = 0;
-  if (kChained && thread == threads - 1) before = leaving(chain);
+  if (kChained && w.thread == w.threads - 1) before = leaving(chain);
   {
-    float state = segment_in[segment * kWidth + channel];
+    float state = segment_in[w.thread];
 #pragma unroll
     for (uint32_t i = 0; i < kSegment; ++i) {
-      float2 *const at = group_ab + (segment * kSegment + i) * kWidth + channel;
-      const float2 c = *at;
-      at->x = state;
-      state = into.of_group(segment * kSegment + i) == 15u ? __builtin_fmaf(c.x, state, c.y) : c.y;
+      const uint32_t at = (w.segment * kSegment + i) * kWidth + w.channel;
+      const float ga = group_a[at], gb = group_b[at];
+      group_a[at] = state;
+      state = no_cut || into.of_group(w.segment * kSegment + i) == 15u ? __builtin_fmaf(ga, state, gb) : gb;
     }
   }
   __syncthreads();
   if (exists) {
-    float state[N];
-#pragma unroll
-    for (uint32_t e = 0; e < N; ++e) state[e] = group_ab[group * kWidth + run + e].x;
+    f32x4 state = *reinterpret_cast<const f32x4 *>(group_a + w.group * kWidth + w.run);
     if (a.carry && t_group % APEX_SCAN_CHUNK == 0 && t_group < len) {
       float *const c = a.carry + ((uint64_t)s * chunks + t_group / APEX_SCAN_CHUNK) * a.D;
-      Run<float, N> r;
+      f32x4 r;
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) r[e] = bits & 1 ? state[e] : 0.0f;
       store_run_of<float, N>(c, d, a.D, r);
     }
-    T *const h = static_cast<T *>(a.h) + (uint64_t)s * a.T * a.D;
+    T *const h = static_cast<T *>(a.h) + ((uint64_t)s * a.T + t_group) * a.D;
+    plainly(plain, [&](auto is_plain) {
+      constexpr bool kPlain = decltype(is_plain)::value;
 #pragma unroll
-    for (uint32_t l = 0; l < kTileRows; ++l) {
-      const uint32_t t = t_group + l;
-      const bool passes = bits >> l & 1;
-      Run<T, N> r;
+      for (uint32_t l = 0; l < kTileRows; ++l) {
+        const uint32_t t = t_group + l;
+        const bool passes = kPlain || (bits >> l & 1);
+        Run<T, N> r;
 #pragma unroll
-      for (uint32_t e = 0; e < N; ++e) {
-        state[e] = passes ? __builtin_fmaf(fa[l][e], state[e], fb[l][e]) : fb[l][e];
-        r[e] = t < len ? (T)state[e] : (T)0.0f;
+        for (uint32_t e = 0; e < N; ++e) {
+          state[e] = passes ? __builtin_fmaf(fa[l][e], state[e], fb[l][e]) : fb[l][e];
+          r[e] = kPlain || t < len ? (T)state[e] : (T)0.0f;
+        }
+        T *const to = h + (uint64_t)l * a.D;
+        if (kPlain)
+          *reinterpret_cast<Run<T, N> *>(to + d) = r;
+        else if (t < a.T)
+          store_run_of<T, N>(to, d, a.D, r);
+        if (a.h_last && t + 1 == len) {
+          const bool on = !a.discount || a.discount[(uint64_t)s * a.T + t] != 0.0f;
+          f32x4 out;
+#pragma unroll
+          for (uint32_t e = 0; e < N; ++e) out[e] = on ? state[e] : 0.0f;
+          store_run_of<float, N>(a.h_last + (uint64_t)s * a.D, d, a.D, out);
+        }
       }
-      if (t < a.T) store_run_of<T, N>(h + (uint64_t)t * a.D, d, a.D, r);
-      if (a.h_last && t + 1 == len) {
-        const bool on = !a.discount || a.discount[(uint64_t)s * a.T + t] != 0.0f;
-        Run<float, N> last;
-#pragma unroll
-        for (uint32_t e = 0; e < N; ++e) last[e] = on ? state[e] : 0.0f;
-        store_run_of<float, N>(a.h_last + (uint64_t)s * a.D, d, a.D, last);
-      }
-    }
+    });
   }
-  if (kChained && thread == threads - 1) left(chain, before, tag);
+  if (kChained && w.thread == w.threads - 1) left(chain, before, tag);
 }
 
 // The gradient in tiles: the states from `carry`, which begins anew every APEX_SCAN_CHUNK steps, and lambda by a chain from the
@@ -418,213 +541,223 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, 4) void
   constexpr uint32_t N = kTileRun, kWidth = kTileWidth;
   constexpr uint32_t kChunkGroups = APEX_SCAN_CHUNK / kTileRows, kChunkSegments = kChunkGroups / kSegment;
   static_assert(APEX_SCAN_CHUNK == kWave);  // a word of RowBits is a chunk
-
-  extern __shared__ uint64_t lds[];
+  extern __shared__ __align__(16) float scan_lds[];
   __shared__ RowBits on;  // whether a row's state passes on
   __shared__ uint2 sh_tile;
-  const uint32_t threads = blockDim.x, thread = threadIdx.x, lane = lane_id(), wave = thread / kWave;
-  const uint32_t groups = threads / kTileLanes, segments = threads / kWidth, steps = groups * kTileRows;
-  float2 *const group_ab = reinterpret_cast<float2 *>(lds);  // [groups][kWidth]; .x later: the state that enters
-  float2 *const group_pq = group_ab + groups * kWidth;       // [groups][kWidth]; .x later: the gradient that enters from behind
-  float2 *const segment_pq = group_pq + groups * kWidth;     // [segments][kWidth]
-  float *const segment_in = reinterpret_cast<float *>(segment_pq + segments * kWidth);
+  __shared__ typename std::conditional<kChained, ChainSpace, uint32_t>::type sh_chain;
+  const TileShape w;
+  float *const group_a = scan_lds, *const group_b = group_a + w.groups * kWidth;                 // [groups][kWidth]; group_a later: the state that enters
+  float *const group_p = group_b + w.groups * kWidth, *const group_q = group_p + w.groups * kWidth;  // group_p: the gradient that enters
+  float *const segment_p = group_q + w.groups * kWidth, *const segment_q = segment_p + w.threads;    // [segments][kWidth]
+  float *const segment_in = segment_q + w.threads;
   const uint32_t pieces = (a.D + kWidth - 1) / kWidth;
-  const uint32_t group = thread / kTileLanes, run = thread % kTileLanes * N;
-  const uint32_t segment = thread / kWidth, channel = thread % kWidth;
   const uint32_t chunks = (a.T + APEX_SCAN_CHUNK - 1) / APEX_SCAN_CHUNK;
   uint32_t tag = 0, tile = 0, column = blockIdx.x;
   if (kChained) {
     tag = next_tag(chain.space->epoch);
-    if (thread == 0) sh_tile = take_tile(chain);
+    if (w.thread == 0) sh_tile = take_tile(chain);
     __syncthreads();
     tile = chain.tiles - 1 - sh_tile.x, column = sh_tile.y;
   }
-  const uint32_t s = column / pieces, d0 = column % pieces * kWidth, t0 = tile * steps;
+  const uint32_t s = column / pieces, d0 = column % pieces * kWidth, t0 = tile * w.steps;
   const uint32_t len = scan_length(a.length, s, a.T);
-  const uint32_t t_group = t0 + group * kTileRows, d = d0 + run;
-  const bool exists = d < a.D;
-  const T *const g = static_cast<const T *>(a.g) + s * a.g_seq, *const x = static_cast<const T *>(a.x) + s * a.x_seq;
-  const T *const dh = static_cast<const T *>(a.dh) + (uint64_t)s * a.T * a.D;
+  const uint32_t t_group = t0 + w.group * kTileRows, d = d0 + w.run;
+  const bool exists = d < a.D, whole = t0 + w.steps <= len && d0 + kWidth <= a.D;
   Run<T, N> gr[kTileRows], xr[kTileRows], hr[kTileRows];
+  {
+    const T *const g = static_cast<const T *>(a.g) + s * a.g_seq + t_group * a.g_time;
+    const T *const x = static_cast<const T *>(a.x) + s * a.x_seq + t_group * a.x_time;
+    const T *const dh = static_cast<const T *>(a.dh) + ((uint64_t)s * a.T + t_group) * a.D;
+    if (whole) {
 #pragma unroll
-  for (uint32_t l = 0; l < kTileRows; ++l) {
-    const uint32_t t = t_group + l;
-    if (exists && t < len) {
-      gr[l] = run_of<T, N>(g + t * a.g_time, d, a.D);
-      xr[l] = run_of<T, N>(x + t * a.x_time, d, a.D);
-      hr[l] = run_of<T, N>(dh + (uint64_t)t * a.D, d, a.D);
+      for (uint32_t l = 0; l < kTileRows; ++l) {
+        gr[l] = load_run<T, N>(g + l * a.g_time + d);
+        xr[l] = load_run<T, N>(x + l * a.x_time + d);
+        hr[l] = load_run<T, N>(dh + (uint64_t)l * a.D + d);
+      }
+    } else {
+#pragma unroll
+      for (uint32_t l = 0; l < kTileRows; ++l)
+        if (exists && t_group + l < len) {
+          gr[l] = run_of<T, N>(g + l * a.g_time, d, a.D);
+          xr[l] = run_of<T, N>(x + l * a.x_time, d, a.D);
+          hr[l] = run_of<T, N>(dh + (uint64_t)l * a.D, d, a.D);
+        }
     }
   }
   // the state that enters the chunk of this thread's segment
-  const bool is = d0 + channel < a.D;
-  const uint32_t chunk = t0 / APEX_SCAN_CHUNK + segment / kChunkSegments;
+  const bool is = d0 + w.channel < a.D, speaks = w.thread < kWidth && is;
+  const uint32_t chunk = t0 / APEX_SCAN_CHUNK + w.segment / kChunkSegments;
   float state = 0.0f;
-  if (is && chunk * APEX_SCAN_CHUNK < len) state = a.carry[((uint64_t)s * chunks + chunk) * a.D + d0 + channel];
-  if (thread < steps) {
-    const uint32_t t = t0 + thread;
+  if (is && chunk * APEX_SCAN_CHUNK < len) state = a.carry[((uint64_t)s * chunks + chunk) * a.D + d0 + w.channel];
+  if (w.thread < w.steps) {
+    const uint32_t t = t0 + w.thread;
     const uint64_t bits = __ballot(!a.discount || t >= len || a.discount[(uint64_t)s * a.T + t] != 0.0f);
-    if (lane == 0) on.word[wave] = bits;
+    if (lane_id() == 0) on.word[w.thread / kWave] = bits;
   }
   __syncthreads();
-  const uint32_t bits = on.of_group(group);
+  const uint32_t bits = on.of_group(w.group);
+  const bool no_cut = uncut(on, w.steps), plain = whole && no_cut;
+  const uint32_t into = (uint32_t)((on.word[w.group / kChunkGroups] << 1 | 1) >> (w.group % kChunkGroups * kTileRows)) & 15u;
   float f[kTileRows][N], rest[kTileRows][N];
-  const uint32_t into = (uint32_t)((on.word[group / kChunkGroups] << 1 | 1) >> (group % kChunkGroups * kTileRows)) & 15u;
-  {
-    float A[N], B[N], P[N], Q[N];
-#pragma unroll
-    for (uint32_t e = 0; e < N; ++e) A[e] = P[e] = 1.0f, B[e] = Q[e] = 0.0f;
+  plainly(plain, [&](auto is_plain) {
+    constexpr bool kPlain = decltype(is_plain)::value;
+    f32x4 A, B, P, Q;
 #pragma unroll
     for (uint32_t l = 0; l < kTileRows; ++l) {
-      const bool inside = exists && t_group + l < len, passes = into >> l & 1;
+      const bool inside = kPlain || (exists && t_group + l < len), passes = kPlain || (into >> l & 1);
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) {
         float b = 0.0f;
         f[l][e] = 1.0f, rest[l][e] = 0.0f;
         if (inside) scan_gate<kGate>(element<N, T>(gr[l], e), element<N, T>(xr[l], e), &f[l][e], &rest[l][e], &b);
-        A[e] = passes ? A[e] * f[l][e] : 0.0f;
-        B[e] = passes ? __builtin_fmaf(f[l][e], B[e], b) : b;
+        if (l == 0) {
+          A[e] = passes ? f[l][e] : 0.0f;
+          B[e] = b;
+        } else {
+          A[e] = passes ? A[e] * f[l][e] : 0.0f;
+          B[e] = passes ? __builtin_fmaf(f[l][e], B[e], b) : b;
+        }
       }
     }
 #pragma unroll
     for (uint32_t l = kTileRows; l-- > 0;) {
-      const bool inside = exists && t_group + l < len, passes = bits >> l & 1;
+      const bool inside = kPlain || (exists && t_group + l < len), passes = kPlain || (bits >> l & 1);
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) {
         const float dht = inside ? element<N, T>(hr[l], e) : 0.0f;
-        P[e] = passes ? P[e] * f[l][e] : 0.0f;
-        Q[e] = f[l][e] * (passes ? Q[e] + dht : dht);
+        if (l == kTileRows - 1) {
+          P[e] = passes ? f[l][e] : 0.0f;
+          Q[e] = f[l][e] * dht;
+        } else {
+          P[e] = passes ? P[e] * f[l][e] : 0.0f;
+          Q[e] = f[l][e] * (passes ? Q[e] + dht : dht);
+        }
       }
     }
-#pragma unroll
-    for (uint32_t e = 0; e < N; ++e) {
-      group_ab[group * kWidth + run + e] = make_float2(A[e], B[e]);
-      group_pq[group * kWidth + run + e] = make_float2(P[e], Q[e]);
-    }
-  }
+    const uint32_t at = w.group * kWidth + w.run;
+    *reinterpret_cast<f32x4 *>(group_a + at) = A;
+    *reinterpret_cast<f32x4 *>(group_b + at) = B;
+    *reinterpret_cast<f32x4 *>(group_p + at) = P;
+    *reinterpret_cast<f32x4 *>(group_q + at) = Q;
+  });
   __syncthreads();
   // the states that enter the groups of a segment, from the chunk's; the segment's composition, from its last group
   float states[kSegment];
   {
-    const uint32_t first = segment / kChunkSegments * kChunkGroups;
+    const uint32_t first = w.segment / kChunkSegments * kChunkGroups;
     const uint64_t chunk_bits = on.word[first / kChunkGroups] << 1 | 1;
-    const auto through = [&](uint32_t i) {
-      const float2 c = group_ab[i * kWidth + channel];
-      state = ((uint32_t)(chunk_bits >> (i - first) * kTileRows) & 15u) == 15u ? __builtin_fmaf(c.x, state, c.y) : c.y;
+    const auto go_through = [&](uint32_t i) {
+      const float ga = group_a[i * kWidth + w.channel], gb = group_b[i * kWidth + w.channel];
+      state = no_cut || ((uint32_t)(chunk_bits >> (i - first) * kTileRows) & 15u) == 15u ? __builtin_fmaf(ga, state, gb) : gb;
     };
-    for (uint32_t i = first; i < segment * kSegment; ++i) through(i);
+    for (uint32_t i = first; i < w.segment * kSegment; ++i) go_through(i);
 #pragma unroll
     for (uint32_t i = 0; i < kSegment; ++i) {
       states[i] = state;
-      through(segment * kSegment + i);
+      go_through(w.segment * kSegment + i);
     }
     float P = 1.0f, Q = 0.0f;
 #pragma unroll
     for (uint32_t i = kSegment; i-- > 0;) {
-      const float2 c = group_pq[(segment * kSegment + i) * kWidth + channel];
-      const bool passes = on.of_group(segment * kSegment + i) == 15u;
-      P = passes ? P * c.x : 0.0f;
-      Q = passes ? __builtin_fmaf(c.x, Q, c.y) : c.y;
+      const uint32_t at = (w.segment * kSegment + i) * kWidth + w.channel;
+      const float gp = group_p[at], gq = group_q[at];
+      const bool passes = no_cut || on.of_group(w.segment * kSegment + i) == 15u;
+      P = passes ? P * gp : 0.0f;
+      Q = passes ? __builtin_fmaf(gp, Q, gq) : gq;
     }
-    segment_pq[segment * kWidth + channel] = make_float2(P, Q);
+    segment_p[w.thread] = P;
+    segment_q[w.thread] = Q;
   }
   __syncthreads();
 #pragma unroll
-  for (uint32_t i = 0; i < kSegment; ++i) group_ab[(segment * kSegment + i) * kWidth + channel].x = states[i];
-  if (thread < kWidth) {
-    const uint64_t at = (uint64_t)s * a.D + d0 + channel;
-    const uint32_t last = len ? (len - 1) / steps : 0;
-    float back = 0.0f;  // what enters the tile from behind
-    if (is && a.dh_last && tile == last) back = a.dh_last[at];
-    if (len == 0 && tile == 0 && is && a.dh0) a.dh0[at] = back;
-    if (kChained && t0 < len && __ballot(is)) {
+  for (uint32_t i = 0; i < kSegment; ++i) group_a[(w.segment * kSegment + i) * kWidth + w.channel] = states[i];
+  const uint32_t last = len ? (len - 1) / w.steps : 0;
+  float back_in = 0.0f;  // what enters the chain from behind; then what enters the tile
+  if (speaks && a.dh_last && tile <= last && last - tile < kStretch) back_in = a.dh_last[(uint64_t)s * a.D + d0 + w.channel];
+  if (speaks && a.dh0 && tile == 0 && len == 0) a.dh0[(uint64_t)s * a.D + d0 + w.channel] = back_in;
+  if constexpr (kChained) {
+    if (t0 < len) {
       float P = 1.0f, Q = 0.0f;
-      bool cut = false;
-      for (uint32_t i = segments; i-- > 0;) {
-        const float2 c = segment_pq[i * kWidth + channel];
-        const bool passes = on.all_of_segment(i);
-        cut = cut || !passes;
-        P = passes ? P * c.x : 0.0f;
-        Q = passes ? __builtin_fmaf(c.x, Q, c.y) : c.y;
-      }
-      const auto words = [&](uint32_t behind) { return TileWords(chain.space, (uint64_t)column * chain.tiles + tile + 1 + behind, kWidth); };
-      const TileWords own(chain.space, (uint64_t)column * chain.tiles + tile, kWidth);
-      if (is && tile < last) {
-        publish(own.a + channel, tagged(P, cut ? tag | kCutTag : tag));
-        publish(own.b + channel, tagged(Q, tag));
-      }
-      if (is && cut) publish(own.state + channel, tagged(Q, tag));
-      if (tile < last) back = look_back(words, channel, is, min(last - tile, kWave), tag);
-      if (is && !cut) publish(own.state + channel, tagged(__builtin_fmaf(P, back, Q), tag));
-    }
-    for (uint32_t i = segments; i-- > 0;) {
-      segment_in[i * kWidth + channel] = back;
-      const float2 c = segment_pq[i * kWidth + channel];
-      back = on.all_of_segment(i) ? __builtin_fmaf(c.x, back, c.y) : c.y;
+      if (w.thread < kWidth)
+        for (uint32_t i = w.segments; i-- > 0;) {
+          const float sp = segment_p[i * kWidth + w.channel], sq = segment_q[i * kWidth + w.channel];
+          const bool passes = on.all_of_segment(i);
+          P = passes ? P * sp : 0.0f;
+          Q = passes ? __builtin_fmaf(sp, Q, sq) : sq;
+        }
+      back_in = chain_state(chain.space->word + (uint64_t)column * chain.tiles * 3 * kWidth, last - tile, is, P, Q, !no_cut, back_in, tag,
+                            sh_chain);
     }
   }
+  if (w.thread < kWidth)
+    for (uint32_t i = w.segments; i-- > 0;) {
+      segment_in[i * kWidth + w.channel] = back_in;
+      const float sp = segment_p[i * kWidth + w.channel], sq = segment_q[i * kWidth + w.channel];
+      back_in = on.all_of_segment(i) ? __builtin_fmaf(sp, back_in, sq) : sq;
+    }
   __syncthreads();
   uint32_t before = 0;
-  if (kChained && thread == threads - 1) before = leaving(chain);
+  if (kChained && w.thread == w.threads - 1) before = leaving(chain);
   {
-    float back = segment_in[segment * kWidth + channel];
+    float back = segment_in[w.thread];
 #pragma unroll
     for (uint32_t i = kSegment; i-- > 0;) {
-      float2 *const at = group_pq + (segment * kSegment + i) * kWidth + channel;
-      const float2 c = *at;
-      at->x = back;
-      back = on.of_group(segment * kSegment + i) == 15u ? __builtin_fmaf(c.x, back, c.y) : c.y;
+      const uint32_t at = (w.segment * kSegment + i) * kWidth + w.channel;
+      const float gp = group_p[at], gq = group_q[at];
+      group_p[at] = back;
+      back = no_cut || on.of_group(w.segment * kSegment + i) == 15u ? __builtin_fmaf(gp, back, gq) : gq;
     }
   }
   __syncthreads();
   if (exists) {
-    float prev[kTileRows][N], back[N];
+    f32x4 back = *reinterpret_cast<const f32x4 *>(group_p + w.group * kWidth + w.run);
+    f32x4 prev[kTileRows];
+    prev[0] = *reinterpret_cast<const f32x4 *>(group_a + w.group * kWidth + w.run);
+    T *const dg = static_cast<T *>(a.dg) + s * a.dg_seq + t_group * a.dg_time;
+    T *const dx = static_cast<T *>(a.dx) + s * a.dx_seq + t_group * a.dx_time;
+    plainly(plain, [&](auto is_plain) {
+      constexpr bool kPlain = decltype(is_plain)::value;
 #pragma unroll
-    for (uint32_t e = 0; e < N; ++e) {
-      prev[0][e] = group_ab[group * kWidth + run + e].x;
-      back[e] = group_pq[group * kWidth + run + e].x;
-    }
+      for (uint32_t l = 0; l < kTileRows; ++l) {
+        const bool inside = kPlain || t_group + l < len, passes = kPlain || (into >> l & 1);
 #pragma unroll
-    for (uint32_t l = 0; l < kTileRows; ++l) {
-      const bool inside = t_group + l < len, passes = into >> l & 1;
-#pragma unroll
-      for (uint32_t e = 0; e < N; ++e) {
-        if (!passes) prev[l][e] = 0.0f;
-        if (l + 1 < kTileRows) {
-          const float xt = inside ? element<N, T>(xr[l], e) : 0.0f;
-          prev[(l + 1) % kTileRows][e] = __builtin_fmaf(f[l][e], prev[l][e], kGate == APEX_GATE_SIGMOID ? rest[l][e] * xt : xt);
+        for (uint32_t e = 0; e < N; ++e) {
+          if (!passes) prev[l][e] = 0.0f;
+          if (l + 1 < kTileRows) {
+            const float xt = inside ? element<N, T>(xr[l], e) : 0.0f;
+            prev[(l + 1) % kTileRows][e] = __builtin_fmaf(f[l][e], prev[l][e], kGate == APEX_GATE_SIGMOID ? rest[l][e] * xt : xt);
+          }
         }
       }
-    }
-    T *const dg = static_cast<T *>(a.dg) + s * a.dg_seq, *const dx = static_cast<T *>(a.dx) + s * a.dx_seq;
 #pragma unroll
-    for (uint32_t l = kTileRows; l-- > 0;) {
-      const uint32_t t = t_group + l;
-      const bool inside = t < len, passes = bits >> l & 1;
-      Run<T, N> dgr, dxr;
+      for (uint32_t l = kTileRows; l-- > 0;) {
+        const uint32_t t = t_group + l;
+        const bool inside = kPlain || t < len, passes = kPlain || (bits >> l & 1);
+        Run<T, N> dgr, dxr;
 #pragma unroll
-      for (uint32_t e = 0; e < N; ++e) {
-        float dgt = 0.0f, dxt = 0.0f;
-        if (inside) {
-          const float lambda = element<N, T>(hr[l], e) + (passes ? back[e] : 0.0f);
-          scan_gate_back<kGate>(f[l][e], rest[l][e], element<N, T>(xr[l], e), prev[l][e], lambda, &dgt, &dxt);
-          back[e] = f[l][e] * lambda;
+        for (uint32_t e = 0; e < N; ++e) {
+          float dgt = 0.0f, dxt = 0.0f;
+          if (inside) {
+            const float lambda = element<N, T>(hr[l], e) + (passes ? back[e] : 0.0f);
+            scan_gate_back<kGate>(f[l][e], rest[l][e], element<N, T>(xr[l], e), prev[l][e], lambda, &dgt, &dxt);
+            back[e] = f[l][e] * lambda;
+          }
+          dgr[e] = (T)dgt;
+          dxr[e] = (T)dxt;
         }
-        dgr[e] = (T)dgt;
-        dxr[e] = (T)dxt;
+        if (kPlain) {
+          *reinterpret_cast<Run<T, N> *>(dg + l * a.dg_time + d) = dgr;
+          *reinterpret_cast<Run<T, N> *>(dx + l * a.dx_time + d) = dxr;
+        } else if (t < a.T) {
+          store_run_of<T, N>(dg + l * a.dg_time, d, a.D, dgr);
+          store_run_of<T, N>(dx + l * a.dx_time, d, a.D, dxr);
+        }
       }
-      if (t < a.T) {
-        store_run_of<T, N>(dg + t * a.dg_time, d, a.D, dgr);
-        store_run_of<T, N>(dx + t * a.dx_time, d, a.D, dxr);
-      }
-    }
-    if (a.dh0 && t_group == 0 && len > 0) {
-      Run<float, N> r;
-#pragma unroll
-      for (uint32_t e = 0; e < N; ++e) r[e] = back[e];
-      store_run_of<float, N>(a.dh0 + (uint64_t)s * a.D, d, a.D, r);
-    }
+    });
+    if (a.dh0 && t_group == 0 && len > 0) store_run_of<float, N>(a.dh0 + (uint64_t)s * a.D, d, a.D, back);
   }
-  if (kChained && thread == threads - 1) left(chain, before, tag);
+  if (kChained && w.thread == w.threads - 1) left(chain, before, tag);
 }
 
 constexpr uint32_t kChannelThreads = 64;
@@ -777,7 +910,7 @@ int scan_launch(uint32_t S, uint32_t T, uint32_t D, bool back, void *workspace, 
     l->threads = kChainThreads;
     l->chain.tiles = blocks_for(T, kChainSteps);
     const uint64_t tiles = (uint64_t)columns * l->chain.tiles;
-    if (tiles > 0xffffffffull / kChainThreads) return APEX_ERR_TOO_LARGE;
+    if (l->chain.tiles > kMostTiles || tiles > 0xffffffffull / kChainThreads) return APEX_ERR_TOO_LARGE;
     l->grid = (uint32_t)tiles;
   }
   l->lds = back ? tile_back_lds(l->threads) : tile_lds(l->threads);
