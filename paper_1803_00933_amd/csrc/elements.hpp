@@ -32,6 +32,18 @@ __device__ __forceinline__ float element(const Run<T, N> &r, int i)
     return (float)r[i];
 }
 
+// Keeps a run of 16-bit elements as it is from here on: what they are in 32 bits, where it was needed before, is not held in
+// registers until it is needed again.
+template <int N, typename T>
+__device__ __forceinline__ void hold_packed(Run<T, N> &r)
+{
+  if constexpr (sizeof(T) == 2 && N == 4) {
+    uint64_t bits = __builtin_bit_cast(uint64_t, r);
+    asm volatile("" : "+v"(bits));
+    r = __builtin_bit_cast(Run<T, N>, bits);
+  }
+}
+
 // One step of a reduction with data-parallel primitives: a lane to which the control routes no value takes `none`.
 template <int kCtrl, int kRowMask>
 __device__ __forceinline__ float dpp_from(float v, float none)

@@ -137,7 +137,7 @@ __device__ __forceinline__ uint32_t next_tag(uint32_t epoch)  // never that of m
 constexpr uint32_t kMostTiles = 1u << 22;  // of a chain: its words are counted in 32 bits
 constexpr uint32_t kMostPolls = 1u << 20;  // a wait gives up (and hands on NaN) where the workspace was not as required
 
-constexpr uint32_t kStretch = 8;  // tiles of a stretch
+constexpr uint32_t kStretch = 4;  // tiles of a stretch
 constexpr uint32_t kWindow = 16;  // compositions that a workgroup fetches at once
 
 __device__ __forceinline__ bool carries(uint64_t word, uint32_t tag) { return ((uint32_t)(word >> 32) & ~kCutTag) == tag; }
@@ -347,14 +347,24 @@ __device__ __forceinline__ bool uncut(const RowBits &bits, uint32_t steps)
   return missing == 0;
 }
 
-// f(integral_constant<bool>): the common case apart, in which no element has to be asked whether it counts.
-template <typename F>
+// f(integral_constant<bool>): tiles in which every row passes on apart, without the branches that would keep the rows' gates
+// from running side by side.  Not where a call is one tile deep: twice the code to fetch cost more there (64 x 96 x 1024 13.8 us
+// with, 11.4 without).
+template <bool kApart, typename F>
 __device__ __forceinline__ void plainly(bool plain, F f)
 {
-  if (plain)
+  if (kApart && plain)
     f(std::integral_constant<bool, true>());
   else
     f(std::integral_constant<bool, false>());
+}
+
+// What stands for a step that a sequence does not have: one that leaves a state as it is, a = 1, b = 0.
+template <typename T, int kGate, int N>
+__device__ __forceinline__ void no_step(Run<T, N> *g, Run<T, N> *x)
+{
+#pragma unroll
+  for (int e = 0; e < N; ++e) (*g)[e] = (T)(kGate == APEX_GATE_SIGMOID ? __builtin_inff() : 1.0f), (*x)[e] = (T)0.0f;
 }
 
 // kChained: tiles of a sequence wait for one another; else a sequence has one tile.
@@ -394,7 +404,10 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     } else {
 #pragma unroll
       for (uint32_t l = 0; l < kTileRows; ++l)
-        if (exists && t_group + l < len) gr[l] = run_of<T, N>(g + l * a.g_time, d, a.D), xr[l] = run_of<T, N>(x + l * a.x_time, d, a.D);
+        if (exists && t_group + l < len)
+          gr[l] = run_of<T, N>(g + l * a.g_time, d, a.D), xr[l] = run_of<T, N>(x + l * a.x_time, d, a.D);
+        else
+          no_step<T, kGate, N>(&gr[l], &xr[l]);
     }
   }
   if (w.thread < w.steps) {
@@ -404,29 +417,22 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
   }
   __syncthreads();
   const uint32_t bits = into.of_group(w.group);
-  const bool no_cut = uncut(into, w.steps), plain = whole && no_cut;
+  const bool no_cut = uncut(into, w.steps);
   float fa[kTileRows][N], fb[kTileRows][N];
-  plainly(plain, [&](auto is_plain) {
+  plainly<kChained>(no_cut, [&](auto is_plain) {
     constexpr bool kPlain = decltype(is_plain)::value;
     f32x4 A, B;
 #pragma unroll
     for (uint32_t e = 0; e < N; ++e) A[e] = 1.0f, B[e] = 0.0f;
 #pragma unroll
     for (uint32_t l = 0; l < kTileRows; ++l) {
-      const bool inside = kPlain || (exists && t_group + l < len), passes = kPlain || (bits >> l & 1);
+      if (!kPlain && !(bits >> l & 1)) A = B = f32x4{};
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) {
-        float f = 1.0f, b = 0.0f, rest;
-        if (inside) scan_gate<kGate>(element<N, T>(gr[l], e), element<N, T>(xr[l], e), &f, &rest, &b);
-        fa[l][e] = f;
-        fb[l][e] = b;
-        if (l == 0) {
-          A[e] = passes ? f : 0.0f;
-          B[e] = b;
-        } else {
-          A[e] = passes ? A[e] * f : 0.0f;
-          B[e] = passes ? __builtin_fmaf(f, B[e], b) : b;
-        }
+        float rest;
+        scan_gate<kGate>(element<N, T>(gr[l], e), element<N, T>(xr[l], e), &fa[l][e], &rest, &fb[l][e]);
+        A[e] *= fa[l][e];
+        B[e] = __builtin_fmaf(fa[l][e], B[e], fb[l][e]);
       }
     }
     *reinterpret_cast<f32x4 *>(group_a + w.group * kWidth + w.run) = A;
@@ -497,31 +503,30 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
       store_run_of<float, N>(c, d, a.D, r);
     }
     T *const h = static_cast<T *>(a.h) + ((uint64_t)s * a.T + t_group) * a.D;
-    plainly(plain, [&](auto is_plain) {
-      constexpr bool kPlain = decltype(is_plain)::value;
+    plainly<kChained>(no_cut, [&](auto is_plain) {
+    constexpr bool kPlain = decltype(is_plain)::value;
 #pragma unroll
-      for (uint32_t l = 0; l < kTileRows; ++l) {
-        const uint32_t t = t_group + l;
-        const bool passes = kPlain || (bits >> l & 1);
-        Run<T, N> r;
+    for (uint32_t l = 0; l < kTileRows; ++l) {
+      const uint32_t t = t_group + l;
+      if (!kPlain && !(bits >> l & 1)) state = f32x4{};
+      Run<T, N> r;
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e) {
-          state[e] = passes ? __builtin_fmaf(fa[l][e], state[e], fb[l][e]) : fb[l][e];
-          r[e] = kPlain || t < len ? (T)state[e] : (T)0.0f;
-        }
-        T *const to = h + (uint64_t)l * a.D;
-        if (kPlain)
-          *reinterpret_cast<Run<T, N> *>(to + d) = r;
-        else if (t < a.T)
-          store_run_of<T, N>(to, d, a.D, r);
-        if (a.h_last && t + 1 == len) {
-          const bool on = !a.discount || a.discount[(uint64_t)s * a.T + t] != 0.0f;
-          f32x4 out;
-#pragma unroll
-          for (uint32_t e = 0; e < N; ++e) out[e] = on ? state[e] : 0.0f;
-          store_run_of<float, N>(a.h_last + (uint64_t)s * a.D, d, a.D, out);
-        }
+      for (uint32_t e = 0; e < N; ++e) {
+        state[e] = __builtin_fmaf(fa[l][e], state[e], fb[l][e]);
+        r[e] = (T)state[e];
       }
+      T *const to = h + (uint64_t)l * a.D;
+      if (whole) {
+        *reinterpret_cast<Run<T, N> *>(to + d) = r;
+      } else if (t < a.T) {
+        if (t >= len) r = Run<T, N>{};
+        store_run_of<T, N>(to, d, a.D, r);
+      }
+      if (a.h_last && t + 1 == len) {
+        const bool on = !a.discount || a.discount[(uint64_t)s * a.T + t] != 0.0f;
+        store_run_of<float, N>(a.h_last + (uint64_t)s * a.D, d, a.D, on ? state : f32x4{});
+      }
+    }
     });
   }
   if (kChained && w.thread == w.threads - 1) left(chain, before, tag);
@@ -582,6 +587,9 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, 4) void
           gr[l] = run_of<T, N>(g + l * a.g_time, d, a.D);
           xr[l] = run_of<T, N>(x + l * a.x_time, d, a.D);
           hr[l] = run_of<T, N>(dh + (uint64_t)l * a.D, d, a.D);
+        } else {
+          no_step<T, kGate, N>(&gr[l], &xr[l]);
+          hr[l] = Run<T, N>{};
         }
     }
   }
@@ -597,42 +605,32 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, 4) void
   }
   __syncthreads();
   const uint32_t bits = on.of_group(w.group);
-  const bool no_cut = uncut(on, w.steps), plain = whole && no_cut;
+  const bool no_cut = uncut(on, w.steps);
   const uint32_t into = (uint32_t)((on.word[w.group / kChunkGroups] << 1 | 1) >> (w.group % kChunkGroups * kTileRows)) & 15u;
   float f[kTileRows][N], rest[kTileRows][N];
-  plainly(plain, [&](auto is_plain) {
+  plainly<kChained>(no_cut, [&](auto is_plain) {
     constexpr bool kPlain = decltype(is_plain)::value;
     f32x4 A, B, P, Q;
 #pragma unroll
+    for (uint32_t e = 0; e < N; ++e) A[e] = P[e] = 1.0f, B[e] = Q[e] = 0.0f;
+#pragma unroll
     for (uint32_t l = 0; l < kTileRows; ++l) {
-      const bool inside = kPlain || (exists && t_group + l < len), passes = kPlain || (into >> l & 1);
+      if (!kPlain && !(into >> l & 1)) A = B = f32x4{};
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) {
-        float b = 0.0f;
-        f[l][e] = 1.0f, rest[l][e] = 0.0f;
-        if (inside) scan_gate<kGate>(element<N, T>(gr[l], e), element<N, T>(xr[l], e), &f[l][e], &rest[l][e], &b);
-        if (l == 0) {
-          A[e] = passes ? f[l][e] : 0.0f;
-          B[e] = b;
-        } else {
-          A[e] = passes ? A[e] * f[l][e] : 0.0f;
-          B[e] = passes ? __builtin_fmaf(f[l][e], B[e], b) : b;
-        }
+        float b;
+        scan_gate<kGate>(element<N, T>(gr[l], e), element<N, T>(xr[l], e), &f[l][e], &rest[l][e], &b);
+        A[e] *= f[l][e];
+        B[e] = __builtin_fmaf(f[l][e], B[e], b);
       }
     }
 #pragma unroll
     for (uint32_t l = kTileRows; l-- > 0;) {
-      const bool inside = kPlain || (exists && t_group + l < len), passes = kPlain || (bits >> l & 1);
+      if (!kPlain && !(bits >> l & 1)) P = Q = f32x4{};
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) {
-        const float dht = inside ? element<N, T>(hr[l], e) : 0.0f;
-        if (l == kTileRows - 1) {
-          P[e] = passes ? f[l][e] : 0.0f;
-          Q[e] = f[l][e] * dht;
-        } else {
-          P[e] = passes ? P[e] * f[l][e] : 0.0f;
-          Q[e] = f[l][e] * (passes ? Q[e] + dht : dht);
-        }
+        P[e] *= f[l][e];
+        Q[e] = f[l][e] * (Q[e] + element<N, T>(hr[l], e));
       }
     }
     const uint32_t at = w.group * kWidth + w.run;
@@ -641,6 +639,13 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, 4) void
     *reinterpret_cast<f32x4 *>(group_p + at) = P;
     *reinterpret_cast<f32x4 *>(group_q + at) = Q;
   });
+#pragma unroll
+  for (uint32_t l = 0; l < kTileRows; ++l) {
+    hold_packed<N, T>(xr[l]);
+    hold_packed<N, T>(hr[l]);
+#pragma unroll
+    for (uint32_t e = 0; e < N; ++e) asm volatile("" : "+v"(rest[l][e]));  // nor are its products held
+  }
   __syncthreads();
   // the states that enter the groups of a segment, from the chunk's; the segment's composition, from its last group
   float states[kSegment];
@@ -716,44 +721,41 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, 4) void
     prev[0] = *reinterpret_cast<const f32x4 *>(group_a + w.group * kWidth + w.run);
     T *const dg = static_cast<T *>(a.dg) + s * a.dg_seq + t_group * a.dg_time;
     T *const dx = static_cast<T *>(a.dx) + s * a.dx_seq + t_group * a.dx_time;
-    plainly(plain, [&](auto is_plain) {
-      constexpr bool kPlain = decltype(is_plain)::value;
+    plainly<kChained>(no_cut, [&](auto is_plain) {
+    constexpr bool kPlain = decltype(is_plain)::value;
 #pragma unroll
-      for (uint32_t l = 0; l < kTileRows; ++l) {
-        const bool inside = kPlain || t_group + l < len, passes = kPlain || (into >> l & 1);
-#pragma unroll
-        for (uint32_t e = 0; e < N; ++e) {
-          if (!passes) prev[l][e] = 0.0f;
-          if (l + 1 < kTileRows) {
-            const float xt = inside ? element<N, T>(xr[l], e) : 0.0f;
-            prev[(l + 1) % kTileRows][e] = __builtin_fmaf(f[l][e], prev[l][e], kGate == APEX_GATE_SIGMOID ? rest[l][e] * xt : xt);
-          }
-        }
-      }
-#pragma unroll
-      for (uint32_t l = kTileRows; l-- > 0;) {
-        const uint32_t t = t_group + l;
-        const bool inside = kPlain || t < len, passes = kPlain || (bits >> l & 1);
-        Run<T, N> dgr, dxr;
+    for (uint32_t l = 0; l < kTileRows; ++l) {
+      if (!kPlain && !(into >> l & 1)) prev[l] = f32x4{};
+      if (l + 1 < kTileRows)
 #pragma unroll
         for (uint32_t e = 0; e < N; ++e) {
-          float dgt = 0.0f, dxt = 0.0f;
-          if (inside) {
-            const float lambda = element<N, T>(hr[l], e) + (passes ? back[e] : 0.0f);
-            scan_gate_back<kGate>(f[l][e], rest[l][e], element<N, T>(xr[l], e), prev[l][e], lambda, &dgt, &dxt);
-            back[e] = f[l][e] * lambda;
-          }
-          dgr[e] = (T)dgt;
-          dxr[e] = (T)dxt;
+          const float xt = element<N, T>(xr[l], e);
+          prev[(l + 1) % kTileRows][e] = __builtin_fmaf(f[l][e], prev[l][e], kGate == APEX_GATE_SIGMOID ? rest[l][e] * xt : xt);
         }
-        if (kPlain) {
-          *reinterpret_cast<Run<T, N> *>(dg + l * a.dg_time + d) = dgr;
-          *reinterpret_cast<Run<T, N> *>(dx + l * a.dx_time + d) = dxr;
-        } else if (t < a.T) {
-          store_run_of<T, N>(dg + l * a.dg_time, d, a.D, dgr);
-          store_run_of<T, N>(dx + l * a.dx_time, d, a.D, dxr);
-        }
+    }
+#pragma unroll
+    for (uint32_t l = kTileRows; l-- > 0;) {
+      const uint32_t t = t_group + l;
+      if (!kPlain && !(bits >> l & 1)) back = f32x4{};
+      Run<T, N> dgr, dxr;
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) {
+        float dgt, dxt;
+        const float lambda = element<N, T>(hr[l], e) + back[e];
+        scan_gate_back<kGate>(f[l][e], rest[l][e], element<N, T>(xr[l], e), prev[l][e], lambda, &dgt, &dxt);
+        back[e] = f[l][e] * lambda;
+        dgr[e] = (T)dgt;
+        dxr[e] = (T)dxt;
       }
+      if (whole) {
+        *reinterpret_cast<Run<T, N> *>(dg + l * a.dg_time + d) = dgr;
+        *reinterpret_cast<Run<T, N> *>(dx + l * a.dx_time + d) = dxr;
+      } else if (t < a.T) {
+        if (t >= len) dgr = dxr = Run<T, N>{};
+        store_run_of<T, N>(dg + l * a.dg_time, d, a.D, dgr);
+        store_run_of<T, N>(dx + l * a.dx_time, d, a.D, dxr);
+      }
+    }
     });
     if (a.dh0 && t_group == 0 && len > 0) store_run_of<float, N>(a.dh0 + (uint64_t)s * a.D, d, a.D, back);
   }
