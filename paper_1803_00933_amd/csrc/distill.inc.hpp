@@ -21,16 +21,26 @@ struct DistillArgs {
   void *grad;
 };
 
-// The named tokens of a row, in LDS: a table by open addressing, and a bit for each run of the row that holds one.
+// The named tokens of a row, in LDS: a table by open addressing, and a bit for every token.
 struct Named {
   int32_t *key;       // [H] token, or -1
   uint32_t *place;    // [H] the first place that names it; later, as a float, the token's gradient
+  float *z;           // [H] the student's logit
   int32_t *slot;      // [K] the table's entry of a place; -1: empty
-  float *value, *z;   // [K] teacher's and student's logits
-  uint64_t *runs;
+  double *q;          // [K] the teacher's probability
+  float *value;       // [K] the teacher's logit
+  uint32_t *bits;     // [ceil(V / 64)] words of 64 bits
   uint32_t H;
 
   __device__ __forceinline__ uint32_t hash(int32_t token) const { return ((uint32_t)token * 2654435761u) >> (32 - __builtin_ctz(H)); }
+
+  // Which of the N tokens of a run are named.
+  template <uint32_t N>
+  __device__ __forceinline__ uint32_t mask(uint32_t run) const
+  {
+    const uint32_t byte = reinterpret_cast<const uint8_t *>(bits)[run * N / 8];
+    return N == 8 ? byte : byte >> (run % 2 * 4) & 15u;
+  }
 
   __device__ __forceinline__ int32_t find(int32_t token) const
   {
@@ -47,22 +57,22 @@ __host__ __device__ constexpr uint32_t distill_table(uint32_t K)
   while (H < 2 * K) H *= 2;
   return H;
 }
-// Bytes of LDS of a row of `runs` runs.
-__host__ __device__ constexpr uint32_t distill_lds(uint32_t K, uint32_t runs)
+__host__ __device__ constexpr uint32_t distill_lds(uint32_t K, uint32_t V)  // bytes
 {
-  return (runs + 63) / 64 * 8 + distill_table(K) * 8 + K * 12;
+  return (V + 63) / 64 * 8 + distill_table(K) * 12 + K * 16;
 }
 
-__device__ __forceinline__ Named named_in(uint64_t *lds, uint32_t K, uint32_t H, uint32_t runs)
+__device__ __forceinline__ Named named_in(uint64_t *lds, uint32_t K, uint32_t H, uint32_t V)
 {
   Named n;
   n.H = H;
-  n.runs = lds;
-  n.key = reinterpret_cast<int32_t *>(lds + (runs + 63) / 64);
+  n.bits = reinterpret_cast<uint32_t *>(lds);
+  n.q = reinterpret_cast<double *>(lds + (V + 63) / 64);
+  n.key = reinterpret_cast<int32_t *>(n.q + K);
   n.place = reinterpret_cast<uint32_t *>(n.key + H);
-  n.slot = reinterpret_cast<int32_t *>(n.place + H);
+  n.z = reinterpret_cast<float *>(n.place + H);
+  n.slot = reinterpret_cast<int32_t *>(n.z + H);
   n.value = reinterpret_cast<float *>(n.slot + K);
-  n.z = n.value + K;
   return n;
 }
 
@@ -78,21 +88,6 @@ struct Sum {
   float m, s;
   __device__ __forceinline__ static float ref(float m, float c) { return m == -__builtin_inff() ? 0.0f : __builtin_rintf(m * c); }
 };
-
-// Logits [run * N, run * N + N) of a row, -inf beyond its end.
-template <typename T, int N>
-__device__ __forceinline__ void logits_of(const T *row, uint32_t run, uint32_t V, float (&z)[N])
-{
-  const uint32_t at = run * N;
-  if (at + N <= V) {
-    const Run<T, N> r = load_run<T, N>(row + at);
-#pragma unroll
-    for (int e = 0; e < N; ++e) z[e] = element<N, T>(r, e);
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e) z[e] = at + e < V ? (float)row[at + e] : -__builtin_inff();
-  }
-}
 
 template <int N>
 __device__ __forceinline__ void add_to(Sum &a, const float (&z)[N], float c)
@@ -142,167 +137,244 @@ struct RowGradient {
   bool zero;  // the row's weight is 0
 };
 
-// The teacher's side, by one wave, once the row's sum `all` (without the named tokens if there is a rest class) is known:
-// writes loss and lse, leaves the gradients of the named tokens in the table.
-__device__ __forceinline__ RowGradient settle_row(const DistillArgs &a, const Named &n, uint32_t row, Sum all)
+// Enters place k's token.
+__device__ __forceinline__ void enter_named(const DistillArgs &a, const Named &n, uint32_t k, int32_t token, float value)
+{
+  int32_t slot = -1;
+  if (token >= 0 && (uint32_t)token < a.V) {
+    for (uint32_t i = n.hash(token); slot < 0; i = (i + 1) & (a.H - 1)) {
+      const int32_t had = atomicCAS(n.key + i, -1, token);
+      if (had == -1 || had == token) slot = (int32_t)i;
+    }
+    atomicMin(n.place + slot, k);
+    atomicOr(n.bits + token / 32, 1u << (token % 32));
+    n.value[k] = value;
+  }
+  n.slot[k] = slot;
+}
+
+// What a wave knows of a row's teacher.
+struct Teacher {
+  double ln_sum;    // log-sum-exp that ln q is relative to
+  float mass;       // sum of q
+  uint32_t named;   // places that count
+  bool teaches;     // not -inf for every one of them
+};
+
+constexpr double kLn2d = 0.6931471805599453;
+
+// ln of a sum of 2^(z c - R) whose largest z is m; c, as rounded, only scales what is relative to m.
+__device__ __forceinline__ double log_sum(const DistillArgs &a, float m, float R, float sum)
+{
+  if (m == -__builtin_inff()) return -__builtin_inf();
+  return __builtin_fma((double)m, a.inv_tau, ln_of(sum) + kLn2d * __builtin_fma(-(double)m, (double)a.c, (double)R));
+}
+
+// The part of a row that needs no sum over the vocabulary, by one wave: drops places whose token an earlier one names, and leaves
+// the q of the others.
+__device__ __forceinline__ Teacher teach(const DistillArgs &a, const Named &n, uint32_t row)
 {
   const uint32_t lane = lane_id();
-  const float c = a.c;
-  const bool rest_class = a.top_lse != nullptr;
   uint32_t mine = 0;
-  float t_top = -__builtin_inff(), z_top = -__builtin_inff();
-  for (uint32_t k = lane; k < a.K; k += kWave)
-    if (n.slot[k] >= 0) {
-      ++mine;
-      t_top = fmaxf(t_top, n.value[k]);
-      z_top = fmaxf(z_top, n.z[k]);
-    }
-  const uint32_t named = (uint32_t)wave_sum((float)mine);  // at most APEX_MAX_TOP
-  t_top = wave_max(t_top);
-  const float t_R = Sum::ref(t_top, c);
-  const float R_rest = Sum::ref(all.m, c), s_rest = all.s;
-  float R = R_rest, s = s_rest;
-  if (rest_class) {
-    z_top = fmaxf(wave_max(z_top), all.m);
-    R = Sum::ref(z_top, c);
+  float top = -__builtin_inff();
+  for (uint32_t k = lane; k < a.K; k += kWave) {
+    const int32_t slot = n.slot[k];
+    if (slot >= 0 && n.place[slot] != k) n.slot[k] = -1;
+    else if (slot >= 0) ++mine, top = fmaxf(top, n.value[k]);
   }
-  float t_sum = 0.0f, z_sum = 0.0f;
+  Teacher t;
+  t.named = (uint32_t)wave_sum((float)mine);  // at most APEX_MAX_TOP
+  top = wave_max(top);
+  const float R = Sum::ref(top, a.c);
+  float sum = 0.0f;
+  for (uint32_t k = lane; k < a.K; k += kWave)
+    if (n.slot[k] >= 0) sum += exp2_of(__builtin_fmaf(n.value[k], a.c, -R));
+  sum = wave_sum(sum);
+  t.teaches = sum != 0.0f;
+  t.ln_sum = a.top_lse ? (double)a.top_lse[row] : log_sum(a, top, R, sum);
+  float mass = 0.0f;
   for (uint32_t k = lane; k < a.K; k += kWave)
     if (n.slot[k] >= 0) {
-      t_sum += exp2_of(__builtin_fmaf(n.value[k], c, -t_R));
-      z_sum += exp2_of(__builtin_fmaf(n.z[k], c, -R));
+      const double q = t.teaches ? exp_of(__builtin_fma((double)n.value[k], a.inv_tau, -t.ln_sum)) : 0.0;
+      n.q[k] = q;
+      mass += (float)q;
     }
-  t_sum = wave_sum(t_sum);
-  if (rest_class) s = wave_sum(z_sum) + (s_rest == 0.0f ? 0.0f : s_rest * exp2_of(R_rest - R));
+  t.mass = wave_sum(mass);
+  return t;
+}
+
+// The rest of it, by the same wave, once the row's sum `all` (without the named tokens if there is a rest class) is known: writes
+// loss and lse, leaves the gradients of the named tokens in the table.
+// Logarithms of nearly equal numbers are subtracted: in 64 bits, a few operations for each named token.
+__device__ __forceinline__ RowGradient settle(const DistillArgs &a, const Named &n, uint32_t row, const Teacher &t, Sum all)
+{
+  const uint32_t lane = lane_id();
+  const float R_rest = Sum::ref(all.m, a.c), w = a.weight ? a.weight[row] : 1.0f, wt = w * a.grad_scale;
+  float top = all.m, R = R_rest, s = all.s;
+  if (a.top_lse) {
+    float z_top = -__builtin_inff(), z_sum = 0.0f;
+    for (uint32_t k = lane; k < a.K; k += kWave)
+      if (n.slot[k] >= 0) z_top = fmaxf(z_top, n.z[n.slot[k]]);
+    top = fmaxf(wave_max(z_top), all.m);
+    R = Sum::ref(top, a.c);
+    for (uint32_t k = lane; k < a.K; k += kWave)
+      if (n.slot[k] >= 0) z_sum += exp2_of(__builtin_fmaf(n.z[n.slot[k]], a.c, -R));
+    s = wave_sum(z_sum) + (all.s == 0.0f ? 0.0f : all.s * exp2_of(R_rest - R));
+  }
   if (s == 0.0f) s = __builtin_nanf("");  // no finite logit
   const float inv_s = 1.0f / s;
-  // Logarithms of nearly equal numbers are subtracted below: in 64 bits, a few operations for each named token.
-  const auto log_sum = [&](float m, float ref, float sum) {  // of a Sum; c, as rounded, only scales what is relative to m
-    if (m == -__builtin_inff()) return -__builtin_inf();
-    return __builtin_fma((double)m, a.inv_tau, (ln_of(sum) + 0.6931471805599453 * __builtin_fma(-(double)m, (double)c, (double)ref)));
-  };
-  const double ln_all = log_sum(rest_class ? z_top : all.m, R, s);
-  const double ln_teacher = rest_class ? (double)a.top_lse[row] : log_sum(t_top, t_R, t_sum);
-  const auto ln_q = [&](uint32_t k) { return __builtin_fma((double)n.value[k], a.inv_tau, -ln_teacher); };
-  const auto ln_p = [&](uint32_t k) { return __builtin_fma((double)n.z[k], a.inv_tau, -ln_all); };
-  const bool teaches = t_sum != 0.0f;  // not -inf for every place
-  float mass = 0.0f, loss = 0.0f;
-  for (uint32_t k = lane; k < a.K; k += kWave)
-    if (n.slot[k] >= 0 && teaches) {
-      const double l = ln_q(k);
-      const float q = (float)exp_of(l);
-      mass += q;
-      loss += q == 0.0f ? 0.0f : q * (float)(l - ln_p(k));
-    }
-  mass = wave_sum(mass);
-  loss = wave_sum(loss);
+  const double ln_all = log_sum(a, top, R, s);
   float rest = 0.0f;
-  if (rest_class && named < a.V) {
-    rest = mass > 1.0f ? 0.0f : 1.0f - mass;
-    if (rest != 0.0f) loss += rest * (float)(ln_of(rest) - (log_sum(all.m, R_rest, s_rest) - ln_all));
-  }
+  if (a.top_lse && t.named < a.V) rest = t.mass > 1.0f ? 0.0f : 1.0f - t.mass;
+  const double given = (double)t.mass + (double)rest;
+  float loss = 0.0f;
+  for (uint32_t k = lane; k < a.K; k += kWave)
+    if (n.slot[k] >= 0) {
+      const double q = n.q[k], ln_p = __builtin_fma((double)n.z[n.slot[k]], a.inv_tau, -ln_all);
+      if ((float)q != 0.0f) loss += (float)q * (float)(__builtin_fma((double)n.value[k], a.inv_tau, -t.ln_sum) - ln_p);
+      n.place[n.slot[k]] = __float_as_uint(w == 0.0f ? 0.0f : (float)(wt * (given * exp_of(ln_p) - q)));
+    }
+  loss = wave_sum(loss);
+  if (rest != 0.0f) loss += rest * (float)(ln_of(rest) - (log_sum(a, all.m, R_rest, all.s) - ln_all));
   if (s != s) loss = s;
   if (lane == 0) {
     a.loss[row] = loss;
     if (a.lse) a.lse[row] = (float)ln_all;
   }
-  const float w = a.weight ? a.weight[row] : 1.0f, wt = w * a.grad_scale;
-  for (uint32_t k = lane; k < a.K; k += kWave)
-    if (n.slot[k] >= 0) {
-      const double q = teaches ? exp_of(ln_q(k)) : 0.0;
-      n.place[n.slot[k]] = __float_as_uint(w == 0.0f ? 0.0f : (float)(wt * (((double)mass + (double)rest) * exp_of(ln_p(k)) - q)));
-    }
-  RowGradient g{R_rest, wt * (mass * inv_s), w == 0.0f};
-  if (rest_class) g.scale = s_rest == 0.0f ? 0.0f : wt * ((mass + rest) * inv_s * exp2_of(R_rest - R) - rest / s_rest);
+  RowGradient g{R_rest, wt * (t.mass * inv_s), w == 0.0f};
+  if (a.top_lse) g.scale = all.s == 0.0f ? 0.0f : wt * ((float)given * inv_s * exp2_of(R_rest - R) - rest / all.s);
   return g;
 }
 
-constexpr uint32_t kDistillThreads = 512;
-
-// A workgroup per row, which it reads twice: for the sum, and for the gradient.
-template <typename T>
-__global__ __launch_bounds__(kDistillThreads) void distill_rows_kernel(DistillArgs a)
+// A workgroup per row.  kHeld runs of 16 bytes of the row stay in a thread's registers from the sum to the gradient, so that the
+// row is read once; kHeld = 0: rows too long for that are read again.
+template <typename T, uint32_t kThreads, uint32_t kHeld>
+__global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
 {
-  constexpr int N = 16 / sizeof(T);
+  constexpr uint32_t N = 16 / sizeof(T), kWaves = kThreads / kWave;
   extern __shared__ uint64_t lds[];
-  __shared__ float red_m[kDistillThreads / kWave], red_s[kDistillThreads / kWave];
+  __shared__ float red_m[kWaves], red_s[kWaves];
   __shared__ RowGradient sh_gradient;
   const uint32_t thread = threadIdx.x, lane = lane_id(), wave = thread / kWave, row = blockIdx.x;
-  const uint32_t runs = (a.V + N - 1) / N;
-  const Named n = named_in(lds, a.K, a.H, runs);
+  const uint32_t runs = a.V / N, left = a.V % N;  // whole runs; the elements behind them: one each
+  const Named n = named_in(lds, a.K, a.H, a.V);
   const T *const z_row = static_cast<const T *>(a.logits) + row * a.row_stride;
-  for (uint32_t i = thread; i < (runs + 63) / 64; i += kDistillThreads) n.runs[i] = 0;
-  for (uint32_t i = thread; i < a.H; i += kDistillThreads) n.key[i] = -1, n.place[i] = 0xffffffffu;
-  __syncthreads();
-  for (uint32_t k = thread; k < a.K; k += kDistillThreads) {
-    const uint64_t at = (uint64_t)row * a.K + k;
-    const int32_t token = a.top_index[at];
-    int32_t slot = -1;
-    if (token >= 0 && (uint32_t)token < a.V) {
-      n.value[k] = typed_element(a.top_value, a.value_dtype, at);
-      n.z[k] = (float)z_row[token];
-      for (uint32_t i = n.hash(token); slot < 0; i = (i + 1) & (a.H - 1)) {
-        const int32_t had = atomicCAS(n.key + i, -1, token);
-        if (had == -1 || had == token) slot = (int32_t)i;
-      }
-      atomicMin(n.place + slot, k);
-      atomicOr(reinterpret_cast<unsigned long long *>(n.runs + (token / N) / 64), 1ull << ((token / N) % 64));
-    }
-    n.slot[k] = slot;
+  // The named tokens first: loads come back in order, and the table has to be there before the row is looked at.
+  int32_t token = -1;
+  float value = 0.0f;
+  if (thread < a.K) {
+    const uint64_t at = (uint64_t)row * a.K + thread;
+    token = a.top_index[at];
+    value = typed_element(a.top_value, a.value_dtype, at);
   }
-  __syncthreads();
-  for (uint32_t k = thread; k < a.K; k += kDistillThreads)
-    if (n.slot[k] >= 0 && n.place[n.slot[k]] != k) n.slot[k] = -1;  // named by an earlier place
-
-  Sum sum{-__builtin_inff(), 0.0f};
-  for (uint32_t run = thread; run < runs; run += kDistillThreads) {
-    float z[N];
-    logits_of<T, N>(z_row, run, a.V, z);
-    if (a.top_lse && (n.runs[run / 64] >> (run % 64) & 1)) {
+  Run<T, N> held[kHeld ? kHeld : 1];
 #pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (n.find((int32_t)(run * N + e)) >= 0) z[e] = -__builtin_inff();
+  for (uint32_t i = 0; i < kHeld; ++i) {
+    const uint32_t run = thread + i * kThreads;
+    if (run < runs) held[i] = load_run<T, N>(z_row + run * N);
+  }
+  float z_left = thread < left ? (float)z_row[runs * N + thread] : -__builtin_inff();
+  for (uint32_t i = thread; i < (a.V + 63) / 64 * 2; i += kThreads) n.bits[i] = 0;
+  for (uint32_t i = thread; i < a.H; i += kThreads) n.key[i] = -1, n.place[i] = 0xffffffffu;
+  lds_barrier();
+  if (thread < a.K) enter_named(a, n, thread, token, value);
+  for (uint32_t k = thread + kThreads; k < a.K; k += kThreads) {
+    const uint64_t at = (uint64_t)row * a.K + k;
+    enter_named(a, n, k, a.top_index[at], typed_element(a.top_value, a.value_dtype, at));
+  }
+  lds_barrier();
+  Teacher teacher;
+  if (wave == 0) teacher = teach(a, n, row);
+  // A named token's logit goes into the table; what the sum takes in its place.
+  const auto taken = [&](uint32_t at, float z) {
+    n.z[n.find((int32_t)at)] = z;
+    return a.top_lse ? -__builtin_inff() : z;
+  };
+  const bool left_named = thread < left && (n.bits[(runs * N + thread) / 32] >> (runs * N + thread) % 32 & 1);
+
+  // the sum of this thread's part of the row, without the named tokens if there is a rest class
+  Sum sum{-__builtin_inff(), 0.0f};
+  if (left_named) z_left = taken(runs * N + thread, z_left);
+  if constexpr (kHeld > 0) {
+    float top = z_left;
+#pragma unroll
+    for (uint32_t i = 0; i < kHeld; ++i) {
+      const uint32_t run = thread + i * kThreads;
+      if (run >= runs) continue;
+      if (const uint32_t named = n.mask<N>(run)) {
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e)
+          if (named >> e & 1) held[i][e] = (T)taken(run * N + e, element<N, T>(held[i], e));
+      }
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) top = fmaxf(top, element<N, T>(held[i], e));
+      hold_packed<N, T>(held[i]);
     }
-    add_to<N>(sum, z, a.c);
+    const float R = Sum::ref(top, a.c);
+    float s = exp2_of(__builtin_fmaf(z_left, a.c, -R));
+#pragma unroll
+    for (uint32_t i = 0; i < kHeld; ++i) {
+      if (thread + i * kThreads >= runs) continue;
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) s += exp2_of(__builtin_fmaf(element<N, T>(held[i], e), a.c, -R));
+      hold_packed<N, T>(held[i]);
+    }
+    sum = Sum{top, s};
+  } else {
+    const float alone[1] = {z_left};
+    add_to<1>(sum, alone, a.c);
+    for (uint32_t run = thread; run < runs; run += kThreads) {
+      const Run<T, N> r = load_run<T, N>(z_row + run * N);
+      float z[N];
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) z[e] = element<N, T>(r, e);
+      if (const uint32_t named = n.mask<N>(run)) {
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e)
+          if (named >> e & 1) z[e] = taken(run * N + e, z[e]);
+      }
+      add_to<N>(sum, z, a.c);
+    }
   }
   const float m = wave_max(sum.m), R = Sum::ref(m, a.c);
   const float s = wave_sum(sum.m == -__builtin_inff() ? sum.s : sum.s * exp2_of(Sum::ref(sum.m, a.c) - R));
   if (lane == 0) red_m[wave] = m, red_s[wave] = s;
   __syncthreads();
   if (wave == 0) {
-    constexpr uint32_t kWaves = kDistillThreads / kWave;
     const float wm = lane < kWaves ? red_m[lane] : -__builtin_inff(), ws = lane < kWaves ? red_s[lane] : 0.0f;
     const float top = wave_max(wm), top_R = Sum::ref(top, a.c);
     const Sum all{top, wave_sum(wm == -__builtin_inff() ? ws : ws * exp2_of(Sum::ref(wm, a.c) - top_R))};
-    const RowGradient g = settle_row(a, n, row, all);
+    const RowGradient g = settle(a, n, row, teacher, all);
     if (lane == 0) sh_gradient = g;
   }
   if (!a.grad) return;
   __syncthreads();
   const RowGradient g = sh_gradient;
   T *const out = static_cast<T *>(a.grad) + row * a.grad_stride;
-  for (uint32_t run = thread; run < runs; run += kDistillThreads) {
-    float z[N];
-    logits_of<T, N>(z_row, run, a.V, z);
-    const bool has_named = n.runs[run / 64] >> (run % 64) & 1;
-    const uint32_t at = run * N;
+  const float scale_low = g.scale * 0x1p-64f;
+  const auto gradient = [&](float z) { return power<T>(__builtin_fmaf(z, a.c, -g.R), g.scale, scale_low); };
+  if (thread < left) {
+    const float v = left_named ? __uint_as_float(n.place[n.find((int32_t)(runs * N + thread))]) : gradient(z_left);
+    out[runs * N + thread] = (T)(g.zero ? 0.0f : v);
+  }
+  const auto write = [&](uint32_t run, const Run<T, N> &z) {
     Run<T, N> r;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      float v = g.zero ? 0.0f : power<T>(__builtin_fmaf(z[e], a.c, -g.R), g.scale, g.scale * 0x1p-64f);
-      if (has_named) {
-        const int32_t slot = n.find((int32_t)(at + e));
-        if (slot >= 0) v = __uint_as_float(n.place[slot]);
-      }
-      r[e] = (T)v;
-    }
-    if (at + N <= a.V) {
-      *reinterpret_cast<Run<T, N> *>(out + at) = r;
-    } else {
+    for (uint32_t e = 0; e < N; ++e) r[e] = (T)gradient(element<N, T>(z, e));
+    if (const uint32_t named = n.mask<N>(run)) {
 #pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (at + e < a.V) out[at + e] = r[e];
+      for (uint32_t e = 0; e < N; ++e)
+        if (named >> e & 1) r[e] = (T)__uint_as_float(n.place[n.find((int32_t)(run * N + e))]);
     }
+    if (g.zero) r = Run<T, N>{};
+    *reinterpret_cast<Run<T, N> *>(out + run * N) = r;
+  };
+  if constexpr (kHeld > 0) {
+#pragma unroll
+    for (uint32_t i = 0; i < kHeld; ++i)
+      if (thread + i * kThreads < runs) write(thread + i * kThreads, held[i]);
+  } else {
+    for (uint32_t run = thread; run < runs; run += kThreads) write(run, load_run<T, N>(z_row + run * N));
   }
 }
 
@@ -335,9 +407,21 @@ int apex_distill_topk(uint32_t N, uint32_t V, uint32_t K, int dtype, const void 
   const double inv_tau = 1.0 / (double)temperature;
   const DistillArgs a{N, V, K, distill_table(K), (uint32_t)value_dtype, row_stride, grad_stride, logits, top_index, top_value, top_lse,
                       weight, inv_tau, (float)(1.4426950408889634 * inv_tau), (float)inv_tau, loss, lse, grad};
-  const uint32_t lds = distill_lds(K, (V + 16 / size - 1) / (16 / size));
+  const uint32_t runs = V / (16 / size), lds = distill_lds(K, V);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  with_type(dtype, [&](auto t) { distill_rows_kernel<decltype(t)><<<dim3(N), dim3(kDistillThreads), lds, stream>>>(a); });
+  with_type(dtype, [&](auto t) {
+    typedef decltype(t) E;
+    if (runs <= 256 * 4)
+      distill_rows_kernel<E, 256, 4><<<N, 256, lds, stream>>>(a);
+    else if (runs <= 512 * 8)
+      distill_rows_kernel<E, 512, 8><<<N, 512, lds, stream>>>(a);
+    else if (runs <= 512 * 16)
+      distill_rows_kernel<E, 512, 16><<<N, 512, lds, stream>>>(a);
+    else if (runs <= 1024 * 16)
+      distill_rows_kernel<E, 1024, 16><<<N, 1024, lds, stream>>>(a);
+    else
+      distill_rows_kernel<E, 512, 0><<<N, 512, lds, stream>>>(a);
+  });
   APEX_HIP(hipGetLastError());
   return APEX_OK;
 }

@@ -37,9 +37,12 @@ __device__ __forceinline__ float element(const Run<T, N> &r, int i)
 template <int N, typename T>
 __device__ __forceinline__ void hold_packed(Run<T, N> &r)
 {
-  if constexpr (sizeof(T) == 2 && N == 4) {
-    uint64_t bits = __builtin_bit_cast(uint64_t, r);
-    asm volatile("" : "+v"(bits));
+  if constexpr (sizeof(T) == 2 && N % 4 == 0) {
+    struct Bits {
+      uint64_t word[N / 4];
+    } bits = __builtin_bit_cast(Bits, r);
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) asm volatile("" : "+v"(bits.word[i]));
     r = __builtin_bit_cast(Run<T, N>, bits);
   }
 }
