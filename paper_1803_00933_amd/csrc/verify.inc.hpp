@@ -8,15 +8,13 @@ namespace apex {
 
 constexpr uint32_t kVerifyThreads = 512, kVerifyShares = 64;  // threads per workgroup, workgroups per sequence at most
 constexpr uint32_t kVerifyItems = 8;                          // neighbouring tokens of a thread when a share is searched
+constexpr uint32_t kVerifyMaxShare = 1u << 19;                // tokens of a share at most: a thread's sums stay within 31 bits
 
-// Per sequence: a word that counts its workgroups (0 before and after every call) and, in a line of their own, their sums.
-struct VerifyShare {
-  uint64_t left, target;  // sums of max(0, m(p) - m(q)) and of m(p)
-};
+// Per sequence: a word that counts its workgroups (0 before and after every call) and, in lines of their own, their sums.
 struct VerifySpace {
   uint32_t done;
   uint32_t pad[31];
-  VerifyShare share[kVerifyShares];
+  uint64_t share[kVerifyShares];
 };
 
 struct VerifyArgs {
@@ -30,16 +28,21 @@ struct VerifyArgs {
   VerifySpace *space;
 };
 
-constexpr int kMassBits = 40;
+// m(x) = floor(min(x, 1) 2^40), 0 for what is not above 0, as high 2^20 + low: the multiple of 2^-20 below x, and the rest,
+// which is exact, in 2^-40.
+struct Mass {
+  uint32_t high, low;
+  __device__ __forceinline__ explicit Mass(float x)
+  {
+    const float scaled = __builtin_amdgcn_fmed3f(x, 0.0f, 1.0f) * 0x1p+20f;  // (NaN: 0)
+    high = (uint32_t)scaled;
+    low = (uint32_t)(__builtin_amdgcn_fractf(scaled) * 0x1p+20f);
+  }
+  __device__ __forceinline__ uint64_t whole() const { return ((uint64_t)high << 20) + low; }
+};
 
-// floor(min(x, 1) 2^40), 0 for what is not above 0.  In two conversions of 32 bits: the multiple of 2^-20 below x, and the
-// rest, which is exact, in 2^-40.
-__device__ __forceinline__ uint64_t probability_mass(float x)
-{
-  x = x > 0.0f ? fminf(x, 1.0f) : 0.0f;
-  const float scaled = x * 0x1p+20f, whole = __builtin_floorf(scaled);
-  return ((uint64_t)(uint32_t)whole << 20) + (uint32_t)((scaled - whole) * 0x1p+20f);
-}
+// max(0, m(p) - m(q)): m does not fall, so that it is p > q that decides.
+__device__ __forceinline__ uint64_t mass_left(float p, float q) { return p > q ? Mass(p).whole() - Mass(q).whole() : 0; }
 
 __device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v)
 {
@@ -66,8 +69,8 @@ __device__ __forceinline__ VerifyRows tokens_that_stand(const VerifyArgs &a, uin
     const int32_t token = a.token[(uint64_t)b * a.G + i];
     const uint64_t u = a.rnd[(uint64_t)b * (a.G + 1) + i];
     if (token >= 0 && (uint32_t)token < a.V) {
-      const uint64_t p = probability_mass((float)static_cast<const T *>(a.target)[b * a.target_seq + i * a.target_row + token]);
-      const uint64_t q = probability_mass((float)static_cast<const T *>(a.draft)[b * a.draft_seq + i * a.draft_row + token]);
+      const uint64_t p = Mass((float)static_cast<const T *>(a.target)[b * a.target_seq + i * a.target_row + token]).whole();
+      const uint64_t q = Mass((float)static_cast<const T *>(a.draft)[b * a.draft_seq + i * a.draft_row + token]).whole();
       stands = __umul64hi(u, q) < p;
     }
   }
@@ -76,31 +79,61 @@ __device__ __forceinline__ VerifyRows tokens_that_stand(const VerifyArgs &a, uin
   return VerifyRows{n, n < len};
 }
 
-// Masses of tokens [at, at + N) of the two rows; none beyond V.
+// What a thread has summed up: differences of masses, the two parts apart.  Up to 2^10 tokens of 2^20.
+struct MassSum {
+  int32_t high = 0, low = 0;
+  __device__ __forceinline__ void add(float p, float q)
+  {
+    const Mass mp(p), mq(q);
+    const bool more = p > q;
+    high += more ? (int32_t)(mp.high - mq.high) : 0;
+    low += more ? (int32_t)(mp.low - mq.low) : 0;
+  }
+  __device__ __forceinline__ uint64_t whole() const { return (uint64_t)(((int64_t)high << 20) + low); }
+};
+
+// The probabilities of tokens [at, at + N), 0 beyond V.
 template <typename T, int N>
-__device__ __forceinline__ void masses_of(const T *p_row, const T *q_row, bool turned, uint32_t at, uint32_t V, uint64_t (&left)[N],
-                                          uint64_t (&target)[N])
+__device__ __forceinline__ void probabilities(const T *row, uint32_t at, uint32_t V, float (&x)[N])
 {
-  float p[N], q[N];
   if (at + N <= V) {
-    const Run<T, N> pr = load_run<T, N>(p_row + at);
-    Run<T, N> qr{};
-    if (turned) qr = load_run<T, N>(q_row + at);
+    const Run<T, N> r = load_run<T, N>(row + at);
 #pragma unroll
-    for (int e = 0; e < N; ++e) p[e] = element<N, T>(pr, e), q[e] = element<N, T>(qr, e);
+    for (int e = 0; e < N; ++e) x[e] = element<N, T>(r, e);
   } else {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      p[e] = at + e < V ? (float)p_row[at + e] : 0.0f;
-      q[e] = turned && at + e < V ? (float)q_row[at + e] : 0.0f;
-    }
+    for (int e = 0; e < N; ++e) x[e] = at + e < V ? (float)row[at + e] : 0.0f;
   }
+}
+
+// This thread's part of the mass that is left of tokens [begin, end), in rounds of the whole workgroup; kTwo: with a row q.
+template <typename T, bool kTwo>
+__device__ __forceinline__ uint64_t sum_of(const T *p_row, const T *q_row, uint32_t begin, uint32_t end, uint32_t V)
+{
+  constexpr uint32_t N = 16 / sizeof(T), kRound = kVerifyThreads * N, kAhead = 4;
+  static_assert(kVerifyMaxShare / kVerifyThreads <= 1u << 10);
+  MassSum sum;
+  uint32_t at = begin + threadIdx.x * N;
+  for (; at + (kAhead - 1) * kRound + N <= min(end, V); at += kAhead * kRound) {
+    Run<T, N> p[kAhead], q[kAhead];
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    target[e] = probability_mass(p[e]);
-    const uint64_t m = probability_mass(q[e]);
-    left[e] = target[e] > m ? target[e] - m : 0;
+    for (uint32_t i = 0; i < kAhead; ++i) {
+      p[i] = load_run<T, N>(p_row + at + i * kRound);
+      if (kTwo) q[i] = load_run<T, N>(q_row + at + i * kRound);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i)
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) sum.add(element<N, T>(p[i], e), kTwo ? element<N, T>(q[i], e) : 0.0f);
   }
+  for (; at < end; at += kRound) {
+    float p[N], q[N] = {};
+    probabilities<T, N>(p_row, at, V, p);
+    if (kTwo) probabilities<T, N>(q_row, at, V, q);
+#pragma unroll
+    for (uint32_t e = 0; e < N; ++e) sum.add(p[e], q[e]);
+  }
+  return sum.whole();
 }
 
 // Every sequence's row is shared by `shares` workgroups, which sum their parts; the last of them to be done knows the
@@ -108,9 +141,8 @@ __device__ __forceinline__ void masses_of(const T *p_row, const T *q_row, bool t
 template <typename T>
 __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
 {
-  constexpr int N = 16 / sizeof(T);
   constexpr uint32_t kWaves = kVerifyThreads / kWave;
-  __shared__ uint64_t red[2][kWaves];
+  __shared__ uint64_t red[kWaves];
   __shared__ VerifyRows sh_rows;
   __shared__ uint32_t sh_done;
   const uint32_t thread = threadIdx.x, lane = lane_id(), wave = thread / kWave;
@@ -121,32 +153,25 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
   }
   __syncthreads();
   const VerifyRows rows = sh_rows;
+  bool two = rows.turned;
   const T *const p_row = static_cast<const T *>(a.target) + b * a.target_seq + rows.n * a.target_row;
-  const T *const q_row = rows.turned ? static_cast<const T *>(a.draft) + b * a.draft_seq + rows.n * a.draft_row : nullptr;
+  const T *const q_row = two ? static_cast<const T *>(a.draft) + b * a.draft_seq + rows.n * a.draft_row : nullptr;
+  // the sum over the workgroup, in every thread of wave 0
+  const auto of_workgroup = [&](uint64_t mine) {
+    mine = wave_sum_u64(mine);
+    if (lane == 0) red[wave] = mine;
+    __syncthreads();
+    return wave == 0 ? wave_sum_u64(lane < kWaves ? red[lane] : 0) : 0;
+  };
 
   const uint32_t begin = share * a.share_tokens, end = min(a.V, begin + a.share_tokens);
-  uint64_t left_sum = 0, target_sum = 0;
-  for (uint32_t at = begin + thread * N; at < end; at += kVerifyThreads * N) {
-    uint64_t left[N], target[N];
-    masses_of<T, N>(p_row, q_row, rows.turned, at, a.V, left, target);
-#pragma unroll
-    for (int e = 0; e < N; ++e) left_sum += left[e], target_sum += target[e];
-  }
-  left_sum = wave_sum_u64(left_sum);
-  target_sum = wave_sum_u64(target_sum);
-  if (lane == 0) red[0][wave] = left_sum, red[1][wave] = target_sum;
-  __syncthreads();
+  const uint64_t sum = of_workgroup(two ? sum_of<T, true>(p_row, q_row, begin, end, a.V) : sum_of<T, false>(p_row, q_row, begin, end, a.V));
   VerifySpace *const space = a.space + b;
-  if (wave == 0) {
-    left_sum = wave_sum_u64(lane < kWaves ? red[0][lane] : 0);
-    target_sum = wave_sum_u64(lane < kWaves ? red[1][lane] : 0);
-    if (lane == 0) {
-      // only these words cross between workgroups: written through to memory, and waited for before the word is counted
-      __hip_atomic_store(&space->share[share].left, left_sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_store(&space->share[share].target, target_sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      sh_done = __hip_atomic_fetch_add(&space->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
+  if (thread == 0) {
+    // only these words cross between workgroups: written through to memory, and waited for before the workgroup is counted
+    __hip_atomic_store(&space->share[share], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    sh_done = __hip_atomic_fetch_add(&space->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
   if (sh_done != a.shares - 1) return;
@@ -154,41 +179,43 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
 
   // which share (every wave finds it for itself)
   static_assert(kVerifyShares == kWave);
-  uint64_t of_left = 0, of_target = 0;
-  if (lane < a.shares) {
-    of_left = __hip_atomic_load(&space->share[lane].left, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    of_target = __hip_atomic_load(&space->share[lane].target, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const uint64_t of_share = lane < a.shares ? __hip_atomic_load(&space->share[lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+  const uint64_t u = a.rnd[(uint64_t)b * (a.G + 1) + a.G];
+  const uint64_t up_to = wave_inclusive_scan(of_share);
+  uint64_t total = __shfl(up_to, kWave - 1), point = __umul64hi(u, total), base = 0;  // base: mass in front of the tokens looked at
+  uint32_t from = 0;
+  if (total) {  // point is below it
+    const int found = __builtin_ctzll(__ballot(up_to > point));
+    base = __shfl(up_to - of_share, found);
+    from = (uint32_t)found * a.share_tokens;
+  } else if (two) {  // nothing is left of a row that was turned down: the target's own, all of it by this workgroup
+    two = false;
+    uint64_t all = 0;
+    for (uint32_t at = 0; at < a.V; at += a.share_tokens) all += sum_of<T, false>(p_row, nullptr, at, min(a.V, at + a.share_tokens), a.V);
+    all = of_workgroup(all);
+    if (thread == 0) red[0] = all;
+    __syncthreads();
+    total = red[0];
+    point = __umul64hi(u, total);
   }
-  const uint64_t left_up_to = wave_inclusive_scan(of_left), target_up_to = wave_inclusive_scan(of_target);
-  const uint64_t left_total = __shfl(left_up_to, kWave - 1), target_total = __shfl(target_up_to, kWave - 1);
-  const bool use_left = left_total != 0;
-  const uint64_t total = use_left ? left_total : target_total, up_to = use_left ? left_up_to : target_up_to;
-  const uint64_t of_share = use_left ? of_left : of_target;
-  const uint64_t point = __umul64hi(a.rnd[(uint64_t)b * (a.G + 1) + a.G], total);
-  const uint64_t over = __ballot(up_to > point);
-  int32_t drawn = -1;
-  if (over) {  // total is above 0, and point below it
-    const int found = __builtin_ctzll(over);
-    uint64_t base = __shfl(up_to - of_share, found);  // mass in front of the tokens looked at
-    const uint32_t from = (uint32_t)found * a.share_tokens;
+  if (total) {
     for (uint32_t at0 = from;; at0 += kVerifyThreads * kVerifyItems) {
       const uint32_t at = at0 + thread * kVerifyItems;
-      uint64_t left[kVerifyItems], target[kVerifyItems], mine = 0;
-      masses_of<T, kVerifyItems>(p_row, q_row, rows.turned, at, a.V, left, target);
+      float p[kVerifyItems], q[kVerifyItems] = {};
+      probabilities<T, kVerifyItems>(p_row, at, a.V, p);
+      if (two) probabilities<T, kVerifyItems>(q_row, at, a.V, q);
+      uint64_t left[kVerifyItems], mine = 0;
 #pragma unroll
-      for (uint32_t e = 0; e < kVerifyItems; ++e) {
-        if (!use_left) left[e] = target[e];
-        mine += left[e];
-      }
+      for (uint32_t e = 0; e < kVerifyItems; ++e) mine += left[e] = mass_left(p[e], q[e]);
       const uint64_t in_wave = wave_inclusive_scan(mine);
       __syncthreads();  // the words of the round before have been read
-      if (lane == kWave - 1) red[0][wave] = in_wave;
+      if (lane == kWave - 1) red[wave] = in_wave;
       __syncthreads();
       uint64_t before = base, all = 0;
 #pragma unroll
       for (uint32_t w = 0; w < kWaves; ++w) {
-        if (w < wave) before += red[0][w];
-        all += red[0][w];
+        if (w < wave) before += red[w];
+        all += red[w];
       }
       before += in_wave - mine;
       if (point >= before && point < before + mine) {  // one thread of the workgroup, in one of the rounds
@@ -199,13 +226,12 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
       base += all;
       if (base > point || at0 + kVerifyThreads * kVerifyItems >= a.V) break;
     }
-    drawn = 0;
   }
   if (thread <= a.G && thread != rows.n)
     a.token_out[(uint64_t)b * (a.G + 1) + thread] = thread < rows.n ? a.token[(uint64_t)b * a.G + thread] : -1;
   if (thread == 0) {
     a.accepted[b] = (int32_t)rows.n;
-    if (drawn < 0) a.token_out[(uint64_t)b * (a.G + 1) + rows.n] = -1;
+    if (!total) a.token_out[(uint64_t)b * (a.G + 1) + rows.n] = -1;
   }
 }
 
@@ -213,14 +239,15 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyArgs a)
 
 namespace {
 
-// Workgroups per sequence and tokens of each.
+// Workgroups per sequence and tokens of each: as many as keep the chip in sixteen times its compute units, no smaller than a
+// round of the search.  (256 x 128001 in 32 bits 68.8 us with 2 workgroups a sequence, 59.6 with 4, 53.5 with 8, 52.8 with 16.)
 void verify_shares(uint32_t B, uint32_t V, uint32_t *shares, uint32_t *tokens)
 {
   constexpr uint32_t kRound = kVerifyThreads * kVerifyItems;
-  const uint32_t rounds = (V + kRound - 1) / kRound;
-  const uint32_t most = std::clamp<uint32_t>(4 * kChipCus / B, 1, std::min(kVerifyShares, rounds));
-  *tokens = (rounds + most - 1) / most * kRound;
-  *shares = (V + *tokens - 1) / *tokens;
+  const uint32_t rounds = blocks_for(V, kRound);
+  const uint32_t most = std::clamp<uint32_t>(16 * kChipCus / B, blocks_for(V, kVerifyMaxShare), std::min(kVerifyShares, rounds));
+  *tokens = blocks_for(rounds, most) * kRound;
+  *shares = blocks_for(V, *tokens);
 }
 
 }  // namespace

@@ -406,6 +406,23 @@ def test_verify_edges(apex, dtype):
     assert accepted[2] == 3 and accepted[3] <= 1 and token[5, 0] == -1 and token[11].tolist() == [3] * 4
 
 
+def test_verify_sums_that_no_normalised_row_reaches(apex):
+    """Every probability 1 (weights that nobody normalised), in so many sequences that a row has one or two workgroups: sums of
+    2^60, and what is drawn is uniform in the uniforms."""
+    rng = np.random.default_rng(8)
+    for B, V in ((5000, 1 << 20), (4100, (1 << 19) + 5)):
+        row = torch.ones((1, 2, V), dtype=torch.bfloat16, device="cuda:0")
+        row[:, :, 0] = 7.0
+        rnd = rng.integers(0, 1 << 64, (B, 2), dtype=np.uint64)
+        token = to_dev(np.full((B, 1), -1, np.int32))
+        rc, out = apex.verify_draft(row.expand(B, 2, V), torch.zeros((1, 1, V), dtype=torch.bfloat16, device="cuda:0").expand(B, 1, V),
+                                    token, to_dev(rnd.view(np.int64)))
+        assert rc == apex.OK
+        torch.cuda.synchronize()
+        want = np.array([(int(u) * (V << 40)) >> 104 for u in rnd[:, 1]])
+        assert (out["accepted"] == 0).all() and np.array_equal(out["token"][:, 0].cpu().numpy(), want)
+
+
 def test_verify_strides_addresses_and_workspace(apex):
     """Padded rows from odd addresses, one target row for all places, a workspace that calls of several sizes share."""
     space = apex.verify_draft_workspace(80, 20000)
