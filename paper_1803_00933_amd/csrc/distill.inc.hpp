@@ -9,7 +9,7 @@
 namespace apex {
 
 struct DistillArgs {
-  uint32_t N, V, K, H, value_dtype;  // H: places of the table of named tokens, a power of two of at least 2 K
+  uint32_t N, V, K, value_dtype;
   uint64_t row_stride, grad_stride;
   const void *logits;
   const int32_t *top_index;
@@ -21,18 +21,12 @@ struct DistillArgs {
   void *grad;
 };
 
-// The named tokens of a row, in LDS: a table by open addressing, and a bit for every token.
+// The named tokens of a row, in LDS.
 struct Named {
-  int32_t *key;       // [H] token, or -1
-  uint32_t *place;    // [H] the first place that names it; later, as a float, the token's gradient
-  float *z;           // [H] the student's logit
-  int32_t *slot;      // [K] the table's entry of a place; -1: empty
-  double *q;          // [K] the teacher's probability
-  float *value;       // [K] the teacher's logit
-  uint32_t *bits;     // [ceil(V / 64)] words of 64 bits
-  uint32_t H;
-
-  __device__ __forceinline__ uint32_t hash(int32_t token) const { return ((uint32_t)token * 2654435761u) >> (32 - __builtin_ctz(H)); }
+  uint32_t *bits;        // [ceil(V / 64)] words of 64 bits: a bit for every token
+  double *q;             // [K] the teacher's probability
+  int32_t *token;        // [K] -1: a place that does not count
+  float *value, *z;      // [K] the teacher's and the student's logits
 
   // Which of the N tokens of a run are named.
   template <uint32_t N>
@@ -41,38 +35,21 @@ struct Named {
     const uint32_t byte = reinterpret_cast<const uint8_t *>(bits)[run * N / 8];
     return N == 8 ? byte : byte >> (run % 2 * 4) & 15u;
   }
-
-  __device__ __forceinline__ int32_t find(int32_t token) const
-  {
-    for (uint32_t i = hash(token);; i = (i + 1) & (H - 1)) {  // at most half of the entries are in use
-      if (key[i] == token) return (int32_t)i;
-      if (key[i] < 0) return -1;
-    }
-  }
 };
 
-__host__ __device__ constexpr uint32_t distill_table(uint32_t K)
-{
-  uint32_t H = 64;
-  while (H < 2 * K) H *= 2;
-  return H;
-}
 __host__ __device__ constexpr uint32_t distill_lds(uint32_t K, uint32_t V)  // bytes
 {
-  return (V + 63) / 64 * 8 + distill_table(K) * 12 + K * 16;
+  return (V + 63) / 64 * 8 + K * 20;
 }
 
-__device__ __forceinline__ Named named_in(uint64_t *lds, uint32_t K, uint32_t H, uint32_t V)
+__device__ __forceinline__ Named named_in(uint64_t *lds, uint32_t K, uint32_t V)
 {
   Named n;
-  n.H = H;
   n.bits = reinterpret_cast<uint32_t *>(lds);
   n.q = reinterpret_cast<double *>(lds + (V + 63) / 64);
-  n.key = reinterpret_cast<int32_t *>(n.q + K);
-  n.place = reinterpret_cast<uint32_t *>(n.key + H);
-  n.z = reinterpret_cast<float *>(n.place + H);
-  n.slot = reinterpret_cast<int32_t *>(n.z + H);
-  n.value = reinterpret_cast<float *>(n.slot + K);
+  n.token = reinterpret_cast<int32_t *>(n.q + K);
+  n.value = reinterpret_cast<float *>(n.token + K);
+  n.z = n.value + K;
   return n;
 }
 
@@ -137,20 +114,13 @@ struct RowGradient {
   bool zero;  // the row's weight is 0
 };
 
-// Enters place k's token.
-__device__ __forceinline__ void enter_named(const DistillArgs &a, const Named &n, uint32_t k, int32_t token, float value)
+// Enters place k's token; whether another place names it too.
+__device__ __forceinline__ bool enter_named(const DistillArgs &a, const Named &n, uint32_t k, int32_t token, float value)
 {
-  int32_t slot = -1;
-  if (token >= 0 && (uint32_t)token < a.V) {
-    for (uint32_t i = n.hash(token); slot < 0; i = (i + 1) & (a.H - 1)) {
-      const int32_t had = atomicCAS(n.key + i, -1, token);
-      if (had == -1 || had == token) slot = (int32_t)i;
-    }
-    atomicMin(n.place + slot, k);
-    atomicOr(n.bits + token / 32, 1u << (token % 32));
-    n.value[k] = value;
-  }
-  n.slot[k] = slot;
+  const bool counts = token >= 0 && (uint32_t)token < a.V;
+  n.token[k] = counts ? token : -1;
+  n.value[k] = value;
+  return counts && (atomicOr(n.bits + token / 32, 1u << (token % 32)) >> (token % 32) & 1);
 }
 
 // What a wave knows of a row's teacher.
@@ -170,31 +140,32 @@ __device__ __forceinline__ double log_sum(const DistillArgs &a, float m, float R
   return __builtin_fma((double)m, a.inv_tau, ln_of(sum) + kLn2d * __builtin_fma(-(double)m, (double)a.c, (double)R));
 }
 
-// The part of a row that needs no sum over the vocabulary, by one wave: drops places whose token an earlier one names, and leaves
-// the q of the others.
-__device__ __forceinline__ Teacher teach(const DistillArgs &a, const Named &n, uint32_t row)
+// The part of a row that needs no sum over the vocabulary, by one wave: drops places whose token an earlier one names (if there
+// are any: `repeated`), and leaves the q of the others.
+__device__ __forceinline__ Teacher teach(const DistillArgs &a, const Named &n, uint32_t row, bool repeated)
 {
   const uint32_t lane = lane_id();
   uint32_t mine = 0;
   float top = -__builtin_inff();
-  for (uint32_t k = lane; k < a.K; k += kWave) {
-    const int32_t slot = n.slot[k];
-    if (slot >= 0 && n.place[slot] != k) n.slot[k] = -1;
-    else if (slot >= 0) ++mine, top = fmaxf(top, n.value[k]);
-  }
+  if (repeated)
+    for (uint32_t k = lane; k < a.K; k += kWave)
+      for (uint32_t i = 0; i < k; ++i)
+        if (n.token[i] == n.token[k]) n.token[k] = -1;  // (whatever goes first, the first place of a token stays, and drops the others)
+  for (uint32_t k = lane; k < a.K; k += kWave)
+    if (n.token[k] >= 0) ++mine, top = fmaxf(top, n.value[k]);
   Teacher t;
   t.named = (uint32_t)wave_sum((float)mine);  // at most APEX_MAX_TOP
   top = wave_max(top);
   const float R = Sum::ref(top, a.c);
   float sum = 0.0f;
   for (uint32_t k = lane; k < a.K; k += kWave)
-    if (n.slot[k] >= 0) sum += exp2_of(__builtin_fmaf(n.value[k], a.c, -R));
+    if (n.token[k] >= 0) sum += exp2_of(__builtin_fmaf(n.value[k], a.c, -R));
   sum = wave_sum(sum);
   t.teaches = sum != 0.0f;
   t.ln_sum = a.top_lse ? (double)a.top_lse[row] : log_sum(a, top, R, sum);
   float mass = 0.0f;
   for (uint32_t k = lane; k < a.K; k += kWave)
-    if (n.slot[k] >= 0) {
+    if (n.token[k] >= 0) {
       const double q = t.teaches ? exp_of(__builtin_fma((double)n.value[k], a.inv_tau, -t.ln_sum)) : 0.0;
       n.q[k] = q;
       mass += (float)q;
@@ -204,9 +175,10 @@ __device__ __forceinline__ Teacher teach(const DistillArgs &a, const Named &n, u
 }
 
 // The rest of it, by the same wave, once the row's sum `all` (without the named tokens if there is a rest class) is known: writes
-// loss and lse, leaves the gradients of the named tokens in the table.
+// loss, lse and the gradients of the named tokens (out: the row's gradient, or null).
 // Logarithms of nearly equal numbers are subtracted: in 64 bits, a few operations for each named token.
-__device__ __forceinline__ RowGradient settle(const DistillArgs &a, const Named &n, uint32_t row, const Teacher &t, Sum all)
+template <typename T>
+__device__ __forceinline__ RowGradient settle(const DistillArgs &a, const Named &n, uint32_t row, const Teacher &t, Sum all, T *out)
 {
   const uint32_t lane = lane_id();
   const float R_rest = Sum::ref(all.m, a.c), w = a.weight ? a.weight[row] : 1.0f, wt = w * a.grad_scale;
@@ -214,11 +186,11 @@ __device__ __forceinline__ RowGradient settle(const DistillArgs &a, const Named 
   if (a.top_lse) {
     float z_top = -__builtin_inff(), z_sum = 0.0f;
     for (uint32_t k = lane; k < a.K; k += kWave)
-      if (n.slot[k] >= 0) z_top = fmaxf(z_top, n.z[n.slot[k]]);
+      if (n.token[k] >= 0) z_top = fmaxf(z_top, n.z[k]);
     top = fmaxf(wave_max(z_top), all.m);
     R = Sum::ref(top, a.c);
     for (uint32_t k = lane; k < a.K; k += kWave)
-      if (n.slot[k] >= 0) z_sum += exp2_of(__builtin_fmaf(n.z[n.slot[k]], a.c, -R));
+      if (n.token[k] >= 0) z_sum += exp2_of(__builtin_fmaf(n.z[k], a.c, -R));
     s = wave_sum(z_sum) + (all.s == 0.0f ? 0.0f : all.s * exp2_of(R_rest - R));
   }
   if (s == 0.0f) s = __builtin_nanf("");  // no finite logit
@@ -229,10 +201,10 @@ __device__ __forceinline__ RowGradient settle(const DistillArgs &a, const Named 
   const double given = (double)t.mass + (double)rest;
   float loss = 0.0f;
   for (uint32_t k = lane; k < a.K; k += kWave)
-    if (n.slot[k] >= 0) {
-      const double q = n.q[k], ln_p = __builtin_fma((double)n.z[n.slot[k]], a.inv_tau, -ln_all);
+    if (n.token[k] >= 0) {
+      const double q = n.q[k], ln_p = __builtin_fma((double)n.z[k], a.inv_tau, -ln_all);
       if ((float)q != 0.0f) loss += (float)q * (float)(__builtin_fma((double)n.value[k], a.inv_tau, -t.ln_sum) - ln_p);
-      n.place[n.slot[k]] = __float_as_uint(w == 0.0f ? 0.0f : (float)(wt * (given * exp_of(ln_p) - q)));
+      if (out) out[n.token[k]] = (T)(w == 0.0f ? 0.0f : (float)(wt * (given * exp_of(ln_p) - q)));
     }
   loss = wave_sum(loss);
   if (rest != 0.0f) loss += rest * (float)(ln_of(rest) - (log_sum(a, all.m, R_rest, all.s) - ln_all));
@@ -255,11 +227,13 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
   extern __shared__ uint64_t lds[];
   __shared__ float red_m[kWaves], red_s[kWaves];
   __shared__ RowGradient sh_gradient;
+  __shared__ uint32_t sh_repeated;
   const uint32_t thread = threadIdx.x, lane = lane_id(), wave = thread / kWave, row = blockIdx.x;
   const uint32_t runs = a.V / N, left = a.V % N;  // whole runs; the elements behind them: one each
-  const Named n = named_in(lds, a.K, a.H, a.V);
+  const Named n = named_in(lds, a.K, a.V);
   const T *const z_row = static_cast<const T *>(a.logits) + row * a.row_stride;
-  // The named tokens first: loads come back in order, and the table has to be there before the row is looked at.
+  T *const out = a.grad ? static_cast<T *>(a.grad) + row * a.grad_stride : nullptr;
+  // The named tokens first: loads come back in order, and their bits have to be there before the row is looked at.
   int32_t token = -1;
   float value = 0.0f;
   if (thread < a.K) {
@@ -275,36 +249,37 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
   }
   float z_left = thread < left ? (float)z_row[runs * N + thread] : -__builtin_inff();
   for (uint32_t i = thread; i < (a.V + 63) / 64 * 2; i += kThreads) n.bits[i] = 0;
-  for (uint32_t i = thread; i < a.H; i += kThreads) n.key[i] = -1, n.place[i] = 0xffffffffu;
+  if (thread == 0) sh_repeated = 0;
   lds_barrier();
-  if (thread < a.K) enter_named(a, n, thread, token, value);
+  float z_named = 0.0f;
+  if (thread < a.K) {
+    if (enter_named(a, n, thread, token, value)) sh_repeated = 1;
+    if (token >= 0 && (uint32_t)token < a.V) z_named = (float)z_row[token];  // on its way while the row is looked at
+  }
   for (uint32_t k = thread + kThreads; k < a.K; k += kThreads) {
     const uint64_t at = (uint64_t)row * a.K + k;
-    enter_named(a, n, k, a.top_index[at], typed_element(a.top_value, a.value_dtype, at));
+    const int32_t other = a.top_index[at];
+    if (enter_named(a, n, k, other, typed_element(a.top_value, a.value_dtype, at))) sh_repeated = 1;
+    if (other >= 0 && (uint32_t)other < a.V) n.z[k] = (float)z_row[other];
   }
   lds_barrier();
   Teacher teacher;
-  if (wave == 0) teacher = teach(a, n, row);
-  // A named token's logit goes into the table; what the sum takes in its place.
-  const auto taken = [&](uint32_t at, float z) {
-    n.z[n.find((int32_t)at)] = z;
-    return a.top_lse ? -__builtin_inff() : z;
-  };
+  if (wave == 0) teacher = teach(a, n, row, sh_repeated);
   const bool left_named = thread < left && (n.bits[(runs * N + thread) / 32] >> (runs * N + thread) % 32 & 1);
 
   // the sum of this thread's part of the row, without the named tokens if there is a rest class
   Sum sum{-__builtin_inff(), 0.0f};
-  if (left_named) z_left = taken(runs * N + thread, z_left);
+  if (a.top_lse && left_named) z_left = -__builtin_inff();
   if constexpr (kHeld > 0) {
     float top = z_left;
 #pragma unroll
     for (uint32_t i = 0; i < kHeld; ++i) {
       const uint32_t run = thread + i * kThreads;
       if (run >= runs) continue;
-      if (const uint32_t named = n.mask<N>(run)) {
+      const uint32_t named = a.top_lse ? n.mask<N>(run) : 0;
+      if (named) {
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e)
-          if (named >> e & 1) held[i][e] = (T)taken(run * N + e, element<N, T>(held[i], e));
+        for (uint32_t e = 0; e < N; ++e) held[i][e] = named >> e & 1 ? (T)-__builtin_inff() : (T)held[i][e];
       }
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) top = fmaxf(top, element<N, T>(held[i], e));
@@ -328,10 +303,10 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
       float z[N];
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) z[e] = element<N, T>(r, e);
-      if (const uint32_t named = n.mask<N>(run)) {
+      const uint32_t named = a.top_lse ? n.mask<N>(run) : 0;
+      if (named) {
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e)
-          if (named >> e & 1) z[e] = taken(run * N + e, z[e]);
+        for (uint32_t e = 0; e < N; ++e) z[e] = named >> e & 1 ? -__builtin_inff() : z[e];
       }
       add_to<N>(sum, z, a.c);
     }
@@ -339,35 +314,35 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
   const float m = wave_max(sum.m), R = Sum::ref(m, a.c);
   const float s = wave_sum(sum.m == -__builtin_inff() ? sum.s : sum.s * exp2_of(Sum::ref(sum.m, a.c) - R));
   if (lane == 0) red_m[wave] = m, red_s[wave] = s;
-  __syncthreads();
+  if (thread < a.K) n.z[thread] = z_named;
+  lds_barrier();
   if (wave == 0) {
     const float wm = lane < kWaves ? red_m[lane] : -__builtin_inff(), ws = lane < kWaves ? red_s[lane] : 0.0f;
     const float top = wave_max(wm), top_R = Sum::ref(top, a.c);
     const Sum all{top, wave_sum(wm == -__builtin_inff() ? ws : ws * exp2_of(Sum::ref(wm, a.c) - top_R))};
-    const RowGradient g = settle(a, n, row, teacher, all);
+    const RowGradient g = settle(a, n, row, teacher, all, out);
     if (lane == 0) sh_gradient = g;
   }
-  if (!a.grad) return;
-  __syncthreads();
+  if (!out) return;
+  lds_barrier();
   const RowGradient g = sh_gradient;
-  T *const out = static_cast<T *>(a.grad) + row * a.grad_stride;
   const float scale_low = g.scale * 0x1p-64f;
   const auto gradient = [&](float z) { return power<T>(__builtin_fmaf(z, a.c, -g.R), g.scale, scale_low); };
-  if (thread < left) {
-    const float v = left_named ? __uint_as_float(n.place[n.find((int32_t)(runs * N + thread))]) : gradient(z_left);
-    out[runs * N + thread] = (T)(g.zero ? 0.0f : v);
-  }
+  // The named tokens' elements are the first wave's, all others of the row are written here.
+  if (thread < left && !left_named) out[runs * N + thread] = (T)(g.zero ? 0.0f : gradient(z_left));
   const auto write = [&](uint32_t run, const Run<T, N> &z) {
     Run<T, N> r;
 #pragma unroll
     for (uint32_t e = 0; e < N; ++e) r[e] = (T)gradient(element<N, T>(z, e));
-    if (const uint32_t named = n.mask<N>(run)) {
+    if (g.zero) r = Run<T, N>{};
+    const uint32_t named = n.mask<N>(run);
+    if (!named) {
+      *reinterpret_cast<Run<T, N> *>(out + run * N) = r;
+    } else {
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e)
-        if (named >> e & 1) r[e] = (T)__uint_as_float(n.place[n.find((int32_t)(run * N + e))]);
+        if (!(named >> e & 1)) out[run * N + e] = r[e];
     }
-    if (g.zero) r = Run<T, N>{};
-    *reinterpret_cast<Run<T, N> *>(out + run * N) = r;
   };
   if constexpr (kHeld > 0) {
 #pragma unroll
@@ -405,7 +380,7 @@ int apex_distill_topk(uint32_t N, uint32_t V, uint32_t K, int dtype, const void 
     return APEX_ERR_INVALID_ARG;
   if (V > APEX_MAX_VOCABULARY || K > APEX_MAX_TOP || N > 0xffffffffu / 1024) return APEX_ERR_TOO_LARGE;
   const double inv_tau = 1.0 / (double)temperature;
-  const DistillArgs a{N, V, K, distill_table(K), (uint32_t)value_dtype, row_stride, grad_stride, logits, top_index, top_value, top_lse,
+  const DistillArgs a{N, V, K, (uint32_t)value_dtype, row_stride, grad_stride, logits, top_index, top_value, top_lse,
                       weight, inv_tau, (float)(1.4426950408889634 * inv_tau), (float)inv_tau, loss, lse, grad};
   const uint32_t runs = V / (16 / size), lds = distill_lds(K, V);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
