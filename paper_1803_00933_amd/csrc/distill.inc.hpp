@@ -19,6 +19,7 @@ struct DistillArgs {
   float c, grad_scale;  // log2(e) / tau, 1 / tau
   float *loss, *lse;
   void *grad;
+  bool past_caches, whole_lines;  // the gradient is stored past the caches; rows begin with cache lines
 };
 
 // The named tokens of a row, in LDS.
@@ -242,10 +243,12 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
     value = typed_element(a.top_value, a.value_dtype, at);
   }
   Run<T, N> held[kHeld ? kHeld : 1];
+  // (A row that is read once, past the caches too where no line is shared by two loads: 3001 x 131072 373 us through them, 364
+  // past them; 777 rows that begin inside lines 33.9 and 39.2.)
 #pragma unroll
   for (uint32_t i = 0; i < kHeld; ++i) {
     const uint32_t run = thread + i * kThreads;
-    if (run < runs) held[i] = load_run<T, N>(z_row + run * N);
+    if (run < runs) held[i] = load_run<T, N>(z_row + run * N, a.past_caches && a.whole_lines);
   }
   float z_left = thread < left ? (float)z_row[runs * N + thread] : -__builtin_inff();
   for (uint32_t i = thread; i < (a.V + 63) / 64 * 2; i += kThreads) n.bits[i] = 0;
@@ -337,7 +340,7 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
     if (g.zero) r = Run<T, N>{};
     const uint32_t named = n.mask<N>(run);
     if (!named) {
-      *reinterpret_cast<Run<T, N> *>(out + run * N) = r;
+      store_run<T, N>(out + run * N, r, a.past_caches);
     } else {
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e)
@@ -380,14 +383,20 @@ int apex_distill_topk(uint32_t N, uint32_t V, uint32_t K, int dtype, const void 
     return APEX_ERR_INVALID_ARG;
   if (V > APEX_MAX_VOCABULARY || K > APEX_MAX_TOP || N > 0xffffffffu / 1024) return APEX_ERR_TOO_LARGE;
   const double inv_tau = 1.0 / (double)temperature;
-  const DistillArgs a{N, V, K, (uint32_t)value_dtype, row_stride, grad_stride, logits, top_index, top_value, top_lse,
-                      weight, inv_tau, (float)(1.4426950408889634 * inv_tau), (float)inv_tau, loss, lse, grad};
+  constexpr uint32_t kLine = 128;
+  const DistillArgs a{N, V, K, (uint32_t)value_dtype, row_stride, grad_stride, logits, top_index, top_value, top_lse, weight, inv_tau,
+                      (float)(1.4426950408889634 * inv_tau), (float)inv_tau, loss, lse, grad,
+                      grad && (uint64_t)N * V * size > kPastCachesBytes, (uintptr_t)logits % kLine == 0 && row_stride * size % kLine == 0};
   const uint32_t runs = V / (16 / size), lds = distill_lds(K, V);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  // As few threads as hold a row, for the registers of more rows on a compute unit; where the chip has a compute unit for every
+  // row, as many as there are runs (12 x 32000 in 32 bits 9.9 us with 512 threads, 8.6 with 1024).
   with_type(dtype, [&](auto t) {
     typedef decltype(t) E;
     if (runs <= 256 * 4)
       distill_rows_kernel<E, 256, 4><<<N, 256, lds, stream>>>(a);
+    else if (runs <= 1024 * 8 && N <= kChipCus)
+      distill_rows_kernel<E, 1024, 8><<<N, 1024, lds, stream>>>(a);
     else if (runs <= 512 * 8)
       distill_rows_kernel<E, 512, 8><<<N, 512, lds, stream>>>(a);
     else if (runs <= 512 * 16)

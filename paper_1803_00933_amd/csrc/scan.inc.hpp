@@ -14,6 +14,7 @@ struct ScanArgs {
   const float *h0;
   void *h;
   float *h_last, *carry;
+  bool past_caches;  // h is stored past the caches
 };
 
 struct ScanBackArgs {
@@ -28,6 +29,7 @@ struct ScanBackArgs {
   uint64_t dg_seq, dg_time, dx_seq, dx_time;
   void *dg, *dx;
   float *dh0;
+  bool past_caches;
 };
 
 __device__ __forceinline__ uint32_t scan_length(const int32_t *length, uint32_t s, uint32_t T)
@@ -517,7 +519,7 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
       }
       T *const to = h + (uint64_t)l * a.D;
       if (whole) {
-        *reinterpret_cast<Run<T, N> *>(to + d) = r;
+        store_run<T, N>(to + d, r, a.past_caches);
       } else if (t < a.T) {
         if (t >= len) r = Run<T, N>{};
         store_run_of<T, N>(to, d, a.D, r);
@@ -748,8 +750,8 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, 4) void
         dxr[e] = (T)dxt;
       }
       if (whole) {
-        *reinterpret_cast<Run<T, N> *>(dg + l * a.dg_time + d) = dgr;
-        *reinterpret_cast<Run<T, N> *>(dx + l * a.dx_time + d) = dxr;
+        store_run<T, N>(dg + l * a.dg_time + d, dgr, a.past_caches);
+        store_run<T, N>(dx + l * a.dx_time + d, dxr, a.past_caches);
       } else if (t < a.T) {
         if (t >= len) dgr = dxr = Run<T, N>{};
         store_run_of<T, N>(dg + l * a.dg_time, d, a.D, dgr);
@@ -943,7 +945,8 @@ int apex_gated_scan(uint32_t S, uint32_t T, uint32_t D, int dtype, int gate, con
   if (const int rc = scan_check(S, T, D, dtype, gate, g, g_seq_stride, g_time_stride, x, x_seq_stride, x_time_stride, discount, length))
     return rc;
   if (!h || (uintptr_t)h % element_size(dtype) || ((uintptr_t)h0 | (uintptr_t)h_last | (uintptr_t)carry) % 4) return APEX_ERR_INVALID_ARG;
-  const ScanArgs a{S, T, D, g_seq_stride, g_time_stride, x_seq_stride, x_time_stride, g, x, discount, length, h0, h, h_last, carry};
+  const ScanArgs a{S, T, D, g_seq_stride, g_time_stride, x_seq_stride, x_time_stride, g, x, discount, length, h0, h, h_last, carry,
+                   (uint64_t)S * T * D * element_size(dtype) > kPastCachesBytes};
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   ScanLaunch l;
   if (const int rc = scan_launch(S, T, D, false, workspace, &l)) return rc;
@@ -976,7 +979,8 @@ int apex_gated_scan_backward(uint32_t S, uint32_t T, uint32_t D, int dtype, int 
       !rows_apart(dg, size, S, dg_seq_stride, T, dg_time_stride, D) || !rows_apart(dx, size, S, dx_seq_stride, T, dx_time_stride, D))
     return APEX_ERR_INVALID_ARG;
   const ScanBackArgs a{S, T, D, g_seq_stride, g_time_stride, x_seq_stride, x_time_stride, g, x, discount, length, carry, dh, dh_last,
-                       dg_seq_stride, dg_time_stride, dx_seq_stride, dx_time_stride, dg, dx, dh0};
+                       dg_seq_stride, dg_time_stride, dx_seq_stride, dx_time_stride, dg, dx, dh0,
+                       (uint64_t)S * T * D * size > kPastCachesBytes};
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   ScanLaunch l;
   if (const int rc = scan_launch(S, T, D, true, workspace, &l)) return rc;
