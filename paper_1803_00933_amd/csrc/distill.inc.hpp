@@ -245,11 +245,13 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
   Run<T, N> held[kHeld ? kHeld : 1];
   // (A row that is read once, past the caches too where no line is shared by two loads: 3001 x 131072 373 us through them, 364
   // past them; 777 rows that begin inside lines 33.9 and 39.2.)
+  in_either_way(a.past_caches && a.whole_lines, [&](auto past) {
 #pragma unroll
-  for (uint32_t i = 0; i < kHeld; ++i) {
-    const uint32_t run = thread + i * kThreads;
-    if (run < runs) held[i] = load_run<T, N>(z_row + run * N, a.past_caches && a.whole_lines);
-  }
+    for (uint32_t i = 0; i < kHeld; ++i) {
+      const uint32_t run = thread + i * kThreads;
+      if (run < runs) held[i] = fetch_run<decltype(past)::value, T, N>(z_row + run * N);
+    }
+  });
   float z_left = thread < left ? (float)z_row[runs * N + thread] : -__builtin_inff();
   for (uint32_t i = thread; i < (a.V + 63) / 64 * 2; i += kThreads) n.bits[i] = 0;
   if (thread == 0) sh_repeated = 0;

@@ -1,5 +1,7 @@
 // Elements of 32 and 16 bits in runs that are aligned to the element only, and reductions over a wave, for the operators.
 #pragma once
+#include <type_traits>
+
 #include "wave.hpp"
 
 namespace apex {
@@ -28,34 +30,37 @@ __device__ __forceinline__ Run<T, N> load_run(const T *p)
 // 57.7; scan of 1 x 32768 x 768 65.5 and 58.1).
 constexpr uint64_t kPastCachesBytes = 32ull << 20;  // what the L2 caches of the chip hold
 
-template <typename T, int N>
-__device__ __forceinline__ void store_run(T *p, const Run<T, N> &r, bool past_caches)
+// f(integral_constant<bool>), the accesses of one way apart from those of the other: the comments in the assembly differ, on both
+// sides, so that the compiler does not make one ordinary access of two.
+template <typename F>
+__device__ __forceinline__ void in_either_way(bool past_caches, F f)
 {
-  // (The comments in the assembly differ, on both sides, so that the compiler does not make one ordinary access of the two.)
   if (past_caches) {
     asm volatile("; past the caches");
-    __builtin_nontemporal_store(r, reinterpret_cast<Run<T, N> *>(p));
+    f(std::integral_constant<bool, true>());
     asm volatile("; past the caches");
   } else {
     asm volatile("; through the caches");
-    *reinterpret_cast<Run<T, N> *>(p) = r;
+    f(std::integral_constant<bool, false>());
     asm volatile("; through the caches");
   }
 }
+
 template <typename T, int N>
-__device__ __forceinline__ Run<T, N> load_run(const T *p, bool past_caches)
+__device__ __forceinline__ void store_run(T *p, const Run<T, N> &r, bool past_caches)
 {
-  Run<T, N> r;
-  if (past_caches) {
-    asm volatile("; past the caches");
-    r = __builtin_nontemporal_load(reinterpret_cast<const Run<T, N> *>(p));
-    asm volatile("; past the caches");
-  } else {
-    asm volatile("; through the caches");
-    r = load_run<T, N>(p);
-    asm volatile("; through the caches");
-  }
-  return r;
+  in_either_way(past_caches, [&](auto past) {
+    if (decltype(past)::value)
+      __builtin_nontemporal_store(r, reinterpret_cast<Run<T, N> *>(p));
+    else
+      *reinterpret_cast<Run<T, N> *>(p) = r;
+  });
+}
+template <bool kPast, typename T, int N>
+__device__ __forceinline__ Run<T, N> fetch_run(const T *p)
+{
+  if (kPast) return __builtin_nontemporal_load(reinterpret_cast<const Run<T, N> *>(p));
+  return load_run<T, N>(p);
 }
 
 template <int N, typename T>

@@ -29,7 +29,7 @@ struct ScanBackArgs {
   uint64_t dg_seq, dg_time, dx_seq, dx_time;
   void *dg, *dx;
   float *dh0;
-  bool past_caches;
+  bool past_caches;  // dg and dx are stored past the caches
 };
 
 __device__ __forceinline__ uint32_t scan_length(const int32_t *length, uint32_t s, uint32_t T)
@@ -395,6 +395,17 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
   const uint32_t len = scan_length(a.length, s, a.T);
   const uint32_t t_group = t0 + w.group * kTileRows, d = d0 + w.run;
   const bool exists = d < a.D, whole = t0 + w.steps <= len && d0 + kWidth <= a.D;
+  if (t0 >= len) {  // nothing but what a sequence's end leaves
+    T *const h = static_cast<T *>(a.h) + ((uint64_t)s * a.T + t_group) * a.D;
+    for (uint32_t l = 0; l < kTileRows; ++l)
+      if (exists && t_group + l < a.T) store_run_of<T, N>(h + (uint64_t)l * a.D, d, a.D, Run<T, N>{});
+    if (tile == 0 && a.h_last && w.thread < kWidth && d0 + w.channel < a.D) {
+      const uint64_t at = (uint64_t)s * a.D + d0 + w.channel;
+      a.h_last[at] = a.h0 ? a.h0[at] : 0.0f;
+    }
+    if (kChained && w.thread == w.threads - 1) left(chain, leaving(chain), tag);
+    return;
+  }
   // the rows of this thread
   Run<T, N> gr[kTileRows], xr[kTileRows];
   {
@@ -458,20 +469,17 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
   const bool speaks = w.thread < kWidth && d0 + w.channel < a.D;
   float state_in = 0.0f;  // what enters the chain; then what enters the tile
   if (speaks && a.h0 && tile < kStretch) state_in = a.h0[(uint64_t)s * a.D + d0 + w.channel];
-  if (speaks && a.h_last && tile == 0 && len == 0) a.h_last[(uint64_t)s * a.D + d0 + w.channel] = state_in;
   if constexpr (kChained) {
-    if (t0 < len) {
-      float A = 1.0f, B = 0.0f;
-      if (w.thread < kWidth)
-        for (uint32_t i = 0; i < w.segments; ++i) {
-          const float sa = segment_a[i * kWidth + w.channel], sb = segment_b[i * kWidth + w.channel];
-          const bool passes = into.all_of_segment(i);
-          A = passes ? A * sa : 0.0f;
-          B = passes ? __builtin_fmaf(sa, B, sb) : sb;
-        }
-      state_in = chain_state(chain.space->word + (uint64_t)column * chain.tiles * 3 * kWidth, tile, d0 + w.channel < a.D, A, B, !no_cut,
-                             state_in, tag, sh_chain);
-    }
+    float A = 1.0f, B = 0.0f;
+    if (w.thread < kWidth)
+      for (uint32_t i = 0; i < w.segments; ++i) {
+        const float sa = segment_a[i * kWidth + w.channel], sb = segment_b[i * kWidth + w.channel];
+        const bool passes = into.all_of_segment(i);
+        A = passes ? A * sa : 0.0f;
+        B = passes ? __builtin_fmaf(sa, B, sb) : sb;
+      }
+    state_in = chain_state(chain.space->word + (uint64_t)column * chain.tiles * 3 * kWidth, tile, d0 + w.channel < a.D, A, B, !no_cut,
+                           state_in, tag, sh_chain);
   }
   if (w.thread < kWidth) {
     segment_in[w.channel] = state_in;
@@ -570,6 +578,21 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, 4) void
   const uint32_t len = scan_length(a.length, s, a.T);
   const uint32_t t_group = t0 + w.group * kTileRows, d = d0 + w.run;
   const bool exists = d < a.D, whole = t0 + w.steps <= len && d0 + kWidth <= a.D;
+  if (t0 >= len) {
+    T *const dg = static_cast<T *>(a.dg) + s * a.dg_seq + t_group * a.dg_time;
+    T *const dx = static_cast<T *>(a.dx) + s * a.dx_seq + t_group * a.dx_time;
+    for (uint32_t l = 0; l < kTileRows; ++l)
+      if (exists && t_group + l < a.T) {
+        store_run_of<T, N>(dg + l * a.dg_time, d, a.D, Run<T, N>{});
+        store_run_of<T, N>(dx + l * a.dx_time, d, a.D, Run<T, N>{});
+      }
+    if (tile == 0 && a.dh0 && w.thread < kWidth && d0 + w.channel < a.D) {
+      const uint64_t at = (uint64_t)s * a.D + d0 + w.channel;
+      a.dh0[at] = a.dh_last ? a.dh_last[at] : 0.0f;
+    }
+    if (kChained && w.thread == w.threads - 1) left(chain, leaving(chain), tag);
+    return;
+  }
   Run<T, N> gr[kTileRows], xr[kTileRows], hr[kTileRows];
   {
     const T *const g = static_cast<const T *>(a.g) + s * a.g_seq + t_group * a.g_time;
@@ -679,23 +702,20 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, 4) void
   __syncthreads();
 #pragma unroll
   for (uint32_t i = 0; i < kSegment; ++i) group_a[(w.segment * kSegment + i) * kWidth + w.channel] = states[i];
-  const uint32_t last = len ? (len - 1) / w.steps : 0;
+  const uint32_t last = (len - 1) / w.steps;
   float back_in = 0.0f;  // what enters the chain from behind; then what enters the tile
   if (speaks && a.dh_last && tile <= last && last - tile < kStretch) back_in = a.dh_last[(uint64_t)s * a.D + d0 + w.channel];
-  if (speaks && a.dh0 && tile == 0 && len == 0) a.dh0[(uint64_t)s * a.D + d0 + w.channel] = back_in;
   if constexpr (kChained) {
-    if (t0 < len) {
-      float P = 1.0f, Q = 0.0f;
-      if (w.thread < kWidth)
-        for (uint32_t i = w.segments; i-- > 0;) {
-          const float sp = segment_p[i * kWidth + w.channel], sq = segment_q[i * kWidth + w.channel];
-          const bool passes = on.all_of_segment(i);
-          P = passes ? P * sp : 0.0f;
-          Q = passes ? __builtin_fmaf(sp, Q, sq) : sq;
-        }
-      back_in = chain_state(chain.space->word + (uint64_t)column * chain.tiles * 3 * kWidth, last - tile, is, P, Q, !no_cut, back_in, tag,
-                            sh_chain);
-    }
+    float P = 1.0f, Q = 0.0f;
+    if (w.thread < kWidth)
+      for (uint32_t i = w.segments; i-- > 0;) {
+        const float sp = segment_p[i * kWidth + w.channel], sq = segment_q[i * kWidth + w.channel];
+        const bool passes = on.all_of_segment(i);
+        P = passes ? P * sp : 0.0f;
+        Q = passes ? __builtin_fmaf(sp, Q, sq) : sq;
+      }
+    back_in = chain_state(chain.space->word + (uint64_t)column * chain.tiles * 3 * kWidth, last - tile, is, P, Q, !no_cut, back_in, tag,
+                          sh_chain);
   }
   if (w.thread < kWidth)
     for (uint32_t i = w.segments; i-- > 0;) {
@@ -759,7 +779,7 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, 4) void
       }
     }
     });
-    if (a.dh0 && t_group == 0 && len > 0) store_run_of<float, N>(a.dh0 + (uint64_t)s * a.D, d, a.D, back);
+    if (a.dh0 && t_group == 0) store_run_of<float, N>(a.dh0 + (uint64_t)s * a.D, d, a.D, back);
   }
   if (kChained && w.thread == w.threads - 1) left(chain, before, tag);
 }
