@@ -438,6 +438,41 @@ def test_verify_strides_addresses_and_workspace(apex):
         c.check(apex, workspace=space)
 
 
+# ---------------------------------------------------------------------------------------------- far apart, and the largest
+
+def test_rows_whose_offsets_pass_32_bits(apex):
+    """Rows 2^31 and more elements apart (13 GB of bf16, of which only the rows are filled)."""
+    far = (1 << 31) + 24
+    held = torch.empty((3, far), dtype=torch.bfloat16, device="cuda:0")
+    c = Distill(3, 2003, 7, "bf16", rest=True, seed=3)
+    want = c.want()
+    held[:, 8:2011] = c.logits
+    c.logits = held[:, 8:2011]
+    c.check(c.run(apex, out=dict(loss=torch.empty(3, device="cuda:0"), grad=c.logits)), want)
+    s = Scan(3, 150, 40, "bf16", "sigmoid", seed=4, cut=True)
+    want = s.want()
+    rows = torch.as_strided(held, (3, 150, 40), (far, 64, 1))
+    rows.copy_(s.g)
+    s.check(s.run(apex, g=rows), want)
+    v = Verify(3, 1, 4000, "bf16", seed=5)
+    t = torch.as_strided(held, (3, 2, 4000), (far, 4096, 1))
+    t.copy_(v.target)
+    v.target = t
+    v.check(apex)
+    v.target = t.contiguous()
+    d = torch.as_strided(held, (3, 1, 4000), (far, 1, 1), storage_offset=16)
+    d.copy_(v.draft)
+    v.draft = d
+    v.check(apex)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_largest_vocabulary(apex, dtype):
+    c = Distill(2, apex.MAX_VOCABULARY, apex.MAX_TOP, dtype, rest=True, seed=6)
+    c.check(c.run(apex))
+    Verify(2, 2, apex.MAX_VOCABULARY, dtype, seed=7).check(apex)
+
+
 # -------------------------------------------------------------------------------------------------- streams and graphs
 
 def test_operators_on_a_stream_of_their_own_and_in_a_graph(apex):
