@@ -140,7 +140,7 @@ constexpr uint32_t kMostTiles = 1u << 22;  // of a chain: its words are counted 
 constexpr uint32_t kMostPolls = 1u << 20;  // a wait gives up (and hands on NaN) where the workspace was not as required
 
 constexpr uint32_t kStretch = 4;  // tiles of a stretch
-constexpr uint32_t kWindow = 16;  // compositions that a workgroup fetches at once
+constexpr uint32_t kWindow = 8;   // compositions that a workgroup fetches at once
 
 __device__ __forceinline__ bool carries(uint64_t word, uint32_t tag) { return ((uint32_t)(word >> 32) & ~kCutTag) == tag; }
 __device__ __forceinline__ float number(uint64_t word) { return __uint_as_float((uint32_t)word); }
@@ -201,7 +201,8 @@ struct ChainSpace {
 // kStretch tiles are a stretch: a tile publishes its composition, the last one of a stretch the stretch's and the state behind
 // it.  A tile goes back to the nearest stretch whose state is there (the first wave looks at 64 at once), through the
 // compositions of the stretches from there on, and through those of the tiles of its own stretch before it, which all threads
-// fetch, up to kWindow with one round trip.
+// fetch, up to kWindow with one round trip.  (Without stretches, from tile to tile, by the threads that have a channel: 1 x
+// 32768 x 768 109 us, where a state comes past 64 tiles at a time.  Stretches of 8: gradient of 4 x 8192 x 2048 208 us, 200 of 4.)
 // Words of position p: word + p * 3 * kTileWidth: A, B, and a third row that the last three tiles of a stretch lend to the
 // stretch: its A, its B, and the state behind it.
 __device__ __forceinline__ float chain_state(uint64_t *word, uint32_t q, bool is, float A, float B, bool cut, float start, uint32_t tag,
@@ -551,7 +552,7 @@ constexpr uint32_t tile_back_lds(uint32_t threads)  // both kinds of composition
 }
 
 template <typename T, int kGate, bool kChained>
-__global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, 4) void scan_tile_back_kernel(ScanBackArgs a, Chain chain)
+__global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChained || sizeof(T) == 4 ? 4 : 6) void scan_tile_back_kernel(ScanBackArgs a, Chain chain)
 {
   constexpr uint32_t N = kTileRun, kWidth = kTileWidth;
   constexpr uint32_t kChunkGroups = APEX_SCAN_CHUNK / kTileRows, kChunkSegments = kChunkGroups / kSegment;
@@ -786,7 +787,8 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, 4) void
 
 constexpr uint32_t kChannelThreads = 64;
 
-// A thread per channel, step after step.
+// A thread per channel, step after step: for an actor's single tokens.  Bound by the round trip of a launch and two loads
+// (64 x 1 x 1024: 2.3 us), and for longer sequences by one step's loads after the other's.
 template <typename T, int kGate>
 __global__ __launch_bounds__(kChannelThreads) void scan_channel_kernel(ScanArgs a)
 {
@@ -909,7 +911,12 @@ void with_gate(int gate, F f)
     f(std::integral_constant<int, APEX_GATE_GIVEN>());
 }
 
-constexpr uint32_t kTileMinSteps = 16;  // shorter sequences: a thread per channel
+// Shorter sequences go by a thread per channel.  us, forward / gradient, by channel and by tile (bf16, a row of workgroups deep):
+//     64 x T x 1024   T = 1   2.3 / 2.6   4.2 / 6.1      512 x T x 512   T = 1    3.3 / 4.3    5.9 / 9.5
+//                         8   3.8 / 5.4   4.6 / 6.9                          8    5.4 / 10.6   6.7 / 11.2
+//                        12   4.6 / 7.1   4.6 / 7.1                         12    6.5 / 16.2   7.1 / 12.7
+//                        16   5.5 / 8.7   4.3 / 6.9                         16    7.5 / 26.4   6.9 / 13.6
+constexpr uint32_t kTileMinSteps = 12;
 
 struct ScanLaunch {
   bool by_channel;

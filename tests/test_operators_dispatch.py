@@ -20,7 +20,7 @@ def bytes_of(entry, *sizes):
 
 def test_scan_by_channel_by_tile_and_by_chains_of_tiles(tmp_path):
     out = recorded_hip.run(tmp_path, SCAN + """
-result = [[scan(S, T, D, back)[1] for S, T, D in ((64, 1, 1000), (3, 15, 64), (3, 16, 130), (64, 96, 1024), (5, 128, 100),
+result = [[scan(S, T, D, back)[1] for S, T, D in ((64, 1, 1000), (3, 11, 64), (3, 12, 130), (64, 96, 1024), (5, 128, 100),
                                                   (2, 129, 300), (4, 8192, 2048))] for back in (False, True)]
 """)
     for back, name in ((0, "scan_"), (1, "scan_")):
