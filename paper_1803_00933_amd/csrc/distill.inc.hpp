@@ -220,7 +220,7 @@ __device__ __forceinline__ RowGradient settle(const DistillArgs &a, const Named 
 }
 
 // A workgroup per row.  kHeld runs of 16 bytes of the row stay in a thread's registers from the sum to the gradient, so that the
-// row is read once; kHeld = 0: rows too long for that are read again.
+// row is read once; kMore: what a row has beyond them is read again.
 // Bound by memory: 2048 x 32768 bf16 57 us for 269 MB (4.7 TB/s; a copy reaches 5.1), 777 x 49999 f16 34 us (4.5), 3001 x 131072
 // bf16 with a rest class 365 us for 1.58 GB (4.3): there a compute unit has one row at a time, and its memory waits while the
 // row is settled.  Reading every row twice took 115, 56 and 588.
@@ -228,7 +228,7 @@ __device__ __forceinline__ RowGradient settle(const DistillArgs &a, const Named 
 // for the third, looking marked elements up 423, a bit each and no look-up this.  Their logits are fetched by themselves, and the
 // wave that settles the row writes their gradients; the others write around them.
 // (Rows one after the other by a workgroup that stays, the next row's loads beside the gradient's stores: 510 us for the third.)
-template <typename T, uint32_t kThreads, uint32_t kHeld>
+template <typename T, uint32_t kThreads, uint32_t kHeld, bool kMore = false>
 __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
 {
   constexpr uint32_t N = 16 / sizeof(T), kWaves = kThreads / kWave;
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
     token = a.top_index[at];
     value = typed_element(a.top_value, a.value_dtype, at);
   }
-  Run<T, N> held[kHeld ? kHeld : 1];
+  Run<T, N> held[kHeld];
   // (A row that is read once, past the caches too where no line is shared by two loads: 3001 x 131072 373 us through them, 364
   // past them; 777 rows that begin inside lines 33.9 and 39.2.)
   in_either_way(a.past_caches && a.whole_lines, [&](auto past) {
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
   // the sum of this thread's part of the row, without the named tokens if there is a rest class
   Sum sum{-__builtin_inff(), 0.0f};
   if (a.top_lse && left_named) z_left = -__builtin_inff();
-  if constexpr (kHeld > 0) {
+  {
     float top = z_left;
 #pragma unroll
     for (uint32_t i = 0; i < kHeld; ++i) {
@@ -307,22 +307,16 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
       hold_packed<N, T>(held[i]);
     }
     sum = Sum{top, s};
-  } else {
-    const float alone[1] = {z_left};
-    add_to<1>(sum, alone, a.c);
-    for (uint32_t run = thread; run < runs; run += kThreads) {
+  }
+  if (kMore)
+    for (uint32_t run = thread + kHeld * kThreads; run < runs; run += kThreads) {
       const Run<T, N> r = load_run<T, N>(z_row + run * N);
+      const uint32_t named = a.top_lse ? n.mask<N>(run) : 0;
       float z[N];
 #pragma unroll
-      for (uint32_t e = 0; e < N; ++e) z[e] = element<N, T>(r, e);
-      const uint32_t named = a.top_lse ? n.mask<N>(run) : 0;
-      if (named) {
-#pragma unroll
-        for (uint32_t e = 0; e < N; ++e) z[e] = named >> e & 1 ? -__builtin_inff() : z[e];
-      }
+      for (uint32_t e = 0; e < N; ++e) z[e] = named >> e & 1 ? -__builtin_inff() : element<N, T>(r, e);
       add_to<N>(sum, z, a.c);
     }
-  }
   const float m = wave_max(sum.m), R = Sum::ref(m, a.c);
   const float s = wave_sum(sum.m == -__builtin_inff() ? sum.s : sum.s * exp2_of(Sum::ref(sum.m, a.c) - R));
   if (lane == 0) red_m[wave] = m, red_s[wave] = s;
@@ -356,13 +350,11 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
         if (!(named >> e & 1)) out[run * N + e] = r[e];
     }
   };
-  if constexpr (kHeld > 0) {
 #pragma unroll
-    for (uint32_t i = 0; i < kHeld; ++i)
-      if (thread + i * kThreads < runs) write(thread + i * kThreads, held[i]);
-  } else {
-    for (uint32_t run = thread; run < runs; run += kThreads) write(run, load_run<T, N>(z_row + run * N));
-  }
+  for (uint32_t i = 0; i < kHeld; ++i)
+    if (thread + i * kThreads < runs) write(thread + i * kThreads, held[i]);
+  if (kMore)
+    for (uint32_t run = thread + kHeld * kThreads; run < runs; run += kThreads) write(run, load_run<T, N>(z_row + run * N));
 }
 
 }  // namespace apex
@@ -413,7 +405,7 @@ int apex_distill_topk(uint32_t N, uint32_t V, uint32_t K, int dtype, const void 
     else if (runs <= 1024 * 16)
       distill_rows_kernel<E, 1024, 16><<<N, 1024, lds, stream>>>(a);
     else
-      distill_rows_kernel<E, 512, 0><<<N, 512, lds, stream>>>(a);
+      distill_rows_kernel<E, 1024, 16, true><<<N, 1024, lds, stream>>>(a);
   });
   APEX_HIP(hipGetLastError());
   return APEX_OK;

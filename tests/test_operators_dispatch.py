@@ -55,10 +55,11 @@ def distill(N, V, dtype=1):
 result = [distill(*a) for a in ((5, 1), (5, 8199), (3000, 8200), (3000, 32775), (3000, 32776), (3000, 65543), (3000, 65544),
                                 (3000, 131079), (3000, 131080), (3000, 1 << 20), (200, 32775), (200, 65544), (3000, 16388, 0))]
 """)
-    assert [l[0]["block"] for l in out] == [256, 256, 512, 512, 512, 512, 1024, 1024, 512, 512, 1024, 1024, 512]
+    assert [l[0]["block"] for l in out] == [256, 256, 512, 512, 512, 512, 1024, 1024, 1024, 1024, 1024, 1024, 512]
     assert all(len(l) == 1 for l in out)
     held = [int(l[0]["kernel"].split("Lj")[2].split("E")[0]) for l in out]
-    assert held == [4, 4, 8, 8, 16, 16, 16, 16, 0, 0, 8, 16, 16]
+    assert held == [4, 4, 8, 8, 16, 16, 16, 16, 16, 16, 8, 16, 16]
+    assert ["Lb1" in l[0]["kernel"] for l in out] == [i in (8, 9) for i in range(13)]      # rows of which a part is read twice
     assert [l[0]["grid"] for l in out[:3]] == [5, 5, 3000]
 
 
