@@ -599,6 +599,8 @@ typedef enum apex_gate {
  * carry [S, ceil(T / APEX_SCAN_CHUNK), D] fp32 (may be NULL): what passes into step t = c * APEX_SCAN_CHUNK, for those t
  * below the length; the others are unspecified.  The gradient asks for it.
  * With T = 1 this is the step of an actor: state in, state out.
+ * (Long sequences are computed in pieces whose factors are multiplied up: a state of +-inf becomes NaN where such a product
+ * underflows to 0.)
  * Workspace: may be NULL if the reported size is 0.
  */
 int apex_gated_scan_workspace_bytes(uint32_t S, uint32_t T, uint32_t D, size_t *bytes /*host*/);
