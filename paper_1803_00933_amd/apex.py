@@ -5,6 +5,7 @@ PyTorch supplies device memory (``tensor.data_ptr()``) and the current stream, n
 The calls of the path itself are marshalled by ``apex_binding.so`` (``csrc/binding.cpp``), set-up and the rest by ctypes.
 There is no fallback: if either has not been built, importing this module raises.
 """
+import contextlib
 import ctypes as C
 import os
 
@@ -210,6 +211,14 @@ def nstep_priorities(q_online, q_target, action, reward, discount, n, alpha, eps
 # Each takes its outputs in `out` (a dict, as it returns) or makes them, and a workspace that the caller keeps (one per stream;
 # without one the call makes its own, at the price of an allocation and a fill).
 
+def _made_on(stream):
+    """Where tensors for a call on `stream` are made: in the allocator's pool of that stream and filled there, so that neither
+    the fill nor an earlier or a later user of the memory overlaps the call."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream))
+
+
 def _workspace(entry, device, *sizes):
     n = C.c_size_t(0)
     rc = entry(*sizes, C.byref(n))
@@ -231,14 +240,16 @@ def gated_scan(g, x, gate="sigmoid", discount=None, length=None, h0=None, carry=
     """h_t = a_t h_{t-1} + b_t over device tensors g, x [S,T,D] (any strides but the channels'), a and b by `gate`: "given"
     or "sigmoid".  discount fp32 [S,T] (0: nothing passes on), length int32 [S], h0 fp32 [S,D].
     Returns (rc, out): h [S,T,D], h_last fp32 [S,D], and with carry=True what gated_scan_backward needs."""
-    if out is None:
+    if out is None or workspace is None:
         S, T, D = g.shape
-        out = dict(h=torch.empty((S, T, D), dtype=g.dtype, device=g.device),
-                   h_last=torch.empty((S, D), dtype=torch.float32, device=g.device))
-        if carry:
-            out["carry"] = torch.empty(gated_scan_carry_shape(S, T, D), dtype=torch.float32, device=g.device)
-    if workspace is None:
-        workspace = gated_scan_workspace(*g.shape, device=g.device)
+        with _made_on(stream):
+            if out is None:
+                out = dict(h=torch.empty((S, T, D), dtype=g.dtype, device=g.device),
+                           h_last=torch.empty((S, D), dtype=torch.float32, device=g.device))
+                if carry:
+                    out["carry"] = torch.empty(gated_scan_carry_shape(S, T, D), dtype=torch.float32, device=g.device)
+            if workspace is None:
+                workspace = gated_scan_workspace(S, T, D, device=g.device)
     get = out.get
     return _call.gated_scan(g, x, GATES[gate], discount, length, h0, out["h"], get("h_last"), get("carry"), workspace, stream), out
 
@@ -247,12 +258,14 @@ def gated_scan_backward(g, x, dh, carry, gate="sigmoid", discount=None, length=N
                         stream=None):
     """Gradients of gated_scan from dh [S,T,D] and dh_last fp32 [S,D], with the carry it left.
     Returns (rc, out): dg and dx [S,T,D] (of any strides where `out` brings them), dh0 fp32 [S,D]."""
-    if out is None:
+    if out is None or workspace is None:
         S, T, D = g.shape
-        out = dict(dg=torch.empty(g.shape, dtype=g.dtype, device=g.device), dx=torch.empty(x.shape, dtype=x.dtype, device=x.device))
-        out["dh0"] = torch.empty((S, D), dtype=torch.float32, device=g.device)
-    if workspace is None:
-        workspace = gated_scan_workspace(*g.shape, device=g.device)
+        with _made_on(stream):
+            if out is None:
+                out = {n: torch.empty((S, T, D), dtype=g.dtype, device=g.device) for n in ("dg", "dx")}
+                out["dh0"] = torch.empty((S, D), dtype=torch.float32, device=g.device)
+            if workspace is None:
+                workspace = gated_scan_workspace(S, T, D, device=g.device)
     return _call.gated_scan_backward(g, x, GATES[gate], discount, length, carry, dh, dh_last, out["dg"], out["dx"], out.get("dh0"),
                                      workspace, stream), out
 
@@ -267,14 +280,15 @@ def distill_topk(logits, top_index, top_value, weight=None, top_lse=None, temper
     """Loss of logits [N,V] (rows of any stride) against a teacher's top logits: top_index int32 [N,K] (-1: empty place),
     top_value [N,K], and with top_lse fp32 [N] the tokens that are not named as a class of their own.
     Returns (rc, out): loss and lse fp32 [N] and, unless grad=False, grad [N,V], the gradient of sum(weight * loss)."""
-    if out is None:
-        N = logits.shape[0]
-        out = dict(loss=torch.empty(N, dtype=torch.float32, device=logits.device),
-                   lse=torch.empty(N, dtype=torch.float32, device=logits.device))
-        if grad:
-            out["grad"] = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    if workspace is None:
-        workspace = distill_topk_workspace(*logits.shape, device=logits.device)
+    if out is None or workspace is None:
+        N, V = logits.shape
+        with _made_on(stream):
+            if out is None:
+                out = {n: torch.empty(N, dtype=torch.float32, device=logits.device) for n in ("loss", "lse")}
+                if grad:
+                    out["grad"] = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
+            if workspace is None:
+                workspace = distill_topk_workspace(N, V, device=logits.device)
     get = out.get
     return _call.distill_topk(logits, top_index, top_value, top_lse, weight, temperature, out["loss"], get("lse"), get("grad"),
                               workspace, stream), out
@@ -289,12 +303,14 @@ def verify_draft(target, draft, token, rnd, length=None, out=None, workspace=Non
     """Which of the drafted tokens int32 [B,G] stand, given the target's probabilities [B,G+1,V], the draft's [B,G,V] and
     uniform 64-bit integers [B,G+1]; length int32 [B].
     Returns (rc, out): accepted int32 [B], and token int32 [B,G+1]: those that stand, the one that follows, -1."""
-    B, places, V = target.shape
-    if out is None:
-        out = dict(accepted=torch.empty(B, dtype=torch.int32, device=target.device),
-                   token=torch.empty((B, places), dtype=torch.int32, device=target.device))
-    if workspace is None:
-        workspace = verify_draft_workspace(B, V, device=target.device)
+    if out is None or workspace is None:
+        B, places, V = target.shape
+        with _made_on(stream):
+            if out is None:
+                out = dict(accepted=torch.empty(B, dtype=torch.int32, device=target.device),
+                           token=torch.empty((B, places), dtype=torch.int32, device=target.device))
+            if workspace is None:
+                workspace = verify_draft_workspace(B, V, device=target.device)
     return _call.verify_draft(target, draft, token, rnd, length, out["accepted"], out["token"], workspace, stream), out
 
 

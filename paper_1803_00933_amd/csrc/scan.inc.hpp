@@ -515,29 +515,29 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     }
     T *const h = static_cast<T *>(a.h) + ((uint64_t)s * a.T + t_group) * a.D;
     plainly<kChained>(no_cut, [&](auto is_plain) {
-    constexpr bool kPlain = decltype(is_plain)::value;
+      constexpr bool kPlain = decltype(is_plain)::value;
 #pragma unroll
-    for (uint32_t l = 0; l < kTileRows; ++l) {
-      const uint32_t t = t_group + l;
-      if (!kPlain && !(bits >> l & 1)) state = f32x4{};
-      Run<T, N> r;
+      for (uint32_t l = 0; l < kTileRows; ++l) {
+        const uint32_t t = t_group + l;
+        if (!kPlain && !(bits >> l & 1)) state = f32x4{};
+        Run<T, N> r;
 #pragma unroll
-      for (uint32_t e = 0; e < N; ++e) {
-        state[e] = __builtin_fmaf(fa[l][e], state[e], fb[l][e]);
-        r[e] = (T)state[e];
+        for (uint32_t e = 0; e < N; ++e) {
+          state[e] = __builtin_fmaf(fa[l][e], state[e], fb[l][e]);
+          r[e] = (T)state[e];
+        }
+        T *const to = h + (uint64_t)l * a.D;
+        if (whole) {
+          store_run<T, N>(to + d, r, a.past_caches);
+        } else if (t < a.T) {
+          if (t >= len) r = Run<T, N>{};
+          store_run_of<T, N>(to, d, a.D, r);
+        }
+        if (a.h_last && t + 1 == len) {
+          const bool on = !a.discount || a.discount[(uint64_t)s * a.T + t] != 0.0f;
+          store_run_of<float, N>(a.h_last + (uint64_t)s * a.D, d, a.D, on ? state : f32x4{});
+        }
       }
-      T *const to = h + (uint64_t)l * a.D;
-      if (whole) {
-        store_run<T, N>(to + d, r, a.past_caches);
-      } else if (t < a.T) {
-        if (t >= len) r = Run<T, N>{};
-        store_run_of<T, N>(to, d, a.D, r);
-      }
-      if (a.h_last && t + 1 == len) {
-        const bool on = !a.discount || a.discount[(uint64_t)s * a.T + t] != 0.0f;
-        store_run_of<float, N>(a.h_last + (uint64_t)s * a.D, d, a.D, on ? state : f32x4{});
-      }
-    }
     });
   }
   if (kChained && w.thread == w.threads - 1) left(chain, before, tag);
@@ -745,40 +745,40 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     T *const dg = static_cast<T *>(a.dg) + s * a.dg_seq + t_group * a.dg_time;
     T *const dx = static_cast<T *>(a.dx) + s * a.dx_seq + t_group * a.dx_time;
     plainly<kChained>(no_cut, [&](auto is_plain) {
-    constexpr bool kPlain = decltype(is_plain)::value;
+      constexpr bool kPlain = decltype(is_plain)::value;
 #pragma unroll
-    for (uint32_t l = 0; l < kTileRows; ++l) {
-      if (!kPlain && !(into >> l & 1)) prev[l] = f32x4{};
-      if (l + 1 < kTileRows)
+      for (uint32_t l = 0; l < kTileRows; ++l) {
+        if (!kPlain && !(into >> l & 1)) prev[l] = f32x4{};
+        if (l + 1 < kTileRows)
+#pragma unroll
+          for (uint32_t e = 0; e < N; ++e) {
+            const float xt = element<N, T>(xr[l], e);
+            prev[(l + 1) % kTileRows][e] = __builtin_fmaf(f[l][e], prev[l][e], kGate == APEX_GATE_SIGMOID ? rest[l][e] * xt : xt);
+          }
+      }
+#pragma unroll
+      for (uint32_t l = kTileRows; l-- > 0;) {
+        const uint32_t t = t_group + l;
+        if (!kPlain && !(bits >> l & 1)) back = f32x4{};
+        Run<T, N> dgr, dxr;
 #pragma unroll
         for (uint32_t e = 0; e < N; ++e) {
-          const float xt = element<N, T>(xr[l], e);
-          prev[(l + 1) % kTileRows][e] = __builtin_fmaf(f[l][e], prev[l][e], kGate == APEX_GATE_SIGMOID ? rest[l][e] * xt : xt);
+          float dgt, dxt;
+          const float lambda = element<N, T>(hr[l], e) + back[e];
+          scan_gate_back<kGate>(f[l][e], rest[l][e], element<N, T>(xr[l], e), prev[l][e], lambda, &dgt, &dxt);
+          back[e] = f[l][e] * lambda;
+          dgr[e] = (T)dgt;
+          dxr[e] = (T)dxt;
         }
-    }
-#pragma unroll
-    for (uint32_t l = kTileRows; l-- > 0;) {
-      const uint32_t t = t_group + l;
-      if (!kPlain && !(bits >> l & 1)) back = f32x4{};
-      Run<T, N> dgr, dxr;
-#pragma unroll
-      for (uint32_t e = 0; e < N; ++e) {
-        float dgt, dxt;
-        const float lambda = element<N, T>(hr[l], e) + back[e];
-        scan_gate_back<kGate>(f[l][e], rest[l][e], element<N, T>(xr[l], e), prev[l][e], lambda, &dgt, &dxt);
-        back[e] = f[l][e] * lambda;
-        dgr[e] = (T)dgt;
-        dxr[e] = (T)dxt;
+        if (whole) {
+          store_run<T, N>(dg + l * a.dg_time + d, dgr, a.past_caches);
+          store_run<T, N>(dx + l * a.dx_time + d, dxr, a.past_caches);
+        } else if (t < a.T) {
+          if (t >= len) dgr = dxr = Run<T, N>{};
+          store_run_of<T, N>(dg + l * a.dg_time, d, a.D, dgr);
+          store_run_of<T, N>(dx + l * a.dx_time, d, a.D, dxr);
+        }
       }
-      if (whole) {
-        store_run<T, N>(dg + l * a.dg_time + d, dgr, a.past_caches);
-        store_run<T, N>(dx + l * a.dx_time + d, dxr, a.past_caches);
-      } else if (t < a.T) {
-        if (t >= len) dgr = dxr = Run<T, N>{};
-        store_run_of<T, N>(dg + l * a.dg_time, d, a.D, dgr);
-        store_run_of<T, N>(dx + l * a.dx_time, d, a.D, dxr);
-      }
-    }
     });
     if (a.dh0 && t_group == 0) store_run_of<float, N>(a.dh0 + (uint64_t)s * a.D, d, a.D, back);
   }

@@ -524,3 +524,30 @@ def test_operators_on_a_stream_of_their_own_and_in_a_graph(apex):
         calls(plainly)
         torch.cuda.synchronize()
         equal(recorded, plainly)
+
+
+def test_operators_on_a_stream_that_is_not_the_current_one(apex):
+    """stream= without outputs and workspace, while the current stream uses and gives back memory of the same sizes: what the
+    calls make for themselves belongs to their stream."""
+    s, d, v = Scan(2, 900, 60, "f32", "sigmoid", cut=True), Distill(30, 5001, 9, "f32", rest=True), Verify(5, 3, 70001, "f32")
+    host = lambda t: t.cpu().numpy()  # noqa: E731
+    wants = s.want(), d.want(), plain.verify(plain.f64(v.target), plain.f64(v.draft), host(v.token), host(v.rnd).view(np.uint64))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for n in (5 * 1152, 30 * 4, 30 * 5001 * 4, 2 * 900 * 60 * 4):
+            used = torch.full((n,), 255, dtype=torch.uint8, device="cuda:0")
+            used.fill_(255)
+            del used
+        rc, out = apex.gated_scan(s.g, s.x, discount=s.discount, h0=s.h0, carry=True, stream=side)
+        assert rc == apex.OK
+        rc, back = apex.gated_scan_backward(s.g, s.x, s.dh, out["carry"], discount=s.discount, dh_last=s.dh_last, stream=side)
+        assert rc == apex.OK
+        rc, loss = apex.distill_topk(d.logits, d.index, d.value, weight=d.weight, top_lse=d.top_lse, stream=side)
+        assert rc == apex.OK
+        rc, verdict = apex.verify_draft(v.target, v.draft, v.token, v.rnd, stream=side)
+        assert rc == apex.OK
+        side.synchronize()
+        s.check({**out, **back}, wants[0])
+        d.check(loss, wants[1])
+        assert np.array_equal(host(verdict["accepted"]), wants[2][0]) and np.array_equal(host(verdict["token"]), wants[2][1])
