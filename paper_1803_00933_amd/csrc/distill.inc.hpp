@@ -91,13 +91,7 @@ __device__ __forceinline__ float power(float x, float scale, float scale_low)
   return exp2_of(low ? x + 64.0f : x) * (low ? scale_low : scale);
 }
 
-// e^x for the teacher's and the student's places: the exponent keeps 48 bits until its whole part is split off.
-__device__ __forceinline__ double exp_of(double x)
-{
-  if (x < -200.0) return 0.0;
-  const double y = x * 1.4426950408889634, n = __builtin_rint(y);
-  return __builtin_ldexp((double)exp2_of((float)(y - n)), (int)fmin(n, 1000.0));
-}
+constexpr double kLn2d = 0.6931471805599453;
 
 // ln x, x > 0: the exponent apart, so that the error is that of a logarithm next to 0.
 __device__ __forceinline__ double ln_of(float x)
@@ -107,6 +101,48 @@ __device__ __forceinline__ double ln_of(float x)
   float m = __uint_as_float((__float_as_uint(x) & 0x007fffffu) | 0x3f800000u);
   if (m > 1.41421354f) m *= 0.5f, ++e;
   return ((double)e + (double)log2_of(m)) * 0.6931471805599453;
+}
+
+// e^x for the teacher's and the student's places: the exponent keeps 48 bits until its whole part is split off.
+__device__ __forceinline__ double exp_of(double x)
+{
+  if (x < -200.0) return 0.0;
+  const double y = x * 1.4426950408889634, n = __builtin_rint(y);
+  return __builtin_ldexp((double)exp2_of((float)(y - n)), (int)fmin(n, 1000.0));
+}
+
+// The same to 1e-12, for what is subtracted from 1: the series within ln 2 / 2 of a whole power of 2.
+__device__ __forceinline__ double exactly_exp_of(double x)
+{
+  if (x < -200.0) return 0.0;
+  const double n = __builtin_rint(x * 1.4426950408889634), f = __builtin_fma(-n, kLn2d, x);
+  double e = 1.0 / 3628800;
+  constexpr double kFactor[] = {1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 0.5, 1.0, 1.0};
+#pragma unroll
+  for (double k : kFactor) e = __builtin_fma(e, f, k);
+  return __builtin_ldexp(e, (int)fmin(n, 1000.0));
+}
+
+// e^u - 1 - u for |u| < 1, not by that difference: u^2 times its series.
+__device__ __forceinline__ float exp_beyond(float u)
+{
+  float e = 1.0f / 39916800;
+  constexpr float kFactor[] = {1.0f / 3628800, 1.0f / 362880, 1.0f / 40320, 1.0f / 5040, 1.0f / 720, 1.0f / 120, 1.0f / 24, 1.0f / 6, 0.5f};
+#pragma unroll
+  for (float k : kFactor) e = __builtin_fmaf(e, u, k);
+  return e * u * u;
+}
+
+// w - ln(1 + w) for -1/2 <= w: up to 1 by ln(1 + w) = 2 artanh t, t = w / (2 + w), of which w - 2 t = w t.
+__device__ __forceinline__ float log_short_of(float w)
+{
+  if (w > 1.0f) return w - (float)ln_of(1.0f + w);
+  const float t = w / (2.0f + w), tt = t * t;
+  float e = 1.0f / 19;
+  constexpr float kFactor[] = {1.0f / 17, 1.0f / 15, 1.0f / 13, 1.0f / 11, 1.0f / 9, 1.0f / 7, 1.0f / 5, 1.0f / 3};
+#pragma unroll
+  for (float k : kFactor) e = __builtin_fmaf(e, tt, k);
+  return w * t - 2.0f * t * tt * e;
 }
 
 // What a row's gradient is made of: of a token not named 2^(z c - R) * scale.
@@ -127,12 +163,10 @@ __device__ __forceinline__ bool enter_named(const DistillArgs &a, const Named &n
 // What a wave knows of a row's teacher.
 struct Teacher {
   double ln_sum;    // log-sum-exp that ln q is relative to
-  float mass;       // sum of q
+  double mass;      // sum of q
   uint32_t named;   // places that count
   bool teaches;     // not -inf for every one of them
 };
-
-constexpr double kLn2d = 0.6931471805599453;
 
 // ln of a sum of 2^(z c - R) whose largest z is m; c, as rounded, only scales what is relative to m.
 __device__ __forceinline__ double log_sum(const DistillArgs &a, float m, float R, float sum)
@@ -164,20 +198,32 @@ __device__ __forceinline__ Teacher teach(const DistillArgs &a, const Named &n, u
   sum = wave_sum(sum);
   t.teaches = sum != 0.0f;
   t.ln_sum = a.top_lse ? (double)a.top_lse[row] : log_sum(a, top, R, sum);
-  float mass = 0.0f;
+  double mass = 0.0;
   for (uint32_t k = lane; k < a.K; k += kWave)
     if (n.token[k] >= 0) {
-      const double q = t.teaches ? exp_of(__builtin_fma((double)n.value[k], a.inv_tau, -t.ln_sum)) : 0.0;
+      const double q = t.teaches ? exactly_exp_of(__builtin_fma((double)n.value[k], a.inv_tau, -t.ln_sum)) : 0.0;
       n.q[k] = q;
-      mass += (float)q;
+      mass += q;
     }
   t.mass = wave_sum(mass);
+  if (!a.top_lse && t.teaches) {  // what the sum in 32 bits was off: 1e-7
+    const double off = t.mass;
+    for (uint32_t k = lane; k < a.K; k += kWave)
+      if (n.token[k] >= 0) n.q[k] *= 2.0 - off;
+    t.ln_sum += off - 1.0;
+    t.mass = 1.0;
+  }
   return t;
 }
 
 // The rest of it, by the same wave, once the row's sum `all` (without the named tokens if there is a rest class) is known: writes
 // loss, lse and the gradients of the named tokens (out: the row's gradient, or null).
-// Logarithms of nearly equal numbers are subtracted: in 64 bits, a few operations for each named token.
+// The loss is not summed up as it is defined: q ln(q/p) and r ln(r/s) cancel to second order where the student is near its teacher,
+// and r and s to first where little is named.  With u = ln(p/q) and w = s/r - 1 (-sum (p - q) / r unless s is the smaller part) it is
+//     sum q (e^u - 1 - u) + r (w - ln(1 + w)),     with - sum (p - q) in place of the second where there is no rest,
+// terms that are not negative, each by a form of its own that does not cancel; and the gradient has p - q = q (e^u - 1), and
+// (M + r) - r/s = w / (1 + w) for the rest.  Errors of p's common factor, from the sum in 32 bits, enter times p - q.  (As defined:
+// losses of V = 40000, K = 1, tau = 4 off by 2e-3.)  64 bits, a few operations for each named token.
 template <typename T>
 __device__ __forceinline__ RowGradient settle(const DistillArgs &a, const Named &n, uint32_t row, const Teacher &t, Sum all, T *out)
 {
@@ -197,25 +243,53 @@ __device__ __forceinline__ RowGradient settle(const DistillArgs &a, const Named 
   if (s == 0.0f) s = __builtin_nanf("");  // no finite logit
   const float inv_s = 1.0f / s;
   const double ln_all = log_sum(a, top, R, s);
-  float rest = 0.0f;
-  if (a.top_lse && t.named < a.V) rest = t.mass > 1.0f ? 0.0f : 1.0f - t.mass;
-  const double given = (double)t.mass + (double)rest;
-  float loss = 0.0f;
+  double rest = 0.0;
+  if (a.top_lse && t.named < a.V) rest = t.mass > 1.0 ? 0.0 : 1.0 - t.mass;
+  const double more = rest > 0.0 ? 0.0 : t.mass - 1.0;  // masses of the teacher beyond 1
+  float terms = 0.0f, apart = 0.0f;                     // sums of q (e^u - 1 - u), of p - q
   for (uint32_t k = lane; k < a.K; k += kWave)
     if (n.token[k] >= 0) {
       const double q = n.q[k], ln_p = __builtin_fma((double)n.z[k], a.inv_tau, -ln_all);
-      if ((float)q != 0.0f) loss += (float)q * (float)(__builtin_fma((double)n.value[k], a.inv_tau, -t.ln_sum) - ln_p);
-      if (out) out[n.token[k]] = (T)(w == 0.0f ? 0.0f : (float)(wt * (given * exp_of(ln_p) - q)));
+      const double u = ln_p - __builtin_fma((double)n.value[k], a.inv_tau, -t.ln_sum);
+      double diff, term;
+      if (__builtin_fabs(u) < 1.0) {
+        const float beyond = exp_beyond((float)u);
+        term = q * beyond;
+        diff = q * (beyond + u);
+      } else {
+        diff = exp_of(ln_p) - q;
+        term = q == 0.0 ? diff : diff - q * u;
+      }
+      terms += (float)term;
+      apart += (float)diff;
+      if (out) out[n.token[k]] = (T)(w == 0.0f ? 0.0f : (float)(wt * (diff + more * (q + diff))));
     }
-  loss = wave_sum(loss);
-  if (rest != 0.0f) loss += rest * (float)(ln_of(rest) - (log_sum(a, all.m, R_rest, all.s) - ln_all));
+  float loss = wave_sum(terms);
+  apart = wave_sum(apart);
+  const float share = inv_s * exp2_of(R_rest - R), others = all.s == 0.0f ? 0.0f : all.s * share;  // others: s
+  const double ratio = others < 0.5f ? (double)others / rest - 1.0 : -(double)apart / rest;         // w
+  const bool plain = rest == 0.0 || !(ratio < -0.5);
+  if (rest == 0.0)
+    loss += t.named == a.V ? (float)more : -apart;
+  else if (plain)
+    loss += (float)rest * log_short_of((float)ratio);
+  else  // far less than the teacher gives the rest
+    loss += (float)(rest * (ratio + ln_of((float)rest) - (log_sum(a, all.m, R_rest, all.s) - ln_all)));
+  if (!a.top_lse && !t.teaches) loss = 0.0f;
   if (s != s) loss = s;
   if (lane == 0) {
     a.loss[row] = loss;
     if (a.lse) a.lse[row] = (float)ln_all;
   }
-  RowGradient g{R_rest, wt * (t.mass * inv_s), w == 0.0f};
-  if (a.top_lse) g.scale = all.s == 0.0f ? 0.0f : wt * ((float)given * inv_s * exp2_of(R_rest - R) - rest / all.s);
+  RowGradient g{R_rest, wt * ((float)t.mass * inv_s), w == 0.0f};
+  if (a.top_lse) {
+    if (all.s == 0.0f)
+      g.scale = 0.0f;
+    else if (plain)
+      g.scale = wt * (share * (float)(rest == 0.0 ? t.mass : ratio / (1.0 + ratio)));
+    else
+      g.scale = wt * (share - (float)rest / all.s);
+  }
   return g;
 }
 
@@ -230,7 +304,7 @@ __device__ __forceinline__ RowGradient settle(const DistillArgs &a, const Named 
 // What is beyond 256 KB of a row is read twice (512 x 200000 bf16 97 us; 116 with all of it read twice).
 // (Rows one after the other by a workgroup that stays, the next row's loads beside the gradient's stores: 510 us for the third.)
 template <typename T, uint32_t kThreads, uint32_t kHeld, bool kMore = false>
-__global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a)
+__global__ __launch_bounds__(kThreads, kHeld == 16 || kThreads == 1024 ? 4 : kHeld == 8 ? 6 : 8) void distill_rows_kernel(DistillArgs a)
 {
   constexpr uint32_t N = 16 / sizeof(T), kWaves = kThreads / kWave;
   extern __shared__ uint64_t lds[];

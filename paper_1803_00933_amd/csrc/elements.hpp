@@ -116,6 +116,25 @@ __device__ __forceinline__ float wave_max(float v)
   return wave_reduce(v, -__builtin_inff(), [](float a, float b) { return fmaxf(a, b); });
 }
 
+__device__ __forceinline__ double wave_sum(double v)
+{
+  const auto step = [&](auto from) {
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __float_as_uint(from(__uint_as_float((uint32_t)bits))), hi = __float_as_uint(from(__uint_as_float((uint32_t)(bits >> 32))));
+    v += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  };
+  step([](float x) { return dpp_from<0x111, 0xf>(x, 0.0f); });
+  step([](float x) { return dpp_from<0x112, 0xf>(x, 0.0f); });
+  step([](float x) { return dpp_from<0x114, 0xf>(x, 0.0f); });
+  step([](float x) { return dpp_from<0x118, 0xf>(x, 0.0f); });
+  step([](float x) { return dpp_from<0x142, 0xa>(x, 0.0f); });
+  step([](float x) { return dpp_from<0x143, 0xc>(x, 0.0f); });
+  const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)bits, kWave - 1);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(bits >> 32), kWave - 1);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
 // 2^x and log2 x as the hardware has them: within 1 ulp; results of 2^x below the normal range are 0.
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
