@@ -62,10 +62,40 @@ __device__ __forceinline__ float typed_element(const void *p, uint32_t dtype, ui
 }
 
 // The sum of 2^(z c - R) over logits whose largest is m, R = m c rounded to a whole number (0 while m is -inf).
+// In 32 bits R misses m c by up to 64 where that is next to 2^31: the sum is relative to R all the same.  Beyond that, as with logits
+// masked by their type's lowest value, R is m c itself, and the power is 1 for z = m and 0 for every other z.
 struct Sum {
   float m, s;
-  __device__ __forceinline__ static float ref(float m, float c) { return m == -__builtin_inff() ? 0.0f : __builtin_rintf(m * c); }
+  __device__ __forceinline__ static bool far(float m, float c) { return !(__builtin_fabsf(m * c) < 0x1p31f) && m != -__builtin_inff(); }
+  __device__ __forceinline__ static double ref(float m, float c)
+  {
+    if (far(m, c)) return (double)m * (double)c;
+    return m == -__builtin_inff() ? 0.0 : (double)__builtin_rintf(m * c);
+  }
 };
+
+// z c - R as z times + plus.  Far from 0 `times` is the power of 2 that brings m into [2^32, 2^33): whatever differs from m is 2^8 away.
+struct Exponent {
+  float times, plus;
+  __device__ __forceinline__ Exponent(float m, float c)
+  {
+    if (Sum::far(m, c)) {
+      times = __uint_as_float(min(286u - (__float_as_uint(m) >> 23 & 255u), 254u) << 23);
+      plus = -m * times;
+    } else {
+      times = c;
+      plus = m == -__builtin_inff() ? 0.0f : -__builtin_rintf(m * c);
+    }
+  }
+  __device__ __forceinline__ float of(float z) const { return __builtin_fmaf(z, times, plus); }
+};
+
+// What a sum relative to `from` is multiplied by to be relative to `to`, from <= to, neither of them -inf.
+__device__ __forceinline__ float relative(float from, float to, float c)
+{
+  if (Sum::far(to, c)) return exp2_of((float)(((double)from - (double)to) * (double)c));
+  return exp2_of(__builtin_rintf(from * c) - __builtin_rintf(to * c));
+}
 
 template <int N>
 __device__ __forceinline__ void add_to(Sum &a, const float (&z)[N], float c)
@@ -73,11 +103,12 @@ __device__ __forceinline__ void add_to(Sum &a, const float (&z)[N], float c)
   float top = z[0];
 #pragma unroll
   for (int e = 1; e < N; ++e) top = fmaxf(top, z[e]);
-  const float m = fmaxf(a.m, top), R = Sum::ref(m, c);
+  const float m = fmaxf(a.m, top);
+  const Exponent x(m, c);
   float s = 0.0f;
 #pragma unroll
-  for (int e = 0; e < N; ++e) s += exp2_of(__builtin_fmaf(z[e], c, -R));
-  a.s = __builtin_fmaf(a.s, a.m == -__builtin_inff() ? 1.0f : exp2_of(Sum::ref(a.m, c) - R), s);  // (NaN may be there without a maximum)
+  for (int e = 0; e < N; ++e) s += exp2_of(x.of(z[e]));
+  a.s = __builtin_fmaf(a.s, a.m == -__builtin_inff() ? 1.0f : relative(a.m, m, c), s);  // (NaN may be there without a maximum)
   a.m = m;
 }
 
@@ -145,9 +176,9 @@ __device__ __forceinline__ float log_short_of(float w)
   return w * t - 2.0f * t * tt * e;
 }
 
-// What a row's gradient is made of: of a token not named 2^(z c - R) * scale.
+// What a row's gradient is made of: of a token not named 2^(z c - R) * scale, R that of m.
 struct RowGradient {
-  float R, scale;
+  float m, scale;
   bool zero;  // the row's weight is 0
 };
 
@@ -162,17 +193,17 @@ __device__ __forceinline__ bool enter_named(const DistillArgs &a, const Named &n
 
 // What a wave knows of a row's teacher.
 struct Teacher {
-  double ln_sum;    // log-sum-exp that ln q is relative to
-  double mass;      // sum of q
-  uint32_t named;   // places that count
-  bool teaches;     // not -inf for every one of them
+  double top, ln_sum;  // ln q = (value - top) / tau - ln_sum
+  double mass;         // sum of q
+  uint32_t named;      // places that count
+  bool teaches;        // not -inf for every one of them
 };
 
-// ln of a sum of 2^(z c - R) whose largest z is m; c, as rounded, only scales what is relative to m.
-__device__ __forceinline__ double log_sum(const DistillArgs &a, float m, float R, float sum)
+// ln of a sum of 2^(z c - R) whose largest z is m, less m / tau; c, as rounded, only scales what is relative to m.
+__device__ __forceinline__ double log_sum(const DistillArgs &a, float m, double R, float sum)
 {
   if (m == -__builtin_inff()) return -__builtin_inf();
-  return __builtin_fma((double)m, a.inv_tau, ln_of(sum) + kLn2d * __builtin_fma(-(double)m, (double)a.c, (double)R));
+  return ln_of(sum) + kLn2d * __builtin_fma(-(double)m, (double)a.c, R);
 }
 
 // The part of a row that needs no sum over the vocabulary, by one wave: drops places whose token an earlier one names (if there
@@ -191,17 +222,19 @@ __device__ __forceinline__ Teacher teach(const DistillArgs &a, const Named &n, u
   Teacher t;
   t.named = (uint32_t)wave_sum((float)mine);  // at most APEX_MAX_TOP
   top = wave_max(top);
-  const float R = Sum::ref(top, a.c);
+  const Exponent x(top, a.c);
   float sum = 0.0f;
   for (uint32_t k = lane; k < a.K; k += kWave)
-    if (n.token[k] >= 0) sum += exp2_of(__builtin_fmaf(n.value[k], a.c, -R));
+    if (n.token[k] >= 0) sum += exp2_of(x.of(n.value[k]));
   sum = wave_sum(sum);
   t.teaches = sum != 0.0f;
-  t.ln_sum = a.top_lse ? (double)a.top_lse[row] : log_sum(a, top, R, sum);
+  t.top = a.top_lse || top == -__builtin_inff() ? 0.0 : (double)top;
+  t.ln_sum = a.top_lse ? (double)a.top_lse[row] : log_sum(a, top, Sum::ref(top, a.c), sum);
   double mass = 0.0;
   for (uint32_t k = lane; k < a.K; k += kWave)
     if (n.token[k] >= 0) {
-      const double q = t.teaches ? exactly_exp_of(__builtin_fma((double)n.value[k], a.inv_tau, -t.ln_sum)) : 0.0;
+      const double ln_q = __builtin_fma((double)n.value[k] - t.top, a.inv_tau, -t.ln_sum);
+      const double q = !t.teaches ? 0.0 : a.top_lse ? exactly_exp_of(ln_q) : exp_of(ln_q);
       n.q[k] = q;
       mass += q;
     }
@@ -217,40 +250,53 @@ __device__ __forceinline__ Teacher teach(const DistillArgs &a, const Named &n, u
 }
 
 // The rest of it, by the same wave, once the row's sum `all` (without the named tokens if there is a rest class) is known: writes
-// loss, lse and the gradients of the named tokens (out: the row's gradient, or null).
+// the gradients of the named tokens (out: the row's gradient, or null).
 // The loss is not summed up as it is defined: q ln(q/p) and r ln(r/s) cancel to second order where the student is near its teacher,
 // and r and s to first where little is named.  With u = ln(p/q) and w = s/r - 1 (-sum (p - q) / r unless s is the smaller part) it is
 //     sum q (e^u - 1 - u) + r (w - ln(1 + w)),     with - sum (p - q) in place of the second where there is no rest,
 // terms that are not negative, each by a form of its own that does not cancel; and the gradient has p - q = q (e^u - 1), and
 // (M + r) - r/s = w / (1 + w) for the rest.  Errors of p's common factor, from the sum in 32 bits, enter times p - q.  (As defined:
 // losses of V = 40000, K = 1, tau = 4 off by 2e-3.)  64 bits, a few operations for each named token.
+struct Settled {
+  RowGradient gradient;
+  double base, ln_all;       // ln p = (z - base) / tau - ln_all
+  double rest, more, ratio;  // r; sum q - 1 where r is 0; w
+  double terms;              // a lane's part of the sum of q (e^u - 1 - u)
+  float apart;               // of p - q: the sum if there is a rest class, else a lane's part
+  bool plain;                // w is not below -1/2
+};
+
 template <typename T>
-__device__ __forceinline__ RowGradient settle(const DistillArgs &a, const Named &n, uint32_t row, const Teacher &t, Sum all, T *out)
+__device__ __forceinline__ Settled settle(const DistillArgs &a, const Named &n, uint32_t row, const Teacher &t, Sum all, T *out)
 {
   const uint32_t lane = lane_id();
-  const float R_rest = Sum::ref(all.m, a.c), w = a.weight ? a.weight[row] : 1.0f, wt = w * a.grad_scale;
-  float top = all.m, R = R_rest, s = all.s;
+  const float w = a.weight ? a.weight[row] : 1.0f, wt = w * a.grad_scale;
+  Settled r;
+  float top = all.m, s = all.s, to_all = 1.0f;  // to_all: from a sum over the rest to one over the row
   if (a.top_lse) {
     float z_top = -__builtin_inff(), z_sum = 0.0f;
     for (uint32_t k = lane; k < a.K; k += kWave)
       if (n.token[k] >= 0) z_top = fmaxf(z_top, n.z[k]);
     top = fmaxf(wave_max(z_top), all.m);
-    R = Sum::ref(top, a.c);
+    const Exponent x(top, a.c);
     for (uint32_t k = lane; k < a.K; k += kWave)
-      if (n.token[k] >= 0) z_sum += exp2_of(__builtin_fmaf(n.z[k], a.c, -R));
-    s = wave_sum(z_sum) + (all.s == 0.0f ? 0.0f : all.s * exp2_of(R_rest - R));
+      if (n.token[k] >= 0) z_sum += exp2_of(x.of(n.z[k]));
+    to_all = all.s == 0.0f ? 0.0f : relative(all.m, top, a.c);
+    s = wave_sum(z_sum) + (all.s == 0.0f ? 0.0f : all.s * to_all);
   }
   if (s == 0.0f) s = __builtin_nanf("");  // no finite logit
   const float inv_s = 1.0f / s;
-  const double ln_all = log_sum(a, top, R, s);
-  double rest = 0.0;
-  if (a.top_lse && t.named < a.V) rest = t.mass > 1.0 ? 0.0 : 1.0 - t.mass;
-  const double more = rest > 0.0 ? 0.0 : t.mass - 1.0;  // masses of the teacher beyond 1
-  float terms = 0.0f, apart = 0.0f;                     // sums of q (e^u - 1 - u), of p - q
+  r.gradient = RowGradient{all.m, wt * ((float)t.mass * inv_s), w == 0.0f};
+  r.base = top == -__builtin_inff() ? 0.0 : (double)top;
+  r.ln_all = log_sum(a, top, Sum::ref(top, a.c), s);
+  r.rest = 0.0;
+  if (a.top_lse && t.named < a.V) r.rest = t.mass > 1.0 ? 0.0 : 1.0 - t.mass;
+  r.more = r.rest > 0.0 ? 0.0 : t.mass - 1.0;
+  r.terms = 0.0, r.apart = 0.0f;
   for (uint32_t k = lane; k < a.K; k += kWave)
     if (n.token[k] >= 0) {
-      const double q = n.q[k], ln_p = __builtin_fma((double)n.z[k], a.inv_tau, -ln_all);
-      const double u = ln_p - __builtin_fma((double)n.value[k], a.inv_tau, -t.ln_sum);
+      const double q = n.q[k], ln_p = __builtin_fma((double)n.z[k] - r.base, a.inv_tau, -r.ln_all);
+      const double u = ln_p - __builtin_fma((double)n.value[k] - t.top, a.inv_tau, -t.ln_sum);
       double diff, term;
       if (__builtin_fabs(u) < 1.0) {
         const float beyond = exp_beyond((float)u);
@@ -260,37 +306,41 @@ __device__ __forceinline__ RowGradient settle(const DistillArgs &a, const Named 
         diff = exp_of(ln_p) - q;
         term = q == 0.0 ? diff : diff - q * u;
       }
-      terms += (float)term;
-      apart += (float)diff;
-      if (out) out[n.token[k]] = (T)(w == 0.0f ? 0.0f : (float)(wt * (diff + more * (q + diff))));
+      r.terms += term;
+      r.apart += (float)diff;
+      if (out) out[n.token[k]] = (T)(w == 0.0f ? 0.0f : (float)(wt * (diff + r.more * (q + diff))));
     }
-  float loss = wave_sum(terms);
-  apart = wave_sum(apart);
-  const float share = inv_s * exp2_of(R_rest - R), others = all.s == 0.0f ? 0.0f : all.s * share;  // others: s
-  const double ratio = others < 0.5f ? (double)others / rest - 1.0 : -(double)apart / rest;         // w
-  const bool plain = rest == 0.0 || !(ratio < -0.5);
-  if (rest == 0.0)
-    loss += t.named == a.V ? (float)more : -apart;
-  else if (plain)
-    loss += (float)rest * log_short_of((float)ratio);
+  if (!a.top_lse) return r;
+  r.apart = wave_sum(r.apart);
+  const float share = inv_s * to_all, others = all.s == 0.0f ? 0.0f : all.s * share;  // others: s
+  r.ratio = others < 0.5f ? (double)others / r.rest - 1.0 : -(double)r.apart / r.rest;
+  r.plain = r.rest == 0.0 || !(r.ratio < -0.5);
+  if (all.s == 0.0f)
+    r.gradient.scale = 0.0f;
+  else if (r.plain)
+    r.gradient.scale = wt * (share * (r.rest == 0.0 ? (float)t.mass : (float)r.ratio / (1.0f + (float)r.ratio)));
+  else
+    r.gradient.scale = wt * (share - (float)r.rest / all.s);
+  return r;
+}
+
+// loss and lse of a settled row: the other waves do not wait for them.
+__device__ __forceinline__ void conclude(const DistillArgs &a, uint32_t row, const Teacher &t, Sum all, const Settled &r)
+{
+  double loss = wave_sum(r.terms);
+  if (r.rest == 0.0)
+    loss += t.named == a.V ? r.more : -(double)(a.top_lse ? r.apart : wave_sum(r.apart));
+  else if (r.plain)
+    loss += (float)r.rest * log_short_of((float)r.ratio);
   else  // far less than the teacher gives the rest
-    loss += (float)(rest * (ratio + ln_of((float)rest) - (log_sum(a, all.m, R_rest, all.s) - ln_all)));
-  if (!a.top_lse && !t.teaches) loss = 0.0f;
-  if (s != s) loss = s;
-  if (lane == 0) {
-    a.loss[row] = loss;
-    if (a.lse) a.lse[row] = (float)ln_all;
+    loss += r.rest * (r.ratio + ln_of((float)r.rest) -
+                      __builtin_fma((double)all.m - r.base, a.inv_tau, log_sum(a, all.m, Sum::ref(all.m, a.c), all.s) - r.ln_all));
+  if (!a.top_lse && !t.teaches) loss = 0.0;
+  if (!(__builtin_fabs(r.ln_all) < __builtin_inf())) loss = __builtin_nan("");  // the sum was NaN
+  if (lane_id() == 0) {
+    a.loss[row] = (float)loss;
+    if (a.lse) a.lse[row] = (float)__builtin_fma(r.base, a.inv_tau, r.ln_all);
   }
-  RowGradient g{R_rest, wt * ((float)t.mass * inv_s), w == 0.0f};
-  if (a.top_lse) {
-    if (all.s == 0.0f)
-      g.scale = 0.0f;
-    else if (plain)
-      g.scale = wt * (share * (float)(rest == 0.0 ? t.mass : ratio / (1.0 + ratio)));
-    else
-      g.scale = wt * (share - (float)rest / all.s);
-  }
-  return g;
 }
 
 // A workgroup per row.  kHeld runs of 16 bytes of the row stay in a thread's registers from the sum to the gradient, so that the
@@ -372,13 +422,13 @@ __global__ __launch_bounds__(kThreads, kHeld == 16 || kThreads == 1024 ? 4 : kHe
       for (uint32_t e = 0; e < N; ++e) top = fmaxf(top, element<N, T>(held[i], e));
       hold_packed<N, T>(held[i]);
     }
-    const float R = Sum::ref(top, a.c);
-    float s = exp2_of(__builtin_fmaf(z_left, a.c, -R));
+    const Exponent x(top, a.c);
+    float s = exp2_of(x.of(z_left));
 #pragma unroll
     for (uint32_t i = 0; i < kHeld; ++i) {
       if (thread + i * kThreads >= runs) continue;
 #pragma unroll
-      for (uint32_t e = 0; e < N; ++e) s += exp2_of(__builtin_fmaf(element<N, T>(held[i], e), a.c, -R));
+      for (uint32_t e = 0; e < N; ++e) s += exp2_of(x.of(element<N, T>(held[i], e)));
       hold_packed<N, T>(held[i]);
     }
     sum = Sum{top, s};
@@ -392,23 +442,26 @@ __global__ __launch_bounds__(kThreads, kHeld == 16 || kThreads == 1024 ? 4 : kHe
       for (uint32_t e = 0; e < N; ++e) z[e] = named >> e & 1 ? -__builtin_inff() : element<N, T>(r, e);
       add_to<N>(sum, z, a.c);
     }
-  const float m = wave_max(sum.m), R = Sum::ref(m, a.c);
-  const float s = wave_sum(sum.m == -__builtin_inff() ? sum.s : sum.s * exp2_of(Sum::ref(sum.m, a.c) - R));
+  const float m = wave_max(sum.m), s = wave_sum(sum.m == -__builtin_inff() ? sum.s : sum.s * relative(sum.m, m, a.c));
   if (lane == 0) red_m[wave] = m, red_s[wave] = s;
   if (thread < a.K) n.z[thread] = z_named;
   lds_barrier();
+  Settled settled;
+  Sum all;
   if (wave == 0) {
     const float wm = lane < kWaves ? red_m[lane] : -__builtin_inff(), ws = lane < kWaves ? red_s[lane] : 0.0f;
-    const float top = wave_max(wm), top_R = Sum::ref(top, a.c);
-    const Sum all{top, wave_sum(wm == -__builtin_inff() ? ws : ws * exp2_of(Sum::ref(wm, a.c) - top_R))};
-    const RowGradient g = settle(a, n, row, teacher, all, out);
-    if (lane == 0) sh_gradient = g;
+    const float top = wave_max(wm);
+    all = Sum{top, wave_sum(wm == -__builtin_inff() ? ws : ws * relative(wm, top, a.c))};
+    settled = settle(a, n, row, teacher, all, out);
+    if (lane == 0) sh_gradient = settled.gradient;
   }
-  if (!out) return;
   lds_barrier();
+  if (wave == 0) conclude(a, row, teacher, all, settled);
+  if (!out) return;
   const RowGradient g = sh_gradient;
   const float scale_low = g.scale * 0x1p-64f;
-  const auto gradient = [&](float z) { return power<T>(__builtin_fmaf(z, a.c, -g.R), g.scale, scale_low); };
+  const Exponent x(g.m, a.c);
+  const auto gradient = [&](float z) { return power<T>(x.of(z), g.scale, scale_low); };
   // The named tokens' elements are the first wave's, all others of the row are written here.
   if (thread < left && !left_named) out[runs * N + thread] = (T)(g.zero ? 0.0f : gradient(z_left));
   const auto write = [&](uint32_t run, const Run<T, N> &z) {
