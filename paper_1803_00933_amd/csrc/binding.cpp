@@ -182,6 +182,21 @@ struct From<View> {
   }
 };
 
+// A workspace, and how large it is where that can be known: that of a tensor.
+struct Space {
+  void *p;
+  size_t bytes;
+  void *of(size_t needed) const
+  {
+    require(!p || bytes >= needed, "workspace: smaller than these sizes need");
+    return p;
+  }
+};
+template <>
+struct From<Space> {
+  static Space get(PyObject *o) { return Space{address(o), o != Py_None && THPVariable_Check(o) ? THPVariable_Unpack(o).nbytes() : SIZE_MAX}; }
+};
+
 // The address of a contiguous fp32 array of `count` elements, or null where there is none.
 float *floats(const View &v, int64_t count, const char *why)
 {
@@ -259,7 +274,8 @@ PyObject *call(R (*f)(A...), PyObject *const *args, Py_ssize_t n)
   X(apex_replay_update_priorities) X(apex_replay_update_from_q) X(apex_replay_evict) X(apex_pipeline_fork)          \
   X(apex_pipeline_join) X(apex_pipeline_steps) X(apex_pipeline_add_begin) X(apex_pipeline_add_end) X(apex_pe_add)   \
   X(apex_pe_sample) X(apex_pe_update_priorities) X(apex_pe_evict_enqueue) X(apex_pe_add_round) X(apex_pe_sample_update) \
-  X(apex_gated_scan) X(apex_gated_scan_backward) X(apex_distill_topk) X(apex_verify_draft)
+  X(apex_gated_scan) X(apex_gated_scan_backward) X(apex_distill_topk) X(apex_verify_draft)                          \
+  X(apex_gated_scan_workspace_bytes) X(apex_verify_draft_workspace_bytes)
 #define X(name) decltype(&::name) p_##name = nullptr;
 APEX_ENTRIES(X)
 #undef X
@@ -356,6 +372,14 @@ VERB(pe_sample_update, [](Pe r, uint32_t k, float beta, U64 rnd, F new_prio, uin
   return p_apex_pe_sample_update(r, k, beta, rnd, new_prio, key, slot, weight, obs, act, ret, gacc, s);
 })
 
+// What an operator's workspace has to hold; sizes that it does not take are the call's own to refuse.
+template <typename F, typename... A>
+size_t needed(F bytes_of, A... sizes)
+{
+  size_t n = 0;
+  return bytes_of(sizes..., &n) == APEX_OK ? n : 0;
+}
+
 // The two strided arrays of a scan, and the shape that everything else of it follows.
 void scan_inputs(const View &g, const View &x)
 {
@@ -364,17 +388,18 @@ void scan_inputs(const View &g, const View &x)
   require(g.rows() && x.rows(), "g and x: contiguous channels");
 }
 
-VERB(gated_scan, [](View g, View x, int gate, View discount, View length, View h0, View h, View h_last, View carry, V workspace, Stream s) {
+VERB(gated_scan, [](View g, View x, int gate, View discount, View length, View h0, View h, View h_last, View carry, Space workspace, Stream s) {
   scan_inputs(g, x);
   const int64_t S = g.n[0], T = g.n[1], D = g.n[2], chunks = (T + APEX_SCAN_CHUNK - 1) / APEX_SCAN_CHUNK;
   require(h.p && h.fits(S, T, D) && h.contiguous && h.dtype == g.dtype, "h: [S,T,D], contiguous, of g's type");
   return p_apex_gated_scan(S, T, D, g.dtype, gate, g.p, g.stride[0], g.stride[1], x.p, x.stride[0], x.stride[1],
                            floats(discount, S * T, "discount: fp32 [S,T]"), ints(length, S, "length: int32 [S]"),
                            floats(h0, S * D, "h0: fp32 [S,D]"), h.p, floats(h_last, S * D, "h_last: fp32 [S,D]"),
-                           floats(carry, S * chunks * D, "carry: fp32 [S,chunks,D]"), const_cast<void *>(workspace), s);
+                           floats(carry, S * chunks * D, "carry: fp32 [S,chunks,D]"),
+                           workspace.of(needed(p_apex_gated_scan_workspace_bytes, S, T, D)), s);
 })
 VERB(gated_scan_backward, [](View g, View x, int gate, View discount, View length, View carry, View dh, View dh_last, View dg, View dx,
-                             View dh0, V workspace, Stream s) {
+                             View dh0, Space workspace, Stream s) {
   scan_inputs(g, x);
   const int64_t S = g.n[0], T = g.n[1], D = g.n[2], chunks = (T + APEX_SCAN_CHUNK - 1) / APEX_SCAN_CHUNK;
   require(dh.p && dh.fits(S, T, D) && dh.contiguous && dh.dtype == g.dtype, "dh: [S,T,D], contiguous, of g's type");
@@ -384,7 +409,8 @@ VERB(gated_scan_backward, [](View g, View x, int gate, View discount, View lengt
                                     floats(discount, S * T, "discount: fp32 [S,T]"), ints(length, S, "length: int32 [S]"),
                                     floats(carry, S * chunks * D, "carry: fp32 [S,chunks,D]"), dh.p,
                                     floats(dh_last, S * D, "dh_last: fp32 [S,D]"), dg.p, dg.stride[0], dg.stride[1], dx.p,
-                                    dx.stride[0], dx.stride[1], floats(dh0, S * D, "dh0: fp32 [S,D]"), const_cast<void *>(workspace), s);
+                                    dx.stride[0], dx.stride[1], floats(dh0, S * D, "dh0: fp32 [S,D]"),
+                                    workspace.of(needed(p_apex_gated_scan_workspace_bytes, S, T, D)), s);
 })
 VERB(distill_topk, [](View logits, View index, View value, View top_lse, View weight, float temperature, View loss, View lse, View grad,
                       V workspace, Stream s) {
@@ -399,7 +425,7 @@ VERB(distill_topk, [](View logits, View index, View value, View top_lse, View we
                              temperature, floats(loss, N, "loss: fp32 [N]"), floats(lse, N, "lse: fp32 [N]"), grad.p, grad.stride[0],
                              const_cast<void *>(workspace), s);
 })
-VERB(verify_draft, [](View target, View draft, View token, View rnd, View length, View accepted, View token_out, V workspace, Stream s) {
+VERB(verify_draft, [](View target, View draft, View token, View rnd, View length, View accepted, View token_out, Space workspace, Stream s) {
   require(target.p && target.dim == 3 && target.dtype >= 0 && target.rows() && target.n[1] > 0,
           "target: [B,G+1,V] of a floating type, contiguous rows");
   const int64_t B = target.n[0], G = target.n[1] - 1, vocabulary = target.n[2];
@@ -409,7 +435,8 @@ VERB(verify_draft, [](View target, View draft, View token, View rnd, View length
   return p_apex_verify_draft(B, G, vocabulary, target.dtype, target.p, target.stride[0], target.stride[1], draft.p, draft.stride[0],
                              draft.stride[1], ints(token, B * G, "token: int32 [B,G]"), static_cast<const uint64_t *>(rnd.p),
                              ints(length, B, "length: int32 [B]"), ints(accepted, B, "accepted: int32 [B]"),
-                             ints(token_out, B * (G + 1), "token_out: int32 [B,G+1]"), const_cast<void *>(workspace), s);
+                             ints(token_out, B * (G + 1), "token_out: int32 [B,G+1]"),
+                             workspace.of(needed(p_apex_verify_draft_workspace_bytes, B, vocabulary)), s);
 })
 
 // load(path of the library, _ptr, _plain, current device, current raw stream)

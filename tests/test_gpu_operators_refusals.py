@@ -1,0 +1,47 @@
+"""What the operators' binding refuses before anything is launched."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def apex():
+    from paper_1803_00933_amd import apex
+    return apex
+
+
+def scan_inputs(S, T, D):
+    return torch.zeros((S, T, D), device="cuda:0"), torch.ones((S, T, D), device="cuda:0")
+
+
+def test_workspaces_that_are_too_small(apex):
+    """One made for smaller sizes, and one a byte short; the smallest that is enough, and a larger one, are taken."""
+    S, T, D = 3, 700, 200
+    g, x = scan_inputs(S, T, D)
+    dh = torch.ones_like(x)
+    whole = apex.gated_scan_workspace(S, T, D)
+    rc, out = apex.gated_scan(g, x, carry=True, workspace=whole)
+    assert rc == apex.OK
+    larger = torch.zeros(whole.numel() + 512, dtype=torch.uint8, device="cuda:0")
+    for space in (whole, larger):
+        assert apex.gated_scan(g, x, workspace=space)[0] == apex.OK
+        assert apex.gated_scan_backward(g, x, dh, out["carry"], workspace=space)[0] == apex.OK
+    for space in (whole[:-1], whole[:256], apex.gated_scan_workspace(S, T - 64, D), apex.gated_scan_workspace(S - 1, T, D),
+                  apex.gated_scan_workspace(S, T, D - 100)):
+        with pytest.raises(AssertionError, match="workspace"):
+            apex.gated_scan(g, x, workspace=space)
+        with pytest.raises(AssertionError, match="workspace"):
+            apex.gated_scan_backward(g, x, dh, out["carry"], workspace=space)
+    # where no workspace is needed one of any size is taken
+    assert apex.gated_scan(g[:, :100], x[:, :100], workspace=whole[:256])[0] == apex.OK
+    B, G, V = 5, 2, 3000
+    target, draft = torch.rand((B, G + 1, V), device="cuda:0"), torch.rand((B, G, V), device="cuda:0")
+    token = torch.zeros((B, G), dtype=torch.int32, device="cuda:0")
+    rnd = torch.zeros((B, G + 1), dtype=torch.int64, device="cuda:0")
+    whole = apex.verify_draft_workspace(B, V)
+    assert apex.verify_draft(target, draft, token, rnd, workspace=whole)[0] == apex.OK
+    for space in (whole[:-1], apex.verify_draft_workspace(B - 1, V)):
+        with pytest.raises(AssertionError, match="workspace"):
+            apex.verify_draft(target, draft, token, rnd, workspace=space)
+    torch.cuda.synchronize()
