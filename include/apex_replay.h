@@ -570,7 +570,7 @@ int apex_pe_stats(apex_pe_replay_t *r, apex_pe_stats_t *out /*host*/, void *hip_
  *   - Element types: apex_dtype.  Sums, maxima, states and logarithms are held in 32 bits whatever the type of the arrays,
  *     and outputs in fewer bits are rounded once, to nearest even.
  *   - A workspace is device memory of the caller's, of at least the size that the operator's _workspace_bytes call reports
- *     for these or larger sizes, 256-byte aligned and filled with zeros before its first use.  Every call leaves it ready
+ *     for these or larger sizes, 256-byte aligned and filled with zeros before its first use (results are unspecified otherwise).  Every call leaves it ready
  *     for the next one, of the same operator and whatever sizes it is large enough for.  Calls that share a workspace must
  *     be ordered (one stream, or events); calls that may overlap take one each.
  *   - Results do not depend on the order in which workgroups run: the same inputs give the same bits.

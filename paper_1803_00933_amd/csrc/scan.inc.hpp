@@ -137,7 +137,7 @@ __device__ __forceinline__ uint32_t next_tag(uint32_t epoch)  // never that of m
   return tag ? tag : 1;
 }
 constexpr uint32_t kMostTiles = 1u << 22;  // of a chain: its words are counted in 32 bits
-constexpr uint32_t kMostPolls = 1u << 20;  // a wait gives up (and hands on NaN) where the workspace was not as required
+constexpr uint32_t kMostPolls = 1u << 20;  // a wait gives up (and hands on NaN) where a word never comes: the workspace was not zero
 
 constexpr uint32_t kStretch = 4;  // tiles of a stretch
 constexpr uint32_t kWindow = 8;   // compositions that a workgroup fetches at once
@@ -391,6 +391,7 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     if (w.thread == 0) sh_tile = take_tile(chain);
     __syncthreads();
     tile = sh_tile.x, column = sh_tile.y;
+    if (tile >= chain.tiles) return;  // no ticket of this call: the counters were not zero
   }
   const uint32_t s = column / pieces, d0 = column % pieces * kWidth, t0 = tile * w.steps;
   const uint32_t len = scan_length(a.length, s, a.T);
@@ -573,6 +574,7 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     tag = next_tag(chain.space->epoch);
     if (w.thread == 0) sh_tile = take_tile(chain);
     __syncthreads();
+    if (sh_tile.x >= chain.tiles) return;  // no ticket of this call: the counters were not zero
     tile = chain.tiles - 1 - sh_tile.x, column = sh_tile.y;
   }
   const uint32_t s = column / pieces, d0 = column % pieces * kWidth, t0 = tile * w.steps;

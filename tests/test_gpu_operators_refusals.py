@@ -45,3 +45,31 @@ def test_workspaces_that_are_too_small(apex):
         with pytest.raises(AssertionError, match="workspace"):
             apex.verify_draft(target, draft, token, rnd, workspace=space)
     torch.cuda.synchronize()
+
+
+def test_tickets_that_are_none_of_the_call_are_dropped(apex):
+    """A workspace whose counters are far from zero: no tile is any of the call's, so nothing but the workspace's own counters is
+    written, and nothing waits."""
+    for S, T, D, back in ((1, 300, 70, False), (1, 300, 70, True), (2, 1000, 300, False), (2, 1000, 300, True)):
+        g, x = scan_inputs(S, T, D)
+        n = apex.gated_scan_workspace(S, T, D).numel()
+        held = torch.full((n + 4096,), 0, dtype=torch.uint8, device="cuda:0")
+        for taken in (1 << 20, 0x7fffff00):
+            held.zero_()
+            counters = held[256:256 + 1024 * 128].view(torch.int32).view(1024, 32)
+            counters[:, 0] = taken
+            had = held.clone()
+            carry = torch.full(apex.gated_scan_carry_shape(S, T, D), 7.0, device="cuda:0")
+            written = [torch.full((S, T, D), 7.0, device="cuda:0") for _ in range(2)] + [torch.full((S, D), 7.0, device="cuda:0")]
+            if back:
+                rc, _ = apex.gated_scan_backward(g, x, torch.ones_like(x), carry, workspace=held[:n],
+                                                 out=dict(dg=written[0], dx=written[1], dh0=written[2]))
+            else:
+                rc, _ = apex.gated_scan(g, x, workspace=held[:n], out=dict(h=written[0], h_last=written[2], carry=carry))
+            assert rc == apex.OK
+            torch.cuda.synchronize()
+            assert all((t == 7.0).all() for t in written + [carry])
+            taken_by = held[256:256 + 1024 * 128].view(torch.int32).view(1024, 32)[:, 0] - taken
+            assert int(taken_by.sum()) == S * -(-T // 64) * -(-D // 128)
+            counters[:, 0] = taken
+            assert torch.equal(held, had)
