@@ -186,9 +186,12 @@ struct From<View> {
 struct Space {
   void *p;
   size_t bytes;
-  void *of(size_t needed) const
+  // bytes_of(sizes): what it has to hold; sizes that the library does not take are the call's own to refuse
+  template <typename F, typename... A>
+  void *of(F bytes_of, A... sizes) const
   {
-    require(!p || bytes >= needed, "workspace: smaller than these sizes need");
+    size_t n = 0;
+    require(!p || bytes_of(sizes..., &n) != APEX_OK || bytes >= n, "workspace: smaller than these sizes need");
     return p;
   }
 };
@@ -372,14 +375,6 @@ VERB(pe_sample_update, [](Pe r, uint32_t k, float beta, U64 rnd, F new_prio, uin
   return p_apex_pe_sample_update(r, k, beta, rnd, new_prio, key, slot, weight, obs, act, ret, gacc, s);
 })
 
-// What an operator's workspace has to hold; sizes that it does not take are the call's own to refuse.
-template <typename F, typename... A>
-size_t needed(F bytes_of, A... sizes)
-{
-  size_t n = 0;
-  return bytes_of(sizes..., &n) == APEX_OK ? n : 0;
-}
-
 // The two strided arrays of a scan, and the shape that everything else of it follows.
 void scan_inputs(const View &g, const View &x)
 {
@@ -396,7 +391,7 @@ VERB(gated_scan, [](View g, View x, int gate, View discount, View length, View h
                            floats(discount, S * T, "discount: fp32 [S,T]"), ints(length, S, "length: int32 [S]"),
                            floats(h0, S * D, "h0: fp32 [S,D]"), h.p, floats(h_last, S * D, "h_last: fp32 [S,D]"),
                            floats(carry, S * chunks * D, "carry: fp32 [S,chunks,D]"),
-                           workspace.of(needed(p_apex_gated_scan_workspace_bytes, S, T, D)), s);
+                           workspace.of(p_apex_gated_scan_workspace_bytes, S, T, D), s);
 })
 VERB(gated_scan_backward, [](View g, View x, int gate, View discount, View length, View carry, View dh, View dh_last, View dg, View dx,
                              View dh0, Space workspace, Stream s) {
@@ -410,7 +405,7 @@ VERB(gated_scan_backward, [](View g, View x, int gate, View discount, View lengt
                                     floats(carry, S * chunks * D, "carry: fp32 [S,chunks,D]"), dh.p,
                                     floats(dh_last, S * D, "dh_last: fp32 [S,D]"), dg.p, dg.stride[0], dg.stride[1], dx.p,
                                     dx.stride[0], dx.stride[1], floats(dh0, S * D, "dh0: fp32 [S,D]"),
-                                    workspace.of(needed(p_apex_gated_scan_workspace_bytes, S, T, D)), s);
+                                    workspace.of(p_apex_gated_scan_workspace_bytes, S, T, D), s);
 })
 VERB(distill_topk, [](View logits, View index, View value, View top_lse, View weight, float temperature, View loss, View lse, View grad,
                       V workspace, Stream s) {
@@ -436,7 +431,7 @@ VERB(verify_draft, [](View target, View draft, View token, View rnd, View length
                              draft.stride[1], ints(token, B * G, "token: int32 [B,G]"), static_cast<const uint64_t *>(rnd.p),
                              ints(length, B, "length: int32 [B]"), ints(accepted, B, "accepted: int32 [B]"),
                              ints(token_out, B * (G + 1), "token_out: int32 [B,G+1]"),
-                             workspace.of(needed(p_apex_verify_draft_workspace_bytes, B, vocabulary)), s);
+                             workspace.of(p_apex_verify_draft_workspace_bytes, B, vocabulary), s);
 })
 
 // load(path of the library, _ptr, _plain, current device, current raw stream)
