@@ -272,6 +272,15 @@ __device__ __forceinline__ float chain_state(uint64_t *word, uint32_t q, bool is
   return state;
 }
 
+// Where h_last is h0, nothing of the chain orders the tiles that read h0, those of the first stretch, before the one that
+// writes h_last: a stretch with a cut in it hands its state on before anything in front of it is there.  So they say that they have
+// read it, in words of position 0 that nothing else uses, and the writer waits for that.
+__device__ __forceinline__ uint64_t *start_read(const Chain &c, uint32_t column, uint32_t tile)
+{
+  return c.space->word + ((uint64_t)column * c.tiles * 3 + 2) * kTileWidth + tile;
+}
+static_assert(kStretch == 4);  // position 0 lends its third row to nobody: chain_state
+
 // A workgroup that waits for nothing any more: the last one of a counter, and of them the last of the call, leave the counters as
 // the next call has to find them.  By one thread; leaving() is the round trip, left() looks at what it brought.
 __device__ __forceinline__ uint32_t leaving(const Chain &c)
@@ -471,7 +480,12 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
   const bool speaks = w.thread < kWidth && d0 + w.channel < a.D;
   float state_in = 0.0f;  // what enters the chain; then what enters the tile
   if (speaks && a.h0 && tile < kStretch) state_in = a.h0[(uint64_t)s * a.D + d0 + w.channel];
+  const bool in_place = a.h0 && a.h0 == a.h_last;
   if constexpr (kChained) {
+    if (__builtin_expect(in_place, false)) {
+      if (tile < kStretch) asm volatile("s_waitcnt vmcnt(0)" : "+v"(state_in) : : "memory");  // it is here, not on its way
+      if (len - t0 <= w.steps && w.thread < min(tile, kStretch)) waited_for(0, start_read(chain, column, w.thread), tag);
+    }
     float A = 1.0f, B = 0.0f;
     if (w.thread < kWidth)
       for (uint32_t i = 0; i < w.segments; ++i) {
@@ -493,7 +507,10 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
   }
   __syncthreads();
   uint32_t before = 0;
-  if (kChained && w.thread == w.threads - 1) before = leaving(chain);
+  if constexpr (kChained) {
+    if (__builtin_expect(in_place && tile < kStretch, false) && w.thread == 0) publish(start_read(chain, column, tile), tagged(0.0f, tag));
+    if (w.thread == w.threads - 1) before = leaving(chain);
+  }
   {
     float state = segment_in[w.thread];
 #pragma unroll
