@@ -31,18 +31,23 @@ struct VerifyArgs {
 // m(x) = floor(min(x, 1) 2^40), 0 for what is not above 0, as high 2^20 + low: the multiple of 2^-20 below x, and the rest,
 // which is exact, in 2^-40.
 struct Mass {
+  float scaled;
   uint32_t high, low;
   __device__ __forceinline__ explicit Mass(float x)
   {
-    const float scaled = __builtin_amdgcn_fmed3f(x, 0.0f, 1.0f) * 0x1p+20f;  // (NaN: 0)
+    scaled = __builtin_amdgcn_fmed3f(x, 0.0f, 1.0f) * 0x1p+20f;  // (NaN: 0)
     high = (uint32_t)scaled;
     low = (uint32_t)(__builtin_amdgcn_fractf(scaled) * 0x1p+20f);
   }
   __device__ __forceinline__ uint64_t whole() const { return ((uint64_t)high << 20) + low; }
 };
 
-// max(0, m(p) - m(q)): m does not fall, so that it is p > q that decides.
-__device__ __forceinline__ uint64_t mass_left(float p, float q) { return p > q ? Mass(p).whole() - Mass(q).whole() : 0; }
+// max(0, m(p) - m(q)): what is scaled decides, which is a number where p or q is none.
+__device__ __forceinline__ uint64_t mass_left(float p, float q)
+{
+  const Mass mp(p), mq(q);
+  return mp.scaled > mq.scaled ? mp.whole() - mq.whole() : 0;
+}
 
 __device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v)
 {
@@ -85,7 +90,7 @@ struct MassSum {
   __device__ __forceinline__ void add(float p, float q)
   {
     const Mass mp(p), mq(q);
-    const bool more = p > q;
+    const bool more = mp.scaled > mq.scaled;
     high += more ? (int32_t)(mp.high - mq.high) : 0;
     low += more ? (int32_t)(mp.low - mq.low) : 0;
   }
