@@ -599,8 +599,10 @@ typedef enum apex_gate {
  * carry [S, ceil(T / APEX_SCAN_CHUNK), D] fp32 (may be NULL): what passes into step t = c * APEX_SCAN_CHUNK, for those t
  * below the length; the others are unspecified.  The gradient asks for it.
  * With T = 1 this is the step of an actor: state in, state out.
- * (Long sequences are computed in pieces whose factors are multiplied up: a state of +-inf becomes NaN where such a product
- * underflows to 0.)
+ * (Sequences of 12 steps and more are computed in pieces whose factors are multiplied up.  A product below 2^-149 counts as 0, so
+ * that a state of +-inf becomes NaN there.  Where given factors above 1 multiply up beyond 2^30 within 64 steps, these go one after
+ * the other, at some 7 us per 64 steps of a sequence; states are right as long as the same recurrence of absolute values stays
+ * within 32-bit numbers.)
  * Workspace: may be NULL if the reported size is 0.
  */
 int apex_gated_scan_workspace_bytes(uint32_t S, uint32_t T, uint32_t D, size_t *bytes /*host*/);

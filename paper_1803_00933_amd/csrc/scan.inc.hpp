@@ -196,7 +196,8 @@ struct ChainSpace {
 
 // The state that enters the tile at position q of a chain, for thread < kTileWidth and its channel (`is`: there is one), from
 // the composition (A, B) of the tile (`cut`: B is its outgoing state whatever enters) and the state that enters the chain.  By
-// the whole workgroup.  Publishes what the tiles behind ask for.
+// the whole workgroup.  Publishes what the tiles behind ask for, unless the tile has no composition (`composed`): then what comes out
+// of it is said by hand_on, once it is known.
 //
 // kStretch tiles are a stretch: a tile publishes its composition, the last one of a stretch the stretch's and the state behind
 // it.  A tile goes back to the nearest stretch whose state is there (the first wave looks at 64 at once), through the
@@ -206,14 +207,14 @@ struct ChainSpace {
 // Words of position p: word + p * 3 * kTileWidth: A, B, and a third row that the last three tiles of a stretch lend to the
 // stretch: its A, its B, and the state behind it.
 __device__ __forceinline__ float chain_state(uint64_t *word, uint32_t q, bool is, float A, float B, bool cut, float start, uint32_t tag,
-                                             ChainSpace &w)
+                                             ChainSpace &w, bool composed)
 {
   const uint32_t thread = threadIdx.x, channel = thread % kTileWidth, stretch = q / kStretch, place = q % kStretch;
   const bool speaks = thread < kTileWidth && is;
   const auto row = [&](uint32_t position, uint32_t i) { return (position * 3 + i) * kTileWidth; };  // (kMostTiles)
   const auto stretch_row = [&](uint32_t k, uint32_t i) { return row(k * kStretch + kStretch - 3 + i, 2); };
   const auto say = [&](uint32_t at, uint64_t v) { publish(word + (at + channel), v); };
-  if (speaks && place < kStretch - 1) {
+  if (speaks && composed && place < kStretch - 1) {
     say(row(q, 0), tagged(A, cut ? tag | kCutTag : tag));
     say(row(q, 1), tagged(B, tag));
   }
@@ -233,7 +234,7 @@ __device__ __forceinline__ float chain_state(uint64_t *word, uint32_t q, bool is
   __syncthreads();
   float SA = 1.0f, SB = 0.0f;
   bool stretch_cut = cut;
-  const bool last = place == kStretch - 1;
+  const bool last = place == kStretch - 1 && composed;
   if (last && thread < kTileWidth) {
     for (uint32_t i = 0; i < kStretch - 1; ++i) {
       stretch_cut = stretch_cut || w.tiles.cut[i];
@@ -270,6 +271,50 @@ __device__ __forceinline__ float chain_state(uint64_t *word, uint32_t q, bool is
   if (thread < kTileWidth)
     for (uint32_t i = 0; i < place; ++i) state = w.tiles.through(i, channel, state);
   return state;
+}
+
+// The state behind a tile that has no composition, by the threads that speak for a channel: to those that ask it is a composition
+// with a cut.
+__device__ __forceinline__ void hand_on(uint64_t *word, uint32_t q, float state, uint32_t tag)
+{
+  const uint32_t channel = threadIdx.x % kTileWidth, place = q % kStretch, first = q - place;
+  if (place < kStretch - 1) {
+    publish(word + ((q * 3 + 0) * kTileWidth + channel), tagged(0.0f, tag | kCutTag));
+    publish(word + ((q * 3 + 1) * kTileWidth + channel), tagged(state, tag));
+  } else {
+    for (uint32_t i = 0; i < 3; ++i)
+      publish(word + (((first + kStretch - 3 + i) * 3 + 2) * kTileWidth + channel), i == 0 ? tagged(0.0f, tag | kCutTag) : tagged(state, tag));
+  }
+}
+
+// How far given factors above 1 may multiply up over a tile, in powers of 2, as kGrowthUnit-ths: four tiles make a stretch, whose
+// product has to be a number.  (A product that falls below the numbers is 0: what is lost of a state is 2^-149 of it, and 2^30
+// times that where it grows again.)  Beyond, an overflow could meet a state of 0, or come back within range: such a tile has no
+// composition.  It waits for the state that enters it and goes from step to step, some 7 us a tile.  (64 steps of 1.38 are within
+// the bound.  4 x 8192 x 2048 bf16 112 us forward, 854 with tiles that all go from step to step; 1 x 32768 x 768 54 and 3850.)
+constexpr uint32_t kGrowthUnit = 16, kMostGrowth = 30 * kGrowthUnit;
+
+// Adds a wave's part to the tile's.
+template <uint32_t N>
+__device__ __forceinline__ void add_growth(const float (&f)[kTileRows][N], uint32_t *growth)
+{
+  float most = 0.0f;
+#pragma unroll
+  for (uint32_t l = 0; l < kTileRows; ++l)
+#pragma unroll
+    for (uint32_t e = 0; e < N; ++e) most = fmaxf(most, __builtin_fabsf(f[l][e]));
+  if (__ballot(most > 1.0f) == 0) return;
+  most = 1.0f;
+#pragma unroll
+  for (uint32_t e = 0; e < N; ++e) {
+    float product = 1.0f;
+#pragma unroll
+    for (uint32_t l = 0; l < kTileRows; ++l) product *= fmaxf(__builtin_fabsf(f[l][e]), 1.0f);
+    most = fmaxf(most, product);
+  }
+  most = fminf(wave_max(most), 0x1p126f);
+  constexpr uint32_t kGroups = kWave / kTileLanes;
+  if (lane_id() == 0) atomicAdd(growth, kGroups * ((uint32_t)(log2_of(most) * kGrowthUnit) + 1));
 }
 
 // Where h_last is h0, nothing of the chain orders the tiles that read h0, those of the first stretch, before the one that
@@ -387,6 +432,7 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
   extern __shared__ __align__(16) float scan_lds[];
   __shared__ RowBits into;  // whether the state passes into a row
   __shared__ uint2 sh_tile;
+  __shared__ uint32_t sh_growth;
   __shared__ typename std::conditional<kChained, ChainSpace, uint32_t>::type sh_chain;
   const TileShape w;
   float *const group_a = scan_lds, *const group_b = group_a + w.groups * kWidth;  // [groups][kWidth]; group_a later: the state that enters
@@ -439,6 +485,7 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     const uint64_t bits = __ballot(!a.discount || t == 0 || t >= len || a.discount[(uint64_t)s * a.T + t - 1] != 0.0f);
     if (lane_id() == 0) into.word[w.thread / kWave] = bits;
   }
+  if (kGate == APEX_GATE_GIVEN && w.thread == 0) sh_growth = 0;
   __syncthreads();
   const uint32_t bits = into.of_group(w.group);
   const bool no_cut = uncut(into, w.steps);
@@ -462,7 +509,9 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     *reinterpret_cast<f32x4 *>(group_a + w.group * kWidth + w.run) = A;
     *reinterpret_cast<f32x4 *>(group_b + w.group * kWidth + w.run) = B;
   });
+  if (kGate == APEX_GATE_GIVEN) add_growth(fa, &sh_growth);
   __syncthreads();
+  const bool composed = kGate != APEX_GATE_GIVEN || sh_growth <= kMostGrowth;
   if (w.segments > 1) {
     float A = 1.0f, B = 0.0f;
 #pragma unroll
@@ -495,9 +544,29 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
         B = passes ? __builtin_fmaf(sa, B, sb) : sb;
       }
     state_in = chain_state(chain.space->word + (uint64_t)column * chain.tiles * 3 * kWidth, tile, d0 + w.channel < a.D, A, B, !no_cut,
-                           state_in, tag, sh_chain);
+                           state_in, tag, sh_chain, composed);
   }
-  if (w.thread < kWidth) {
+  if (!composed) {
+    if (w.thread < kWidth) {
+      const uint64_t at = d0 + min(w.channel, a.D - 1 - d0);
+      const T *const g = static_cast<const T *>(a.g) + s * a.g_seq + t0 * a.g_time + at;
+      const T *const x = static_cast<const T *>(a.x) + s * a.x_seq + t0 * a.x_time + at;
+      const uint32_t steps = min(len - t0, w.steps);
+      for (uint32_t i = 0; i < w.groups; ++i) {
+        group_a[i * kWidth + w.channel] = state_in;
+        float gt[kTileRows], xt[kTileRows];
+#pragma unroll
+        for (uint32_t l = 0; l < kTileRows; ++l) {
+          const uint32_t t = min(i * kTileRows + l, steps - 1);
+          gt[l] = (float)g[t * a.g_time], xt[l] = (float)x[t * a.x_time];
+        }
+#pragma unroll
+        for (uint32_t l = 0; l < kTileRows; ++l)
+          if (i * kTileRows + l < steps) state_in = __builtin_fmaf(gt[l], into.of_group(i) >> l & 1 ? state_in : 0.0f, xt[l]);
+      }
+      if (kChained && speaks) hand_on(chain.space->word + (uint64_t)column * chain.tiles * 3 * kWidth, tile, state_in, tag);
+    }
+  } else if (w.thread < kWidth) {
     segment_in[w.channel] = state_in;
     for (uint32_t i = 0; i + 1 < w.segments; ++i) {
       const float sa = segment_a[i * kWidth + w.channel], sb = segment_b[i * kWidth + w.channel];
@@ -511,7 +580,7 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     if (__builtin_expect(in_place && tile < kStretch, false) && w.thread == 0) publish(start_read(chain, column, tile), tagged(0.0f, tag));
     if (w.thread == w.threads - 1) before = leaving(chain);
   }
-  {
+  if (composed) {
     float state = segment_in[w.thread];
 #pragma unroll
     for (uint32_t i = 0; i < kSegment; ++i) {
@@ -578,6 +647,7 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
   extern __shared__ __align__(16) float scan_lds[];
   __shared__ RowBits on;  // whether a row's state passes on
   __shared__ uint2 sh_tile;
+  __shared__ uint32_t sh_growth;
   __shared__ typename std::conditional<kChained, ChainSpace, uint32_t>::type sh_chain;
   const TileShape w;
   float *const group_a = scan_lds, *const group_b = group_a + w.groups * kWidth;                 // [groups][kWidth]; group_a later: the state that enters
@@ -648,6 +718,7 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     const uint64_t bits = __ballot(!a.discount || t >= len || a.discount[(uint64_t)s * a.T + t] != 0.0f);
     if (lane_id() == 0) on.word[w.thread / kWave] = bits;
   }
+  if (kGate == APEX_GATE_GIVEN && w.thread == 0) sh_growth = 0;
   __syncthreads();
   const uint32_t bits = on.of_group(w.group);
   const bool no_cut = uncut(on, w.steps);
@@ -684,6 +755,7 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     *reinterpret_cast<f32x4 *>(group_p + at) = P;
     *reinterpret_cast<f32x4 *>(group_q + at) = Q;
   });
+  if (kGate == APEX_GATE_GIVEN) add_growth(f, &sh_growth);
 #pragma unroll
   for (uint32_t l = 0; l < kTileRows; ++l) {
     hold_packed<N, T>(xr[l]);
@@ -692,9 +764,30 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     for (uint32_t e = 0; e < N; ++e) asm volatile("" : "+v"(rest[l][e]));  // nor are its products held
   }
   __syncthreads();
+  const bool composed = kGate != APEX_GATE_GIVEN || sh_growth <= kMostGrowth;
   // the states that enter the groups of a segment, from the chunk's; the segment's composition, from its last group
   float states[kSegment];
-  {
+  const uint64_t at_channel = d0 + min(w.channel, a.D - 1 - d0);
+  const uint32_t steps = min(len - t0, w.steps);
+  if (!composed) {
+    const T *const g = static_cast<const T *>(a.g) + s * a.g_seq + t0 * a.g_time + at_channel;
+    const T *const x = static_cast<const T *>(a.x) + s * a.x_seq + t0 * a.x_time + at_channel;
+    const uint32_t first = w.segment / kChunkSegments * kChunkGroups, mine = w.segment * kSegment;
+    const uint64_t chunk_bits = on.word[first / kChunkGroups] << 1 | 1;
+    for (uint32_t i = first; i < mine + kSegment; ++i) {
+      if (i >= mine) group_a[i * kWidth + w.channel] = state;
+      float gt[kTileRows], xt[kTileRows];
+#pragma unroll
+      for (uint32_t l = 0; l < kTileRows; ++l) {
+        const uint32_t t = min(i * kTileRows + l, steps - 1);
+        gt[l] = (float)g[t * a.g_time], xt[l] = (float)x[t * a.x_time];
+      }
+#pragma unroll
+      for (uint32_t l = 0; l < kTileRows; ++l)
+        if (i * kTileRows + l < steps)
+          state = __builtin_fmaf(gt[l], chunk_bits >> ((i - first) * kTileRows + l) & 1 ? state : 0.0f, xt[l]);
+    }
+  } else {
     const uint32_t first = w.segment / kChunkSegments * kChunkGroups;
     const uint64_t chunk_bits = on.word[first / kChunkGroups] << 1 | 1;
     const auto go_through = [&](uint32_t i) {
@@ -720,8 +813,9 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     segment_q[w.thread] = Q;
   }
   __syncthreads();
+  if (composed)
 #pragma unroll
-  for (uint32_t i = 0; i < kSegment; ++i) group_a[(w.segment * kSegment + i) * kWidth + w.channel] = states[i];
+    for (uint32_t i = 0; i < kSegment; ++i) group_a[(w.segment * kSegment + i) * kWidth + w.channel] = states[i];
   const uint32_t last = (len - 1) / w.steps;
   float back_in = 0.0f;  // what enters the chain from behind; then what enters the tile
   if (speaks && a.dh_last && tile <= last && last - tile < kStretch) back_in = a.dh_last[(uint64_t)s * a.D + d0 + w.channel];
@@ -735,9 +829,27 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
         Q = passes ? __builtin_fmaf(sp, Q, sq) : sq;
       }
     back_in = chain_state(chain.space->word + (uint64_t)column * chain.tiles * 3 * kWidth, last - tile, is, P, Q, !no_cut, back_in, tag,
-                          sh_chain);
+                          sh_chain, composed);
   }
-  if (w.thread < kWidth)
+  if (!composed) {
+    if (w.thread < kWidth) {
+      const T *const g = static_cast<const T *>(a.g) + s * a.g_seq + t0 * a.g_time + at_channel;
+      const T *const dh = static_cast<const T *>(a.dh) + ((uint64_t)s * a.T + t0) * a.D + at_channel;
+      for (uint32_t i = w.groups; i-- > 0;) {
+        group_p[i * kWidth + w.channel] = back_in;
+        float gt[kTileRows], ht[kTileRows];
+#pragma unroll
+        for (uint32_t l = 0; l < kTileRows; ++l) {
+          const uint32_t t = min(i * kTileRows + l, steps - 1);
+          gt[l] = (float)g[t * a.g_time], ht[l] = (float)dh[(uint64_t)t * a.D];
+        }
+#pragma unroll
+        for (uint32_t l = kTileRows; l-- > 0;)
+          if (i * kTileRows + l < steps) back_in = gt[l] * (ht[l] + (on.of_group(i) >> l & 1 ? back_in : 0.0f));
+      }
+      if (kChained && speaks) hand_on(chain.space->word + (uint64_t)column * chain.tiles * 3 * kWidth, last - tile, back_in, tag);
+    }
+  } else if (w.thread < kWidth)
     for (uint32_t i = w.segments; i-- > 0;) {
       segment_in[i * kWidth + w.channel] = back_in;
       const float sp = segment_p[i * kWidth + w.channel], sq = segment_q[i * kWidth + w.channel];
@@ -746,7 +858,7 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
   __syncthreads();
   uint32_t before = 0;
   if (kChained && w.thread == w.threads - 1) before = leaving(chain);
-  {
+  if (composed) {
     float back = segment_in[w.thread];
 #pragma unroll
     for (uint32_t i = kSegment; i-- > 0;) {
