@@ -239,7 +239,10 @@ def gated_scan_workspace(S, T, D, device="cuda:0"):
 def gated_scan(g, x, gate="sigmoid", discount=None, length=None, h0=None, carry=False, out=None, workspace=None, stream=None):
     """h_t = a_t h_{t-1} + b_t over device tensors g, x [S,T,D] (any strides but the channels'), a and b by `gate`: "given"
     or "sigmoid".  discount fp32 [S,T] (0: nothing passes on), length int32 [S], h0 fp32 [S,D].
-    Returns (rc, out): h [S,T,D], h_last fp32 [S,D], and with carry=True what gated_scan_backward needs."""
+    Returns (rc, out): h [S,T,D], h_last fp32 [S,D], and with carry=True (or a place for it in `out`) what
+    gated_scan_backward needs."""
+    if carry and out is not None and out.get("carry") is None:
+        raise ValueError("carry=True, and no place for it in out")
     if out is None or workspace is None:
         S, T, D = g.shape
         with _made_on(stream):
