@@ -138,6 +138,7 @@ struct View {
   int64_t n[3] = {0, 0, 0}, stride[3] = {0, 0, 0}, count = 0;
   int dim = 0, dtype = -1;  // apex_dtype, or -1
   bool contiguous = false, is_int = false, is_long = false;
+  bool is_none() const { return dim == 0; }  // (a tensor without elements has no address either)
   bool fits(int64_t a, int64_t b) const { return dim == 2 && n[0] == a && n[1] == b; }
   bool fits(int64_t a, int64_t b, int64_t c) const { return dim == 3 && n[0] == a && n[1] == b && n[2] == c; }
   // the last index is contiguous (where there is anything to step over), the others step forward
@@ -203,12 +204,12 @@ struct From<Space> {
 // The address of a contiguous fp32 array of `count` elements, or null where there is none.
 float *floats(const View &v, int64_t count, const char *why)
 {
-  require(!v.p || (v.dtype == APEX_F32 && v.contiguous && v.count == count), why);
+  require(v.is_none() || (v.dtype == APEX_F32 && v.contiguous && v.count == count), why);
   return static_cast<float *>(v.p);
 }
 int32_t *ints(const View &v, int64_t count, const char *why)
 {
-  require(!v.p || (v.is_int && v.contiguous && v.count == count), why);
+  require(v.is_none() || (v.count == count && (count == 0 || (v.is_int && v.contiguous))), why);
   return static_cast<int32_t *>(v.p);
 }
 
@@ -414,7 +415,7 @@ VERB(distill_topk, [](View logits, View index, View value, View top_lse, View we
   require(index.p && index.dim == 2 && index.n[0] == N, "top_index: int32 [N,K]");
   const int64_t K = index.n[1];
   require(value.p && value.fits(N, K) && value.contiguous && value.dtype >= 0, "top_value: [N,K] of a floating type");
-  require(!grad.p || (grad.fits(N, vocabulary) && grad.dtype == logits.dtype && grad.rows()), "grad: [N,V] of the logits' type");
+  require(grad.is_none() || (grad.fits(N, vocabulary) && grad.dtype == logits.dtype && grad.rows()), "grad: [N,V] of the logits' type");
   return p_apex_distill_topk(N, vocabulary, K, logits.dtype, logits.p, logits.stride[0], ints(index, N * K, "top_index: int32 [N,K]"),
                              value.dtype, value.p, floats(top_lse, N, "top_lse: fp32 [N]"), floats(weight, N, "weight: fp32 [N]"),
                              temperature, floats(loss, N, "loss: fp32 [N]"), floats(lse, N, "lse: fp32 [N]"), grad.p, grad.stride[0],

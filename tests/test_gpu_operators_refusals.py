@@ -73,3 +73,35 @@ def test_tickets_that_are_none_of_the_call_are_dropped(apex):
             assert int(taken_by.sum()) == S * -(-T // 64) * -(-D // 128)
             counters[:, 0] = taken
             assert torch.equal(held, had)
+
+
+def test_arrays_without_elements_are_not_taken_for_none(apex):
+    """An empty tensor has no address, like None; where an array of some size belongs it is refused all the same."""
+    S, T, D = 2, 20, 8
+    g, x = scan_inputs(S, T, D)
+    nothing, no_ints = torch.empty(0, device="cuda:0"), torch.empty(0, dtype=torch.int32, device="cuda:0")
+    for name, a in (("discount", nothing), ("length", no_ints), ("h0", nothing)):
+        with pytest.raises(AssertionError, match=name):
+            apex.gated_scan(g, x, **{name: a})
+    rc, out = apex.gated_scan(g, x, carry=True)
+    for name in ("h_last", "carry"):
+        with pytest.raises(AssertionError, match=name):
+            apex.gated_scan(g, x, out={**out, name: nothing})
+    with pytest.raises(AssertionError, match="dh_last"):
+        apex.gated_scan_backward(g, x, x, out["carry"], dh_last=nothing)
+    logits, index, value = torch.zeros((3, 40), device="cuda:0"), torch.zeros((3, 2), dtype=torch.int32, device="cuda:0"), torch.zeros((3, 2), device="cuda:0")
+    for name in ("weight", "top_lse"):
+        with pytest.raises(AssertionError, match=name):
+            apex.distill_topk(logits, index, value, **{name: nothing})
+    loss = torch.zeros(3, device="cuda:0")
+    for name in ("lse", "grad"):
+        with pytest.raises(AssertionError, match=name):
+            apex.distill_topk(logits, index, value, out=dict(loss=loss, **{name: nothing}))
+    target, rnd = torch.rand((3, 1, 40), device="cuda:0"), torch.zeros((3, 1), dtype=torch.int64, device="cuda:0")
+    with pytest.raises(AssertionError, match="length"):
+        apex.verify_draft(target, None, None, rnd, length=no_ints)
+    # a draft of no tokens has no tokens, of whatever type
+    draft = torch.empty((3, 0, 40), device="cuda:0")
+    for dtype in (torch.int32, torch.int64):
+        assert apex.verify_draft(target, draft, torch.empty((3, 0), dtype=dtype, device="cuda:0"), rnd)[0] == apex.OK
+    torch.cuda.synchronize()
