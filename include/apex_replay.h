@@ -628,7 +628,8 @@ int apex_gated_scan_backward(uint32_t S, uint32_t T, uint32_t D, int dtype, int 
  * Distillation from a teacher's top logits, with the gradient.  For each of N rows, of logits z [V] (row i at i *
  * row_stride, of type dtype) and a teacher's K largest logits: top_index [N,K] int32 and top_value [N,K] of value_dtype.
  * A place whose index is not in [0, V), or stands in an earlier place of the row already, is empty: its value is not
- * looked at.  With temperature tau > 0:
+ * looked at.  With temperature tau, above 0 and such that
+ * log2(e) / tau is a number of 32 bits:
  *     p_j = exp(z_j / tau - lse),  lse = log sum_j exp(z_j / tau);
  *     without top_lse: q_k = the softmax of top_value / tau over the row's places, r = 0;
  *     with top_lse [N] (the teacher's log-sum-exp of all its logits / tau): q_k = exp(top_value_k / tau - top_lse),

@@ -512,6 +512,7 @@ int apex_distill_topk(uint32_t N, uint32_t V, uint32_t K, int dtype, const void 
     return APEX_ERR_INVALID_ARG;
   if (V > APEX_MAX_VOCABULARY || K > APEX_MAX_TOP || N > 0xffffffffu / 1024) return APEX_ERR_TOO_LARGE;
   const double inv_tau = 1.0 / (double)temperature;
+  if (!((float)(1.4426950408889634 * inv_tau) < __builtin_inff())) return APEX_ERR_INVALID_ARG;
   constexpr uint32_t kLine = 128;
   const DistillArgs a{N, V, K, (uint32_t)value_dtype, row_stride, grad_stride, logits, top_index, top_value, top_lse, weight, inv_tau,
                       (float)(1.4426950408889634 * inv_tau), (float)inv_tau, loss, lse, grad,

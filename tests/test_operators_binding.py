@@ -15,3 +15,10 @@ def test_a_carry_that_has_no_place(apex, out):
     x = torch.zeros((1, 2, 3))
     with pytest.raises(ValueError, match="carry"):
         apex.gated_scan(x, x, carry=True, out=out, workspace=x)
+
+
+@pytest.mark.parametrize("temperature", [1e-45, 1e-40, 4e-39])
+def test_temperatures_whose_reciprocal_is_no_number(apex, temperature):
+    """log2(e) / temperature is beyond 32 bits: logits times that would be infinite or NaN."""
+    a = 1 << 20
+    assert apex.lib.apex_distill_topk(1, 8, 1, 0, a, 8, a, 0, a, None, None, temperature, a, None, None, 0, None, None) == apex.ERR_INVALID_ARG
