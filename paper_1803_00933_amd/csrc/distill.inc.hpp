@@ -97,19 +97,22 @@ __device__ __forceinline__ float relative(float from, float to, float c)
   return exp2_of(__builtin_rintf(from * c) - __builtin_rintf(to * c));
 }
 
+// Adds a run; x is that of the sum's largest.
 template <int N>
-__device__ __forceinline__ void add_to(Sum &a, const float (&z)[N], float c)
+__device__ __forceinline__ void add_to(Sum &a, Exponent &x, const float (&z)[N], float c)
 {
   float top = z[0];
 #pragma unroll
   for (int e = 1; e < N; ++e) top = fmaxf(top, z[e]);
-  const float m = fmaxf(a.m, top);
-  const Exponent x(m, c);
+  if (top > a.m) {  // (NaN may be there without a maximum)
+    if (a.m != -__builtin_inff()) a.s *= relative(a.m, top, c);
+    a.m = top;
+    x = Exponent(top, c);
+  }
   float s = 0.0f;
 #pragma unroll
   for (int e = 0; e < N; ++e) s += exp2_of(x.of(z[e]));
-  a.s = __builtin_fmaf(a.s, a.m == -__builtin_inff() ? 1.0f : relative(a.m, m, c), s);  // (NaN may be there without a maximum)
-  a.m = m;
+  a.s += s;
 }
 
 // 2^x scale, an element of the gradient: gradual down to the smallest numbers where the gradient has them (scale_low = scale
@@ -406,6 +409,7 @@ __global__ __launch_bounds__(kThreads, kHeld == 16 || kThreads == 1024 ? 4 : kHe
 
   // the sum of this thread's part of the row, without the named tokens if there is a rest class
   Sum sum{-__builtin_inff(), 0.0f};
+  Exponent x(sum.m, a.c);
   if (a.top_lse && left_named) z_left = -__builtin_inff();
   {
     float top = z_left;
@@ -422,7 +426,7 @@ __global__ __launch_bounds__(kThreads, kHeld == 16 || kThreads == 1024 ? 4 : kHe
       for (uint32_t e = 0; e < N; ++e) top = fmaxf(top, element<N, T>(held[i], e));
       hold_packed<N, T>(held[i]);
     }
-    const Exponent x(top, a.c);
+    x = Exponent(top, a.c);
     float s = exp2_of(x.of(z_left));
 #pragma unroll
     for (uint32_t i = 0; i < kHeld; ++i) {
@@ -433,15 +437,20 @@ __global__ __launch_bounds__(kThreads, kHeld == 16 || kThreads == 1024 ? 4 : kHe
     }
     sum = Sum{top, s};
   }
-  if (kMore)
-    for (uint32_t run = thread + kHeld * kThreads; run < runs; run += kThreads) {
-      const Run<T, N> r = load_run<T, N>(z_row + run * N);
+  if (kMore) {
+    uint32_t run = thread + kHeld * kThreads;
+    Run<T, N> next{};
+    if (run < runs) next = load_run<T, N>(z_row + run * N);
+    for (; run < runs; run += kThreads) {  // the run behind it is on its way
+      const Run<T, N> r = next;
+      if (run + kThreads < runs) next = load_run<T, N>(z_row + (run + kThreads) * N);
       const uint32_t named = a.top_lse ? n.mask<N>(run) : 0;
       float z[N];
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) z[e] = named >> e & 1 ? -__builtin_inff() : element<N, T>(r, e);
-      add_to<N>(sum, z, a.c);
+      add_to<N>(sum, x, z, a.c);
     }
+  }
   const float m = wave_max(sum.m), s = wave_sum(sum.m == -__builtin_inff() ? sum.s : sum.s * relative(sum.m, m, a.c));
   if (lane == 0) red_m[wave] = m, red_s[wave] = s;
   if (thread < a.K) n.z[thread] = z_named;
@@ -460,8 +469,8 @@ __global__ __launch_bounds__(kThreads, kHeld == 16 || kThreads == 1024 ? 4 : kHe
   if (!out) return;
   const RowGradient g = sh_gradient;
   const float scale_low = g.scale * 0x1p-64f;
-  const Exponent x(g.m, a.c);
-  const auto gradient = [&](float z) { return power<T>(x.of(z), g.scale, scale_low); };
+  const Exponent of_row(g.m, a.c);
+  const auto gradient = [&](float z) { return power<T>(of_row.of(z), g.scale, scale_low); };
   // The named tokens' elements are the first wave's, all others of the row are written here.
   if (thread < left && !left_named) out[runs * N + thread] = (T)(g.zero ? 0.0f : gradient(z_left));
   const auto write = [&](uint32_t run, const Run<T, N> &z) {
