@@ -2,8 +2,10 @@
 //
 // With c = log2(e) / tau everything that is summed over the vocabulary is 2^(z c - R), R the whole number next to max z c: one
 // fused multiply-add and one instruction of the transcendental unit an element, and R, a whole number, adds and cancels exactly.
+// (Far from 0 it is no longer next to max z c: Sum.)
 // With a rest class the sum runs over the tokens that are not named, with a maximum of its own, and the named ones, which are
-// gathered, join it afterwards: the rest's share keeps its precision however little of the student's mass it has.
+// gathered, join it afterwards: the rest's share keeps its precision however little of the student's mass it has.  Where that is
+// nearly all of it, or the student is near its teacher, what cancels is not subtracted: settle.
 #include "elements.hpp"
 
 namespace apex {
@@ -348,13 +350,15 @@ __device__ __forceinline__ void conclude(const DistillArgs &a, uint32_t row, con
 
 // A workgroup per row.  kHeld runs of 16 bytes of the row stay in a thread's registers from the sum to the gradient, so that the
 // row is read once; kMore: what a row has beyond them is read again.
-// Bound by memory: 2048 x 32768 bf16 57 us for 269 MB (4.7 TB/s; a copy reaches 5.1), 777 x 49999 f16 34 us (4.5), 3001 x 131072
-// bf16 with a rest class 365 us for 1.58 GB (4.3): there a compute unit has one row at a time, and its memory waits while the
-// row is settled.  Reading every row twice took 115, 56 and 588.
+// Bound by memory: 2048 x 32768 bf16 58.5 us for 269 MB (4.6 TB/s; a copy reaches 5.1), 777 x 49999 f16 34-36 us (4.3-4.6), 3001 x
+// 131072 bf16 with a rest class 369 us for 1.58 GB (4.3): there a compute unit has one row at a time, and its memory waits while
+// the row is settled.  Reading every row twice took 115, 56 and 588.  The loss alone 27 us for the first.
 // Named tokens cost instructions where the row is gone through: looking every element of a marked run up in a table took 804 us
 // for the third, looking marked elements up 423, a bit each and no look-up this.  Their logits are fetched by themselves, and the
 // wave that settles the row writes their gradients; the others write around them.
-// What is beyond 256 KB of a row is read twice (512 x 200000 bf16 97 us; 116 with all of it read twice).
+// What is beyond 256 KB of a row is read twice (512 x 200000 bf16 95 us; 116 with all of it read twice).
+// Registers are bounded so that as many workgroups share a compute unit as the rows that they hold leave room for: unbounded,
+// what settles a row took 96 and 136, the first 63 us, the second 49.
 // (Rows one after the other by a workgroup that stays, the next row's loads beside the gradient's stores: 510 us for the third.)
 template <typename T, uint32_t kThreads, uint32_t kHeld, bool kMore = false>
 __global__ __launch_bounds__(kThreads, kHeld == 16 || kThreads == 1024 ? 4 : kHeld == 8 ? 6 : 8) void distill_rows_kernel(DistillArgs a)
@@ -529,7 +533,7 @@ int apex_distill_topk(uint32_t N, uint32_t V, uint32_t K, int dtype, const void 
   const uint32_t runs = V / (16 / size), lds = distill_lds(K, V);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   // As few threads as hold a row, for the registers of more rows on a compute unit; where the chip has a compute unit for every
-  // row, as many as there are runs (12 x 32000 in 32 bits 9.9 us with 512 threads, 8.6 with 1024).
+  // row, as many as there are runs (12 x 32000 in 32 bits 10.6 us with 512 threads, 9.0 with 1024).
   with_type(dtype, [&](auto t) {
     typedef decltype(t) E;
     if (runs <= 256 * 4)

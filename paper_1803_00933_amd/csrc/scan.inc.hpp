@@ -425,6 +425,9 @@ __device__ __forceinline__ void no_step(Run<T, N> *g, Run<T, N> *x)
 }
 
 // kChained: tiles of a sequence wait for one another; else a sequence has one tile.
+// Chained bound by memory and by waits for states: 4 x 8192 x 2048 bf16 125 us for 403 MB (3.2 TB/s), 101 without the waits; one
+// prompt of 32768 x 768 61 and 38.  Else by loads, gates, barriers and stores one after the other, of one round of workgroups: 64 x
+// 96 x 1024 bf16 12 us.
 template <typename T, int kGate, bool kChained>
 __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChained ? 6 : 4) void scan_tile_kernel(ScanArgs a, Chain chain)
 {
@@ -633,6 +636,8 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
 // The gradient in tiles: the states from `carry`, which begins anew every APEX_SCAN_CHUNK steps, and lambda by a chain from the
 // last step to the first.  A row's bit says whether its state passes on; the rows of a chunk take each other's, and what enters
 // a chunk's first row has been through its bit already.
+// Bound as the forward pass is: 4 x 8192 x 2048 bf16 193 us for 671 MB (3.5 TB/s), 179 without the waits; 64 x 96 x 1024 18 us.  In
+// fp32, 2 x 8192 x 2048, 140 us for as much (4.8), 97 forward.
 constexpr uint32_t tile_back_lds(uint32_t threads)  // both kinds of compositions of the groups, segments' compositions, what enters
 {
   return threads * kTileRun * 16 + threads * 12;
@@ -919,7 +924,7 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
 constexpr uint32_t kChannelThreads = 64;
 
 // A thread per channel, step after step: for an actor's single tokens.  Bound by the round trip of a launch and two loads
-// (64 x 1 x 1024: 2.3 us), and for longer sequences by one step's loads after the other's.
+// (64 x 1 x 1024: 2.5 us), and for longer sequences by one step's loads after the other's.
 template <typename T, int kGate>
 __global__ __launch_bounds__(kChannelThreads) void scan_channel_kernel(ScanArgs a)
 {

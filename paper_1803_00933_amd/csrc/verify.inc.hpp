@@ -143,8 +143,9 @@ __device__ __forceinline__ uint64_t sum_of(const T *p_row, const T *q_row, uint3
 
 // Every sequence's row is shared by `shares` workgroups, which sum their parts; the last of them to be done knows the
 // total, finds the part that the drawn point lies in and goes through it once more.
-// Bound by memory for many sequences (256 x 128001 in 32 bits 54 us for 228 MB, 4.2 TB/s), for few by a chain of round trips:
-// token, its two probabilities, the row, the sums, the part of the row again (one sequence of 131072: 5.2 us).
+// Bound by memory for many sequences (256 x 128001 in 32 bits 52-53 us for 228 MB, 4.3 TB/s; 67 in 16 bits, for
+// half as much), for few by a chain of round trips: token, its two probabilities, the row, the sums, the part of the row again (one
+// sequence of 131072: 5.4-6.4 us).
 // One sum a row: with the target's own beside what is left of it, for the row of which nothing is left, the first took 61 us;
 // that row is summed up again when it comes.  Masses in two parts of 32 bits: with 64-bit masses and sums 76.
 template <typename T>
