@@ -120,6 +120,9 @@ __device__ __forceinline__ uint2 take_tile(const Chain &c)
   return make_uint2(n / columns, g + c.groups * (n % columns));
 }
 
+// What is the same in every lane, in a scalar register.
+__device__ __forceinline__ uint32_t one_for_all(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
 __device__ __forceinline__ uint64_t tagged(float v, uint32_t tag) { return ((uint64_t)tag << 32) | __float_as_uint(v); }
 __device__ __forceinline__ void publish(uint64_t *word, uint64_t v)
 {
@@ -448,7 +451,7 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     tag = next_tag(chain.space->epoch);
     if (w.thread == 0) sh_tile = take_tile(chain);
     __syncthreads();
-    tile = sh_tile.x, column = sh_tile.y;
+    tile = one_for_all(sh_tile.x), column = one_for_all(sh_tile.y);
     if (tile >= chain.tiles) return;  // no ticket of this call: the counters were not zero
   }
   const uint32_t s = column / pieces, d0 = column % pieces * kWidth, t0 = tile * w.steps;
@@ -666,8 +669,9 @@ __global__ __launch_bounds__(kChained ? kChainThreads : kTileMaxThreads, kChaine
     tag = next_tag(chain.space->epoch);
     if (w.thread == 0) sh_tile = take_tile(chain);
     __syncthreads();
-    if (sh_tile.x >= chain.tiles) return;  // no ticket of this call: the counters were not zero
-    tile = chain.tiles - 1 - sh_tile.x, column = sh_tile.y;
+    tile = one_for_all(sh_tile.x), column = one_for_all(sh_tile.y);
+    if (tile >= chain.tiles) return;  // no ticket of this call: the counters were not zero
+    tile = chain.tiles - 1 - tile;
   }
   const uint32_t s = column / pieces, d0 = column % pieces * kWidth, t0 = tile * w.steps;
   const uint32_t len = scan_length(a.length, s, a.T);
