@@ -199,7 +199,7 @@ __device__ __forceinline__ bool enter_named(const DistillArgs &a, const Named &n
 // What a wave knows of a row's teacher.
 struct Teacher {
   double top, ln_sum;  // ln q = (value - top) / tau - ln_sum
-  double mass;         // sum of q
+  double mass, part;   // sum of q: 1 without a rest class, off which the lanes' parts are by 1e-7
   uint32_t named;      // places that count
   bool teaches;        // not -inf for every one of them
 };
@@ -243,14 +243,8 @@ __device__ __forceinline__ Teacher teach(const DistillArgs &a, const Named &n, u
       n.q[k] = q;
       mass += q;
     }
-  t.mass = wave_sum(mass);
-  if (!a.top_lse && t.teaches) {  // what the sum in 32 bits was off: 1e-7
-    const double off = t.mass;
-    for (uint32_t k = lane; k < a.K; k += kWave)
-      if (n.token[k] >= 0) n.q[k] *= 2.0 - off;
-    t.ln_sum += off - 1.0;
-    t.mass = 1.0;
-  }
+  t.part = mass;
+  t.mass = a.top_lse ? wave_sum(mass) : t.teaches ? 1.0 : 0.0;
   return t;
 }
 
@@ -340,7 +334,10 @@ __device__ __forceinline__ void conclude(const DistillArgs &a, uint32_t row, con
   else  // far less than the teacher gives the rest
     loss += r.rest * (r.ratio + ln_of((float)r.rest) -
                       __builtin_fma((double)all.m - r.base, a.inv_tau, log_sum(a, all.m, Sum::ref(all.m, a.c), all.s) - r.ln_all));
-  if (!a.top_lse && !t.teaches) loss = 0.0;
+  if (!a.top_lse) {  // q as if it summed up to 1
+    const double off = wave_sum(t.part) - 1.0;
+    loss = t.teaches ? loss - off * (t.named == a.V ? loss : 1.0 + loss) : 0.0;
+  }
   if (!(__builtin_fabs(r.ln_all) < __builtin_inf())) loss = __builtin_nan("");  // the sum was NaN
   if (lane_id() == 0) {
     a.loss[row] = (float)loss;
@@ -350,8 +347,8 @@ __device__ __forceinline__ void conclude(const DistillArgs &a, uint32_t row, con
 
 // A workgroup per row.  kHeld runs of 16 bytes of the row stay in a thread's registers from the sum to the gradient, so that the
 // row is read once; kMore: what a row has beyond them is read again.
-// Bound by memory: 2048 x 32768 bf16 58.5 us for 269 MB (4.6 TB/s; a copy reaches 5.1), 777 x 49999 f16 34-36 us (4.3-4.6), 3001 x
-// 131072 bf16 with a rest class 369 us for 1.58 GB (4.3): there a compute unit has one row at a time, and its memory waits while
+// Bound by memory: 2048 x 32768 bf16 58.5 us for 269 MB (4.6 TB/s; a copy reaches 5.1), 777 x 49999 f16 34-37 us (4.2-4.6), 3001 x
+// 131072 bf16 with a rest class 370 us for 1.58 GB (4.3): there a compute unit has one row at a time, and its memory waits while
 // the row is settled.  Reading every row twice took 115, 56 and 588.  The loss alone 27 us for the first.
 // Named tokens cost instructions where the row is gone through: looking every element of a marked run up in a table took 804 us
 // for the third, looking marked elements up 423, a bit each and no look-up this.  Their logits are fetched by themselves, and the
@@ -533,7 +530,7 @@ int apex_distill_topk(uint32_t N, uint32_t V, uint32_t K, int dtype, const void 
   const uint32_t runs = V / (16 / size), lds = distill_lds(K, V);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   // As few threads as hold a row, for the registers of more rows on a compute unit; where the chip has a compute unit for every
-  // row, as many as there are runs (12 x 32000 in 32 bits 10.6 us with 512 threads, 9.0 with 1024).
+  // row, as many as there are runs (12 x 32000 in 32 bits 10.4 us with 512 threads, 8.8 with 1024).
   with_type(dtype, [&](auto t) {
     typedef decltype(t) E;
     if (runs <= 256 * 4)
