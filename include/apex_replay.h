@@ -562,7 +562,9 @@ int apex_pe_stats(apex_pe_replay_t *r, apex_pe_stats_t *out /*host*/, void *hip_
  * ahead of it, actors and learner need three operators beside the replay verbs: the recurrence that is the draft model's
  * memory (apex_gated_scan; a sequence's start state and its discounts come out of the replay memory), the loss against the
  * target's stored top logits with its gradient (apex_distill_topk: the importance weights enter it, the new priorities
- * leave it), and the verification of what the draft proposed (apex_verify_draft).
+ * leave it), and the verification of what the draft proposed (apex_verify_draft).  A draft whose memory is a matrix per head has
+ * apex_delta_rule in the place of apex_gated_scan; tokens come in by apex_embedding, and before the learner applies its gradients
+ * apex_clip_gradients bounds their norm (the paper: 40).
  *
  * Conventions, beyond those above
  *   - Stateless.  Arrays are device, strides are counted in elements, the last index is contiguous, and a pointer is
@@ -585,6 +587,11 @@ typedef enum apex_gate {
 #define APEX_MAX_VOCABULARY 1048576u  /* V of apex_distill_topk and apex_verify_draft                */
 #define APEX_MAX_TOP 1024u            /* K of apex_distill_topk                                      */
 #define APEX_MAX_DRAFT 64u            /* G of apex_verify_draft                                      */
+#define APEX_DELTA_CHUNK 64u          /* steps per stored state of apex_delta_rule's carry           */
+#define APEX_DELTA_MAX_WIDTH 128u     /* Dk and Dv of apex_delta_rule                                */
+#define APEX_MAX_TOKENS 8388608u      /* N of apex_embedding                                         */
+#define APEX_MAX_WIDTH 8192u          /* D of apex_embedding                                         */
+#define APEX_MAX_TENSORS 65536u       /* count of apex_clip_gradients                                */
 
 /*
  * A gated linear recurrence over S sequences of T steps of D independent channels.  For t in [0, len_s), per channel:
@@ -671,6 +678,76 @@ int apex_verify_draft(uint32_t B, uint32_t G, uint32_t V, int dtype, const void 
                       uint64_t target_row_stride, const void *draft, uint64_t draft_seq_stride, uint64_t draft_row_stride,
                       const int32_t *token, const uint64_t *rnd, const int32_t *length, int32_t *accepted,
                       int32_t *token_out, void *workspace, void *hip_stream);
+
+/*
+ * The gated delta rule: a recurrence whose state is a matrix [Dk,Dv] per value head, over S sequences of T steps of H value heads,
+ * each H / Hk of which share one of Hk query and key heads (value head h: h / (H / Hk)).  For t in [0, len_s), per sequence and head:
+ *     L_t = exp(g_t) * c_{t-1} S_{t-1},                  c_t = 1 if discount[s,t] != 0, else 0 (the episode ended on that step);
+ *     S_t = L_t + k_t u_t^T,   u_t = beta_t (v_t - L_t^T k_t),
+ *     o_t = scale * S_t^T q_t;                           c_{-1} S_{-1} = h0[s].
+ * q, k: element (s, t, h, d) at s * seq_stride + t * time_stride + h * Dk + d; v likewise with Dv; of type dtype, each with strides
+ * of its own (parts of one projection, time-major arrays).  g, beta [S,T,H] fp32: the logarithm of the decay (usually <= 0; -inf, or
+ * any whose exponential is 0 in 32 bits, cuts as an episode's end does) and the strength.  discount [S,T], length [S] as of
+ * apex_gated_scan (may be NULL).  h0 [S,H,Dk,Dv] fp32 (NULL: zeros).
+ * Outputs: o [S,T,H,Dv] of dtype, 0 for steps past a sequence's length, whose inputs are not looked at; h_last [S,H,Dk,Dv] fp32 =
+ * c_{len-1} S_{len-1}, or h0 where len = 0 (may be NULL; may be h0); carry [S, ceil(T / APEX_DELTA_CHUNK), H, Dk, Dv] fp32 (may be
+ * NULL): what passes into step t = c * APEX_DELTA_CHUNK, for those t below the length, the others are unspecified.  The gradient
+ * asks for it.
+ * With T = 1 this is the step of an actor: state in, state out.
+ * (Keys are meant to be of unit length, or no longer, and 0 <= beta <= 2, so that the recurrence does not grow.  Longer sequences
+ * are computed in pieces of 64 steps by products of matrices, as sums of products in 32 bits: a NaN or an infinity among the inputs
+ * or the state of a head makes that head's results NaN from its piece on; behind an episode's end, from the next piece on it has
+ * no effect any more.  Products whose magnitude passes the range of 32-bit numbers do the same.)
+ */
+int apex_delta_rule_workspace_bytes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, int backward,
+                                    size_t *bytes /*host*/);
+int apex_delta_rule(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv, int dtype, const void *q,
+                    uint64_t q_seq_stride, uint64_t q_time_stride, const void *k, uint64_t k_seq_stride, uint64_t k_time_stride,
+                    const void *v, uint64_t v_seq_stride, uint64_t v_time_stride, const float *g, const float *beta, float scale,
+                    const float *discount, const int32_t *length, const float *h0, void *o, float *h_last, float *carry,
+                    void *workspace, void *hip_stream);
+/*
+ * Its gradient, from do [S,T,H,Dv] of dtype and dh_last [S,H,Dk,Dv] fp32 (NULL: zeros), the gradients of o and h_last, and from
+ * `carry` as apex_delta_rule left it for the same inputs.  dq, dk, dv: arrays of dtype, strided as q, k and v, whose rows do not
+ * overlap; dg, dbeta [S,T,H] fp32; 0 for steps past the length (dg also where nothing passes into the step); dh0 [S,H,Dk,Dv] fp32
+ * (dh_last where len = 0; may be NULL).  A query's and a key's gradient is the sum over the value heads that share it.
+ * The workspace is that of apex_delta_rule_workspace_bytes with backward != 0, which is enough for apex_delta_rule, too.
+ */
+int apex_delta_rule_backward(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv, int dtype, const void *q,
+                             uint64_t q_seq_stride, uint64_t q_time_stride, const void *k, uint64_t k_seq_stride,
+                             uint64_t k_time_stride, const void *v, uint64_t v_seq_stride, uint64_t v_time_stride, const float *g,
+                             const float *beta, float scale, const float *discount, const int32_t *length, const float *carry,
+                             const void *d_o, const float *dh_last, void *dq, uint64_t dq_seq_stride, uint64_t dq_time_stride, void *dk,
+                             uint64_t dk_seq_stride, uint64_t dk_time_stride, void *dv, uint64_t dv_seq_stride, uint64_t dv_time_stride,
+                             float *dg, float *dbeta, float *dh0, void *workspace, void *hip_stream);
+
+/*
+ * Lookup of tokens' rows: out[n] = scale * table[token[n]], a row of zeros for a token outside [0, V).  table [V,D] (row v at
+ * v * table_stride) and out [N,D] of dtype, token [N] int32.  scale: any number that is finite.
+ */
+int apex_embedding(uint32_t N, uint32_t V, uint32_t D, int dtype, const void *table, uint64_t table_stride, const int32_t *token,
+                   float scale, void *out, uint64_t out_stride, void *hip_stream);
+/*
+ * The gradient of its table: dtable[v] = scale * the sum of dout[n] over the n with token[n] = v, in their order, in 32 bits; zeros
+ * for a token that is not named.  With add != 0 it is added to what dtable holds (a head that is tied to the table, several batches):
+ * rows that are not named stay as they are, the others are rounded once more.
+ */
+int apex_embedding_backward_workspace_bytes(uint32_t N, uint32_t V, uint32_t D, size_t *bytes /*host*/);
+int apex_embedding_backward(uint32_t N, uint32_t V, uint32_t D, int dtype, const void *dout, uint64_t dout_stride, const int32_t *token,
+                            float scale, int add, void *dtable, uint64_t dtable_stride, void *workspace, void *hip_stream);
+
+/*
+ * Clipping by the norm over `count` tensors: norm = sqrt(the sum of all their elements' squares, in 64 bits),
+ *     out_i = grad_i * min(1, max_norm / norm),
+ * rounded once.  grad, out, elements, dtype: host arrays, read before the call returns; tensor i has elements[i] contiguous elements
+ * (0: it is skipped) of dtype[i] (apex_dtype).  out NULL, or out[i] = grad[i]: in place.  Where the norm is not finite (a NaN or an
+ * infinity among the elements) nothing is scaled: out_i = grad_i, and the norm tells.  (A norm beyond the range of 32 bits reads +inf;
+ * the tensors are scaled by it all the same, unless one of their elements is none.)  max_norm: above 0, +inf for the norm alone
+ * (and copies, where out is another array).  norm [1] fp32 (device, may be NULL).
+ */
+int apex_clip_gradients_workspace_bytes(uint32_t count, size_t *bytes /*host*/);
+int apex_clip_gradients(uint32_t count, const void *const *grad /*host*/, void *const *out /*host*/, const uint64_t *elements /*host*/,
+                        const int *dtype /*host*/, float max_norm, float *norm, void *workspace, void *hip_stream);
 
 /* hipError_t of the last failed HIP call of the calling thread (0 if none). */
 int apex_last_hip_error(void);

@@ -24,6 +24,7 @@ NOALLOC_MAX_SAMPLES = 16384
 F32, BF16, F16 = 0, 1, 2
 GATES = {"given": 0, "sigmoid": 1}
 SCAN_CHUNK, MAX_VOCABULARY, MAX_TOP, MAX_DRAFT = 64, 1 << 20, 1024, 64
+DELTA_CHUNK, DELTA_MAX_WIDTH, MAX_TOKENS, MAX_WIDTH, MAX_TENSORS = 64, 128, 1 << 23, 8192, 65536
 TREE_MAX_LEVELS = 8
 
 EXPORTS = ["apex_replay_workspace_bytes", "apex_replay_create", "apex_replay_destroy", "apex_replay_layout",
@@ -41,7 +42,9 @@ EXPORTS = ["apex_replay_workspace_bytes", "apex_replay_create", "apex_replay_des
            "apex_pipeline_set_codec",
            "apex_gated_scan_workspace_bytes", "apex_gated_scan", "apex_gated_scan_backward",
            "apex_distill_topk_workspace_bytes", "apex_distill_topk", "apex_verify_draft_workspace_bytes",
-           "apex_verify_draft"]
+           "apex_verify_draft", "apex_delta_rule_workspace_bytes", "apex_delta_rule", "apex_delta_rule_backward",
+           "apex_embedding", "apex_embedding_backward_workspace_bytes", "apex_embedding_backward",
+           "apex_clip_gradients_workspace_bytes", "apex_clip_gradients"]
 
 
 class Config(C.Structure):
@@ -151,6 +154,15 @@ lib.apex_distill_topk.argtypes = [_u32, _u32, _u32, C.c_int, _vp, _u64, _vp, C.c
                                   _vp, _vp]
 lib.apex_verify_draft_workspace_bytes.argtypes = [_u32, _u32, _size]
 lib.apex_verify_draft.argtypes = [_u32, _u32, _u32, C.c_int, _vp, _u64, _u64, _vp, _u64, _u64] + [_vp] * 7
+_wide = [_vp, _u64, _u64]
+lib.apex_delta_rule_workspace_bytes.argtypes = [_u32] * 5 + [C.c_int, _size]
+lib.apex_delta_rule.argtypes = [_u32] * 6 + [C.c_int] + _wide * 3 + [_vp, _vp, _f32] + [_vp] * 8
+lib.apex_delta_rule_backward.argtypes = [_u32] * 6 + [C.c_int] + _wide * 3 + [_vp, _vp, _f32] + [_vp] * 5 + _wide * 3 + [_vp] * 5
+lib.apex_embedding.argtypes = [_u32] * 3 + [C.c_int, _vp, _u64, _vp, _f32, _vp, _u64, _vp]
+lib.apex_embedding_backward_workspace_bytes.argtypes = [_u32] * 3 + [_size]
+lib.apex_embedding_backward.argtypes = [_u32] * 3 + [C.c_int, _vp, _u64, _vp, _f32, C.c_int, _vp, _u64, _vp, _vp]
+lib.apex_clip_gradients_workspace_bytes.argtypes = [_u32, _size]
+lib.apex_clip_gradients.argtypes = [_u32, _vp, _vp, _vp, _vp, _f32, _vp, _vp, _vp]
 for _name in EXPORTS:
     getattr(lib, _name).restype = C.c_int
 
@@ -315,6 +327,109 @@ def verify_draft(target, draft, token, rnd, length=None, out=None, workspace=Non
             if workspace is None:
                 workspace = verify_draft_workspace(B, V, device=target.device)
     return _call.verify_draft(target, draft, token, rnd, length, out["accepted"], out["token"], workspace, stream), out
+
+
+def delta_rule_carry_shape(S, T, H, Dk, Dv):
+    return S, -(-T // DELTA_CHUNK), H, Dk, Dv
+
+
+def delta_rule_workspace(S, T, H, Dk, Dv, backward=False, device="cuda:0"):
+    """Workspace of delta_rule (with backward=True of delta_rule_backward as well) for these sizes, or None where it needs none."""
+    return _workspace(lib.apex_delta_rule_workspace_bytes, device, S, T, H, Dk, Dv, int(backward))
+
+
+def delta_rule(q, k, v, g, beta, discount=None, length=None, h0=None, scale=1.0, carry=False, out=None, workspace=None, stream=None):
+    """S_t = exp(g_t) S_{t-1} + k_t u_t^T with u_t = beta_t (v_t - exp(g_t) S_{t-1}^T k_t), o_t = scale S_t^T q_t, over device
+    tensors q, k [S,T,Hk,Dk] and v [S,T,H,Dv] (any strides but those within a step), g and beta fp32 [S,T,H]; H / Hk value heads
+    share a query and key head.  discount fp32 [S,T] (0: nothing passes on), length int32 [S], h0 fp32 [S,H,Dk,Dv].
+    Returns (rc, out): o [S,T,H,Dv], h_last fp32 [S,H,Dk,Dv], and with carry=True (or a place for it in `out`) what
+    delta_rule_backward needs."""
+    if carry and out is not None and out.get("carry") is None:
+        raise ValueError("carry=True, and no place for it in out")
+    if out is None or workspace is None:
+        (S, T, _, Dk), (_, _, H, Dv) = q.shape, v.shape
+        with _made_on(stream):
+            if out is None:
+                out = dict(o=torch.empty((S, T, H, Dv), dtype=v.dtype, device=v.device),
+                           h_last=torch.empty((S, H, Dk, Dv), dtype=torch.float32, device=v.device))
+                if carry:
+                    out["carry"] = torch.empty(delta_rule_carry_shape(S, T, H, Dk, Dv), dtype=torch.float32, device=v.device)
+            if workspace is None:
+                workspace = delta_rule_workspace(S, T, H, Dk, Dv, device=v.device)
+    get = out.get
+    return _call.delta_rule(q, k, v, g, beta, scale, discount, length, h0, out["o"], get("h_last"), get("carry"), workspace, stream), out
+
+
+def delta_rule_backward(q, k, v, g, beta, do, carry, discount=None, length=None, dh_last=None, scale=1.0, out=None, workspace=None,
+                        stream=None):
+    """Gradients of delta_rule from do [S,T,H,Dv] and dh_last fp32 [S,H,Dk,Dv], with the carry it left.
+    Returns (rc, out): dq, dk, dv as q, k and v (of any strides where `out` brings them), dg and dbeta fp32 [S,T,H], dh0 fp32
+    [S,H,Dk,Dv]."""
+    if out is None or workspace is None:
+        (S, T, _, Dk), (_, _, H, Dv) = q.shape, v.shape
+        with _made_on(stream):
+            if out is None:
+                out = {"d" + n: torch.empty(x.shape, dtype=x.dtype, device=x.device) for n, x in (("q", q), ("k", k), ("v", v))}
+                out.update({n: torch.empty((S, T, H), dtype=torch.float32, device=v.device) for n in ("dg", "dbeta")})
+                out["dh0"] = torch.empty((S, H, Dk, Dv), dtype=torch.float32, device=v.device)
+            if workspace is None:
+                workspace = delta_rule_workspace(S, T, H, Dk, Dv, backward=True, device=v.device)
+    return _call.delta_rule_backward(q, k, v, g, beta, scale, discount, length, carry, do, dh_last, out["dq"], out["dk"], out["dv"],
+                                     out["dg"], out["dbeta"], out.get("dh0"), workspace, stream), out
+
+
+def embedding(table, token, scale=1.0, out=None, stream=None):
+    """scale * table[token] for a table [V,D] and tokens int32 of any shape; zeros for tokens outside the table.
+    Returns (rc, out): out [N,D], N the number of tokens."""
+    if out is None:
+        with _made_on(stream):
+            out = dict(out=torch.empty((token.numel(), table.shape[1]), dtype=table.dtype, device=table.device))
+    return _call.embedding(table, token, scale, out["out"], stream), out
+
+
+def embedding_backward_workspace(N, V, D, device="cuda:0"):
+    """Workspace of embedding_backward for these sizes."""
+    return _workspace(lib.apex_embedding_backward_workspace_bytes, device, N, V, D)
+
+
+def embedding_backward(dout, token, V, scale=1.0, add=False, out=None, workspace=None, stream=None):
+    """Gradient of a table of V rows from dout [N,D] and the tokens; with add=True it is added to what out["dtable"] holds.
+    Returns (rc, out): dtable [V,D]."""
+    if add and out is None:
+        raise ValueError("add=True, and no table to add to in out")
+    if out is None or workspace is None:
+        N, D = dout.shape
+        with _made_on(stream):
+            if out is None:
+                out = dict(dtable=torch.empty((V, D), dtype=dout.dtype, device=dout.device))
+            if workspace is None:
+                workspace = embedding_backward_workspace(N, V, D, device=dout.device)
+    if out["dtable"].shape[0] != V:
+        raise ValueError("out['dtable'] has %d rows, not %d" % (out["dtable"].shape[0], V))
+    return _call.embedding_backward(dout, token, scale, int(add), out["dtable"], workspace, stream), out
+
+
+def clip_gradients_workspace(grads, device=None):
+    """Workspace of clip_gradients for these tensors (or that many)."""
+    count = grads if isinstance(grads, int) else len(grads)
+    if device is None:
+        device = grads[0].device if not isinstance(grads, int) and count else "cuda:0"
+    return _workspace(lib.apex_clip_gradients_workspace_bytes, device, count)
+
+
+def clip_gradients(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
+    """The tensors of the list `grads` times min(1, max_norm / norm), norm the one over all their elements, into the tensors of the
+    list `out` (laid out alike), or in place.  A norm that is not finite scales nothing.
+    Returns (rc, out): norm fp32 [1] and out, the list."""
+    if norm is None or workspace is None:
+        with _made_on(stream):
+            if norm is None:
+                norm = torch.empty(1, dtype=torch.float32, device=grads[0].device if len(grads) else "cuda:0")
+            if workspace is None:
+                workspace = clip_gradients_workspace(grads)
+    if out is not None and any(a.stride() != b.stride() for a, b in zip(grads, out)):
+        raise ValueError("out: laid out as the gradients")
+    return _call.clip_gradients(grads, out, max_norm, norm, workspace, stream), dict(norm=norm, out=grads if out is None else out)
 
 
 class Replay:

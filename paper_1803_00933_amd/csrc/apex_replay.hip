@@ -1361,3 +1361,6 @@ int apex_replay_stats(apex_replay_t *r, apex_replay_stats_t *out, void *hip_stre
 #include "scan.inc.hpp"
 #include "distill.inc.hpp"
 #include "verify.inc.hpp"
+#include "delta.inc.hpp"
+#include "embed.inc.hpp"
+#include "clip.inc.hpp"

@@ -11,6 +11,7 @@
 #include <exception>
 #include <tuple>
 #include <utility>
+#include <vector>
 
 #include "apex_replay.h"
 
@@ -183,6 +184,113 @@ struct From<View> {
   }
 };
 
+// A tensor [S,T,heads,width] on the GPU whose heads lie side by side.
+struct Heads {
+  void *p;
+  int64_t n[4], seq, time;
+  int dtype;
+  bool contiguous;
+  bool fits(int64_t a, int64_t b, int64_t c, int64_t d) const { return n[0] == a && n[1] == b && n[2] == c && n[3] == d; }
+};
+template <>
+struct From<Heads> {
+  static Heads get(PyObject *o)
+  {
+    if (!THPVariable_Check(o)) {
+      PyErr_Format(PyExc_TypeError, "a tensor is required, not %.80s", Py_TYPE(o)->tp_name);
+      throw Failed{};
+    }
+    const at::Tensor &t = THPVariable_Unpack(o);
+    const bool fits = t.is_cuda() && t.dim() == 4;
+    if (!fits || (t.size(3) > 1 && t.stride(3) != 1) || (t.size(2) > 1 && t.stride(2) != t.size(3)) || t.stride(0) < 0 || t.stride(1) < 0) {
+      PyErr_SetString(PyExc_AssertionError, "device tensors [S,T,heads,width] only, the heads of a step side by side");
+      throw Failed{};
+    }
+    Heads h{t.data_ptr(), {}, t.stride(0), t.stride(1), -1, t.is_contiguous()};
+    for (int i = 0; i < 4; ++i) {
+      h.n[i] = t.size(i);
+      if (h.n[i] > INT32_MAX) {
+        PyErr_SetString(PyExc_AssertionError, "sizes of 31 bits only");
+        throw Failed{};
+      }
+    }
+    const at::ScalarType s = t.scalar_type();
+    h.dtype = s == at::kFloat ? APEX_F32 : s == at::kBFloat16 ? APEX_BF16 : s == at::kHalf ? APEX_F16 : -1;
+    return h;
+  }
+};
+
+// A fp32 state, of any dimensions; None: no address and no elements.
+struct State {
+  float *p = nullptr;
+  int64_t count = 0;
+  bool none = true;
+  float *of(int64_t elements, const char *why) const
+  {
+    require(none || count == elements, why);
+    return p;
+  }
+};
+template <>
+struct From<State> {
+  static State get(PyObject *o)
+  {
+    State s;
+    if (o == Py_None) return s;
+    if (!THPVariable_Check(o)) {
+      PyErr_Format(PyExc_TypeError, "a tensor is required, not %.80s", Py_TYPE(o)->tp_name);
+      throw Failed{};
+    }
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.scalar_type() != at::kFloat || !t.is_contiguous()) {
+      PyErr_SetString(PyExc_AssertionError, "states and gates: device, contiguous fp32 tensors only");
+      throw Failed{};
+    }
+    s.p = static_cast<float *>(t.data_ptr());
+    s.count = t.numel();
+    s.none = false;
+    return s;
+  }
+};
+
+// A list or tuple of contiguous tensors of floating types on the GPU; None: none.
+struct Tensors {
+  std::vector<void *> p;
+  std::vector<uint64_t> elements;
+  std::vector<int> dtype;
+  bool none = false;
+};
+template <>
+struct From<Tensors> {
+  static Tensors get(PyObject *o)
+  {
+    Tensors r;
+    r.none = o == Py_None;
+    if (r.none) return r;
+    const Ref seq(PySequence_Fast(o, "a list or a tuple of tensors is required"));
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq.o);
+    r.p.reserve(n), r.elements.reserve(n), r.dtype.reserve(n);
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      PyObject *const item = PySequence_Fast_GET_ITEM(seq.o, i);
+      if (!THPVariable_Check(item)) {
+        PyErr_Format(PyExc_TypeError, "a tensor is required, not %.80s", Py_TYPE(item)->tp_name);
+        throw Failed{};
+      }
+      const at::Tensor &t = THPVariable_Unpack(item);
+      const at::ScalarType s = t.scalar_type();
+      const int dtype = s == at::kFloat ? APEX_F32 : s == at::kBFloat16 ? APEX_BF16 : s == at::kHalf ? APEX_F16 : -1;
+      if (!t.is_cuda() || !t.is_non_overlapping_and_dense() || dtype < 0) {
+        PyErr_SetString(PyExc_AssertionError, "device, dense tensors of a floating type only");
+        throw Failed{};
+      }
+      r.p.push_back(t.data_ptr());
+      r.elements.push_back((uint64_t)t.numel());
+      r.dtype.push_back(dtype);
+    }
+    return r;
+  }
+};
+
 // A workspace, and how large it is where that can be known: that of a tensor.
 struct Space {
   void *p;
@@ -279,7 +387,10 @@ PyObject *call(R (*f)(A...), PyObject *const *args, Py_ssize_t n)
   X(apex_pipeline_join) X(apex_pipeline_steps) X(apex_pipeline_add_begin) X(apex_pipeline_add_end) X(apex_pe_add)   \
   X(apex_pe_sample) X(apex_pe_update_priorities) X(apex_pe_evict_enqueue) X(apex_pe_add_round) X(apex_pe_sample_update) \
   X(apex_gated_scan) X(apex_gated_scan_backward) X(apex_distill_topk) X(apex_verify_draft)                          \
-  X(apex_gated_scan_workspace_bytes) X(apex_verify_draft_workspace_bytes)
+  X(apex_gated_scan_workspace_bytes) X(apex_verify_draft_workspace_bytes)                                           \
+  X(apex_delta_rule) X(apex_delta_rule_backward) X(apex_delta_rule_workspace_bytes)                                 \
+  X(apex_embedding) X(apex_embedding_backward) X(apex_embedding_backward_workspace_bytes)                           \
+  X(apex_clip_gradients) X(apex_clip_gradients_workspace_bytes)
 #define X(name) decltype(&::name) p_##name = nullptr;
 APEX_ENTRIES(X)
 #undef X
@@ -435,6 +546,67 @@ VERB(verify_draft, [](View target, View draft, View token, View rnd, View length
                              workspace.of(p_apex_verify_draft_workspace_bytes, B, vocabulary), s);
 })
 
+struct DeltaSizes {
+  int64_t S, T, Hk, H, Dk, Dv, state, gates;
+  DeltaSizes(const Heads &q, const Heads &k, const Heads &v)
+      : S(q.n[0]), T(q.n[1]), Hk(q.n[2]), H(v.n[2]), Dk(q.n[3]), Dv(v.n[3]), state(S * H * Dk * Dv), gates(S * T * H)
+  {
+    require(q.dtype >= 0 && k.dtype == q.dtype && v.dtype == q.dtype, "q, k and v: of one floating type");
+    require(k.fits(S, T, Hk, Dk) && v.n[0] == S && v.n[1] == T, "q and k: [S,T,Hk,Dk], v: [S,T,H,Dv]");
+  }
+};
+
+VERB(delta_rule, [](Heads q, Heads k, Heads v, State g, State beta, float scale, View discount, View length, State h0, Heads o, State h_last,
+                    State carry, Space workspace, Stream s) {
+  const DeltaSizes n(q, k, v);
+  require(o.dtype == q.dtype && o.fits(n.S, n.T, n.H, n.Dv) && o.contiguous, "o: [S,T,H,Dv], contiguous, of q's type");
+  require(!g.none && !beta.none, "g and beta: fp32 [S,T,H]");
+  const int64_t chunks = (n.T + APEX_DELTA_CHUNK - 1) / APEX_DELTA_CHUNK;
+  return p_apex_delta_rule(n.S, n.T, n.Hk, n.H, n.Dk, n.Dv, q.dtype, q.p, q.seq, q.time, k.p, k.seq, k.time, v.p, v.seq, v.time,
+                           g.of(n.gates, "g: fp32 [S,T,H]"), beta.of(n.gates, "beta: fp32 [S,T,H]"), scale,
+                           floats(discount, n.S * n.T, "discount: fp32 [S,T]"), ints(length, n.S, "length: int32 [S]"),
+                           h0.of(n.state, "h0: fp32 [S,H,Dk,Dv]"), o.p, h_last.of(n.state, "h_last: fp32 [S,H,Dk,Dv]"),
+                           carry.of(chunks * n.state, "carry: fp32 [S,chunks,H,Dk,Dv]"),
+                           workspace.of(p_apex_delta_rule_workspace_bytes, n.S, n.T, n.H, n.Dk, n.Dv, 0), s);
+})
+VERB(delta_rule_backward, [](Heads q, Heads k, Heads v, State g, State beta, float scale, View discount, View length, State carry, Heads d_o,
+                             State dh_last, Heads dq, Heads dk, Heads dv, State dg, State dbeta, State dh0, Space workspace, Stream s) {
+  const DeltaSizes n(q, k, v);
+  require(d_o.dtype == q.dtype && d_o.fits(n.S, n.T, n.H, n.Dv) && d_o.contiguous, "do: [S,T,H,Dv], contiguous, of q's type");
+  require(dq.dtype == q.dtype && dk.dtype == q.dtype && dv.dtype == q.dtype && dq.fits(n.S, n.T, n.Hk, n.Dk) &&
+              dk.fits(n.S, n.T, n.Hk, n.Dk) && dv.fits(n.S, n.T, n.H, n.Dv), "dq, dk and dv: as q, k and v");
+  require(!g.none && !beta.none && !carry.none && !dg.none && !dbeta.none, "g, beta, dg, dbeta: fp32 [S,T,H], and a carry");
+  const int64_t chunks = (n.T + APEX_DELTA_CHUNK - 1) / APEX_DELTA_CHUNK;
+  return p_apex_delta_rule_backward(n.S, n.T, n.Hk, n.H, n.Dk, n.Dv, q.dtype, q.p, q.seq, q.time, k.p, k.seq, k.time, v.p, v.seq, v.time,
+                                    g.of(n.gates, "g: fp32 [S,T,H]"), beta.of(n.gates, "beta: fp32 [S,T,H]"), scale,
+                                    floats(discount, n.S * n.T, "discount: fp32 [S,T]"), ints(length, n.S, "length: int32 [S]"),
+                                    carry.of(chunks * n.state, "carry: fp32 [S,chunks,H,Dk,Dv]"), d_o.p,
+                                    dh_last.of(n.state, "dh_last: fp32 [S,H,Dk,Dv]"), dq.p, dq.seq, dq.time, dk.p, dk.seq, dk.time, dv.p,
+                                    dv.seq, dv.time, dg.of(n.gates, "dg: fp32 [S,T,H]"), dbeta.of(n.gates, "dbeta: fp32 [S,T,H]"),
+                                    dh0.of(n.state, "dh0: fp32 [S,H,Dk,Dv]"),
+                                    workspace.of(p_apex_delta_rule_workspace_bytes, n.S, n.T, n.H, n.Dk, n.Dv, 1), s);
+})
+VERB(embedding, [](View table, View token, float scale, View out, Stream s) {
+  require(table.dim == 2 && table.dtype >= 0 && table.rows(), "table: [V,D] of a floating type, contiguous rows");
+  require(!token.is_none() && out.fits(token.count, table.n[1]) && out.dtype == table.dtype && out.rows(),
+          "out: [N,D] of the table's type, contiguous rows");
+  return p_apex_embedding(token.count, table.n[0], table.n[1], table.dtype, table.p, table.stride[0], ints(token, token.count, "token: int32"),
+                          scale, out.p, out.stride[0], s);
+})
+VERB(embedding_backward, [](View dout, View token, float scale, int add, View dtable, Space workspace, Stream s) {
+  require(dtable.dim == 2 && dtable.dtype >= 0 && dtable.rows(), "dtable: [V,D] of a floating type, contiguous rows");
+  require(!token.is_none() && dout.fits(token.count, dtable.n[1]) && dout.dtype == dtable.dtype && dout.rows(),
+          "dout: [N,D] of the table's type, contiguous rows");
+  return p_apex_embedding_backward(token.count, dtable.n[0], dtable.n[1], dout.dtype, dout.p, dout.stride[0],
+                                   ints(token, token.count, "token: int32"), scale, add, dtable.p, dtable.stride[0],
+                                   workspace.of(p_apex_embedding_backward_workspace_bytes, token.count, dtable.n[0], dtable.n[1]), s);
+})
+VERB(clip_gradients, [](Tensors grad, Tensors out, float max_norm, View norm, Space workspace, Stream s) {
+  require(!grad.none && (out.none || (out.elements == grad.elements && out.dtype == grad.dtype)), "out: as the gradients");
+  return p_apex_clip_gradients(grad.p.size(), grad.p.data(), out.none ? nullptr : out.p.data(), grad.elements.data(), grad.dtype.data(),
+                               max_norm, floats(norm, 1, "norm: fp32 [1]"), workspace.of(p_apex_clip_gradients_workspace_bytes, grad.p.size()), s);
+})
+
 // load(path of the library, _ptr, _plain, current device, current raw stream)
 PyObject *load(PyObject *, PyObject *args)
 {
@@ -464,6 +636,7 @@ PyMethodDef methods[] = {
     FAST(pipeline_steps), FAST(pipeline_add_begin), FAST(pipeline_add_end), FAST(pe_add), FAST(pe_sample),
     FAST(pe_update_priorities), FAST(pe_evict_enqueue), FAST(pe_add_round), FAST(pe_sample_update),
     FAST(gated_scan), FAST(gated_scan_backward), FAST(distill_topk), FAST(verify_draft),
+    FAST(delta_rule), FAST(delta_rule_backward), FAST(embedding), FAST(embedding_backward), FAST(clip_gradients),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "apex_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
