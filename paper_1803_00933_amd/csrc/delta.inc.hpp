@@ -39,7 +39,6 @@ struct DeltaArgs {
   float scale;
   const float *discount;
   const int32_t *length;
-  float *M;  // [S][pieces][H][64][64]
 };
 
 struct DeltaForward {
@@ -57,6 +56,7 @@ struct DeltaBack {
   uint64_t dq_seq, dq_time, dk_seq, dk_time, dv_seq, dv_time;
   void *dq, *dk, *dv;
   float *dg, *dbeta, *dh0;
+  const float *M;  // [S][pieces][H][64][64]
   float *dS;  // [S][pieces][H][Dk][Dv]: of the state behind a piece
   float *Y;   // [S][T][H][Dv]
 };
@@ -75,7 +75,7 @@ __device__ __forceinline__ bool delta_passes(const DeltaArgs &a, uint32_t s, uin
 
 // What a piece's steps have of their gates, in LDS.  Steps that a sequence does not have: g = beta = 0.
 struct Gates {
-  double G[kPiece];       // sum of g from the piece's begin on: differences of 32-bit sums would lose what is small beside them
+  double G[kPiece];       // sum of g log2(e) from the piece's begin on: differences of 32-bit sums would lose what is small beside them
   uint32_t episode[kPiece];  // episodes that ended in the piece in front of the step or on its begin
   float beta[kPiece], begin[kPiece], end[kPiece];  // strength; what is left of the start state, and of the step at the end
   uint32_t cut[kPiece];   // nothing passes into the step
@@ -91,7 +91,7 @@ __device__ __forceinline__ void load_gates(const DeltaArgs &a, uint32_t s, uint3
   float g = have ? a.g[at] : 0.0f;
   const bool cut = have && (delta_cuts(g) || (t > 0 && !delta_passes(a, s, t - 1)));
   if (cut) g = 0.0f;
-  double sum = g;
+  double sum = (double)g * 1.4426950408889634;
   uint32_t episode = cut;
   for (int d = 1; d < kWave; d *= 2) {
     const double up = __shfl_up(sum, d);
@@ -103,16 +103,16 @@ __device__ __forceinline__ void load_gates(const DeltaArgs &a, uint32_t s, uint3
   x.G[lane] = sum;
   x.episode[lane] = episode;
   x.beta[lane] = have ? a.beta[at] : 0.0f;
-  x.begin[lane] = episode == 0 ? expf((float)sum) : 0.0f;
-  x.end[lane] = episode == episodes ? expf((float)(all - sum)) : 0.0f;
+  x.begin[lane] = episode == 0 ? exp2_of((float)sum) : 0.0f;
+  x.end[lane] = episode == episodes ? exp2_of((float)(all - sum)) : 0.0f;
   x.cut[lane] = cut;
-  if (lane == 0) x.last = episodes == 0 ? expf((float)all) : 0.0f;
+  if (lane == 0) x.last = episodes == 0 ? exp2_of((float)all) : 0.0f;
 }
 
 // D of a step t and an earlier one.
 __device__ __forceinline__ float decay(const Gates &x, uint32_t t, uint32_t i)
 {
-  return x.episode[t] == x.episode[i] ? expf((float)(x.G[t] - x.G[i])) : 0.0f;
+  return x.episode[t] == x.episode[i] ? exp2_of((float)(x.G[t] - x.G[i])) : 0.0f;
 }
 
 // acc + A B over `depth` (a multiple of 16): a(k) of row lane % 16, b(k) of column lane % 16.
@@ -139,285 +139,662 @@ __device__ __forceinline__ void load_rows(float *to, uint32_t row, uint32_t colu
   }
 }
 
-// M of a piece: products of its keys, decayed, and the substitution row by row, a lane per column.
-template <typename T>
-__global__ __launch_bounds__(kDeltaThreads) void delta_solve_kernel(DeltaArgs a)
-{
-  __shared__ Gates gates;
-  __shared__ float K[kPiece * (kDeltaMaxWidth + 4)], L[kPiece * kPieceRow];
-  const uint32_t h = blockIdx.x % a.H, piece = blockIdx.x / a.H % a.pieces, s = blockIdx.x / a.H / a.pieces;
-  const uint32_t len = delta_length(a, s), t0 = piece * kPiece;
-  if (t0 >= len) return;
-  const uint32_t lane = lane_id(), wave = threadIdx.x / kWave, depth = up16(a.Dk), row = depth + 4;
-  const T *const k = static_cast<const T *>(a.k) + s * a.k_seq + t0 * a.k_time + (uint64_t)(h / a.share) * a.Dk;
-  load_rows(K, row, depth, k, a.k_time, len - t0, a.Dk, kDeltaThreads);
-  if (wave == 0) load_gates(a, s, h, t0, len, gates);
-  __syncthreads();
-  for (uint32_t tile = wave; tile < 16; tile += kDeltaWaves) {
-    const uint32_t r = tile / 4 * 16, c = tile % 4 * 16;
-    if (c > r) continue;
-    const Tile kk = product(Tile{}, depth, [&](uint32_t i) { return K[(r + lane % 16) * row + i]; },
-                            [&](uint32_t i) { return K[(c + lane % 16) * row + i]; });
-#pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) {
-      const uint32_t t = r + lane / 16 * 4 + i, j = c + lane % 16;
-      L[t * kPieceRow + j] = j < t ? kk[i] * decay(gates, t, j) : 0.0f;
-    }
-  }
-  __syncthreads();
-  if (wave) return;
-  // a lane's column of M, from the top
-  float m[kPiece];
-  float *const out = a.M + (uint64_t)blockIdx.x * kPiece * kPiece;
-#pragma unroll
-  for (uint32_t t = 0; t < kPiece; ++t) {
-    float sum = lane < t ? L[t * kPieceRow + lane] : 0.0f;
-#pragma unroll
-    for (uint32_t i = 1; i < t; ++i) sum -= L[t * kPieceRow + i] * m[i];
-    out[t * kPiece + lane] = sum;
-    m[t] = sum * gates.beta[t];  // (as the rows below take it)
-  }
-}
+// ---- products.  Matrix instructions take numbers of 8 bits (bf16), 16 times as many as of 32 bits, so a 32-bit number is the sum
+// of three of them (cut off, not rounded: 24 bits in three parts of 8, which is exact), and a product of two is the sum of the six
+// products of parts that are not below its last bit.  Numbers of 16 bits are one part (bf16) or two (f16).
+typedef __bf16 Parts8 __attribute__((ext_vector_type(8)));  // one part of 8 numbers: an operand's share of a lane
 
-template <uint32_t kColumns>
-struct DeltaSpace {
-  static constexpr uint32_t kRow = kColumns + 4;
-  Gates gates;
-  float K[kPiece * (kDeltaMaxWidth + 4)], Q[kPiece * (kDeltaMaxWidth + 4)];
-  float M[kPiece * kPieceRow], P[kPiece * kPieceRow];
-  float S[kDeltaMaxWidth * kRow];
-  float X[kPiece * kRow], U[kPiece * kRow];
+template <typename T>
+constexpr uint32_t kPartsOf = std::is_same<T, __bf16>::value ? 1 : std::is_same<T, _Float16>::value ? 2 : 3;
+
+template <uint32_t N>
+struct Operand {
+  Parts8 part[N];
 };
 
-// P of a wave's 16 rows.
-template <typename Space>
-__device__ __forceinline__ void attend(Space &x, uint32_t depth, uint32_t row)
+template <uint32_t N>
+__device__ __forceinline__ Operand<N> split(const float (&x)[8])
 {
-  const uint32_t lane = lane_id(), r = threadIdx.x / kWave * 16;
-  for (uint32_t c = 0; c < kPiece; c += 16) {
-    Tile p{};
-    if (c <= r)
-      p = product(p, depth, [&](uint32_t i) { return x.Q[(r + lane % 16) * row + i]; }, [&](uint32_t i) { return x.K[(c + lane % 16) * row + i]; });
+  Operand<N> r;
+  float left[8];
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) {
-      const uint32_t t = r + lane / 16 * 4 + i, j = c + lane % 16;
-      x.P[t * kPieceRow + j] = j <= t ? p[i] * decay(x.gates, t, j) : 0.0f;
+  for (uint32_t i = 0; i < 8; ++i) left[i] = x[i];
+#pragma unroll
+  for (uint32_t p = 0; p < N; ++p) {
+    uint32_t word[4];
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) word[i] = __builtin_amdgcn_perm(__float_as_uint(left[2 * i + 1]), __float_as_uint(left[2 * i]), 0x07060302);
+    __builtin_memcpy(&r.part[p], word, 16);
+    if (p + 1 < N) {
+#pragma unroll
+      for (uint32_t i = 0; i < 8; ++i) left[i] -= __uint_as_float(__float_as_uint(left[i]) & 0xffff0000u);
     }
+  }
+  return r;
+}
+
+template <typename T>
+__device__ __forceinline__ Operand<kPartsOf<T>> operand(const Run<T, 8> &x)
+{
+  if constexpr (std::is_same<T, __bf16>::value) {
+    Operand<1> r;
+    r.part[0] = __builtin_bit_cast(Parts8, x);
+    return r;
+  } else {
+    float f[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) f[i] = element<8, T>(x, i);
+    return split<kPartsOf<T>>(f);
   }
 }
 
-__device__ __forceinline__ void load_piece_matrix(float *to, const float *from)
+// acc + A B over 32: operands' parts together below the `limit`-th.
+template <uint32_t kLimit, uint32_t NA, uint32_t NB>
+__device__ __forceinline__ void multiply(Tile &acc, const Operand<NA> &a, const Operand<NB> &b)
 {
-  for (uint32_t i = threadIdx.x; i < kPiece * kPiece; i += kDeltaThreads) to[i / kPiece * kPieceRow + i % kPiece] = from[i];
+#pragma unroll
+  for (uint32_t i = 0; i < NA; ++i)
+#pragma unroll
+    for (uint32_t j = 0; j < NB; ++j)
+      if (i + j < kLimit) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.part[i], b.part[j], acc, 0, 0, 0);
 }
 
-// A workgroup per sequence, value head and kColumns columns of its state goes through the pieces.  A wave holds 32 rows of the
-// state, as two rows of tiles, and writes them to LDS for the products of all; of what belongs to steps it has 16.
-template <typename T, uint32_t kColumns>
-__global__ __launch_bounds__(kDeltaThreads) void delta_pieces_kernel(DeltaForward f)
+// Two tiles on top of each other as the right operand of the next product: a lane of group q has rows 8 q .. 8 q + 7 of the 32 if
+// row 4 q + e of the first tile is row 8 q + e, and of the second row 8 q + 4 + e.  Tiles of steps and of a state's rows are
+// laid out that way, so that what one product leaves is what the next one takes, without a lane's data leaving it.
+__device__ __forceinline__ uint32_t tile_row(uint32_t tile, uint32_t m) { return tile / 2 * 32 + m / 4 * 8 + tile % 2 * 4 + m % 4; }
+
+template <uint32_t N>
+__device__ __forceinline__ Operand<N> operand_of(const Tile &x, const Tile &y)
 {
-  constexpr uint32_t kTiles = kColumns / 16, kRow = DeltaSpace<kColumns>::kRow;
-  const DeltaArgs &a = f.n;
-  __shared__ DeltaSpace<kColumns> x;
-  const uint32_t blocks = (a.Dv + kColumns - 1) / kColumns;
-  const uint32_t c0 = blockIdx.x % blocks * kColumns, h = blockIdx.x / blocks % a.H, s = blockIdx.x / blocks / a.H;
-  const uint32_t lane = lane_id(), wave = threadIdx.x / kWave, col = lane % 16, quad = lane / 16 * 4;
-  const uint32_t len = delta_length(a, s), depth = up16(a.Dk), row = depth + 4, r = wave * 16;
-  const uint64_t state = ((uint64_t)s * a.H + h) * a.Dk * a.Dv;
-  const auto each = [&](auto do_) {  // of this wave's part of the state: (tile, element, row, column)
+  const float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+  return split<N>(f);
+}
+
+// ---- what does not depend on a state, for every piece: its gates, M and P (or their transposes) and, by the first of the value
+// heads that share them, the keys' (and queries') transposes, in the order in which the kernels behind take them as left operands:
+// 64 lanes times 8 numbers, lane l has row l % 16 of the tile and numbers 8 (l / 16) .. + 7 of the 32.
+constexpr uint32_t kOperand = 64 * 8;                         // numbers
+constexpr uint32_t kTriangle = 6;                             // operands of a triangular matrix: 4 tiles of rows by 2 of 32 steps, less 2
+constexpr uint32_t kGateWords = 256;
+
+struct PieceGates {  // of a piece and value head
+  float beta[kPiece], begin[kPiece], end[kPiece], last;
+};
+static_assert(sizeof(PieceGates) <= kGateWords * 4);
+
+struct Prepared {
+  float *gates;      // [heads][kGateWords]
+  __bf16 *M, *P;     // [heads][kTriangle][3][kOperand]
+  void *Kt, *Qt;     // [key heads][2 KS][2][kOperand] of the inputs' type
+  float *whole;      // [heads][64][64]: M as it is (for the gradient)
+};
+
+// The operand of rows and columns of a triangular matrix: f -> (tile of rows, 32 steps).
+__device__ __forceinline__ void triangle(uint32_t f, bool upper, uint32_t *r, uint32_t *s)
+{
+  if (upper)
+    *r = f < 4 ? f / 2 : f - 2, *s = f < 4 ? f % 2 : 1;
+  else
+    *r = f < 2 ? f : 2 + (f - 2) / 2, *s = f < 2 ? 0 : (f - 2) % 2;
+}
+
+// Eight numbers of a row from `d` on, zeros beyond `width`; kWhole: there are none beyond.
+template <typename T>
+__device__ __forceinline__ Run<T, 8> load_eight(const T *row, uint32_t d, uint32_t width)
+{
+  if (d + 8 <= width) return load_run<T, 8>(row + d);
+  Run<T, 8> r{};
 #pragma unroll
-    for (uint32_t i = 0; i < 2; ++i)
+  for (uint32_t i = 0; i < 8; ++i)
+    if (d + i < width) r[i] = row[d + i];
+  return r;
+}
+
+// Row t of a piece's `have` steps; beyond them zeros, and the last one is fetched.
+template <typename T>
+__device__ __forceinline__ Run<T, 8> load_step(const T *piece, uint64_t stride, uint32_t t, uint32_t have, uint32_t d, uint32_t width)
+{
+  const Run<T, 8> r = load_eight<T>(piece + min(t, have - 1) * stride, d, width);
+  return t < have ? r : Run<T, 8>{};
+}
+
+template <typename T, uint32_t KS, bool kBack>
+__global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs a, Prepared w)
+{
+  constexpr uint32_t kRaw = KS * 32 + 2;
+  __shared__ Gates gates;
+  __shared__ float L[kPiece * kPieceRow], P[kPiece * kPieceRow], inverse[4][16][17];
+  __shared__ T raw[kBack ? 2 : 1][kPiece][kRaw];
+  const uint32_t h = blockIdx.x % a.H, piece = blockIdx.x / a.H % a.pieces, s = blockIdx.x / a.H / a.pieces, hk = h / a.share;
+  const uint32_t len = delta_length(a, s), t0 = piece * kPiece;
+  if (t0 >= len) return;
+  const uint32_t have = min(kPiece, len - t0);
+  const uint32_t lane = lane_id(), wave = threadIdx.x / kWave, m = lane % 16, q = lane / 16;
+  const bool first = h % a.share == 0;  // of those that share a key head
+  const T *const k_rows = static_cast<const T *>(a.k) + s * a.k_seq + t0 * a.k_time + (uint64_t)hk * a.Dk;
+  const T *const q_rows = static_cast<const T *>(a.q) + s * a.q_seq + t0 * a.q_time + (uint64_t)hk * a.Dk;
+  Operand<kPartsOf<T>> k_own[KS], q_own[KS];
 #pragma unroll
-      for (uint32_t j = 0; j < kTiles; ++j)
+  for (uint32_t i = 0; i < KS; ++i) {
+    const uint32_t t = wave * 16 + m, d = i * 32 + q * 8;
+    const Run<T, 8> kr = load_step<T>(k_rows, a.k_time, t, have, d, a.Dk), qr = load_step<T>(q_rows, a.q_time, t, have, d, a.Dk);
+    k_own[i] = operand<T>(kr), q_own[i] = operand<T>(qr);
+    if (first) {
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) do_(i, j, e, (wave * 2 + i) * 16 + quad + e, j * 16 + col);
-  };
-  Tile S[2][kTiles];
-  each([&](uint32_t i, uint32_t j, uint32_t e, uint32_t d, uint32_t c) {
-    S[i][j][e] = f.h0 && d < a.Dk && c0 + c < a.Dv ? f.h0[state + (uint64_t)d * a.Dv + c0 + c] : 0.0f;
-  });
-  const uint32_t hk = h / a.share;
-  for (uint32_t piece = 0; piece < a.pieces; ++piece) {
-    const uint32_t t0 = piece * kPiece, steps = min(kPiece, a.T - t0);
-    T *const o = static_cast<T *>(f.o) + (((uint64_t)s * a.T + t0) * a.H + h) * a.Dv + c0;
-    const uint64_t o_row = (uint64_t)a.H * a.Dv;
-    if (t0 >= len) {
-      for (uint32_t i = threadIdx.x; i < steps * kColumns; i += kDeltaThreads)
-        if (c0 + i % kColumns < a.Dv) o[i / kColumns * o_row + i % kColumns] = (T)0.0f;
-      continue;
-    }
-    __syncthreads();
-    load_rows(x.K, row, depth, static_cast<const T *>(a.k) + s * a.k_seq + t0 * a.k_time + (uint64_t)hk * a.Dk, a.k_time, len - t0, a.Dk, kDeltaThreads);
-    load_rows(x.Q, row, depth, static_cast<const T *>(a.q) + s * a.q_seq + t0 * a.q_time + (uint64_t)hk * a.Dk, a.q_time, len - t0, a.Dk, kDeltaThreads);
-    load_rows(x.X, kRow, kColumns, static_cast<const T *>(a.v) + s * a.v_seq + t0 * a.v_time + (uint64_t)h * a.Dv + c0, a.v_time, len - t0, a.Dv - c0,
-              kDeltaThreads);
-    load_piece_matrix(x.M, a.M + (((uint64_t)s * a.pieces + piece) * a.H + h) * kPiece * kPiece);
-    if (wave == 0) load_gates(a, s, h, t0, len, x.gates);
-    each([&](uint32_t i, uint32_t j, uint32_t e, uint32_t d, uint32_t c) {
-      x.S[d * kRow + c] = S[i][j][e];
-      if (f.carry && d < a.Dk && c0 + c < a.Dv)
-        f.carry[(((uint64_t)s * a.pieces + piece) * a.H + h) * a.Dk * a.Dv + (uint64_t)d * a.Dv + c0 + c] = S[i][j][e];
-    });
-    __syncthreads();
-    attend(x, depth, row);
-    Tile X[kTiles], O[kTiles];
-#pragma unroll
-    for (uint32_t j = 0; j < kTiles; ++j) {
-      const auto state_of = [&](uint32_t i) { return x.S[i * kRow + j * 16 + col]; };
-      const Tile kS = product(Tile{}, depth, [&](uint32_t i) { return x.K[(r + col) * row + i]; }, state_of);
-      O[j] = product(Tile{}, depth, [&](uint32_t i) { return x.Q[(r + col) * row + i]; }, state_of);
-#pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) {
-        const uint32_t t = r + quad + e;
-        const bool passes = x.gates.episode[t] == 0;  // a selection: nothing of what has ended
-        float &v = x.X[t * kRow + j * 16 + col];
-        X[j][e] = v - (passes ? x.gates.begin[t] * kS[e] : 0.0f);
-        O[j][e] = passes ? x.gates.begin[t] * O[j][e] : 0.0f;
-        v = x.gates.beta[t] * X[j][e];
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (uint32_t j = 0; j < kTiles; ++j) {
-      const Tile mX = product(Tile{}, kPiece, [&](uint32_t i) { return x.M[(r + col) * kPieceRow + i]; },
-                              [&](uint32_t i) { return x.X[i * kRow + j * 16 + col]; });
-#pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) {
-        const uint32_t t = r + quad + e;
-        x.U[t * kRow + j * 16 + col] = x.gates.beta[t] * (X[j][e] - mX[e]);
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (uint32_t j = 0; j < kTiles; ++j) {
-      O[j] = product(O[j], kPiece, [&](uint32_t i) { return x.P[(r + col) * kPieceRow + i]; },
-                     [&](uint32_t i) { return x.U[i * kRow + j * 16 + col]; });
-#pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) {
-        const uint32_t t = r + quad + e, c = j * 16 + col;
-        if (t < steps && c0 + c < a.Dv) o[t * o_row + c] = t0 + t < len ? (T)(a.scale * O[j][e]) : (T)0.0f;
-      }
-#pragma unroll
-      for (uint32_t i = 0; i < 2; ++i) {
-        const uint32_t d0 = (wave * 2 + i) * 16;
-        if (d0 >= depth) continue;
-        const Tile left = x.gates.episode[kPiece - 1] == 0 ? S[i][j] * x.gates.last : Tile{};
-        S[i][j] = product(left, kPiece, [&](uint32_t t) { return x.K[t * row + d0 + col]; },
-                          [&](uint32_t t) { return x.U[t * kRow + j * 16 + col] * x.gates.end[t]; });
+      for (uint32_t e = 0; e < 8; ++e) {
+        raw[0][t][d + e] = kr[e];
+        if (kBack) raw[kBack][t][d + e] = qr[e];
       }
     }
   }
-  if (f.h_last) {
-    const bool passes = len == 0 || delta_passes(a, s, len - 1);
-    each([&](uint32_t i, uint32_t j, uint32_t e, uint32_t d, uint32_t c) {
-      if (d < a.Dk && c0 + c < a.Dv) f.h_last[state + (uint64_t)d * a.Dv + c0 + c] = passes ? S[i][j][e] : 0.0f;
-    });
-  }
-}
-
-// The same from the last piece to the first, with dS: its values for every piece, Y and dV.
-template <typename T, uint32_t kColumns>
-__global__ __launch_bounds__(kDeltaThreads) void delta_pieces_back_kernel(DeltaBack b)
-{
-  constexpr uint32_t kTiles = kColumns / 16, kRow = DeltaSpace<kColumns>::kRow;
-  const DeltaArgs &a = b.n;
-  __shared__ DeltaSpace<kColumns> x;  // X: dO, U: beta dU, then c dV
-  const uint32_t blocks = (a.Dv + kColumns - 1) / kColumns;
-  const uint32_t c0 = blockIdx.x % blocks * kColumns, h = blockIdx.x / blocks % a.H, s = blockIdx.x / blocks / a.H;
-  const uint32_t lane = lane_id(), wave = threadIdx.x / kWave, col = lane % 16, quad = lane / 16 * 4;
-  const uint32_t len = delta_length(a, s), depth = up16(a.Dk), row = depth + 4, r = wave * 16;
-  const uint64_t state = ((uint64_t)s * a.H + h) * a.Dk * a.Dv;
-  const auto each = [&](auto do_) {
+  if (wave == 0) load_gates(a, s, h, t0, len, gates);
+  __syncthreads();
+  for (uint32_t c = 0; c < 4; ++c) {
+    Tile kk{}, qk{};
+    if (c <= wave) {
 #pragma unroll
-    for (uint32_t i = 0; i < 2; ++i)
-#pragma unroll
-      for (uint32_t j = 0; j < kTiles; ++j)
-#pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) do_(i, j, e, (wave * 2 + i) * 16 + quad + e, j * 16 + col);
-  };
-  Tile S[2][kTiles];
-  const bool passes = len == 0 || delta_passes(a, s, len - 1);
-  each([&](uint32_t i, uint32_t j, uint32_t e, uint32_t d, uint32_t c) {
-    S[i][j][e] = b.dh_last && passes && d < a.Dk && c0 + c < a.Dv ? b.dh_last[state + (uint64_t)d * a.Dv + c0 + c] : 0.0f;
-  });
-  const uint32_t hk = h / a.share;
-  for (uint32_t piece = a.pieces; piece-- > 0;) {
-    const uint32_t t0 = piece * kPiece, steps = min(kPiece, a.T - t0);
-    T *const dv = static_cast<T *>(b.dv) + s * b.dv_seq + t0 * b.dv_time + (uint64_t)h * a.Dv + c0;
-    if (t0 >= len) {
-      for (uint32_t i = threadIdx.x; i < steps * kColumns; i += kDeltaThreads)
-        if (c0 + i % kColumns < a.Dv) dv[i / kColumns * b.dv_time + i % kColumns] = (T)0.0f;
-      continue;
-    }
-    __syncthreads();
-    load_rows(x.K, row, depth, static_cast<const T *>(a.k) + s * a.k_seq + t0 * a.k_time + (uint64_t)hk * a.Dk, a.k_time, len - t0, a.Dk, kDeltaThreads);
-    load_rows(x.Q, row, depth, static_cast<const T *>(a.q) + s * a.q_seq + t0 * a.q_time + (uint64_t)hk * a.Dk, a.q_time, len - t0, a.Dk, kDeltaThreads);
-    load_rows(x.X, kRow, kColumns, static_cast<const T *>(b.d_o) + (((uint64_t)s * a.T + t0) * a.H + h) * a.Dv + c0, (uint64_t)a.H * a.Dv, len - t0,
-              a.Dv - c0, kDeltaThreads);
-    load_piece_matrix(x.M, a.M + (((uint64_t)s * a.pieces + piece) * a.H + h) * kPiece * kPiece);
-    if (wave == 0) load_gates(a, s, h, t0, len, x.gates);
-    each([&](uint32_t i, uint32_t j, uint32_t e, uint32_t d, uint32_t c) {
-      x.S[d * kRow + c] = S[i][j][e];
-      if (d < a.Dk && c0 + c < a.Dv)
-        b.dS[(((uint64_t)s * a.pieces + piece) * a.H + h) * a.Dk * a.Dv + (uint64_t)d * a.Dv + c0 + c] = S[i][j][e];
-    });
-    __syncthreads();
-    attend(x, depth, row);
-    __syncthreads();
-    Tile dU[kTiles];
-#pragma unroll
-    for (uint32_t j = 0; j < kTiles; ++j) {
-      const Tile of_o = product(Tile{}, kPiece, [&](uint32_t t) { return x.P[t * kPieceRow + r + col]; },
-                                [&](uint32_t t) { return x.X[t * kRow + j * 16 + col]; });
-      const Tile kS = product(Tile{}, depth, [&](uint32_t i) { return x.K[(r + col) * row + i]; },
-                              [&](uint32_t i) { return x.S[i * kRow + j * 16 + col]; });
-#pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) {
-        const uint32_t t = r + quad + e;
-        dU[j][e] = a.scale * of_o[e] + x.gates.end[t] * kS[e];
-        x.U[t * kRow + j * 16 + col] = x.gates.beta[t] * dU[j][e];
+      for (uint32_t i = 0; i < KS; ++i) {
+        const auto key = operand<T>(load_step<T>(k_rows, a.k_time, c * 16 + m, have, i * 32 + q * 8, a.Dk));
+        multiply<3>(kk, k_own[i], key);
+        multiply<3>(qk, q_own[i], key);
       }
     }
-    __syncthreads();
 #pragma unroll
-    for (uint32_t j = 0; j < kTiles; ++j) {
-      const Tile mU = product(Tile{}, kPiece, [&](uint32_t t) { return x.M[t * kPieceRow + r + col]; },
-                              [&](uint32_t t) { return x.U[t * kRow + j * 16 + col]; });
-#pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) dU[j][e] -= mU[e];  // Y
+    for (uint32_t e = 0; e < 4; ++e) {
+      const uint32_t t = wave * 16 + q * 4 + e, j = c * 16 + m;
+      const float d = j <= t ? decay(gates, t, j) : 0.0f;
+      L[t * kPieceRow + j] = j < t ? kk[e] * d : 0.0f;
+      P[t * kPieceRow + j] = j <= t ? qk[e] * d : 0.0f;
     }
-    __syncthreads();
+  }
+  __syncthreads();
+  // (1 + L diag(beta))^-1 of the four blocks on the diagonal: a lane has a column
+  if (wave == 0) {
+    float x[16];
 #pragma unroll
-    for (uint32_t j = 0; j < kTiles; ++j)
+    for (uint32_t t = 0; t < 16; ++t) {
+      x[t] = t == m ? 1.0f : 0.0f;
 #pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) {
-        const uint32_t t = r + quad + e, c = j * 16 + col;
-        const float of_v = x.gates.beta[t] * dU[j][e];
-        x.U[t * kRow + c] = x.gates.begin[t] * of_v;
-        if (t < steps && c0 + c < a.Dv) {
-          dv[t * b.dv_time + c] = t0 + t < len ? (T)of_v : (T)0.0f;
-          b.Y[(((uint64_t)s * a.T + t0 + t) * a.H + h) * a.Dv + c0 + c] = dU[j][e];
+      for (uint32_t i = 0; i < t; ++i) x[t] -= L[(q * 16 + t) * kPieceRow + q * 16 + i] * x[i];
+      inverse[q][t][m] = x[t];
+      x[t] *= gates.beta[q * 16 + t];  // (as the rows below take it)
+    }
+  }
+  __syncthreads();
+  // M, block row by block row: a wave has a column of blocks, in the layout that the next product takes
+  Tile M[4];
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) {
+    M[i] = Tile{};
+    if (i < wave) continue;
+    Tile x;
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) x[e] = L[(i * 16 + q * 4 + e) * kPieceRow + wave * 16 + m];
+#pragma unroll
+    for (uint32_t j = 0; j < i; ++j)
+      if (j >= wave) {
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) {
+          const uint32_t k = j * 16 + q * 4 + e;
+          x = __builtin_amdgcn_mfma_f32_16x16x4f32(-L[(i * 16 + m) * kPieceRow + k] * gates.beta[k], M[j][e], x, 0, 0, 0);
         }
       }
-    __syncthreads();
 #pragma unroll
-    for (uint32_t j = 0; j < kTiles; ++j)
-#pragma unroll
-      for (uint32_t i = 0; i < 2; ++i) {
-        const uint32_t d0 = (wave * 2 + i) * 16;
-        if (d0 >= depth) continue;
-        const Tile of_q = product(Tile{}, kPiece, [&](uint32_t t) { return x.Q[t * row + d0 + col]; },
-                                  [&](uint32_t t) { return x.X[t * kRow + j * 16 + col] * (a.scale * x.gates.begin[t]); });
-        const Tile of_k = product(Tile{}, kPiece, [&](uint32_t t) { return x.K[t * row + d0 + col]; },
-                                  [&](uint32_t t) { return x.U[t * kRow + j * 16 + col]; });
-        const Tile left = x.gates.episode[kPiece - 1] == 0 ? S[i][j] * x.gates.last : Tile{};
-        S[i][j] = of_q + left - of_k;
-      }
+    for (uint32_t e = 0; e < 4; ++e) M[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(inverse[i][m][q * 4 + e], x[e], M[i], 0, 0, 0);
   }
-  if (b.dh0)
-    each([&](uint32_t i, uint32_t j, uint32_t e, uint32_t d, uint32_t c) {
-      if (d < a.Dk && c0 + c < a.Dv) b.dh0[state + (uint64_t)d * a.Dv + c0 + c] = S[i][j][e];
-    });
+  __syncthreads();
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) L[(i * 16 + q * 4 + e) * kPieceRow + wave * 16 + m] = M[i][e];
+  __syncthreads();
+  const uint64_t head = blockIdx.x;
+  for (uint32_t i = threadIdx.x; i < 2 * kTriangle * kWave; i += kDeltaThreads) {
+    const uint32_t f = i / kWave % kTriangle, l = i % kWave;
+    const bool of_p = i / kWave >= kTriangle;
+    const float *const from = of_p ? P : L;
+    uint32_t r, ks;
+    triangle(f, kBack, &r, &ks);
+    const uint32_t row = tile_row(r, l % 16), col = ks * 32 + l / 16 * 8;
+    float x[8];
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) x[e] = kBack ? from[(col + e) * kPieceRow + row] : from[row * kPieceRow + col + e];
+    const Operand<3> parts = split<3>(x);
+    __bf16 *const to = (of_p ? w.P : w.M) + ((head * kTriangle + f) * 3) * kOperand + l * 8;
+#pragma unroll
+    for (uint32_t p = 0; p < 3; ++p) *reinterpret_cast<Parts8 *>(to + p * kOperand) = parts.part[p];
+  }
+  if (kBack)
+    for (uint32_t i = threadIdx.x; i < kPiece * kPiece; i += kDeltaThreads) w.whole[head * kPiece * kPiece + i] = L[i / kPiece * kPieceRow + i % kPiece];
+  if (threadIdx.x < kPiece) {
+    PieceGates &to = *reinterpret_cast<PieceGates *>(w.gates + head * kGateWords);
+    to.beta[threadIdx.x] = gates.beta[threadIdx.x], to.begin[threadIdx.x] = gates.begin[threadIdx.x], to.end[threadIdx.x] = gates.end[threadIdx.x];
+    if (threadIdx.x == 0) to.last = gates.last;
+  }
+  if (first) {
+    const uint64_t key_head = ((uint64_t)s * a.pieces + piece) * a.Hk + hk;
+    for (uint32_t i = threadIdx.x; i < (kBack ? 2 : 1) * 2 * KS * 2 * kWave; i += kDeltaThreads) {
+      const uint32_t l = i % kWave, ks = i / kWave % 2, tile = i / kWave / 2 % (2 * KS), which = i / kWave / 2 / (2 * KS);
+      const uint32_t d = tile_row(tile, l % 16), t = ks * 32 + l / 16 * 8;
+      Run<T, 8> x;
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e) x[e] = raw[which][t + e][d];
+      T *const to = static_cast<T *>(which ? w.Qt : w.Kt) + ((key_head * 2 * KS + tile) * 2 + ks) * kOperand + l * 8;
+      *reinterpret_cast<Run<T, 8> *>(to) = x;
+    }
+  }
+}
+
+// ---- from piece to piece.  A workgroup of two waves has 16 columns of a state, all its rows, and a wave's products need nothing
+// but what the wave has itself and left operands from memory: no barrier within a piece.  One wave carries the state on, the other
+// does what nobody waits for, a piece behind (outputs) or ahead (what the gradient of the state takes in from outside).
+// Workgroups of a head, which read the same operands, are 8 apart: on one chiplet, whose L2 cache they share.
+struct PiecePlace {
+  uint32_t s, h, c0;
+  bool none;
+};
+__device__ __forceinline__ PiecePlace piece_place(const DeltaArgs &a)
+{
+  const uint32_t slices = (a.Dv + 15) / 16, heads = a.S * a.H;
+  const uint32_t head = blockIdx.x / (8 * slices) * 8 + blockIdx.x % 8;
+  return PiecePlace{head / a.H, head % a.H, blockIdx.x / 8 % slices * 16, head >= heads};
+}
+
+// Both waves have arrived, and what they wrote to LDS is there.  Loads from memory stay on their way.
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <uint32_t N>
+__device__ __forceinline__ void put(__bf16 *to, const Operand<N> &x)
+{
+#pragma unroll
+  for (uint32_t p = 0; p < N; ++p) *reinterpret_cast<Parts8 *>(to + p * kOperand + lane_id() * 8) = x.part[p];
+}
+template <uint32_t N>
+__device__ __forceinline__ Operand<N> get(const __bf16 *from)
+{
+  Operand<N> x;
+#pragma unroll
+  for (uint32_t p = 0; p < N; ++p) x.part[p] = *reinterpret_cast<const Parts8 *>(from + p * kOperand + lane_id() * 8);
+  return x;
+}
+
+// The gates of the rows of a lane's part of a tile of steps.
+struct RowGates {
+  Tile tile[4];
+};
+__device__ __forceinline__ RowGates row_gates(const float *gates)
+{
+  RowGates r;
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) r.tile[i] = *reinterpret_cast<const Tile *>(gates + i / 2 * 32 + lane_id() / 16 * 8 + i % 2 * 4);
+  return r;
+}
+
+__device__ __forceinline__ Tile scaled(const Tile &x, const Tile &by)
+{
+  Tile r;
+#pragma unroll
+  for (uint32_t e = 0; e < 4; ++e) r[e] = x[e] * by[e];
+  return r;
+}
+// by x, or 0 where by is, whatever x is: nothing of what has ended passes.
+__device__ __forceinline__ Tile passed(const Tile &x, const Tile &by)
+{
+  Tile r;
+#pragma unroll
+  for (uint32_t e = 0; e < 4; ++e) r[e] = by[e] != 0.0f ? x[e] * by[e] : 0.0f;
+  return r;
+}
+__device__ __forceinline__ Tile passed(const Tile &x, float by) { return passed(x, Tile{by, by, by, by}); }
+
+// A lane's numbers of a tile of steps: rows of a strided array, this lane's column; zeros where there is none.
+template <typename T>
+__device__ __forceinline__ void load_tiles(Tile (&x)[4], const T *piece, uint64_t stride, uint32_t have, bool column)
+{
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) {
+      const uint32_t t = tile_row(i, lane_id() / 16 * 4 + e);
+      const float v = column ? (float)piece[min(t, have - 1) * stride] : 0.0f;
+      x[i][e] = t < have ? v : 0.0f;
+    }
+}
+
+template <typename T, uint32_t KS>
+struct PieceKeys {  // rows of keys or queries as left operands
+  Operand<kPartsOf<T>> x[4][KS];
+  __device__ __forceinline__ void load(const T *piece, uint64_t stride, uint32_t have, uint32_t width)
+  {
+    const uint32_t lane = lane_id();
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+      for (uint32_t s = 0; s < KS; ++s) x[i][s] = operand<T>(load_step<T>(piece, stride, tile_row(i, lane % 16), have, s * 32 + lane / 16 * 8, width));
+  }
+};
+template <typename T, uint32_t KS>
+struct PieceColumns {  // their transposes, prepared
+  Operand<kPartsOf<T>> x[2 * KS][2];
+  __device__ __forceinline__ void load(const void *from, uint64_t key_head)
+  {
+    const T *const p = static_cast<const T *>(from) + key_head * (2 * KS * 2 * kOperand) + lane_id() * 8;
+#pragma unroll
+    for (uint32_t i = 0; i < 2 * KS; ++i)
+#pragma unroll
+      for (uint32_t s = 0; s < 2; ++s) x[i][s] = operand<T>(*reinterpret_cast<const Run<T, 8> *>(p + (i * 2 + s) * kOperand));
+  }
+};
+template <uint32_t N>
+struct PieceTriangle {
+  Operand<N> x[kTriangle];
+  __device__ __forceinline__ void load(const __bf16 *from, uint64_t head)
+  {
+    const __bf16 *const p = from + head * (kTriangle * 3 * kOperand) + lane_id() * 8;
+#pragma unroll
+    for (uint32_t f = 0; f < kTriangle; ++f)
+#pragma unroll
+      for (uint32_t n = 0; n < N; ++n) x[f].part[n] = *reinterpret_cast<const Parts8 *>(p + (f * 3 + n) * kOperand);
+  }
+  // acc + the matrix times right, whose operands are its rows 0..31 and 32..63
+  template <uint32_t kLimit, bool kUpper, uint32_t NB>
+  __device__ __forceinline__ void times(Tile (&acc)[4], const Operand<NB> (&right)[2]) const
+  {
+#pragma unroll
+    for (uint32_t f = 0; f < kTriangle; ++f) {
+      const uint32_t r = kUpper ? (f < 4 ? f / 2 : f - 2) : (f < 2 ? f : 2 + (f - 2) / 2);
+      const uint32_t s = kUpper ? (f < 4 ? f % 2 : 1) : (f < 2 ? 0 : (f - 2) % 2);
+      multiply<kLimit>(acc[r], x[f], right[s]);
+    }
+  }
+};
+
+// A state's tile i, element e of a lane is its row.
+__device__ __forceinline__ uint32_t state_row(uint32_t tile, uint32_t e) { return tile_row(tile, lane_id() / 16 * 4 + e); }
+
+template <uint32_t KS>
+__device__ __forceinline__ void load_state(Tile (&S)[2 * KS], const float *from, uint32_t Dk, uint32_t Dv, bool column)
+{
+#pragma unroll
+  for (uint32_t i = 0; i < 2 * KS; ++i)
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) {
+      const uint32_t d = state_row(i, e);
+      S[i][e] = from && column && d < Dk ? from[(uint64_t)d * Dv] : 0.0f;
+    }
+}
+template <uint32_t KS>
+__device__ __forceinline__ void store_state(const Tile (&S)[2 * KS], float *to, uint32_t Dk, uint32_t Dv, bool column)
+{
+#pragma unroll
+  for (uint32_t i = 0; i < 2 * KS; ++i)
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) {
+      const uint32_t d = state_row(i, e);
+      if (column && d < Dk) to[(uint64_t)d * Dv] = S[i][e];
+    }
+}
+// A state of which the three parts are held: their sum is exact.
+template <uint32_t KS>
+__device__ __forceinline__ void store_parts(const Operand<3> (&S)[KS], float *to, uint32_t Dk, uint32_t Dv, bool column)
+{
+  Tile x[2 * KS];
+#pragma unroll
+  for (uint32_t s = 0; s < KS; ++s)
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) x[2 * s + e / 4][e % 4] = ((float)S[s].part[2][e] + (float)S[s].part[1][e]) + (float)S[s].part[0][e];
+  store_state<KS>(x, to, Dk, Dv, column);
+}
+
+// Two waves on a SIMD's registers each: left operands of the next piece are on their way while this one is computed.
+template <typename T, uint32_t KS>
+__global__ __launch_bounds__(2 * kWave) void delta_pieces_kernel(DeltaForward f, Prepared w)
+{
+  // outputs of 8 bits are computed from two parts of what they are sums of: 2^-16 of it, where they are rounded to 2^-9
+  constexpr uint32_t kOut = std::is_same<T, __bf16>::value ? 2 : 3;
+  __shared__ __align__(16) __bf16 states[2][KS][3 * kOperand], corrections[2][2][kOut * kOperand];
+  const DeltaArgs &a = f.n;
+  const PiecePlace place = piece_place(a);
+  if (place.none) return;
+  const uint32_t s = place.s, h = place.h, hk = h / a.share, lane = lane_id(), c = place.c0 + lane % 16;
+  const bool column = c < a.Dv, carries = threadIdx.x < kWave;
+  const uint32_t len = delta_length(a, s), pieces = (len + kPiece - 1) / kPiece;
+  const uint64_t state = ((uint64_t)s * a.H + h) * a.Dk * a.Dv + c;
+  const auto head_of = [&](uint32_t piece) { return ((uint64_t)s * a.pieces + piece) * a.H + h; };
+  const auto have_of = [&](uint32_t piece) { return min(kPiece, len - piece * kPiece); };
+  if (carries) {
+    const T *const k_rows = static_cast<const T *>(a.k) + s * a.k_seq + (uint64_t)hk * a.Dk, *const v_rows = static_cast<const T *>(a.v) + s * a.v_seq + (uint64_t)h * a.Dv + c;
+    Tile S[2 * KS];
+    load_state<KS>(S, f.h0 ? f.h0 + state : nullptr, a.Dk, a.Dv, column);
+    for (uint32_t piece = 0; piece < pieces; ++piece) {
+      const uint64_t head = head_of(piece);
+      const uint32_t have = have_of(piece);
+      const float *const gates = w.gates + head * kGateWords;
+      const RowGates beta = row_gates(gates), begin = row_gates(gates + kPiece), end = row_gates(gates + 2 * kPiece);
+      const float last = gates[3 * kPiece];
+      PieceKeys<T, KS> K;
+      K.load(k_rows + (uint64_t)piece * kPiece * a.k_time, a.k_time, have, a.Dk);
+      Tile X[4];
+      load_tiles(X, v_rows + (uint64_t)piece * kPiece * a.v_time, a.v_time, have, column);
+      PieceTriangle<3> M;
+      M.load(w.M, head);
+      PieceColumns<T, KS> Kt;
+      Kt.load(w.Kt, ((uint64_t)s * a.pieces + piece) * a.Hk + hk);
+      Tile kS[4] = {};
+#pragma unroll
+      for (uint32_t i = 0; i < KS; ++i) {
+        const Operand<3> parts = operand_of<3>(S[2 * i], S[2 * i + 1]);
+        put(states[piece % 2][i], parts);
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r) multiply<3>(kS[r], K.x[r][i], parts);
+      }
+#pragma unroll
+      for (uint32_t r = 0; r < 4; ++r) X[r] -= passed(kS[r], begin.tile[r]);
+      const Operand<3> bX[2] = {operand_of<3>(scaled(X[0], beta.tile[0]), scaled(X[1], beta.tile[1])),
+                                operand_of<3>(scaled(X[2], beta.tile[2]), scaled(X[3], beta.tile[3]))};
+      Tile mX[4] = {}, U[4];
+      M.template times<3, false>(mX, bX);
+#pragma unroll
+      for (uint32_t r = 0; r < 4; ++r) U[r] = scaled(X[r] - mX[r], beta.tile[r]);
+#pragma unroll
+      for (uint32_t i = 0; i < 2; ++i) put(corrections[piece % 2][i], operand_of<kOut>(U[2 * i], U[2 * i + 1]));
+      const Operand<3> left[2] = {operand_of<3>(scaled(U[0], end.tile[0]), scaled(U[1], end.tile[1])),
+                                  operand_of<3>(scaled(U[2], end.tile[2]), scaled(U[3], end.tile[3]))};
+#pragma unroll
+      for (uint32_t i = 0; i < 2 * KS; ++i) {
+        S[i] = passed(S[i], last);
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) multiply<3>(S[i], Kt.x[i][j], left[j]);
+      }
+      meet();
+    }
+    if (f.h_last) {
+      if (len && !delta_passes(a, s, len - 1)) {
+#pragma unroll
+        for (uint32_t i = 0; i < 2 * KS; ++i) S[i] = Tile{};
+      }
+      store_state<KS>(S, f.h_last + state, a.Dk, a.Dv, column);
+    }
+  } else {
+    const T *const q_rows = static_cast<const T *>(a.q) + s * a.q_seq + (uint64_t)hk * a.Dk;
+    T *const o = static_cast<T *>(f.o) + ((uint64_t)s * a.T * a.H + h) * a.Dv + c;
+    const uint64_t o_row = (uint64_t)a.H * a.Dv;
+    for (uint32_t piece = 0; piece < pieces; ++piece) {
+      const uint64_t head = head_of(piece);
+      const uint32_t have = have_of(piece);
+      PieceKeys<T, KS> Q;
+      Q.load(q_rows + (uint64_t)piece * kPiece * a.q_time, a.q_time, have, a.Dk);
+      PieceTriangle<kOut> P;
+      P.load(w.P, head);
+      const RowGates begin = row_gates(w.gates + head * kGateWords + kPiece);
+      meet();
+      Tile O[4] = {};
+      Operand<3> S[KS];
+#pragma unroll
+      for (uint32_t i = 0; i < KS; ++i) {
+        S[i] = get<3>(states[piece % 2][i]);
+        Operand<kOut> used;
+#pragma unroll
+        for (uint32_t p = 0; p < kOut; ++p) used.part[p] = S[i].part[p];
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r) multiply<kOut>(O[r], Q.x[r][i], used);
+      }
+      if (f.carry) store_parts<KS>(S, f.carry + head * a.Dk * a.Dv + c, a.Dk, a.Dv, column);
+#pragma unroll
+      for (uint32_t r = 0; r < 4; ++r) O[r] = passed(O[r], begin.tile[r]);
+      const Operand<kOut> U[2] = {get<kOut>(corrections[piece % 2][0]), get<kOut>(corrections[piece % 2][1])};
+      P.template times<kOut, false>(O, U);
+      if (column) {
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r)
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e) {
+            const uint32_t t = state_row(r, e);
+            if (t < have) o[(piece * kPiece + t) * o_row] = (T)(a.scale * O[r][e]);
+          }
+      }
+    }
+    if (column)
+      for (uint64_t t = len + lane / 16; t < a.T; t += 4) o[t * o_row] = (T)0.0f;
+  }
+}
+
+// The same from the last piece to the first, with dS.  The first wave carries it, the second brings P^T dO and Q^T (c dO) and
+// stores dS, Y and dV.
+template <typename T, uint32_t KS>
+__global__ __launch_bounds__(2 * kWave) void delta_pieces_back_kernel(DeltaBack b, Prepared w)
+{
+  struct Brought {
+    Tile o[4][kWave], state[2 * KS][kWave];
+  };
+  __shared__ Brought brought[2];
+  __shared__ __align__(16) __bf16 states[2][KS][3 * kOperand];
+  __shared__ Tile found[2][4][kWave];  // Y
+  const DeltaArgs &a = b.n;
+  const PiecePlace place = piece_place(a);
+  if (place.none) return;
+  const uint32_t s = place.s, h = place.h, hk = h / a.share, lane = lane_id(), c = place.c0 + lane % 16;
+  const bool column = c < a.Dv, carries = threadIdx.x < kWave;
+  const uint32_t len = delta_length(a, s), pieces = (len + kPiece - 1) / kPiece;
+  const uint64_t state = ((uint64_t)s * a.H + h) * a.Dk * a.Dv + c;
+  const auto head_of = [&](uint32_t piece) { return ((uint64_t)s * a.pieces + piece) * a.H + h; };
+  const auto key_head_of = [&](uint32_t piece) { return ((uint64_t)s * a.pieces + piece) * a.Hk + hk; };
+  const auto have_of = [&](uint32_t piece) { return min(kPiece, len - piece * kPiece); };
+  if (carries) {
+    const T *const k_rows = static_cast<const T *>(a.k) + s * a.k_seq + (uint64_t)hk * a.Dk;
+    Tile S[2 * KS];
+    const bool passes = len == 0 || delta_passes(a, s, len - 1);
+    load_state<KS>(S, b.dh_last && passes ? b.dh_last + state : nullptr, a.Dk, a.Dv, column);
+    if (pieces) meet();
+    for (uint32_t piece = pieces; piece-- > 0;) {
+      const uint64_t head = head_of(piece);
+      const float *const gates = w.gates + head * kGateWords;
+      const RowGates beta = row_gates(gates), begin = row_gates(gates + kPiece), end = row_gates(gates + 2 * kPiece);
+      const float last = gates[3 * kPiece];
+      PieceKeys<T, KS> K;
+      K.load(k_rows + (uint64_t)piece * kPiece * a.k_time, a.k_time, have_of(piece), a.Dk);
+      PieceTriangle<3> M;
+      M.load(w.M, head);
+      PieceColumns<T, KS> Kt;
+      Kt.load(w.Kt, key_head_of(piece));
+      Tile kS[4] = {};
+#pragma unroll
+      for (uint32_t i = 0; i < KS; ++i) {
+        const Operand<3> parts = operand_of<3>(S[2 * i], S[2 * i + 1]);
+        put(states[piece % 2][i], parts);
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r) multiply<3>(kS[r], K.x[r][i], parts);
+      }
+      Tile dU[4];
+#pragma unroll
+      for (uint32_t r = 0; r < 4; ++r) dU[r] = brought[piece % 2].o[r][lane] + scaled(kS[r], end.tile[r]);
+      const Operand<3> bU[2] = {operand_of<3>(scaled(dU[0], beta.tile[0]), scaled(dU[1], beta.tile[1])),
+                                operand_of<3>(scaled(dU[2], beta.tile[2]), scaled(dU[3], beta.tile[3]))};
+      Tile mU[4] = {}, V[4];
+      M.template times<3, true>(mU, bU);
+#pragma unroll
+      for (uint32_t r = 0; r < 4; ++r) {
+        dU[r] -= mU[r];  // Y
+        found[piece % 2][r][lane] = dU[r];
+        V[r] = -scaled(scaled(dU[r], beta.tile[r]), begin.tile[r]);
+      }
+      const Operand<3> left[2] = {operand_of<3>(V[0], V[1]), operand_of<3>(V[2], V[3])};
+#pragma unroll
+      for (uint32_t i = 0; i < 2 * KS; ++i) {
+        S[i] = passed(S[i], last) + brought[piece % 2].state[i][lane];
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) multiply<3>(S[i], Kt.x[i][j], left[j]);
+      }
+      meet();
+    }
+    if (b.dh0) store_state<KS>(S, b.dh0 + state, a.Dk, a.Dv, column);
+  } else {
+    const uint64_t o_row = (uint64_t)a.H * a.Dv;
+    const T *const d_o = static_cast<const T *>(b.d_o) + ((uint64_t)s * a.T * a.H + h) * a.Dv + c;
+    float *const Y = b.Y + ((uint64_t)s * a.T * a.H + h) * a.Dv + c;
+    T *const dv = static_cast<T *>(b.dv) + s * b.dv_seq + (uint64_t)h * a.Dv + c;
+    const auto bring = [&](uint32_t piece) {
+      const uint64_t head = head_of(piece);
+      const uint32_t have = have_of(piece);
+      Tile dO[4];
+      load_tiles(dO, d_o + (uint64_t)piece * kPiece * o_row, o_row, have, column);
+      PieceTriangle<3> P;
+      P.load(w.P, head);
+      PieceColumns<T, KS> Qt;
+      Qt.load(w.Qt, key_head_of(piece));
+      const RowGates begin = row_gates(w.gates + head * kGateWords + kPiece);
+      const Operand<kPartsOf<T>> right[2] = {operand_of<kPartsOf<T>>(dO[0], dO[1]), operand_of<kPartsOf<T>>(dO[2], dO[3])};
+      Tile of_o[4] = {};
+      P.template times<3, true>(of_o, right);
+#pragma unroll
+      for (uint32_t r = 0; r < 4; ++r) {
+        brought[piece % 2].o[r][lane] = a.scale * of_o[r];
+        dO[r] = scaled(a.scale * dO[r], begin.tile[r]);
+      }
+      const Operand<3> left[2] = {operand_of<3>(dO[0], dO[1]), operand_of<3>(dO[2], dO[3])};
+#pragma unroll
+      for (uint32_t i = 0; i < 2 * KS; ++i) {
+        Tile x{};
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) multiply<3>(x, Qt.x[i][j], left[j]);
+        brought[piece % 2].state[i][lane] = x;
+      }
+    };
+    const auto store = [&](uint32_t piece) {
+      const uint64_t head = head_of(piece);
+      const uint32_t have = have_of(piece);
+      Operand<3> S[KS];
+#pragma unroll
+      for (uint32_t i = 0; i < KS; ++i) S[i] = get<3>(states[piece % 2][i]);
+      store_parts<KS>(S, b.dS + head * a.Dk * a.Dv + c, a.Dk, a.Dv, column);
+      const RowGates beta = row_gates(w.gates + head * kGateWords);
+#pragma unroll
+      for (uint32_t r = 0; r < 4; ++r) {
+        const Tile y = found[piece % 2][r][lane];
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) {
+          const uint32_t t = state_row(r, e);
+          if (column && t < have) {
+            Y[(piece * kPiece + t) * o_row] = y[e];
+            dv[(uint64_t)(piece * kPiece + t) * b.dv_time] = (T)(beta.tile[r][e] * y[e]);
+          }
+        }
+      }
+    };
+    if (pieces) {
+      bring(pieces - 1);
+      meet();
+      for (uint32_t piece = pieces; piece-- > 0;) {
+        if (piece) bring(piece - 1);
+        if (piece + 1 < pieces) store(piece + 1);
+        meet();
+      }
+      store(0);
+    }
+    if (column)
+      for (uint64_t t = len + lane / 16; t < a.T; t += 4) dv[t * b.dv_time] = (T)0.0f;
+  }
 }
 
 // What is left of the gradient, a workgroup per piece and key head: eight waves, of which wave w has rows 16 (w % 4) of what
@@ -486,7 +863,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
     const uint64_t piece_head = ((uint64_t)s * a.pieces + piece) * a.H + h;
     if (wave == 0) load_gates(a, s, h, t0, len, x.gates);
     for (uint32_t i = threadIdx.x; i < kPiece * kPiece; i += kGradThreads)
-      x.M[i / kPiece * kPieceRow + i % kPiece] = a.M[piece_head * kPiece * kPiece + i];
+      x.M[i / kPiece * kPieceRow + i % kPiece] = b.M[piece_head * kPiece * kPiece + i];
     Tile dq_h[kMaxTiles] = {}, B[2] = {}, C[2] = {};  // B and C: columns 16 (2 half + i)
     float of_v[4] = {}, of_beta[4] = {};
     double at_end = 0.0;
@@ -759,20 +1136,18 @@ namespace {
 
 constexpr uint32_t kDeltaSteps = 16;  // sequences of at most so many steps are computed step by step
 
-uint32_t delta_columns(uint32_t S, uint32_t H, uint32_t Dv) { return (uint64_t)S * H * blocks_for(Dv, 32) >= kChipCus ? 32 : 16; }
-
-// f(integral_constant<uint32_t>): the columns of a state that a workgroup takes.
+// f(integral_constant<uint32_t>): the width of keys and queries, in 32.
 template <typename F>
-void with_columns(uint32_t columns, F f)
+void with_width(uint32_t Dk, F f)
 {
-  if (columns == 32)
-    f(std::integral_constant<uint32_t, 32>());
+  if (Dk > 64)
+    f(std::integral_constant<uint32_t, 4>());
   else
-    f(std::integral_constant<uint32_t, 16>());
+    f(std::integral_constant<uint32_t, 2>());
 }
 
 struct DeltaBytes {
-  uint64_t M, dS, Y, bytes;
+  uint64_t gates, M, P, Kt, Qt, whole, dS, Y, bytes;
 };
 
 int delta_sizes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, bool backward, DeltaBytes *n)
@@ -782,18 +1157,36 @@ int delta_sizes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, bo
   // workgroups of 512 threads, fewer than 2^32 threads in all
   uint64_t heads;
   if (__builtin_mul_overflow((uint64_t)S * blocks_for(T, kPiece), (uint64_t)H, &heads) || heads >= 1u << 23) return APEX_ERR_TOO_LARGE;
-  n->M = n->dS = n->Y = 0;
-  uint64_t at = 0;
-  if (backward || T > kDeltaSteps) at = heads * kPiece * kPiece * 4;
+  *n = DeltaBytes{};
+  if (!backward && T <= kDeltaSteps) return APEX_OK;
+  const auto take = [&](uint64_t bytes) {
+    const uint64_t at = n->bytes;
+    n->bytes += round_up(bytes, 256);
+    return at;
+  };
+  const uint64_t columns = heads * (Dk > 64 ? 8 : 4) * 2 * kOperand * 4;  // (for the widest type, and every head with a key of its own)
+  n->gates = take(heads * kGateWords * 4);
+  n->M = take(heads * kTriangle * 3 * kOperand * 2);
+  n->P = take(heads * kTriangle * 3 * kOperand * 2);
+  n->Kt = take(columns);
   if (backward) {
-    n->dS = at;
-    at += round_up(heads * Dk * Dv * 4, 256);
-    n->Y = at;
-    at += round_up((uint64_t)S * T * H * Dv * 4, 256);
+    n->Qt = take(columns);
+    n->whole = take(heads * kPiece * kPiece * 4);
+    n->dS = take(heads * Dk * Dv * 4);
+    n->Y = take((uint64_t)S * T * H * Dv * 4);
   }
-  n->bytes = at;
   return APEX_OK;
 }
+
+Prepared delta_prepared(const DeltaBytes &n, void *workspace)
+{
+  char *const p = static_cast<char *>(workspace);
+  return Prepared{reinterpret_cast<float *>(p + n.gates), reinterpret_cast<__bf16 *>(p + n.M), reinterpret_cast<__bf16 *>(p + n.P), p + n.Kt, p + n.Qt,
+                  reinterpret_cast<float *>(p + n.whole)};
+}
+
+// Workgroups of the kernels that go from piece to piece: eight heads' slices of 16 columns at a time.
+uint32_t delta_slices(uint32_t S, uint32_t H, uint32_t Dv) { return blocks_for((uint64_t)S * H, 8) * 8 * blocks_for(Dv, 16); }
 
 int delta_check(const DeltaArgs &a, int dtype)
 {
@@ -828,7 +1221,7 @@ int apex_delta_rule(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, uint32_t Dk
   DeltaBytes n;
   if (const int rc = delta_sizes(S, T, H, Dk, Dv, false, &n)) return rc;
   DeltaForward f{{S, T, Hk, H, Dk, Dv, blocks_for(T, kPiece), Hk ? H / Hk : 0, q_seq_stride, q_time_stride, k_seq_stride, k_time_stride,
-                  v_seq_stride, v_time_stride, q, k, v, g, beta, scale, discount, length, static_cast<float *>(workspace)},
+                  v_seq_stride, v_time_stride, q, k, v, g, beta, scale, discount, length},
                  h0, o, h_last, carry};
   if (const int rc = delta_check(f.n, dtype)) return rc;
   if (!o || (uintptr_t)o % element_size(dtype) || ((uintptr_t)h0 | (uintptr_t)h_last | (uintptr_t)carry) % 4 ||
@@ -842,13 +1235,13 @@ int apex_delta_rule(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, uint32_t Dk
     APEX_HIP(hipGetLastError());
     return APEX_OK;
   }
-  const uint32_t columns = delta_columns(S, H, Dv);
+  const Prepared w = delta_prepared(n, workspace);
   with_type(dtype, [&](auto t) {
     typedef decltype(t) E;
-    delta_solve_kernel<E><<<dim3(S * f.n.pieces * H), dim3(kDeltaThreads), 0, stream>>>(f.n);
-    with_columns(columns, [&](auto c) {
-      constexpr uint32_t kC = decltype(c)::value;
-      delta_pieces_kernel<E, kC><<<dim3(S * H * blocks_for(Dv, kC)), dim3(kDeltaThreads), 0, stream>>>(f);
+    with_width(Dk, [&](auto width) {
+      constexpr uint32_t KS = decltype(width)::value;
+      delta_prepare_kernel<E, KS, false><<<dim3(S * f.n.pieces * H), dim3(kDeltaThreads), 0, stream>>>(f.n, w);
+      delta_pieces_kernel<E, KS><<<dim3(delta_slices(S, H, Dv)), dim3(2 * kWave), 0, stream>>>(f, w);
     });
   });
   APEX_HIP(hipGetLastError());
@@ -867,9 +1260,9 @@ int apex_delta_rule_backward(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, ui
   if (const int rc = delta_sizes(S, T, H, Dk, Dv, true, &n)) return rc;
   char *const space = static_cast<char *>(workspace);
   DeltaBack b{{S, T, Hk, H, Dk, Dv, blocks_for(T, kPiece), Hk ? H / Hk : 0, q_seq_stride, q_time_stride, k_seq_stride, k_time_stride,
-               v_seq_stride, v_time_stride, q, k, v, g, beta, scale, discount, length, reinterpret_cast<float *>(space)},
+               v_seq_stride, v_time_stride, q, k, v, g, beta, scale, discount, length},
               carry, d_o, dh_last, dq_seq_stride, dq_time_stride, dk_seq_stride, dk_time_stride, dv_seq_stride, dv_time_stride, dq, dk, dv, dg,
-              dbeta, dh0, reinterpret_cast<float *>(space + n.dS), reinterpret_cast<float *>(space + n.Y)};
+              dbeta, dh0, reinterpret_cast<const float *>(space + n.whole), reinterpret_cast<float *>(space + n.dS), reinterpret_cast<float *>(space + n.Y)};
   if (const int rc = delta_check(b.n, dtype)) return rc;
   const uint32_t size = element_size(dtype);
   if (!carry || !d_o || !dg || !dbeta || !workspace || (uintptr_t)workspace % 256 || (uintptr_t)d_o % size ||
@@ -879,13 +1272,13 @@ int apex_delta_rule_backward(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, ui
       !rows_apart(dv, size, S, dv_seq_stride, T, dv_time_stride, (uint64_t)H * Dv))
     return APEX_ERR_INVALID_ARG;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const uint32_t columns = delta_columns(S, H, Dv);
+  const Prepared w = delta_prepared(n, workspace);
   with_type(dtype, [&](auto t) {
     typedef decltype(t) E;
-    delta_solve_kernel<E><<<dim3(S * b.n.pieces * H), dim3(kDeltaThreads), 0, stream>>>(b.n);
-    with_columns(columns, [&](auto c) {
-      constexpr uint32_t kC = decltype(c)::value;
-      delta_pieces_back_kernel<E, kC><<<dim3(S * H * blocks_for(Dv, kC)), dim3(kDeltaThreads), 0, stream>>>(b);
+    with_width(Dk, [&](auto width) {
+      constexpr uint32_t KS = decltype(width)::value;
+      delta_prepare_kernel<E, KS, true><<<dim3(S * b.n.pieces * H), dim3(kDeltaThreads), 0, stream>>>(b.n, w);
+      delta_pieces_back_kernel<E, KS><<<dim3(delta_slices(S, H, Dv)), dim3(2 * kWave), 0, stream>>>(b, w);
     });
     delta_gradients_kernel<E><<<dim3(S * b.n.pieces * Hk), dim3(kGradThreads), 0, stream>>>(b);
   });
