@@ -56,7 +56,6 @@ struct DeltaBack {
   uint64_t dq_seq, dq_time, dk_seq, dk_time, dv_seq, dv_time;
   void *dq, *dk, *dv;
   float *dg, *dbeta, *dh0;
-  const float *M;  // [S][pieces][H][64][64]
   float *dS;  // [S][pieces][H][Dk][Dv]: of the state behind a piece
   float *Y;   // [S][T][H][Dv]
 };
@@ -113,30 +112,6 @@ __device__ __forceinline__ void load_gates(const DeltaArgs &a, uint32_t s, uint3
 __device__ __forceinline__ float decay(const Gates &x, uint32_t t, uint32_t i)
 {
   return x.episode[t] == x.episode[i] ? exp2_of((float)(x.G[t] - x.G[i])) : 0.0f;
-}
-
-// acc + A B over `depth` (a multiple of 16): a(k) of row lane % 16, b(k) of column lane % 16.
-template <typename A, typename B>
-__device__ __forceinline__ Tile product(Tile acc, uint32_t depth, A a, B b)
-{
-  const uint32_t k0 = lane_id() / 16;
-  for (uint32_t k = 0; k < depth; k += 16)
-#pragma unroll
-    for (uint32_t i = 0; i < 16; i += 4) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a(k + i + k0), b(k + i + k0), acc, 0, 0, 0);
-  return acc;
-}
-
-__device__ __forceinline__ uint32_t up16(uint32_t n) { return (n + 15) / 16 * 16; }
-
-// Rows [0, 64) of one head, columns [c0, c0 + columns), of a strided array into LDS rows of `row` numbers; zeros beyond `have` rows and `width`.
-template <typename T>
-__device__ __forceinline__ void load_rows(float *to, uint32_t row, uint32_t columns, const T *from, uint64_t stride, uint32_t have,
-                                          uint32_t width, uint32_t threads)
-{
-  for (uint32_t i = threadIdx.x; i < kPiece * columns; i += threads) {
-    const uint32_t t = i / columns, d = i % columns;
-    to[t * row + d] = t < have && d < width ? (float)from[t * stride + d] : 0.0f;
-  }
 }
 
 // ---- products.  Matrix instructions take numbers of 8 bits (bf16), 16 times as many as of 32 bits, so a 32-bit number is the sum
@@ -216,18 +191,15 @@ __device__ __forceinline__ Operand<N> operand_of(const Tile &x, const Tile &y)
 // 64 lanes times 8 numbers, lane l has row l % 16 of the tile and numbers 8 (l / 16) .. + 7 of the 32.
 constexpr uint32_t kOperand = 64 * 8;                         // numbers
 constexpr uint32_t kTriangle = 6;                             // operands of a triangular matrix: 4 tiles of rows by 2 of 32 steps, less 2
-constexpr uint32_t kGateWords = 256;
+constexpr uint32_t kGateWords = 512;
 
-struct PieceGates {  // of a piece and value head
-  float beta[kPiece], begin[kPiece], end[kPiece], last;
-};
-static_assert(sizeof(PieceGates) <= kGateWords * 4);
+static_assert(sizeof(Gates) <= kGateWords * 4);
 
 struct Prepared {
-  float *gates;      // [heads][kGateWords]
+  uint32_t *gates;   // [heads][kGateWords]: Gates
   __bf16 *M, *P;     // [heads][kTriangle][3][kOperand]
   void *Kt, *Qt;     // [key heads][2 KS][2][kOperand] of the inputs' type
-  float *whole;      // [heads][64][64]: M as it is (for the gradient)
+  __bf16 *rows;      // M beside its transpose (for the gradient)
 };
 
 // The operand of rows and columns of a triangular matrix: f -> (tile of rows, 32 steps).
@@ -239,33 +211,36 @@ __device__ __forceinline__ void triangle(uint32_t f, bool upper, uint32_t *r, ui
     *r = f < 2 ? f : 2 + (f - 2) / 2, *s = f < 2 ? 0 : (f - 2) % 2;
 }
 
-// Eight numbers of a row from `d` on, zeros beyond `width`; kWhole: there are none beyond.
+// Eight numbers of a row from `d` on, zeros beyond `width`: one by one, without a branch, so that many such loads are on their way
+// at once.
 template <typename T>
 __device__ __forceinline__ Run<T, 8> load_eight(const T *row, uint32_t d, uint32_t width)
 {
-  if (d + 8 <= width) return load_run<T, 8>(row + d);
-  Run<T, 8> r{};
+  Run<T, 8> r;
 #pragma unroll
-  for (uint32_t i = 0; i < 8; ++i)
-    if (d + i < width) r[i] = row[d + i];
+  for (uint32_t i = 0; i < 8; ++i) {
+    const T x = row[min(d + i, width - 1)];
+    r[i] = d + i < width ? x : (T)0.0f;
+  }
   return r;
 }
 
-// Row t of a piece's `have` steps; beyond them zeros, and the last one is fetched.
-template <typename T>
+// Row t of a piece's `have` steps; beyond them zeros, and the last one is fetched.  kWhole: eights end within the width.
+template <typename T, bool kWhole>
 __device__ __forceinline__ Run<T, 8> load_step(const T *piece, uint64_t stride, uint32_t t, uint32_t have, uint32_t d, uint32_t width)
 {
-  const Run<T, 8> r = load_eight<T>(piece + min(t, have - 1) * stride, d, width);
+  const T *const row = piece + min(t, have - 1) * stride;
+  const Run<T, 8> r = kWhole ? load_run<T, 8>(row + d) : load_eight<T>(row, d, width);
   return t < have ? r : Run<T, 8>{};
 }
 
 template <typename T, uint32_t KS, bool kBack>
 __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs a, Prepared w)
 {
-  constexpr uint32_t kRaw = KS * 32 + 2;
+  constexpr uint32_t kRaw = KS * 32 + 16 / sizeof(T);  // (rows begin on 16 bytes)
   __shared__ Gates gates;
   __shared__ float L[kPiece * kPieceRow], P[kPiece * kPieceRow], inverse[4][16][17];
-  __shared__ T raw[kBack ? 2 : 1][kPiece][kRaw];
+  __shared__ __align__(16) T raw[kBack ? 2 : 1][kPiece][kRaw];
   const uint32_t h = blockIdx.x % a.H, piece = blockIdx.x / a.H % a.pieces, s = blockIdx.x / a.H / a.pieces, hk = h / a.share;
   const uint32_t len = delta_length(a, s), t0 = piece * kPiece;
   if (t0 >= len) return;
@@ -274,30 +249,37 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
   const bool first = h % a.share == 0;  // of those that share a key head
   const T *const k_rows = static_cast<const T *>(a.k) + s * a.k_seq + t0 * a.k_time + (uint64_t)hk * a.Dk;
   const T *const q_rows = static_cast<const T *>(a.q) + s * a.q_seq + t0 * a.q_time + (uint64_t)hk * a.Dk;
-  Operand<kPartsOf<T>> k_own[KS], q_own[KS];
+  Run<T, 8> k_own[KS], q_own[KS];
+  const auto load_own = [&](auto whole) {
 #pragma unroll
-  for (uint32_t i = 0; i < KS; ++i) {
-    const uint32_t t = wave * 16 + m, d = i * 32 + q * 8;
-    const Run<T, 8> kr = load_step<T>(k_rows, a.k_time, t, have, d, a.Dk), qr = load_step<T>(q_rows, a.q_time, t, have, d, a.Dk);
-    k_own[i] = operand<T>(kr), q_own[i] = operand<T>(qr);
-    if (first) {
-#pragma unroll
-      for (uint32_t e = 0; e < 8; ++e) {
-        raw[0][t][d + e] = kr[e];
-        if (kBack) raw[kBack][t][d + e] = qr[e];
-      }
+    for (uint32_t i = 0; i < KS; ++i) {
+      k_own[i] = load_step<T, decltype(whole)::value>(k_rows, a.k_time, wave * 16 + m, have, i * 32 + q * 8, a.Dk);
+      q_own[i] = load_step<T, decltype(whole)::value>(q_rows, a.q_time, wave * 16 + m, have, i * 32 + q * 8, a.Dk);
     }
-  }
+  };
+  if (a.Dk == KS * 32)
+    load_own(std::true_type());
+  else
+    load_own(std::false_type());
   if (wave == 0) load_gates(a, s, h, t0, len, gates);
+#pragma unroll
+  for (uint32_t i = 0; i < KS; ++i)
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) {
+      raw[0][wave * 16 + m][i * 32 + q * 8 + e] = k_own[i][e];
+      if (kBack) raw[kBack][wave * 16 + m][i * 32 + q * 8 + e] = q_own[i][e];
+    }
   __syncthreads();
   for (uint32_t c = 0; c < 4; ++c) {
     Tile kk{}, qk{};
     if (c <= wave) {
 #pragma unroll
       for (uint32_t i = 0; i < KS; ++i) {
-        const auto key = operand<T>(load_step<T>(k_rows, a.k_time, c * 16 + m, have, i * 32 + q * 8, a.Dk));
-        multiply<3>(kk, k_own[i], key);
-        multiply<3>(qk, q_own[i], key);
+        Run<T, 8> key;
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) key[e] = raw[0][c * 16 + m][i * 32 + q * 8 + e];
+        multiply<3>(kk, operand<T>(k_own[i]), operand<T>(key));
+        multiply<3>(qk, operand<T>(q_own[i]), operand<T>(key));
       }
     }
 #pragma unroll
@@ -350,28 +332,22 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
     for (uint32_t e = 0; e < 4; ++e) L[(i * 16 + q * 4 + e) * kPieceRow + wave * 16 + m] = M[i][e];
   __syncthreads();
   const uint64_t head = blockIdx.x;
-  for (uint32_t i = threadIdx.x; i < 2 * kTriangle * kWave; i += kDeltaThreads) {
-    const uint32_t f = i / kWave % kTriangle, l = i % kWave;
-    const bool of_p = i / kWave >= kTriangle;
-    const float *const from = of_p ? P : L;
+  for (uint32_t i = threadIdx.x; i < (kBack ? 3 : 2) * kTriangle * kWave; i += kDeltaThreads) {
+    const uint32_t f = i / kWave % kTriangle, l = i % kWave, which = i / kWave / kTriangle;  // M, P, M beside its transpose
+    const float *const from = which == 1 ? P : L;
+    const bool turned = kBack && which < 2;
     uint32_t r, ks;
-    triangle(f, kBack, &r, &ks);
+    triangle(f, turned, &r, &ks);
     const uint32_t row = tile_row(r, l % 16), col = ks * 32 + l / 16 * 8;
     float x[8];
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) x[e] = kBack ? from[(col + e) * kPieceRow + row] : from[row * kPieceRow + col + e];
+    for (uint32_t e = 0; e < 8; ++e) x[e] = turned ? from[(col + e) * kPieceRow + row] : from[row * kPieceRow + col + e];
     const Operand<3> parts = split<3>(x);
-    __bf16 *const to = (of_p ? w.P : w.M) + ((head * kTriangle + f) * 3) * kOperand + l * 8;
+    __bf16 *const to = (which == 0 ? w.M : which == 1 ? w.P : w.rows) + ((head * kTriangle + f) * 3) * kOperand + l * 8;
 #pragma unroll
     for (uint32_t p = 0; p < 3; ++p) *reinterpret_cast<Parts8 *>(to + p * kOperand) = parts.part[p];
   }
-  if (kBack)
-    for (uint32_t i = threadIdx.x; i < kPiece * kPiece; i += kDeltaThreads) w.whole[head * kPiece * kPiece + i] = L[i / kPiece * kPieceRow + i % kPiece];
-  if (threadIdx.x < kPiece) {
-    PieceGates &to = *reinterpret_cast<PieceGates *>(w.gates + head * kGateWords);
-    to.beta[threadIdx.x] = gates.beta[threadIdx.x], to.begin[threadIdx.x] = gates.begin[threadIdx.x], to.end[threadIdx.x] = gates.end[threadIdx.x];
-    if (threadIdx.x == 0) to.last = gates.last;
-  }
+  for (uint32_t i = threadIdx.x; i < sizeof(Gates) / 4; i += kDeltaThreads) w.gates[head * kGateWords + i] = reinterpret_cast<const uint32_t *>(&gates)[i];
   if (first) {
     const uint64_t key_head = ((uint64_t)s * a.pieces + piece) * a.Hk + hk;
     for (uint32_t i = threadIdx.x; i < (kBack ? 2 : 1) * 2 * KS * 2 * kWave; i += kDeltaThreads) {
@@ -423,12 +399,22 @@ __device__ __forceinline__ Operand<N> get(const __bf16 *from)
 struct RowGates {
   Tile tile[4];
 };
+struct AllGates {
+  RowGates beta, begin, end;
+  float last;
+};
 __device__ __forceinline__ RowGates row_gates(const float *gates)
 {
   RowGates r;
 #pragma unroll
   for (uint32_t i = 0; i < 4; ++i) r.tile[i] = *reinterpret_cast<const Tile *>(gates + i / 2 * 32 + lane_id() / 16 * 8 + i % 2 * 4);
   return r;
+}
+
+__device__ __forceinline__ const Gates &gates_of(const Prepared &w, uint64_t head) { return *reinterpret_cast<const Gates *>(w.gates + head * kGateWords); }
+__device__ __forceinline__ AllGates all_gates(const Gates &gates)
+{
+  return AllGates{row_gates(gates.beta), row_gates(gates.begin), row_gates(gates.end), gates.last};
 }
 
 __device__ __forceinline__ Tile scaled(const Tile &x, const Tile &by)
@@ -446,44 +432,103 @@ __device__ __forceinline__ Tile passed(const Tile &x, const Tile &by)
   for (uint32_t e = 0; e < 4; ++e) r[e] = by[e] != 0.0f ? x[e] * by[e] : 0.0f;
   return r;
 }
-__device__ __forceinline__ Tile passed(const Tile &x, float by) { return passed(x, Tile{by, by, by, by}); }
 
-// A lane's numbers of a tile of steps: rows of a strided array, this lane's column; zeros where there is none.
-template <typename T>
-__device__ __forceinline__ void load_tiles(Tile (&x)[4], const T *piece, uint64_t stride, uint32_t have, bool column)
+// x, of which the compiler knows nothing more: what is computed from it is computed where it is used, not ahead of a loop and kept
+// in registers through it.
+__device__ __forceinline__ uint32_t anew(uint32_t x)
 {
-#pragma unroll
-  for (uint32_t i = 0; i < 4; ++i)
-#pragma unroll
-    for (uint32_t e = 0; e < 4; ++e) {
-      const uint32_t t = tile_row(i, lane_id() / 16 * 4 + e);
-      const float v = column ? (float)piece[min(t, have - 1) * stride] : 0.0f;
-      x[i][e] = t < have ? v : 0.0f;
-    }
+  asm volatile("" : "+v"(x));
+  return x;
 }
 
-template <typename T, uint32_t KS>
-struct PieceKeys {  // rows of keys or queries as left operands
-  Operand<kPartsOf<T>> x[4][KS];
-  __device__ __forceinline__ void load(const T *piece, uint64_t stride, uint32_t have, uint32_t width)
+// What the kernels take of a piece, as it is in memory: asked for a piece ahead, made operands when it is used.  Behind a
+// sequence's last step that one is fetched again: its strength there is 0, and so is all that comes of it.
+// `near`: 64 rows apart are less than 2^32 bytes apart, and there are 64: a lane's place is an offset from an address that all share.
+constexpr uint64_t kNearStride = 1u << 23;
+
+template <typename T>
+struct PieceColumn {  // a lane's numbers of tiles of steps: rows of a strided array, this lane's column
+  T x[4][4];
+  __device__ __forceinline__ void load(const T *piece, uint64_t stride, uint32_t have, uint32_t column)
   {
-    const uint32_t lane = lane_id();
+    const uint32_t q = lane_id() / 16;
+    if (have == kPiece && stride <= kNearStride) {
+      const uint32_t offset = (q * 8 * (uint32_t)stride + column) * sizeof(T);
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) x[i][e] = *reinterpret_cast<const T *>(reinterpret_cast<const char *>(piece + (i / 2 * 32 + i % 2 * 4 + e) * stride) + offset);
+    } else {
+      const uint32_t m = anew(q * 4);
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) x[i][e] = piece[min(tile_row(i, m + e), have - 1) * stride + column];
+    }
+  }
+  __device__ __forceinline__ Tile tile(uint32_t i) const { return Tile{(float)x[i][0], (float)x[i][1], (float)x[i][2], (float)x[i][3]}; }
+};
+// f(t, address): every step of a lane's part of tiles of steps that a sequence has, and where its number is.
+template <typename T, typename F>
+__device__ __forceinline__ void each_step(T *piece, uint64_t stride, uint32_t have, uint32_t column, F f)
+{
+  const uint32_t q = lane_id() / 16;
+  if (have == kPiece && stride <= kNearStride) {
+    const uint32_t offset = (q * 8 * (uint32_t)stride + column) * sizeof(T);
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i)
 #pragma unroll
-      for (uint32_t s = 0; s < KS; ++s) x[i][s] = operand<T>(load_step<T>(piece, stride, tile_row(i, lane % 16), have, s * 32 + lane / 16 * 8, width));
+      for (uint32_t e = 0; e < 4; ++e) f(i, e, reinterpret_cast<T *>(reinterpret_cast<char *>(piece + (i / 2 * 32 + i % 2 * 4 + e) * stride) + offset));
+  } else {
+    const uint32_t m = anew(q * 4);
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) {
+        const uint32_t t = tile_row(i, m + e);
+        if (t < have) f(i, e, piece + t * stride + column);
+      }
+  }
+}
+template <typename T, uint32_t KS>
+struct PieceKeys {  // rows of keys or queries as left operands
+  Run<T, 8> x[4][KS];
+  __device__ __forceinline__ void load(const T *piece, uint64_t stride, uint32_t have, uint32_t width)
+  {
+    const uint32_t m = lane_id() % 16, q = lane_id() / 16;
+    if (have == kPiece && stride <= kNearStride && width == KS * 32) {
+      const uint32_t offset = ((m / 4 * 8 + m % 4) * (uint32_t)stride + q * 8) * sizeof(T);
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+        for (uint32_t s = 0; s < KS; ++s)
+          x[i][s] = load_run<T, 8>(reinterpret_cast<const T *>(reinterpret_cast<const char *>(piece + (i / 2 * 32 + i % 2 * 4) * stride + s * 32) + offset));
+    } else {
+      const uint32_t row = anew(m), d = anew(q * 8);
+      if (width == KS * 32) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+          for (uint32_t s = 0; s < KS; ++s) x[i][s] = load_run<T, 8>(piece + min(tile_row(i, row), have - 1) * stride + s * 32 + d);
+      } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+          for (uint32_t s = 0; s < KS; ++s) x[i][s] = load_eight<T>(piece + min(tile_row(i, row), have - 1) * stride, s * 32 + d, width);
+      }
+    }
   }
 };
 template <typename T, uint32_t KS>
 struct PieceColumns {  // their transposes, prepared
-  Operand<kPartsOf<T>> x[2 * KS][2];
+  Run<T, 8> x[2 * KS][2];
   __device__ __forceinline__ void load(const void *from, uint64_t key_head)
   {
     const T *const p = static_cast<const T *>(from) + key_head * (2 * KS * 2 * kOperand) + lane_id() * 8;
 #pragma unroll
     for (uint32_t i = 0; i < 2 * KS; ++i)
 #pragma unroll
-      for (uint32_t s = 0; s < 2; ++s) x[i][s] = operand<T>(*reinterpret_cast<const Run<T, 8> *>(p + (i * 2 + s) * kOperand));
+      for (uint32_t s = 0; s < 2; ++s) x[i][s] = *reinterpret_cast<const Run<T, 8> *>(p + (i * 2 + s) * kOperand);
   }
 };
 template <uint32_t N>
@@ -525,88 +570,106 @@ __device__ __forceinline__ void load_state(Tile (&S)[2 * KS], const float *from,
     }
 }
 template <uint32_t KS>
-__device__ __forceinline__ void store_state(const Tile (&S)[2 * KS], float *to, uint32_t Dk, uint32_t Dv, bool column)
+__device__ __forceinline__ void store_state(const Tile (&S)[2 * KS], float *to, uint32_t Dk, uint32_t Dv, uint32_t c0)
 {
+  const uint32_t q = lane_id() / 16, c = c0 + lane_id() % 16;
+  if (Dk == KS * 32 && c0 + 16 <= Dv) {
+    const uint32_t offset = (q * 8 * Dv + c) * 4;
 #pragma unroll
-  for (uint32_t i = 0; i < 2 * KS; ++i)
+    for (uint32_t i = 0; i < 2 * KS; ++i)
 #pragma unroll
-    for (uint32_t e = 0; e < 4; ++e) {
-      const uint32_t d = state_row(i, e);
-      if (column && d < Dk) to[(uint64_t)d * Dv] = S[i][e];
-    }
+      for (uint32_t e = 0; e < 4; ++e) *reinterpret_cast<float *>(reinterpret_cast<char *>(to + (i / 2 * 32 + i % 2 * 4 + e) * Dv) + offset) = S[i][e];
+  } else if (c < Dv) {
+    const uint32_t m = anew(q * 4);
+#pragma unroll
+    for (uint32_t i = 0; i < 2 * KS; ++i)
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) {
+        const uint32_t d = tile_row(i, m + e);
+        if (d < Dk) to[d * Dv + c] = S[i][e];
+      }
+  }
 }
 // A state of which the three parts are held: their sum is exact.
 template <uint32_t KS>
-__device__ __forceinline__ void store_parts(const Operand<3> (&S)[KS], float *to, uint32_t Dk, uint32_t Dv, bool column)
+__device__ __forceinline__ void store_parts(const Operand<3> (&S)[KS], float *to, uint32_t Dk, uint32_t Dv, uint32_t c0)
 {
   Tile x[2 * KS];
 #pragma unroll
   for (uint32_t s = 0; s < KS; ++s)
 #pragma unroll
     for (uint32_t e = 0; e < 8; ++e) x[2 * s + e / 4][e % 4] = ((float)S[s].part[2][e] + (float)S[s].part[1][e]) + (float)S[s].part[0][e];
-  store_state<KS>(x, to, Dk, Dv, column);
+  store_state<KS>(x, to, Dk, Dv, c0);
 }
 
-// Two waves on a SIMD's registers each: left operands of the next piece are on their way while this one is computed.
+// What the next piece takes is asked for as soon as this one has taken its own: in the same registers, which a wave has 512 of.
+// (Numbers of 32 bits are twice as many; there a piece's are asked for at its begin.)
 template <typename T, uint32_t KS>
 __global__ __launch_bounds__(2 * kWave) void delta_pieces_kernel(DeltaForward f, Prepared w)
 {
-  // outputs of 8 bits are computed from two parts of what they are sums of: 2^-16 of it, where they are rounded to 2^-9
-  constexpr uint32_t kOut = std::is_same<T, __bf16>::value ? 2 : 3;
-  __shared__ __align__(16) __bf16 states[2][KS][3 * kOperand], corrections[2][2][kOut * kOperand];
+  constexpr bool kAhead = sizeof(T) == 2;
+  __shared__ __align__(16) __bf16 states[2][KS][3 * kOperand];
+  __shared__ Tile corrections[2][4][kWave];  // U
   const DeltaArgs &a = f.n;
   const PiecePlace place = piece_place(a);
   if (place.none) return;
   const uint32_t s = place.s, h = place.h, hk = h / a.share, lane = lane_id(), c = place.c0 + lane % 16;
   const bool column = c < a.Dv, carries = threadIdx.x < kWave;
   const uint32_t len = delta_length(a, s), pieces = (len + kPiece - 1) / kPiece;
-  const uint64_t state = ((uint64_t)s * a.H + h) * a.Dk * a.Dv + c;
+  const uint64_t state = ((uint64_t)s * a.H + h) * a.Dk * a.Dv;
   const auto head_of = [&](uint32_t piece) { return ((uint64_t)s * a.pieces + piece) * a.H + h; };
   const auto have_of = [&](uint32_t piece) { return min(kPiece, len - piece * kPiece); };
   if (carries) {
-    const T *const k_rows = static_cast<const T *>(a.k) + s * a.k_seq + (uint64_t)hk * a.Dk, *const v_rows = static_cast<const T *>(a.v) + s * a.v_seq + (uint64_t)h * a.Dv + c;
+    const T *const k_rows = static_cast<const T *>(a.k) + s * a.k_seq + (uint64_t)hk * a.Dk;
+    const T *const v_rows = static_cast<const T *>(a.v) + s * a.v_seq + (uint64_t)h * a.Dv;
     Tile S[2 * KS];
-    load_state<KS>(S, f.h0 ? f.h0 + state : nullptr, a.Dk, a.Dv, column);
-    for (uint32_t piece = 0; piece < pieces; ++piece) {
-      const uint64_t head = head_of(piece);
-      const uint32_t have = have_of(piece);
-      const float *const gates = w.gates + head * kGateWords;
-      const RowGates beta = row_gates(gates), begin = row_gates(gates + kPiece), end = row_gates(gates + 2 * kPiece);
-      const float last = gates[3 * kPiece];
-      PieceKeys<T, KS> K;
-      K.load(k_rows + (uint64_t)piece * kPiece * a.k_time, a.k_time, have, a.Dk);
-      Tile X[4];
-      load_tiles(X, v_rows + (uint64_t)piece * kPiece * a.v_time, a.v_time, have, column);
-      PieceTriangle<3> M;
-      M.load(w.M, head);
-      PieceColumns<T, KS> Kt;
+    load_state<KS>(S, f.h0 ? f.h0 + state + c : nullptr, a.Dk, a.Dv, column);
+    PieceKeys<T, KS> K;
+    PieceColumn<T> V;
+    PieceTriangle<3> M;
+    PieceColumns<T, KS> Kt;
+    AllGates gates;
+    const auto load_keys = [&](uint32_t piece) {
+      K.load(k_rows + (uint64_t)piece * kPiece * a.k_time, a.k_time, have_of(piece), a.Dk);
+      V.load(v_rows + (uint64_t)piece * kPiece * a.v_time, a.v_time, have_of(piece), min(c, a.Dv - 1));
+    };
+    const auto load_columns = [&](uint32_t piece) {
       Kt.load(w.Kt, ((uint64_t)s * a.pieces + piece) * a.Hk + hk);
-      Tile kS[4] = {};
+      gates = all_gates(gates_of(w, head_of(piece)));
+    };
+    if (pieces) load_keys(0), M.load(w.M, head_of(0)), load_columns(0);
+    for (uint32_t piece = 0; piece < pieces; ++piece) {
+      const uint32_t next = min(piece + 1, pieces - 1);
+      if (!kAhead && piece) load_keys(piece), M.load(w.M, head_of(piece)), load_columns(piece);
+      Tile kS[4] = {}, X[4];
 #pragma unroll
       for (uint32_t i = 0; i < KS; ++i) {
         const Operand<3> parts = operand_of<3>(S[2 * i], S[2 * i + 1]);
         put(states[piece % 2][i], parts);
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) multiply<3>(kS[r], K.x[r][i], parts);
+        for (uint32_t r = 0; r < 4; ++r) multiply<3>(kS[r], operand<T>(K.x[r][i]), parts);
       }
 #pragma unroll
-      for (uint32_t r = 0; r < 4; ++r) X[r] -= passed(kS[r], begin.tile[r]);
-      const Operand<3> bX[2] = {operand_of<3>(scaled(X[0], beta.tile[0]), scaled(X[1], beta.tile[1])),
-                                operand_of<3>(scaled(X[2], beta.tile[2]), scaled(X[3], beta.tile[3]))};
+      for (uint32_t r = 0; r < 4; ++r) X[r] = V.tile(r) - passed(kS[r], gates.begin.tile[r]);
+      if (kAhead) load_keys(next);
+      const Operand<3> bX[2] = {operand_of<3>(scaled(X[0], gates.beta.tile[0]), scaled(X[1], gates.beta.tile[1])),
+                                operand_of<3>(scaled(X[2], gates.beta.tile[2]), scaled(X[3], gates.beta.tile[3]))};
       Tile mX[4] = {}, U[4];
       M.template times<3, false>(mX, bX);
+      if (kAhead) M.load(w.M, head_of(next));
 #pragma unroll
-      for (uint32_t r = 0; r < 4; ++r) U[r] = scaled(X[r] - mX[r], beta.tile[r]);
+      for (uint32_t r = 0; r < 4; ++r) U[r] = scaled(X[r] - mX[r], gates.beta.tile[r]);
 #pragma unroll
-      for (uint32_t i = 0; i < 2; ++i) put(corrections[piece % 2][i], operand_of<kOut>(U[2 * i], U[2 * i + 1]));
-      const Operand<3> left[2] = {operand_of<3>(scaled(U[0], end.tile[0]), scaled(U[1], end.tile[1])),
-                                  operand_of<3>(scaled(U[2], end.tile[2]), scaled(U[3], end.tile[3]))};
+      for (uint32_t r = 0; r < 4; ++r) corrections[piece % 2][r][lane] = U[r];
+      const Operand<3> left[2] = {operand_of<3>(scaled(U[0], gates.end.tile[0]), scaled(U[1], gates.end.tile[1])),
+                                  operand_of<3>(scaled(U[2], gates.end.tile[2]), scaled(U[3], gates.end.tile[3]))};
 #pragma unroll
       for (uint32_t i = 0; i < 2 * KS; ++i) {
-        S[i] = passed(S[i], last);
+        S[i] = gates.last != 0.0f ? S[i] * gates.last : Tile{};
 #pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) multiply<3>(S[i], Kt.x[i][j], left[j]);
+        for (uint32_t j = 0; j < 2; ++j) multiply<3>(S[i], operand<T>(Kt.x[i][j]), left[j]);
       }
+      if (kAhead) load_columns(next);
       meet();
     }
     if (f.h_last) {
@@ -614,49 +677,44 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_kernel(DeltaForward f,
 #pragma unroll
         for (uint32_t i = 0; i < 2 * KS; ++i) S[i] = Tile{};
       }
-      store_state<KS>(S, f.h_last + state, a.Dk, a.Dv, column);
+      store_state<KS>(S, f.h_last + state, a.Dk, a.Dv, place.c0);
     }
   } else {
     const T *const q_rows = static_cast<const T *>(a.q) + s * a.q_seq + (uint64_t)hk * a.Dk;
-    T *const o = static_cast<T *>(f.o) + ((uint64_t)s * a.T * a.H + h) * a.Dv + c;
+    T *const o = static_cast<T *>(f.o) + ((uint64_t)s * a.T * a.H + h) * a.Dv;
     const uint64_t o_row = (uint64_t)a.H * a.Dv;
+    PieceKeys<T, KS> Q;
+    PieceTriangle<3> P;
+    RowGates begin;
+    const auto load = [&](uint32_t piece) {
+      Q.load(q_rows + (uint64_t)piece * kPiece * a.q_time, a.q_time, have_of(piece), a.Dk);
+      P.load(w.P, head_of(piece));
+      begin = row_gates(gates_of(w, head_of(piece)).begin);
+    };
+    if (pieces) load(0);
     for (uint32_t piece = 0; piece < pieces; ++piece) {
-      const uint64_t head = head_of(piece);
-      const uint32_t have = have_of(piece);
-      PieceKeys<T, KS> Q;
-      Q.load(q_rows + (uint64_t)piece * kPiece * a.q_time, a.q_time, have, a.Dk);
-      PieceTriangle<kOut> P;
-      P.load(w.P, head);
-      const RowGates begin = row_gates(w.gates + head * kGateWords + kPiece);
+      if (!kAhead && piece) load(piece);
       meet();
       Tile O[4] = {};
       Operand<3> S[KS];
 #pragma unroll
       for (uint32_t i = 0; i < KS; ++i) {
         S[i] = get<3>(states[piece % 2][i]);
-        Operand<kOut> used;
 #pragma unroll
-        for (uint32_t p = 0; p < kOut; ++p) used.part[p] = S[i].part[p];
-#pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) multiply<kOut>(O[r], Q.x[r][i], used);
+        for (uint32_t r = 0; r < 4; ++r) multiply<3>(O[r], operand<T>(Q.x[r][i]), S[i]);
       }
-      if (f.carry) store_parts<KS>(S, f.carry + head * a.Dk * a.Dv + c, a.Dk, a.Dv, column);
 #pragma unroll
       for (uint32_t r = 0; r < 4; ++r) O[r] = passed(O[r], begin.tile[r]);
-      const Operand<kOut> U[2] = {get<kOut>(corrections[piece % 2][0]), get<kOut>(corrections[piece % 2][1])};
-      P.template times<kOut, false>(O, U);
-      if (column) {
-#pragma unroll
-        for (uint32_t r = 0; r < 4; ++r)
-#pragma unroll
-          for (uint32_t e = 0; e < 4; ++e) {
-            const uint32_t t = state_row(r, e);
-            if (t < have) o[(piece * kPiece + t) * o_row] = (T)(a.scale * O[r][e]);
-          }
-      }
+      const Tile(&found)[4][kWave] = corrections[piece % 2];
+      const Operand<3> U[2] = {operand_of<3>(found[0][lane], found[1][lane]), operand_of<3>(found[2][lane], found[3][lane])};
+      P.template times<3, false>(O, U);
+      if (kAhead) load(min(piece + 1, pieces - 1));
+      if (f.carry) store_parts<KS>(S, f.carry + head_of(piece) * a.Dk * a.Dv, a.Dk, a.Dv, place.c0);
+      if (column)
+        each_step(o + (uint64_t)piece * kPiece * o_row, o_row, have_of(piece), c, [&](uint32_t r, uint32_t e, T *to) { *to = (T)(a.scale * O[r][e]); });
     }
     if (column)
-      for (uint64_t t = len + lane / 16; t < a.T; t += 4) o[t * o_row] = (T)0.0f;
+      for (uint64_t t = len + lane / 16; t < a.T; t += 4) o[t * o_row + c] = (T)0.0f;
   }
 }
 
@@ -665,6 +723,7 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_kernel(DeltaForward f,
 template <typename T, uint32_t KS>
 __global__ __launch_bounds__(2 * kWave) void delta_pieces_back_kernel(DeltaBack b, Prepared w)
 {
+  constexpr bool kAhead = sizeof(T) == 2;
   struct Brought {
     Tile o[4][kWave], state[2 * KS][kWave];
   };
@@ -677,7 +736,7 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_back_kernel(DeltaBack 
   const uint32_t s = place.s, h = place.h, hk = h / a.share, lane = lane_id(), c = place.c0 + lane % 16;
   const bool column = c < a.Dv, carries = threadIdx.x < kWave;
   const uint32_t len = delta_length(a, s), pieces = (len + kPiece - 1) / kPiece;
-  const uint64_t state = ((uint64_t)s * a.H + h) * a.Dk * a.Dv + c;
+  const uint64_t state = ((uint64_t)s * a.H + h) * a.Dk * a.Dv;
   const auto head_of = [&](uint32_t piece) { return ((uint64_t)s * a.pieces + piece) * a.H + h; };
   const auto key_head_of = [&](uint32_t piece) { return ((uint64_t)s * a.pieces + piece) * a.Hk + hk; };
   const auto have_of = [&](uint32_t piece) { return min(kPiece, len - piece * kPiece); };
@@ -685,65 +744,81 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_back_kernel(DeltaBack 
     const T *const k_rows = static_cast<const T *>(a.k) + s * a.k_seq + (uint64_t)hk * a.Dk;
     Tile S[2 * KS];
     const bool passes = len == 0 || delta_passes(a, s, len - 1);
-    load_state<KS>(S, b.dh_last && passes ? b.dh_last + state : nullptr, a.Dk, a.Dv, column);
-    if (pieces) meet();
-    for (uint32_t piece = pieces; piece-- > 0;) {
-      const uint64_t head = head_of(piece);
-      const float *const gates = w.gates + head * kGateWords;
-      const RowGates beta = row_gates(gates), begin = row_gates(gates + kPiece), end = row_gates(gates + 2 * kPiece);
-      const float last = gates[3 * kPiece];
-      PieceKeys<T, KS> K;
-      K.load(k_rows + (uint64_t)piece * kPiece * a.k_time, a.k_time, have_of(piece), a.Dk);
-      PieceTriangle<3> M;
-      M.load(w.M, head);
-      PieceColumns<T, KS> Kt;
+    load_state<KS>(S, b.dh_last && passes ? b.dh_last + state + c : nullptr, a.Dk, a.Dv, column);
+    PieceKeys<T, KS> K;
+    PieceTriangle<3> M;
+    PieceColumns<T, KS> Kt;
+    AllGates gates;
+    const auto load_keys = [&](uint32_t piece) { K.load(k_rows + (uint64_t)piece * kPiece * a.k_time, a.k_time, have_of(piece), a.Dk); };
+    const auto load_columns = [&](uint32_t piece) {
       Kt.load(w.Kt, key_head_of(piece));
+      gates = all_gates(gates_of(w, head_of(piece)));
+    };
+    if (pieces) {
+      load_keys(pieces - 1), M.load(w.M, head_of(pieces - 1)), load_columns(pieces - 1);
+      meet();
+    }
+    for (uint32_t piece = pieces; piece-- > 0;) {
+      const uint32_t next = piece ? piece - 1 : 0;
+      if (!kAhead && piece + 1 < pieces) load_keys(piece), M.load(w.M, head_of(piece)), load_columns(piece);
       Tile kS[4] = {};
 #pragma unroll
       for (uint32_t i = 0; i < KS; ++i) {
         const Operand<3> parts = operand_of<3>(S[2 * i], S[2 * i + 1]);
         put(states[piece % 2][i], parts);
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) multiply<3>(kS[r], K.x[r][i], parts);
+        for (uint32_t r = 0; r < 4; ++r) multiply<3>(kS[r], operand<T>(K.x[r][i]), parts);
       }
+      if (kAhead) load_keys(next);
       Tile dU[4];
 #pragma unroll
-      for (uint32_t r = 0; r < 4; ++r) dU[r] = brought[piece % 2].o[r][lane] + scaled(kS[r], end.tile[r]);
-      const Operand<3> bU[2] = {operand_of<3>(scaled(dU[0], beta.tile[0]), scaled(dU[1], beta.tile[1])),
-                                operand_of<3>(scaled(dU[2], beta.tile[2]), scaled(dU[3], beta.tile[3]))};
+      for (uint32_t r = 0; r < 4; ++r) dU[r] = brought[piece % 2].o[r][lane] + scaled(kS[r], gates.end.tile[r]);
+      const Operand<3> bU[2] = {operand_of<3>(scaled(dU[0], gates.beta.tile[0]), scaled(dU[1], gates.beta.tile[1])),
+                                operand_of<3>(scaled(dU[2], gates.beta.tile[2]), scaled(dU[3], gates.beta.tile[3]))};
       Tile mU[4] = {}, V[4];
       M.template times<3, true>(mU, bU);
+      if (kAhead) M.load(w.M, head_of(next));
 #pragma unroll
       for (uint32_t r = 0; r < 4; ++r) {
         dU[r] -= mU[r];  // Y
         found[piece % 2][r][lane] = dU[r];
-        V[r] = -scaled(scaled(dU[r], beta.tile[r]), begin.tile[r]);
+        V[r] = -scaled(scaled(dU[r], gates.beta.tile[r]), gates.begin.tile[r]);
       }
       const Operand<3> left[2] = {operand_of<3>(V[0], V[1]), operand_of<3>(V[2], V[3])};
 #pragma unroll
       for (uint32_t i = 0; i < 2 * KS; ++i) {
-        S[i] = passed(S[i], last) + brought[piece % 2].state[i][lane];
+        S[i] = (gates.last != 0.0f ? S[i] * gates.last : Tile{}) + brought[piece % 2].state[i][lane];
 #pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) multiply<3>(S[i], Kt.x[i][j], left[j]);
+        for (uint32_t j = 0; j < 2; ++j) multiply<3>(S[i], operand<T>(Kt.x[i][j]), left[j]);
       }
+      if (kAhead) load_columns(next);
       meet();
     }
-    if (b.dh0) store_state<KS>(S, b.dh0 + state, a.Dk, a.Dv, column);
+    if (b.dh0) store_state<KS>(S, b.dh0 + state, a.Dk, a.Dv, place.c0);
   } else {
     const uint64_t o_row = (uint64_t)a.H * a.Dv;
-    const T *const d_o = static_cast<const T *>(b.d_o) + ((uint64_t)s * a.T * a.H + h) * a.Dv + c;
-    float *const Y = b.Y + ((uint64_t)s * a.T * a.H + h) * a.Dv + c;
-    T *const dv = static_cast<T *>(b.dv) + s * b.dv_seq + (uint64_t)h * a.Dv + c;
+    const T *const d_o = static_cast<const T *>(b.d_o) + ((uint64_t)s * a.T * a.H + h) * a.Dv;
+    float *const Y = b.Y + ((uint64_t)s * a.T * a.H + h) * a.Dv;
+    T *const dv = static_cast<T *>(b.dv) + s * b.dv_seq + (uint64_t)h * a.Dv;
+    PieceColumn<T> taken;
+    PieceTriangle<3> P;
+    PieceColumns<T, KS> Qt;
+    RowGates begin;
+    const auto load = [&](uint32_t piece) {
+      taken.load(d_o + (uint64_t)piece * kPiece * o_row, o_row, have_of(piece), min(c, a.Dv - 1));
+      P.load(w.P, head_of(piece));
+      Qt.load(w.Qt, key_head_of(piece));
+      begin = row_gates(gates_of(w, head_of(piece)).begin);
+    };
     const auto bring = [&](uint32_t piece) {
-      const uint64_t head = head_of(piece);
       const uint32_t have = have_of(piece);
       Tile dO[4];
-      load_tiles(dO, d_o + (uint64_t)piece * kPiece * o_row, o_row, have, column);
-      PieceTriangle<3> P;
-      P.load(w.P, head);
-      PieceColumns<T, KS> Qt;
-      Qt.load(w.Qt, key_head_of(piece));
-      const RowGates begin = row_gates(w.gates + head * kGateWords + kPiece);
+#pragma unroll
+      for (uint32_t r = 0; r < 4; ++r) {
+        dO[r] = taken.tile(r);
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) dO[r][e] = state_row(r, e) < have ? dO[r][e] : 0.0f;
+      }
       const Operand<kPartsOf<T>> right[2] = {operand_of<kPartsOf<T>>(dO[0], dO[1]), operand_of<kPartsOf<T>>(dO[2], dO[3])};
       Tile of_o[4] = {};
       P.template times<3, true>(of_o, right);
@@ -757,9 +832,10 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_back_kernel(DeltaBack 
       for (uint32_t i = 0; i < 2 * KS; ++i) {
         Tile x{};
 #pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) multiply<3>(x, Qt.x[i][j], left[j]);
+        for (uint32_t j = 0; j < 2; ++j) multiply<3>(x, operand<T>(Qt.x[i][j]), left[j]);
         brought[piece % 2].state[i][lane] = x;
       }
+      if (piece) load(piece - 1);
     };
     const auto store = [&](uint32_t piece) {
       const uint64_t head = head_of(piece);
@@ -767,22 +843,18 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_back_kernel(DeltaBack 
       Operand<3> S[KS];
 #pragma unroll
       for (uint32_t i = 0; i < KS; ++i) S[i] = get<3>(states[piece % 2][i]);
-      store_parts<KS>(S, b.dS + head * a.Dk * a.Dv + c, a.Dk, a.Dv, column);
-      const RowGates beta = row_gates(w.gates + head * kGateWords);
+      store_parts<KS>(S, b.dS + head * a.Dk * a.Dv, a.Dk, a.Dv, place.c0);
+      const RowGates beta = row_gates(gates_of(w, head).beta);
+      Tile y[4];
 #pragma unroll
-      for (uint32_t r = 0; r < 4; ++r) {
-        const Tile y = found[piece % 2][r][lane];
-#pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) {
-          const uint32_t t = state_row(r, e);
-          if (column && t < have) {
-            Y[(piece * kPiece + t) * o_row] = y[e];
-            dv[(uint64_t)(piece * kPiece + t) * b.dv_time] = (T)(beta.tile[r][e] * y[e]);
-          }
-        }
+      for (uint32_t r = 0; r < 4; ++r) y[r] = found[piece % 2][r][lane];
+      if (column) {
+        each_step(Y + (uint64_t)piece * kPiece * o_row, o_row, have, c, [&](uint32_t r, uint32_t e, float *to) { *to = y[r][e]; });
+        each_step(dv + (uint64_t)piece * kPiece * b.dv_time, b.dv_time, have, c, [&](uint32_t r, uint32_t e, T *to) { *to = (T)(beta.tile[r][e] * y[r][e]); });
       }
     };
     if (pieces) {
+      load(pieces - 1);
       bring(pieces - 1);
       meet();
       for (uint32_t piece = pieces; piece-- > 0;) {
@@ -793,36 +865,25 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_back_kernel(DeltaBack 
       store(0);
     }
     if (column)
-      for (uint64_t t = len + lane / 16; t < a.T; t += 4) dv[t * b.dv_time] = (T)0.0f;
+      for (uint64_t t = len + lane / 16; t < a.T; t += 4) dv[t * b.dv_time + c] = (T)0.0f;
   }
 }
 
-// What is left of the gradient, a workgroup per piece and key head: eight waves, of which wave w has rows 16 (w % 4) of what
-// belongs to steps, and of their columns one half.
-constexpr uint32_t kGradThreads = 512, kGradWaves = kGradThreads / kWave, kGradColumns = 32;
+// What is left of the gradient, a workgroup of eight waves per piece and key head: first a wave has 16 of the state's columns and all
+// steps, and finds U anew; then a wave has a tile of the state's rows and KS tiles of steps, and sums over the columns.  Between the
+// two U and dV cross LDS, in parts.
+constexpr uint32_t kGradThreads = 512, kGradWaves = kGradThreads / kWave, kGradRow = kDeltaMaxWidth + 8;
 
 struct GradSpace {
-  static constexpr uint32_t kRow = kGradColumns + 4;
   Gates gates;
-  float K[kPiece * (kDeltaMaxWidth + 4)];
   union {
-    struct {
-      float S0[kDeltaMaxWidth * kRow], dS[kDeltaMaxWidth * kRow];
-    };
-    float Q[kPiece * (kDeltaMaxWidth + 4)];
+    __bf16 part[2][3][kPiece][kGradRow];  // U, dV
+    float B[2][kPiece * kPieceRow];       // B, C
   };
-  union {
-    struct {
-      float X[kPiece * kRow], U[kPiece * kRow], dO[kPiece * kRow], dV[kPiece * kRow];
-    };
-    struct {
-      float B[kPiece * kPieceRow], C[kPiece * kPieceRow];
-    };
-  };
-  float M[kPiece * kPieceRow];
-  float of_g[2][kPiece], of_v[2][kPiece], of_beta[2][kPiece];  // sums over a half of the columns
+  float of_g[kGradWaves][kPiece], of_v[kGradWaves][kPiece], of_beta[kGradWaves][kPiece];  // sums over a wave's share
   double at_end[kGradWaves];
 };
+static_assert(kDeltaMaxWidth == 16 * kGradWaves);
 
 // The sum over the 16 lanes of a row of a tile, in each of them.
 __device__ __forceinline__ float row_sum(float v)
@@ -831,17 +892,31 @@ __device__ __forceinline__ float row_sum(float v)
   return v;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack b)
+// A 32-bit number's parts.
+__device__ __forceinline__ void put_parts(__bf16 (*part)[kPiece][kGradRow], uint32_t t, uint32_t c, float x)
 {
-  constexpr uint32_t kRow = GradSpace::kRow, kMaxTiles = kDeltaMaxWidth / 16 / 2;
+#pragma unroll
+  for (uint32_t p = 0; p < 3; ++p) {
+    const uint32_t bits = __float_as_uint(x) & 0xffff0000u;
+    part[p][t][c] = __builtin_bit_cast(__bf16, (uint16_t)(bits >> 16));
+    x -= __uint_as_float(bits);
+  }
+}
+__device__ __forceinline__ Operand<3> get_parts(const __bf16 (*part)[kPiece][kGradRow], uint32_t t, uint32_t c)
+{
+  Operand<3> x;
+#pragma unroll
+  for (uint32_t p = 0; p < 3; ++p) x.part[p] = *reinterpret_cast<const Parts8 *>(&part[p][t][c]);
+  return x;
+}
+template <typename T, uint32_t KS, bool kWhole>
+__global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack b, Prepared w)
+{
+  __shared__ __align__(16) GradSpace x;
   const DeltaArgs &a = b.n;
-  __shared__ GradSpace x;
   const uint32_t hk = blockIdx.x % a.Hk, piece = blockIdx.x / a.Hk % a.pieces, s = blockIdx.x / a.Hk / a.pieces;
-  const uint32_t lane = lane_id(), wave = threadIdx.x / kWave, col = lane % 16, quad = lane / 16 * 4;
-  const uint32_t r = wave % 4 * 16, half = wave / 4;
+  const uint32_t lane = lane_id(), wave = threadIdx.x / kWave;
   const uint32_t len = delta_length(a, s), t0 = piece * kPiece, steps = min(kPiece, a.T - t0);
-  const uint32_t depth = up16(a.Dk), row = depth + 4;
   T *const dq = static_cast<T *>(b.dq) + s * b.dq_seq + t0 * b.dq_time + (uint64_t)hk * a.Dk;
   T *const dk = static_cast<T *>(b.dk) + s * b.dk_seq + t0 * b.dk_time + (uint64_t)hk * a.Dk;
   const uint64_t gates_at = ((uint64_t)s * a.T + t0) * a.H;
@@ -856,148 +931,223 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
     }
     return;
   }
-  load_rows(x.K, row, depth, static_cast<const T *>(a.k) + s * a.k_seq + t0 * a.k_time + (uint64_t)hk * a.Dk, a.k_time, len - t0, a.Dk, kGradThreads);
-  Tile dq_all[kMaxTiles] = {}, dk_all[kMaxTiles] = {};  // tile i: columns 16 (2 i + half)
+  const uint32_t have = min(kPiece, len - t0);
+  const T *const k_rows = static_cast<const T *>(a.k) + s * a.k_seq + t0 * a.k_time + (uint64_t)hk * a.Dk;
+  const T *const q_rows = static_cast<const T *>(a.q) + s * a.q_seq + t0 * a.q_time + (uint64_t)hk * a.Dk;
+  const uint64_t o_row = (uint64_t)a.H * a.Dv, key_head = ((uint64_t)s * a.pieces + piece) * a.Hk + hk;
+  // this wave's tile of the state's rows, and its first tile of steps
+  const uint32_t own = wave % (2 * KS), r0 = wave / (2 * KS) * KS;
+  Tile dq_all[KS] = {}, dk_all[KS] = {};
+#pragma unroll 1
   for (uint32_t h = hk * a.share; h < (hk + 1) * a.share; ++h) {
+    const uint64_t head = ((uint64_t)s * a.pieces + piece) * a.H + h;
+    const uint32_t m = anew(lane % 16), q = anew(lane / 16), own_d = tile_row(own, m);
+    const auto state_row = [&](uint32_t tile, uint32_t e) { return tile_row(tile, q * 4 + e); };
     __syncthreads();
-    const uint64_t piece_head = ((uint64_t)s * a.pieces + piece) * a.H + h;
-    if (wave == 0) load_gates(a, s, h, t0, len, x.gates);
-    for (uint32_t i = threadIdx.x; i < kPiece * kPiece; i += kGradThreads)
-      x.M[i / kPiece * kPieceRow + i % kPiece] = b.M[piece_head * kPiece * kPiece + i];
-    Tile dq_h[kMaxTiles] = {}, B[2] = {}, C[2] = {};  // B and C: columns 16 (2 half + i)
-    float of_v[4] = {}, of_beta[4] = {};
-    double at_end = 0.0;
-    for (uint32_t c0 = 0; c0 < a.Dv; c0 += kGradColumns) {
-      __syncthreads();
-      const float *const S0 = b.carry + piece_head * a.Dk * a.Dv + c0, *const dS = b.dS + piece_head * a.Dk * a.Dv + c0;
-      for (uint32_t i = threadIdx.x; i < depth * kGradColumns; i += kGradThreads) {
-        const uint32_t d = i / kGradColumns, c = i % kGradColumns;
-        const bool have = d < a.Dk && c0 + c < a.Dv;
-        x.S0[d * kRow + c] = have ? S0[(uint64_t)d * a.Dv + c] : 0.0f;
-        x.dS[d * kRow + c] = have ? dS[(uint64_t)d * a.Dv + c] : 0.0f;
-      }
-      load_rows(x.X, kRow, kGradColumns, static_cast<const T *>(a.v) + s * a.v_seq + t0 * a.v_time + (uint64_t)h * a.Dv + c0, a.v_time, len - t0,
-                a.Dv - c0, kGradThreads);
-      load_rows(x.dO, kRow, kGradColumns, static_cast<const T *>(b.d_o) + gates_at * a.Dv + (uint64_t)h * a.Dv + c0, (uint64_t)a.H * a.Dv, len - t0,
-                a.Dv - c0, kGradThreads);
-      load_rows(x.dV, kRow, kGradColumns, b.Y + gates_at * a.Dv + (uint64_t)h * a.Dv + c0, (uint64_t)a.H * a.Dv, len - t0, a.Dv - c0, kGradThreads);
-      __syncthreads();
-      const uint32_t c = half * 16 + col;
-      const Tile kS = product(Tile{}, depth, [&](uint32_t i) { return x.K[(r + col) * row + i]; }, [&](uint32_t i) { return x.S0[i * kRow + c]; });
-      Tile X, Y, V;
+    for (uint32_t i = threadIdx.x; i < sizeof(Gates) / 4; i += kGradThreads) reinterpret_cast<uint32_t *>(&x.gates)[i] = w.gates[head * kGateWords + i];
+    __syncthreads();
+    const float *const S0 = b.carry + head * a.Dk * a.Dv, *const dS = b.dS + head * a.Dk * a.Dv;
+    const T *const v_rows = static_cast<const T *>(a.v) + s * a.v_seq + t0 * a.v_time + (uint64_t)h * a.Dv;
+    const T *const o_rows = static_cast<const T *>(b.d_o) + gates_at * a.Dv + (uint64_t)h * a.Dv;
+    const float *const y_rows = b.Y + gates_at * a.Dv + (uint64_t)h * a.Dv;
+    {
+      const uint32_t column = wave * 16 + m, c = min(column, a.Dv - 1);
+      Tile U[4] = {}, Y[4] = {}, of_v[4] = {}, of_beta[4] = {};
+      if (wave * 16 < a.Dv) {
+        Tile kS[4] = {}, S[2 * KS];
 #pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) {
-        const uint32_t t = r + quad + e;
-        V[e] = x.X[t * kRow + c];
-        Y[e] = x.dV[t * kRow + c];
-        X[e] = V[e] - (x.gates.episode[t] == 0 ? x.gates.begin[t] * kS[e] : 0.0f);
-        x.X[t * kRow + c] = x.gates.beta[t] * X[e];
-        x.dV[t * kRow + c] = x.gates.beta[t] * Y[e];
-      }
-      __syncthreads();
-      const Tile mX = product(Tile{}, kPiece, [&](uint32_t i) { return x.M[(r + col) * kPieceRow + i]; }, [&](uint32_t i) { return x.X[i * kRow + c]; });
+        for (uint32_t i = 0; i < 2 * KS; ++i)
 #pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) {
-        const uint32_t t = r + quad + e;
-        const float E = X[e] - mX[e];
-        of_beta[e] += Y[e] * E;
-        of_v[e] += V[e] * (x.gates.beta[t] * Y[e]);
-        x.U[t * kRow + c] = x.gates.beta[t] * E;
-      }
-      if (x.gates.episode[kPiece - 1] == 0)
-        for (uint32_t i = threadIdx.x; i < depth * kGradColumns; i += kGradThreads) {
-          const uint32_t at = i / kGradColumns * kRow + i % kGradColumns;
-          at_end += (double)(x.gates.last * x.S0[at]) * x.dS[at];
+          for (uint32_t e = 0; e < 4; ++e) S[i][e] = S0[min(state_row(i, e), a.Dk - 1) * a.Dv + c];
+        PieceKeys<T, KS> K;
+        K.load(k_rows, a.k_time, have, a.Dk);
+#pragma unroll
+        for (uint32_t i = 0; i < KS; ++i) {
+          const Operand<3> parts = operand_of<3>(S[2 * i], S[2 * i + 1]);
+#pragma unroll
+          for (uint32_t r = 0; r < 4; ++r) multiply<3>(kS[r], operand<T>(K.x[r][i]), parts);
         }
-      __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);  // (what follows is asked for when the keys' registers are free)
+        const RowGates beta = row_gates(x.gates.beta), begin = row_gates(x.gates.begin);
+        PieceColumn<T> V;
+        PieceColumn<float> y;
+        V.load(v_rows, a.v_time, have, c);
+        y.load(y_rows, o_row, have, c);
+        PieceTriangle<3> M;
+        M.load(w.rows, head);
+        Tile X[4], mX[4] = {};
 #pragma unroll
-      for (uint32_t i = 0; i < kMaxTiles; ++i) {
-        const uint32_t d0 = (2 * i + half) * 16;
-        if (d0 >= depth) continue;
-        const auto start = [&](uint32_t k) { return x.S0[(d0 + col) * kRow + k]; };
-        const Tile oS = product(Tile{}, kGradColumns, [&](uint32_t k) { return x.dO[(r + col) * kRow + k]; }, start);
-        const Tile vS = product(Tile{}, kGradColumns, [&](uint32_t k) { return x.dV[(r + col) * kRow + k]; }, start);
-        const Tile uS = product(Tile{}, kGradColumns, [&](uint32_t k) { return x.U[(r + col) * kRow + k]; },
-                                [&](uint32_t k) { return x.dS[(d0 + col) * kRow + k]; });
+        for (uint32_t r = 0; r < 4; ++r) X[r] = V.tile(r) - passed(kS[r], begin.tile[r]);
+        const Operand<3> bX[2] = {operand_of<3>(scaled(X[0], beta.tile[0]), scaled(X[1], beta.tile[1])),
+                                  operand_of<3>(scaled(X[2], beta.tile[2]), scaled(X[3], beta.tile[3]))};
+        M.template times<3, false>(mX, bX);
+        if (column < a.Dv) {
+#pragma unroll
+          for (uint32_t r = 0; r < 4; ++r) {
+            const Tile E = X[r] - mX[r];
+            U[r] = scaled(E, beta.tile[r]);
+            Y[r] = scaled(y.tile(r), beta.tile[r]);
+            of_beta[r] = scaled(y.tile(r), E);
+            of_v[r] = scaled(V.tile(r), Y[r]);
+          }
+        }
+      }
+#pragma unroll
+      for (uint32_t r = 0; r < 4; ++r)
 #pragma unroll
         for (uint32_t e = 0; e < 4; ++e) {
-          const uint32_t t = r + quad + e;
-          const bool passes = x.gates.episode[t] == 0;
-          const float begin = x.gates.begin[t], end = x.gates.end[t];
-          dq_h[i][e] += passes ? a.scale * begin * oS[e] : 0.0f;
-          dk_all[i][e] += end * uS[e] - (passes ? begin * vS[e] : 0.0f);
-          at_end += (double)(end * uS[e]) * x.K[t * row + d0 + col];
+          const uint32_t t = state_row(r, e);
+          put_parts(x.part[0], t, column, U[r][e]);
+          put_parts(x.part[1], t, column, Y[r][e]);
+          const float v = row_sum(of_v[r][e]), beta = row_sum(of_beta[r][e]);
+          if (m == 0) x.of_v[wave][t] = v, x.of_beta[wave][t] = beta;
         }
+    }
+    __syncthreads();
+    Tile oS[KS] = {}, uS[KS] = {}, vS[KS] = {}, B[2] = {}, C[2] = {};
+    double at_end = 0.0;
+    // tiles of B and C: of 16, those four of later columns than rows left out
+    const auto tile_of = [&](uint32_t i, uint32_t *r, uint32_t *j) {
+      const uint32_t f = wave + i * kGradWaves;
+      *r = f < 4 ? f / 2 : 2 + (f - 4) / 4, *j = f < 4 ? f % 2 : (f - 4) % 4;
+      return f < 12;
+    };
+#pragma unroll 1
+    for (uint32_t c0 = 0; c0 < a.Dv; c0 += 32) {
+      const uint32_t c = c0 + q * 8, row = min(own_d, a.Dk - 1) * a.Dv;
+      Run<T, 8> o[KS], of_tile[2] = {};
+      const Run<float, 8> sr = load_step<float, kWhole>(S0 + row, 0, 0, 1, c, a.Dv), er = load_step<float, kWhole>(dS + row, 0, 0, 1, c, a.Dv);
+#pragma unroll
+      for (uint32_t i = 0; i < KS; ++i) o[i] = load_step<T, kWhole>(o_rows, o_row, tile_row(r0 + i, m), have, c, a.Dv);
+#pragma unroll
+      for (uint32_t i = 0; i < 2; ++i) {
+        uint32_t r, j;
+        tile_of(i, &r, &j);
+        of_tile[i] = load_step<T, kWhole>(o_rows, o_row, tile_row(min(r, 3u), m), have, c, a.Dv);
+      }
+      const Operand<3> start = operand<float>(sr), end = operand<float>(er);
+      if (x.gates.last != 0.0f && own_d < a.Dk && r0 == 0) {
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) at_end += (double)(x.gates.last * sr[e]) * er[e];
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < KS; ++i) {
+        const uint32_t t = tile_row(r0 + i, m);
+        multiply<3>(oS[i], operand<T>(o[i]), start);
+        multiply<3>(uS[i], get_parts(x.part[0], t, c), end);
+        multiply<3>(vS[i], get_parts(x.part[1], t, c), start);
       }
 #pragma unroll
       for (uint32_t i = 0; i < 2; ++i) {
-        const uint32_t j0 = (2 * half + i) * 16;
-        if (j0 > r) continue;
-        const auto u = [&](uint32_t k) { return x.U[(j0 + col) * kRow + k]; };
-        B[i] = product(B[i], kGradColumns, [&](uint32_t k) { return x.dO[(r + col) * kRow + k]; }, u);
-        C[i] = product(C[i], kGradColumns, [&](uint32_t k) { return x.dV[(r + col) * kRow + k]; }, u);
+        uint32_t r, j;
+        if (!tile_of(i, &r, &j)) continue;
+        const Operand<3> u = get_parts(x.part[0], tile_row(j, m), c);
+        multiply<3>(B[i], operand<T>(of_tile[i]), u);
+        multiply<3>(C[i], get_parts(x.part[1], tile_row(r, m), c), u);
       }
     }
     __syncthreads();
-    load_rows(x.Q, row, depth, static_cast<const T *>(a.q) + s * a.q_seq + t0 * a.q_time + (uint64_t)hk * a.Dk, a.q_time, len - t0, a.Dk, kGradThreads);
 #pragma unroll
-    for (uint32_t i = 0; i < 2; ++i)
+    for (uint32_t i = 0; i < 2; ++i) {
+      uint32_t r, j;
+      if (!tile_of(i, &r, &j)) continue;
+      j = tile_row(j, m);
 #pragma unroll
       for (uint32_t e = 0; e < 4; ++e) {
-        const uint32_t t = r + quad + e, j = (2 * half + i) * 16 + col;
+        const uint32_t t = state_row(r, e);
         const float d = j <= t ? decay(x.gates, t, j) : 0.0f;
-        x.B[t * kPieceRow + j] = j <= t ? a.scale * B[i][e] * d : 0.0f;
-        x.C[t * kPieceRow + j] = j < t ? C[i][e] * d : 0.0f;
+        x.B[0][t * kPieceRow + j] = j <= t ? a.scale * B[i][e] * d : 0.0f;
+        x.B[1][t * kPieceRow + j] = j < t ? C[i][e] * d : 0.0f;
       }
+    }
     __syncthreads();
-    float of_g[4] = {};
+    const T *const kt = static_cast<const T *>(w.Kt) + (key_head * 2 * KS + own) * 2 * kOperand + lane * 8;
+    const T *const qt = static_cast<const T *>(w.Qt) + (key_head * 2 * KS + own) * 2 * kOperand + lane * 8;
 #pragma unroll
-    for (uint32_t i = 0; i < kMaxTiles; ++i) {
-      const uint32_t d0 = (2 * i + half) * 16;
-      if (d0 >= depth) continue;
-      const auto key = [&](uint32_t k) { return x.K[k * row + d0 + col]; };
-      dq_h[i] = product(dq_h[i], kPiece, [&](uint32_t k) { return x.B[(r + col) * kPieceRow + k]; }, key);
-      const Tile bQ = product(Tile{}, kPiece, [&](uint32_t k) { return x.B[k * kPieceRow + r + col]; }, [&](uint32_t k) { return x.Q[k * row + d0 + col]; });
-      const Tile cK = product(Tile{}, kPiece, [&](uint32_t k) { return x.C[(r + col) * kPieceRow + k] + x.C[k * kPieceRow + r + col]; }, key);
-      dk_all[i] += bQ - cK;
-      dq_all[i] += dq_h[i];
+    for (uint32_t i = 0; i < KS; ++i) {
+      const Tile begin = *reinterpret_cast<const Tile *>(&x.gates.begin[state_row(r0 + i, 0)]);
+      const Tile end = *reinterpret_cast<const Tile *>(&x.gates.end[state_row(r0 + i, 0)]);
+      oS[i] = a.scale * passed(oS[i], begin);
+      uS[i] = scaled(uS[i], end);
+      if (own_d < a.Dk) {
 #pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) of_g[e] += x.Q[(r + quad + e) * row + d0 + col] * dq_h[i][e];
+        for (uint32_t e = 0; e < 4; ++e) at_end += (double)uS[i][e] * (float)k_rows[min(state_row(r0 + i, e), have - 1) * a.k_time + own_d];
+      }
+      dk_all[i] += uS[i] - passed(vS[i], begin);
+    }
+#pragma unroll
+    for (uint32_t ks = 0; ks < 2; ++ks) {
+      const Operand<kPartsOf<T>> key = operand<T>(*reinterpret_cast<const Run<T, 8> *>(kt + ks * kOperand));
+      const Operand<kPartsOf<T>> query = operand<T>(*reinterpret_cast<const Run<T, 8> *>(qt + ks * kOperand));
+#pragma unroll
+      for (uint32_t i = 0; i < KS; ++i) {
+        const uint32_t r = r0 + i, t = tile_row(r, m), j = ks * 32 + q * 8;
+        const bool lower = ks <= r / 2, upper = ks >= r / 2;  // (of the matrix: what lies there is not all zeros)
+        float f[8];
+        if (lower) {
+#pragma unroll
+          for (uint32_t e = 0; e < 8; ++e) f[e] = x.B[0][t * kPieceRow + j + e];
+          multiply<3>(oS[i], split<3>(f), key);
+        }
+        if (upper) {
+#pragma unroll
+          for (uint32_t e = 0; e < 8; ++e) f[e] = x.B[0][(j + e) * kPieceRow + t];
+          multiply<3>(dk_all[i], split<3>(f), query);
+        }
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) f[e] = -((lower ? x.B[1][t * kPieceRow + j + e] : 0.0f) + (upper ? x.B[1][(j + e) * kPieceRow + t] : 0.0f));
+        multiply<3>(dk_all[i], split<3>(f), key);
+      }
     }
     at_end = wave_sum(at_end);
     if (lane == 0) x.at_end[wave] = at_end;
 #pragma unroll
-    for (uint32_t e = 0; e < 4; ++e) {
-      const uint32_t t = r + quad + e;
-      const float g = row_sum(of_g[e]), v = row_sum(of_v[e]), beta = row_sum(of_beta[e]);
-      if (col == 0) x.of_g[half][t] = g, x.of_v[half][t] = v, x.of_beta[half][t] = beta;
+    for (uint32_t i = 0; i < KS; ++i) {
+      dq_all[i] += oS[i];
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) {
+        const uint32_t t = state_row(r0 + i, e);
+        const float g = row_sum(own_d < a.Dk ? (float)q_rows[min(t, have - 1) * a.q_time + own_d] * oS[i][e] : 0.0f);
+        if (m == 0) x.of_g[own][t] = g;
+      }
     }
     __syncthreads();
-    if (threadIdx.x < steps) {
-      const uint32_t t = threadIdx.x;
-      const uint64_t at = gates_at + (uint64_t)t * a.H + h;
-      double sum = 0.0;
-      for (uint32_t i = t; i < kPiece && x.gates.episode[i] == x.gates.episode[t]; ++i)
-        sum += (double)x.of_g[0][i] + x.of_g[1][i] - ((double)x.of_v[0][i] + x.of_v[1][i]);
-      if (x.gates.episode[t] == x.gates.episode[kPiece - 1])
-        for (uint32_t w = 0; w < kGradWaves; ++w) sum += x.at_end[w];
-      const bool have = t0 + t < len;
-      b.dg[at] = have && !x.gates.cut[t] ? (float)sum : 0.0f;
-      b.dbeta[at] = have ? x.of_beta[0][t] + x.of_beta[1][t] : 0.0f;
+    if (wave == 0) {
+      const uint32_t t = lane, episode = x.gates.episode[t];
+      double sum = 0.0, to_end = 0.0;
+      float beta = 0.0f;
+      if (t < have)
+        for (uint32_t n = 0; n < 2 * KS; ++n) sum += x.of_g[n][t];
+      for (uint32_t n = 0; n < kGradWaves; ++n) {
+        if (t < have) sum -= x.of_v[n][t];
+        beta += x.of_beta[n][t];
+        to_end += x.at_end[n];
+      }
+      // from t to the end of its episode
+      for (uint32_t d = 1; d < kPiece; d *= 2) {
+        const double next = __shfl_down(sum, d);
+        const uint32_t its = __shfl_down(episode, d);
+        if (t + d < kPiece && its == episode) sum += next;
+      }
+      if (episode == x.gates.episode[kPiece - 1]) sum += to_end;
+      if (t < steps) {
+        const uint64_t at = gates_at + (uint64_t)t * a.H + h;
+        b.dg[at] = t < have && !x.gates.cut[t] ? (float)sum : 0.0f;
+        b.dbeta[at] = t < have ? beta : 0.0f;
+      }
     }
   }
+  const uint32_t own_d = tile_row(own, lane % 16);
+  if (own_d >= a.Dk) return;
 #pragma unroll
-  for (uint32_t i = 0; i < kMaxTiles; ++i) {
-    const uint32_t d = (2 * i + half) * 16 + col;
-    if (d >= a.Dk) continue;
+  for (uint32_t i = 0; i < KS; ++i)
 #pragma unroll
     for (uint32_t e = 0; e < 4; ++e) {
-      const uint32_t t = r + quad + e;
+      const uint32_t t = state_row(r0 + i, e);
       if (t >= steps) continue;
-      dq[t * b.dq_time + d] = t0 + t < len ? (T)dq_all[i][e] : (T)0.0f;
-      dk[t * b.dk_time + d] = t0 + t < len ? (T)dk_all[i][e] : (T)0.0f;
+      dq[t * b.dq_time + own_d] = t < have ? (T)dq_all[i][e] : (T)0.0f;
+      dk[t * b.dk_time + own_d] = t < have ? (T)dk_all[i][e] : (T)0.0f;
     }
-  }
 }
 
 // ---- few steps: one after the other, the state in registers.  A workgroup has 64 columns of a state, a thread 8 rows of 4 of
@@ -1147,7 +1297,7 @@ void with_width(uint32_t Dk, F f)
 }
 
 struct DeltaBytes {
-  uint64_t gates, M, P, Kt, Qt, whole, dS, Y, bytes;
+  uint64_t gates, M, P, Kt, Qt, rows, dS, Y, bytes;
 };
 
 int delta_sizes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, bool backward, DeltaBytes *n)
@@ -1171,7 +1321,7 @@ int delta_sizes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, bo
   n->Kt = take(columns);
   if (backward) {
     n->Qt = take(columns);
-    n->whole = take(heads * kPiece * kPiece * 4);
+    n->rows = take(heads * kTriangle * 3 * kOperand * 2);
     n->dS = take(heads * Dk * Dv * 4);
     n->Y = take((uint64_t)S * T * H * Dv * 4);
   }
@@ -1181,8 +1331,8 @@ int delta_sizes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, bo
 Prepared delta_prepared(const DeltaBytes &n, void *workspace)
 {
   char *const p = static_cast<char *>(workspace);
-  return Prepared{reinterpret_cast<float *>(p + n.gates), reinterpret_cast<__bf16 *>(p + n.M), reinterpret_cast<__bf16 *>(p + n.P), p + n.Kt, p + n.Qt,
-                  reinterpret_cast<float *>(p + n.whole)};
+  return Prepared{reinterpret_cast<uint32_t *>(p + n.gates), reinterpret_cast<__bf16 *>(p + n.M), reinterpret_cast<__bf16 *>(p + n.P), p + n.Kt, p + n.Qt,
+                  reinterpret_cast<__bf16 *>(p + n.rows)};
 }
 
 // Workgroups of the kernels that go from piece to piece: eight heads' slices of 16 columns at a time.
@@ -1262,7 +1412,7 @@ int apex_delta_rule_backward(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, ui
   DeltaBack b{{S, T, Hk, H, Dk, Dv, blocks_for(T, kPiece), Hk ? H / Hk : 0, q_seq_stride, q_time_stride, k_seq_stride, k_time_stride,
                v_seq_stride, v_time_stride, q, k, v, g, beta, scale, discount, length},
               carry, d_o, dh_last, dq_seq_stride, dq_time_stride, dk_seq_stride, dk_time_stride, dv_seq_stride, dv_time_stride, dq, dk, dv, dg,
-              dbeta, dh0, reinterpret_cast<const float *>(space + n.whole), reinterpret_cast<float *>(space + n.dS), reinterpret_cast<float *>(space + n.Y)};
+              dbeta, dh0, reinterpret_cast<float *>(space + n.dS), reinterpret_cast<float *>(space + n.Y)};
   if (const int rc = delta_check(b.n, dtype)) return rc;
   const uint32_t size = element_size(dtype);
   if (!carry || !d_o || !dg || !dbeta || !workspace || (uintptr_t)workspace % 256 || (uintptr_t)d_o % size ||
@@ -1279,8 +1429,11 @@ int apex_delta_rule_backward(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, ui
       constexpr uint32_t KS = decltype(width)::value;
       delta_prepare_kernel<E, KS, true><<<dim3(S * b.n.pieces * H), dim3(kDeltaThreads), 0, stream>>>(b.n, w);
       delta_pieces_back_kernel<E, KS><<<dim3(delta_slices(S, H, Dv)), dim3(2 * kWave), 0, stream>>>(b, w);
+      if (Dv % 32)
+        delta_gradients_kernel<E, KS, false><<<dim3(S * b.n.pieces * Hk), dim3(kGradThreads), 0, stream>>>(b, w);
+      else
+        delta_gradients_kernel<E, KS, true><<<dim3(S * b.n.pieces * Hk), dim3(kGradThreads), 0, stream>>>(b, w);
     });
-    delta_gradients_kernel<E><<<dim3(S * b.n.pieces * Hk), dim3(kGradThreads), 0, stream>>>(b);
   });
   APEX_HIP(hipGetLastError());
   return APEX_OK;
