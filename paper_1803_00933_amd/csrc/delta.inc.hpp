@@ -56,7 +56,7 @@ struct DeltaBack {
   uint64_t dq_seq, dq_time, dk_seq, dk_time, dv_seq, dv_time;
   void *dq, *dk, *dv;
   float *dg, *dbeta, *dh0;
-  float *dS;  // [S][pieces][H][Dk][Dv]: of the state behind a piece
+  float *dS;  // [S][pieces][H]: of the state behind a piece, by 16 columns
   float *Y;   // [S][T][H][Dv]
 };
 
@@ -73,7 +73,7 @@ __device__ __forceinline__ bool delta_passes(const DeltaArgs &a, uint32_t s, uin
 }
 
 // What a piece's steps have of their gates, in LDS.  Steps that a sequence does not have: g = beta = 0.
-struct Gates {
+struct alignas(16) Gates {
   double G[kPiece];       // sum of g log2(e) from the piece's begin on: differences of 32-bit sums would lose what is small beside them
   uint32_t episode[kPiece];  // episodes that ended in the piece in front of the step or on its begin
   float beta[kPiece], begin[kPiece], end[kPiece];  // strength; what is left of the start state, and of the step at the end
@@ -111,7 +111,8 @@ __device__ __forceinline__ void load_gates(const DeltaArgs &a, uint32_t s, uint3
 // D of a step t and an earlier one.
 __device__ __forceinline__ float decay(const Gates &x, uint32_t t, uint32_t i)
 {
-  return x.episode[t] == x.episode[i] ? exp2_of((float)(x.G[t] - x.G[i])) : 0.0f;
+  const float d = exp2_of((float)(x.G[t] - x.G[i]));
+  return x.episode[t] == x.episode[i] ? d : 0.0f;
 }
 
 // ---- products.  Matrix instructions take numbers of 8 bits (bf16), 16 times as many as of 32 bits, so a 32-bit number is the sum
@@ -187,7 +188,7 @@ __device__ __forceinline__ Operand<N> operand_of(const Tile &x, const Tile &y)
 }
 
 // ---- what does not depend on a state, for every piece: its gates, M and P (or their transposes) and, by the first of the value
-// heads that share them, the keys' (and queries') transposes, in the order in which the kernels behind take them as left operands:
+// heads that share them, the keys and queries and their transposes, in the order in which the kernels behind take them as operands:
 // 64 lanes times 8 numbers, lane l has row l % 16 of the tile and numbers 8 (l / 16) .. + 7 of the 32.
 constexpr uint32_t kOperand = 64 * 8;                         // numbers
 constexpr uint32_t kTriangle = 6;                             // operands of a triangular matrix: 4 tiles of rows by 2 of 32 steps, less 2
@@ -198,7 +199,8 @@ static_assert(sizeof(Gates) <= kGateWords * 4);
 struct Prepared {
   uint32_t *gates;   // [heads][kGateWords]: Gates
   __bf16 *M, *P;     // [heads][kTriangle][3][kOperand]
-  void *Kt, *Qt;     // [key heads][2 KS][2][kOperand] of the inputs' type
+  void *K, *Q;       // [key heads][4][KS][kOperand] of the inputs' type: keys and queries
+  void *Kt, *Qt;     // [key heads][2 KS][2][kOperand]: their transposes
   __bf16 *rows;      // M beside its transpose (for the gradient)
 };
 
@@ -239,7 +241,8 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
 {
   constexpr uint32_t kRaw = KS * 32 + 16 / sizeof(T);  // (rows begin on 16 bytes)
   __shared__ Gates gates;
-  __shared__ float L[kPiece * kPieceRow], P[kPiece * kPieceRow], inverse[4][16][17];
+  __shared__ __align__(16) float L[kPiece * kPieceRow], P[kPiece * kPieceRow];
+  __shared__ float inverse[4][16][17];
   __shared__ __align__(16) T raw[kBack ? 2 : 1][kPiece][kRaw];
   const uint32_t h = blockIdx.x % a.H, piece = blockIdx.x / a.H % a.pieces, s = blockIdx.x / a.H / a.pieces, hk = h / a.share;
   const uint32_t len = delta_length(a, s), t0 = piece * kPiece;
@@ -285,7 +288,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
 #pragma unroll
     for (uint32_t e = 0; e < 4; ++e) {
       const uint32_t t = wave * 16 + q * 4 + e, j = c * 16 + m;
-      const float d = j <= t ? decay(gates, t, j) : 0.0f;
+      const float d = decay(gates, t, j);
       L[t * kPieceRow + j] = j < t ? kk[e] * d : 0.0f;
       P[t * kPieceRow + j] = j <= t ? qk[e] * d : 0.0f;
     }
@@ -358,6 +361,21 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
       for (uint32_t e = 0; e < 8; ++e) x[e] = raw[which][t + e][d];
       T *const to = static_cast<T *>(which ? w.Qt : w.Kt) + ((key_head * 2 * KS + tile) * 2 + ks) * kOperand + l * 8;
       *reinterpret_cast<Run<T, 8> *>(to) = x;
+    }
+    // rows: of keys, and forwards of queries, too
+    for (uint32_t i = threadIdx.x; i < 4 * KS * kWave; i += kDeltaThreads) {
+      const uint32_t l = i % kWave, at = (i / kWave % KS) * 32 + l / 16 * 8;
+      Run<T, 8> x;
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e) x[e] = raw[0][tile_row(i / kWave / KS, l % 16)][at + e];
+      *reinterpret_cast<Run<T, 8> *>(static_cast<T *>(w.K) + key_head * (4 * KS * kOperand) + i / kWave * kOperand + l * 8) = x;
+    }
+    if (!kBack) {
+#pragma unroll
+      for (uint32_t i = 0; i < KS; ++i) {  // (this wave's rows, in tiles of 16 steps as they follow one another: row t is row m of tile r)
+        const uint32_t t = wave * 16 + m, r = t / 32 * 2 + t / 4 % 2, row = t / 8 % 4 * 4 + t % 4;
+        *reinterpret_cast<Run<T, 8> *>(static_cast<T *>(w.Q) + key_head * (4 * KS * kOperand) + (r * KS + i) * kOperand + (q * 16 + row) * 8) = q_own[i];
+      }
     }
   }
 }
@@ -490,33 +508,16 @@ __device__ __forceinline__ void each_step(T *piece, uint64_t stride, uint32_t ha
       }
   }
 }
-template <typename T, uint32_t KS>
-struct PieceKeys {  // rows of keys or queries as left operands
-  Run<T, 8> x[4][KS];
-  __device__ __forceinline__ void load(const T *piece, uint64_t stride, uint32_t have, uint32_t width)
+template <typename T, uint32_t KS, uint32_t kTiles = 4>
+struct PieceKeys {  // rows of keys or queries, prepared: tiles of steps from `first` on
+  Run<T, 8> x[kTiles][KS];
+  __device__ __forceinline__ void load(const void *from, uint64_t key_head, uint32_t first = 0)
   {
-    const uint32_t m = lane_id() % 16, q = lane_id() / 16;
-    if (have == kPiece && stride <= kNearStride && width == KS * 32) {
-      const uint32_t offset = ((m / 4 * 8 + m % 4) * (uint32_t)stride + q * 8) * sizeof(T);
+    const T *const p = static_cast<const T *>(from) + (key_head * 4 + first) * KS * kOperand + lane_id() * 8;
 #pragma unroll
-      for (uint32_t i = 0; i < 4; ++i)
+    for (uint32_t i = 0; i < kTiles; ++i)
 #pragma unroll
-        for (uint32_t s = 0; s < KS; ++s)
-          x[i][s] = load_run<T, 8>(reinterpret_cast<const T *>(reinterpret_cast<const char *>(piece + (i / 2 * 32 + i % 2 * 4) * stride + s * 32) + offset));
-    } else {
-      const uint32_t row = anew(m), d = anew(q * 8);
-      if (width == KS * 32) {
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i)
-#pragma unroll
-          for (uint32_t s = 0; s < KS; ++s) x[i][s] = load_run<T, 8>(piece + min(tile_row(i, row), have - 1) * stride + s * 32 + d);
-      } else {
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i)
-#pragma unroll
-          for (uint32_t s = 0; s < KS; ++s) x[i][s] = load_eight<T>(piece + min(tile_row(i, row), have - 1) * stride, s * 32 + d, width);
-      }
-    }
+      for (uint32_t s = 0; s < KS; ++s) x[i][s] = *reinterpret_cast<const Run<T, 8> *>(p + (i * KS + s) * kOperand);
   }
 };
 template <typename T, uint32_t KS>
@@ -559,15 +560,26 @@ struct PieceTriangle {
 __device__ __forceinline__ uint32_t state_row(uint32_t tile, uint32_t e) { return tile_row(tile, lane_id() / 16 * 4 + e); }
 
 template <uint32_t KS>
-__device__ __forceinline__ void load_state(Tile (&S)[2 * KS], const float *from, uint32_t Dk, uint32_t Dv, bool column)
+__device__ __forceinline__ void load_state(Tile (&S)[2 * KS], const float *from, uint32_t Dk, uint32_t Dv, uint32_t c0)
 {
+  const uint32_t q = lane_id() / 16, c = c0 + lane_id() % 16;
+  if (Dk == KS * 32 && c0 + 16 <= Dv) {
+    const uint32_t offset = (q * 8 * Dv + c) * 4;
 #pragma unroll
-  for (uint32_t i = 0; i < 2 * KS; ++i)
+    for (uint32_t i = 0; i < 2 * KS; ++i)
 #pragma unroll
-    for (uint32_t e = 0; e < 4; ++e) {
-      const uint32_t d = state_row(i, e);
-      S[i][e] = from && column && d < Dk ? from[(uint64_t)d * Dv] : 0.0f;
-    }
+      for (uint32_t e = 0; e < 4; ++e) S[i][e] = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(from + (i / 2 * 32 + i % 2 * 4 + e) * Dv) + offset);
+  } else {
+    const uint32_t m = anew(q * 4);
+#pragma unroll
+    for (uint32_t i = 0; i < 2 * KS; ++i)
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) {
+        const uint32_t d = tile_row(i, m + e);
+        const float x = from[min(d, Dk - 1) * Dv + min(c, Dv - 1)];
+        S[i][e] = d < Dk && c < Dv ? x : 0.0f;
+      }
+  }
 }
 template <uint32_t KS>
 __device__ __forceinline__ void store_state(const Tile (&S)[2 * KS], float *to, uint32_t Dk, uint32_t Dv, uint32_t c0)
@@ -590,16 +602,34 @@ __device__ __forceinline__ void store_state(const Tile (&S)[2 * KS], float *to, 
       }
   }
 }
-// A state of which the three parts are held: their sum is exact.
+// States that only these kernels read (the carry and its gradient) lie by 16 columns, [ceil(Dv / 16)][Dk][16]: what a wave reads or
+// writes of them is in one place.  (By rows of Dv, 64 bytes out of every 512 were asked for at a time, which is a quarter of the
+// channels of an L2 cache: the gradient of 4 x 8192 steps of 16 heads 1.74 ms, by columns XXXX.)
+__device__ __forceinline__ uint64_t slices_size(uint32_t Dk, uint32_t Dv) { return (uint64_t)((Dv + 15) / 16) * Dk * 16; }
+
+// A state of which the three parts are held: their sum is exact.  Zeros beyond the columns.
 template <uint32_t KS>
-__device__ __forceinline__ void store_parts(const Operand<3> (&S)[KS], float *to, uint32_t Dk, uint32_t Dv, uint32_t c0)
+__device__ __forceinline__ void store_slice(const Operand<3> (&S)[KS], float *to, uint32_t Dk, uint32_t slice, bool column)
 {
-  Tile x[2 * KS];
+  const uint32_t q = lane_id() / 16, m = lane_id() % 16;
+  float *const lane_to = to + (uint64_t)slice * Dk * 16 + (q * 8 * 16 + m);
 #pragma unroll
   for (uint32_t s = 0; s < KS; ++s)
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) x[2 * s + e / 4][e % 4] = ((float)S[s].part[2][e] + (float)S[s].part[1][e]) + (float)S[s].part[0][e];
-  store_state<KS>(x, to, Dk, Dv, c0);
+    for (uint32_t e = 0; e < 8; ++e) {
+      const float x = ((float)S[s].part[2][e] + (float)S[s].part[1][e]) + (float)S[s].part[0][e];
+      if (Dk == KS * 32 || s * 32 + q * 8 + e < Dk) lane_to[(s * 32 + e) * 16] = column ? x : 0.0f;
+    }
+}
+template <uint32_t KS>
+__device__ __forceinline__ void load_slice(Tile (&S)[2 * KS], const float *from, uint32_t Dk, uint32_t slice)
+{
+  const uint32_t q = lane_id() / 16, m = lane_id() % 16;
+  const float *const lane_from = from + (uint64_t)slice * Dk * 16 + m;
+#pragma unroll
+  for (uint32_t s = 0; s < KS; ++s)
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) S[2 * s + e / 4][e % 4] = lane_from[min(s * 32 + q * 8 + e, Dk - 1) * 16];  // (keys beyond are 0)
 }
 
 // What the next piece takes is asked for as soon as this one has taken its own: in the same registers, which a wave has 512 of.
@@ -620,17 +650,16 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_kernel(DeltaForward f,
   const auto head_of = [&](uint32_t piece) { return ((uint64_t)s * a.pieces + piece) * a.H + h; };
   const auto have_of = [&](uint32_t piece) { return min(kPiece, len - piece * kPiece); };
   if (carries) {
-    const T *const k_rows = static_cast<const T *>(a.k) + s * a.k_seq + (uint64_t)hk * a.Dk;
     const T *const v_rows = static_cast<const T *>(a.v) + s * a.v_seq + (uint64_t)h * a.Dv;
-    Tile S[2 * KS];
-    load_state<KS>(S, f.h0 ? f.h0 + state + c : nullptr, a.Dk, a.Dv, column);
+    Tile S[2 * KS] = {};
+    if (f.h0) load_state<KS>(S, f.h0 + state, a.Dk, a.Dv, place.c0);
     PieceKeys<T, KS> K;
     PieceColumn<T> V;
     PieceTriangle<3> M;
     PieceColumns<T, KS> Kt;
     AllGates gates;
     const auto load_keys = [&](uint32_t piece) {
-      K.load(k_rows + (uint64_t)piece * kPiece * a.k_time, a.k_time, have_of(piece), a.Dk);
+      K.load(w.K, ((uint64_t)s * a.pieces + piece) * a.Hk + hk);
       V.load(v_rows + (uint64_t)piece * kPiece * a.v_time, a.v_time, have_of(piece), min(c, a.Dv - 1));
     };
     const auto load_columns = [&](uint32_t piece) {
@@ -680,14 +709,13 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_kernel(DeltaForward f,
       store_state<KS>(S, f.h_last + state, a.Dk, a.Dv, place.c0);
     }
   } else {
-    const T *const q_rows = static_cast<const T *>(a.q) + s * a.q_seq + (uint64_t)hk * a.Dk;
     T *const o = static_cast<T *>(f.o) + ((uint64_t)s * a.T * a.H + h) * a.Dv;
     const uint64_t o_row = (uint64_t)a.H * a.Dv;
     PieceKeys<T, KS> Q;
     PieceTriangle<3> P;
     RowGates begin;
     const auto load = [&](uint32_t piece) {
-      Q.load(q_rows + (uint64_t)piece * kPiece * a.q_time, a.q_time, have_of(piece), a.Dk);
+      Q.load(w.Q, ((uint64_t)s * a.pieces + piece) * a.Hk + hk);
       P.load(w.P, head_of(piece));
       begin = row_gates(gates_of(w, head_of(piece)).begin);
     };
@@ -709,7 +737,7 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_kernel(DeltaForward f,
       const Operand<3> U[2] = {operand_of<3>(found[0][lane], found[1][lane]), operand_of<3>(found[2][lane], found[3][lane])};
       P.template times<3, false>(O, U);
       if (kAhead) load(min(piece + 1, pieces - 1));
-      if (f.carry) store_parts<KS>(S, f.carry + head_of(piece) * a.Dk * a.Dv, a.Dk, a.Dv, place.c0);
+      if (f.carry) store_slice<KS>(S, f.carry + head_of(piece) * slices_size(a.Dk, a.Dv), a.Dk, place.c0 / 16, column);
       if (column)
         each_step(o + (uint64_t)piece * kPiece * o_row, o_row, have_of(piece), c, [&](uint32_t r, uint32_t e, T *to) { *to = (T)(a.scale * O[r][e]); });
     }
@@ -741,15 +769,13 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_back_kernel(DeltaBack 
   const auto key_head_of = [&](uint32_t piece) { return ((uint64_t)s * a.pieces + piece) * a.Hk + hk; };
   const auto have_of = [&](uint32_t piece) { return min(kPiece, len - piece * kPiece); };
   if (carries) {
-    const T *const k_rows = static_cast<const T *>(a.k) + s * a.k_seq + (uint64_t)hk * a.Dk;
-    Tile S[2 * KS];
-    const bool passes = len == 0 || delta_passes(a, s, len - 1);
-    load_state<KS>(S, b.dh_last && passes ? b.dh_last + state + c : nullptr, a.Dk, a.Dv, column);
+    Tile S[2 * KS] = {};
+    if (b.dh_last && (len == 0 || delta_passes(a, s, len - 1))) load_state<KS>(S, b.dh_last + state, a.Dk, a.Dv, place.c0);
     PieceKeys<T, KS> K;
     PieceTriangle<3> M;
     PieceColumns<T, KS> Kt;
     AllGates gates;
-    const auto load_keys = [&](uint32_t piece) { K.load(k_rows + (uint64_t)piece * kPiece * a.k_time, a.k_time, have_of(piece), a.Dk); };
+    const auto load_keys = [&](uint32_t piece) { K.load(w.K, key_head_of(piece)); };
     const auto load_columns = [&](uint32_t piece) {
       Kt.load(w.Kt, key_head_of(piece));
       gates = all_gates(gates_of(w, head_of(piece)));
@@ -843,7 +869,7 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_back_kernel(DeltaBack 
       Operand<3> S[KS];
 #pragma unroll
       for (uint32_t i = 0; i < KS; ++i) S[i] = get<3>(states[piece % 2][i]);
-      store_parts<KS>(S, b.dS + head * a.Dk * a.Dv, a.Dk, a.Dv, place.c0);
+      store_slice<KS>(S, b.dS + head * slices_size(a.Dk, a.Dv), a.Dk, place.c0 / 16, column);
       const RowGates beta = row_gates(gates_of(w, head).beta);
       Tile y[4];
 #pragma unroll
@@ -876,23 +902,26 @@ constexpr uint32_t kGradThreads = 512, kGradWaves = kGradThreads / kWave, kGradR
 
 struct GradSpace {
   Gates gates;
-  union {
-    __bf16 part[2][3][kPiece][kGradRow];  // U, dV
+  union alignas(16) {  // (eight at a time: at half the alignment a read of them took eight times as long)
+    __bf16 part[2][3][kPiece][kGradRow];  // U, dV; zeros beyond the state's columns
     float B[2][kPiece * kPieceRow];       // B, C
   };
-  float of_g[kGradWaves][kPiece], of_v[kGradWaves][kPiece], of_beta[kGradWaves][kPiece];  // sums over a wave's share
+  alignas(16) float of_g[kGradWaves][kPiece], of_v[kGradWaves][kPiece], of_beta[kGradWaves][kPiece];  // sums over a wave's share
   double at_end[kGradWaves];
 };
 static_assert(kDeltaMaxWidth == 16 * kGradWaves);
 
-// The sum over the 16 lanes of a row of a tile, in each of them.
+// The sum over the 16 lanes of a row of a tile, in each of them: rotated by 8, 4, 2 and 1 lanes.
 __device__ __forceinline__ float row_sum(float v)
 {
-  for (int d = 1; d < 16; d *= 2) v += __shfl_xor(v, d);
-  return v;
+  v += dpp_from<0x128, 0xf>(v, 0.0f);
+  v += dpp_from<0x124, 0xf>(v, 0.0f);
+  v += dpp_from<0x122, 0xf>(v, 0.0f);
+  return v + dpp_from<0x121, 0xf>(v, 0.0f);
 }
 
-// A 32-bit number's parts.
+// A 32-bit number's parts, and eight numbers of a row as an operand.  Row: 16 times the tile of steps, and its row of that (neighbours
+// are 4 banks apart, whatever steps they are).
 __device__ __forceinline__ void put_parts(__bf16 (*part)[kPiece][kGradRow], uint32_t t, uint32_t c, float x)
 {
 #pragma unroll
@@ -936,45 +965,51 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
   const T *const q_rows = static_cast<const T *>(a.q) + s * a.q_seq + t0 * a.q_time + (uint64_t)hk * a.Dk;
   const uint64_t o_row = (uint64_t)a.H * a.Dv, key_head = ((uint64_t)s * a.pieces + piece) * a.Hk + hk;
   // this wave's tile of the state's rows, and its first tile of steps
-  const uint32_t own = wave % (2 * KS), r0 = wave / (2 * KS) * KS;
+  static_assert(KS == 2 || KS == 4);
+  const uint32_t own = KS == 4 ? wave : wave % 4, r0 = KS == 4 ? 0 : wave / 4 * 2;
   Tile dq_all[KS] = {}, dk_all[KS] = {};
 #pragma unroll 1
   for (uint32_t h = hk * a.share; h < (hk + 1) * a.share; ++h) {
     const uint64_t head = ((uint64_t)s * a.pieces + piece) * a.H + h;
     const uint32_t m = anew(lane % 16), q = anew(lane / 16), own_d = tile_row(own, m);
     const auto state_row = [&](uint32_t tile, uint32_t e) { return tile_row(tile, q * 4 + e); };
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < sizeof(Gates) / 4; i += kGradThreads) reinterpret_cast<uint32_t *>(&x.gates)[i] = w.gates[head * kGateWords + i];
-    __syncthreads();
-    const float *const S0 = b.carry + head * a.Dk * a.Dv, *const dS = b.dS + head * a.Dk * a.Dv;
+    const float *const S0 = b.carry + head * slices_size(a.Dk, a.Dv), *const dS = b.dS + head * slices_size(a.Dk, a.Dv);
     const T *const v_rows = static_cast<const T *>(a.v) + s * a.v_seq + t0 * a.v_time + (uint64_t)h * a.Dv;
     const T *const o_rows = static_cast<const T *>(b.d_o) + gates_at * a.Dv + (uint64_t)h * a.Dv;
     const float *const y_rows = b.Y + gates_at * a.Dv + (uint64_t)h * a.Dv;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < sizeof(Gates) / 4; i += kGradThreads) reinterpret_cast<uint32_t *>(&x.gates)[i] = w.gates[head * kGateWords + i];
+    __syncthreads();
     {
       const uint32_t column = wave * 16 + m, c = min(column, a.Dv - 1);
       Tile U[4] = {}, Y[4] = {}, of_v[4] = {}, of_beta[4] = {};
       if (wave * 16 < a.Dv) {
         Tile kS[4] = {}, S[2 * KS];
-#pragma unroll
-        for (uint32_t i = 0; i < 2 * KS; ++i)
-#pragma unroll
-          for (uint32_t e = 0; e < 4; ++e) S[i][e] = S0[min(state_row(i, e), a.Dk - 1) * a.Dv + c];
-        PieceKeys<T, KS> K;
-        K.load(k_rows, a.k_time, have, a.Dk);
+        load_slice<KS>(S, S0, a.Dk, wave);
+        // (half of the keys at a time, and so on: a wave has 256 registers here)
+        PieceKeys<T, KS, 2> K;
+        K.load(w.K, key_head);
+        Operand<3> parts[KS];
 #pragma unroll
         for (uint32_t i = 0; i < KS; ++i) {
-          const Operand<3> parts = operand_of<3>(S[2 * i], S[2 * i + 1]);
+          parts[i] = operand_of<3>(S[2 * i], S[2 * i + 1]);
 #pragma unroll
-          for (uint32_t r = 0; r < 4; ++r) multiply<3>(kS[r], operand<T>(K.x[r][i]), parts);
+          for (uint32_t r = 0; r < 2; ++r) multiply<3>(kS[r], operand<T>(K.x[r][i]), parts[i]);
         }
-        __builtin_amdgcn_sched_barrier(0);  // (what follows is asked for when the keys' registers are free)
-        const RowGates beta = row_gates(x.gates.beta), begin = row_gates(x.gates.begin);
+        __builtin_amdgcn_sched_barrier(0);
+        K.load(w.K, key_head, 2);
         PieceColumn<T> V;
         PieceColumn<float> y;
         V.load(v_rows, a.v_time, have, c);
         y.load(y_rows, o_row, have, c);
+#pragma unroll
+        for (uint32_t i = 0; i < KS; ++i)
+#pragma unroll
+          for (uint32_t r = 0; r < 2; ++r) multiply<3>(kS[2 + r], operand<T>(K.x[r][i]), parts[i]);
+        __builtin_amdgcn_sched_barrier(0);
         PieceTriangle<3> M;
         M.load(w.rows, head);
+        const RowGates beta = row_gates(x.gates.beta), begin = row_gates(x.gates.begin);
         Tile X[4], mX[4] = {};
 #pragma unroll
         for (uint32_t r = 0; r < 4; ++r) X[r] = V.tile(r) - passed(kS[r], begin.tile[r]);
@@ -996,56 +1031,99 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
       for (uint32_t r = 0; r < 4; ++r)
 #pragma unroll
         for (uint32_t e = 0; e < 4; ++e) {
-          const uint32_t t = state_row(r, e);
-          put_parts(x.part[0], t, column, U[r][e]);
-          put_parts(x.part[1], t, column, Y[r][e]);
-          const float v = row_sum(of_v[r][e]), beta = row_sum(of_beta[r][e]);
-          if (m == 0) x.of_v[wave][t] = v, x.of_beta[wave][t] = beta;
+          put_parts(x.part[0], r * 16 + q * 4 + e, column, U[r][e]);
+          put_parts(x.part[1], r * 16 + q * 4 + e, column, Y[r][e]);
+          of_v[r][e] = row_sum(of_v[r][e]), of_beta[r][e] = row_sum(of_beta[r][e]);
         }
+      if (m == 0) {
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r) {
+          *reinterpret_cast<Tile *>(&x.of_v[wave][state_row(r, 0)]) = of_v[r];
+          *reinterpret_cast<Tile *>(&x.of_beta[wave][state_row(r, 0)]) = of_beta[r];
+        }
+      }
     }
     __syncthreads();
-    Tile oS[KS] = {}, uS[KS] = {}, vS[KS] = {}, B[2] = {}, C[2] = {};
+    Tile oS[KS] = {}, uS[KS] = {}, vS[KS] = {};
     double at_end = 0.0;
-    // tiles of B and C: of 16, those four of later columns than rows left out
+    // what 32 columns take from memory, asked for 32 columns ahead
+    struct Taken {
+      Run<T, 8> o[KS];
+      Run<float, 8> start, end;
+    } next;
+    // (clamped: what is fetched beyond the widths meets zeros)
+    const auto eight = [&](auto *row, uint32_t c) {
+      typedef std::remove_cv_t<std::remove_pointer_t<decltype(row)>> E;
+      Run<E, 8> r;
+      if constexpr (kWhole) {
+        r = load_run<E, 8>(row + min(c, a.Dv - 8));
+      } else {
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) r[e] = row[min(c + e, a.Dv - 1)];
+      }
+      return r;
+    };
+    const uint32_t own_row = min(own_d, a.Dk - 1) * 16 + q % 2 * 8, slices = (a.Dv + 15) / 16;
+    const auto take = [&](uint32_t c0) {
+      const uint64_t at = (uint64_t)min(c0 / 16 + q / 2, slices - 1) * a.Dk * 16 + own_row;
+      next.start = *reinterpret_cast<const Run<float, 8> *>(S0 + at), next.end = *reinterpret_cast<const Run<float, 8> *>(dS + at);
+#pragma unroll
+      for (uint32_t i = 0; i < KS; ++i) next.o[i] = eight(o_rows + min(tile_row(r0 + i, m), have - 1) * o_row, c0 + q * 8);
+    };
+    take(0);
+#pragma unroll 1
+    for (uint32_t c0 = 0; c0 < a.Dv; c0 += 32) {
+      const uint32_t c = c0 + q * 8;
+      Taken now = next;
+      if (c0 + 32 < a.Dv) take(c0 + 32);
+      if (!kWhole && c >= slices * 16) now.start = Run<float, 8>{};  // (a slice that there is not)
+      const Operand<3> start = operand<float>(now.start), end = operand<float>(now.end);
+      if (x.gates.last != 0.0f && own_d < a.Dk && r0 == 0) {
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) at_end += (double)(x.gates.last * now.start[e]) * now.end[e];
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < KS; ++i) {
+        multiply<3>(oS[i], operand<T>(now.o[i]), start);
+        multiply<3>(uS[i], get_parts(x.part[0], (r0 + i) * 16 + m, c), end);
+        multiply<3>(vS[i], get_parts(x.part[1], (r0 + i) * 16 + m, c), start);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // B and C: of 16 tiles, those four of later columns than rows are left out; a wave has one, four waves another one
+    Tile B[2] = {}, C[2] = {};
     const auto tile_of = [&](uint32_t i, uint32_t *r, uint32_t *j) {
       const uint32_t f = wave + i * kGradWaves;
       *r = f < 4 ? f / 2 : 2 + (f - 4) / 4, *j = f < 4 ? f % 2 : (f - 4) % 4;
       return f < 12;
     };
-#pragma unroll 1
-    for (uint32_t c0 = 0; c0 < a.Dv; c0 += 32) {
-      const uint32_t c = c0 + q * 8, row = min(own_d, a.Dk - 1) * a.Dv;
-      Run<T, 8> o[KS], of_tile[2] = {};
-      const Run<float, 8> sr = load_step<float, kWhole>(S0 + row, 0, 0, 1, c, a.Dv), er = load_step<float, kWhole>(dS + row, 0, 0, 1, c, a.Dv);
+    Run<T, 8> of_tile[2][4];
 #pragma unroll
-      for (uint32_t i = 0; i < KS; ++i) o[i] = load_step<T, kWhole>(o_rows, o_row, tile_row(r0 + i, m), have, c, a.Dv);
+    for (uint32_t i = 0; i < 2; ++i) {
+      uint32_t r, j;
+      tile_of(i, &r, &j);
 #pragma unroll
-      for (uint32_t i = 0; i < 2; ++i) {
-        uint32_t r, j;
-        tile_of(i, &r, &j);
-        of_tile[i] = load_step<T, kWhole>(o_rows, o_row, tile_row(min(r, 3u), m), have, c, a.Dv);
-      }
-      const Operand<3> start = operand<float>(sr), end = operand<float>(er);
-      if (x.gates.last != 0.0f && own_d < a.Dk && r0 == 0) {
+      for (uint32_t n = 0; n < 4; ++n) of_tile[i][n] = eight(o_rows + min(tile_row(min(r, 3u), m), have - 1) * o_row, n * 32 + q * 8);
+    }
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) at_end += (double)(x.gates.last * sr[e]) * er[e];
-      }
+    for (uint32_t i = 0; i < 2; ++i) {
+      uint32_t r, j;
+      if (!tile_of(i, &r, &j)) continue;
 #pragma unroll
-      for (uint32_t i = 0; i < KS; ++i) {
-        const uint32_t t = tile_row(r0 + i, m);
-        multiply<3>(oS[i], operand<T>(o[i]), start);
-        multiply<3>(uS[i], get_parts(x.part[0], t, c), end);
-        multiply<3>(vS[i], get_parts(x.part[1], t, c), start);
-      }
-#pragma unroll
-      for (uint32_t i = 0; i < 2; ++i) {
-        uint32_t r, j;
-        if (!tile_of(i, &r, &j)) continue;
-        const Operand<3> u = get_parts(x.part[0], tile_row(j, m), c);
-        multiply<3>(B[i], operand<T>(of_tile[i]), u);
-        multiply<3>(C[i], get_parts(x.part[1], tile_row(r, m), c), u);
+      for (uint32_t n = 0; n < 4; ++n) {
+        const Operand<3> u = get_parts(x.part[0], j * 16 + m, n * 32 + q * 8);
+        multiply<3>(B[i], operand<T>(of_tile[i][n]), u);
+        multiply<3>(C[i], get_parts(x.part[1], r * 16 + m, n * 32 + q * 8), u);
       }
     }
+    T key_at[KS][4], query_at[KS][4];  // this lane's of the keys and queries, as tiles
+#pragma unroll
+    for (uint32_t i = 0; i < KS; ++i)
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) {
+        const uint64_t t = min(state_row(r0 + i, e), have - 1);
+        key_at[i][e] = k_rows[t * a.k_time + min(own_d, a.Dk - 1)], query_at[i][e] = q_rows[t * a.q_time + min(own_d, a.Dk - 1)];
+      }
     __syncthreads();
 #pragma unroll
     for (uint32_t i = 0; i < 2; ++i) {
@@ -1055,8 +1133,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
 #pragma unroll
       for (uint32_t e = 0; e < 4; ++e) {
         const uint32_t t = state_row(r, e);
-        const float d = j <= t ? decay(x.gates, t, j) : 0.0f;
-        x.B[0][t * kPieceRow + j] = j <= t ? a.scale * B[i][e] * d : 0.0f;
+        const float d = decay(x.gates, t, j);
+        x.B[0][t * kPieceRow + j] = j <= t && t < have ? a.scale * B[i][e] * d : 0.0f;
         x.B[1][t * kPieceRow + j] = j < t ? C[i][e] * d : 0.0f;
       }
     }
@@ -1069,10 +1147,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
       const Tile end = *reinterpret_cast<const Tile *>(&x.gates.end[state_row(r0 + i, 0)]);
       oS[i] = a.scale * passed(oS[i], begin);
       uS[i] = scaled(uS[i], end);
-      if (own_d < a.Dk) {
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) at_end += (double)uS[i][e] * (float)k_rows[min(state_row(r0 + i, e), have - 1) * a.k_time + own_d];
-      }
+      for (uint32_t e = 0; e < 4; ++e) at_end += own_d < a.Dk ? (double)uS[i][e] * (float)key_at[i][e] : 0.0;
       dk_all[i] += uS[i] - passed(vS[i], begin);
     }
 #pragma unroll
@@ -1101,15 +1177,16 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
     }
     at_end = wave_sum(at_end);
     if (lane == 0) x.at_end[wave] = at_end;
+    Tile of_g[KS];
 #pragma unroll
     for (uint32_t i = 0; i < KS; ++i) {
       dq_all[i] += oS[i];
 #pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) {
-        const uint32_t t = state_row(r0 + i, e);
-        const float g = row_sum(own_d < a.Dk ? (float)q_rows[min(t, have - 1) * a.q_time + own_d] * oS[i][e] : 0.0f);
-        if (m == 0) x.of_g[own][t] = g;
-      }
+      for (uint32_t e = 0; e < 4; ++e) of_g[i][e] = row_sum(own_d < a.Dk ? (float)query_at[i][e] * oS[i][e] : 0.0f);
+    }
+    if (m == 0) {
+#pragma unroll
+      for (uint32_t i = 0; i < KS; ++i) *reinterpret_cast<Tile *>(&x.of_g[own][state_row(r0 + i, 0)]) = of_g[i];
     }
     __syncthreads();
     if (wave == 0) {
@@ -1234,7 +1311,16 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_steps_kernel(DeltaForward
     }
 #pragma unroll
     for (uint32_t c = 0; c < C; ++c) v[c] = c0 + c < a.Dv ? (float)v_row[c] : 0.0f;
-    if (f.carry && t % kPiece == 0) store(f.carry + (((uint64_t)s * a.pieces + t / kPiece) * a.H + h) * a.Dk * a.Dv, passes);
+    if (f.carry && t % kPiece == 0 && c0 < (a.Dv + 15) / 16 * 16) {
+      float *const to = f.carry + (((uint64_t)s * a.pieces + t / kPiece) * a.H + h) * slices_size(a.Dk, a.Dv) + (uint64_t)(c0 / 16) * a.Dk * 16 + c0 % 16;
+#pragma unroll
+      for (uint32_t i = 0; i < kStepRows; ++i) {
+        Run<float, C> v;
+#pragma unroll
+        for (uint32_t c = 0; c < C; ++c) v[c] = passes && c0 + c < a.Dv ? S[i][c] : 0.0f;
+        if (d0 + i < a.Dk) *reinterpret_cast<Run<float, C> *>(to + (d0 + i) * 16) = v;
+      }
+    }
     const bool in = passes && keep != 0.0f;  // a selection: nothing of what has ended
     float kS[C] = {}, qS[C] = {}, qk = 0.0f;
 #pragma unroll
@@ -1297,7 +1383,7 @@ void with_width(uint32_t Dk, F f)
 }
 
 struct DeltaBytes {
-  uint64_t gates, M, P, Kt, Qt, rows, dS, Y, bytes;
+  uint64_t gates, M, P, K, Q, Kt, Qt, rows, dS, Y, bytes;
 };
 
 int delta_sizes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, bool backward, DeltaBytes *n)
@@ -1318,11 +1404,13 @@ int delta_sizes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, bo
   n->gates = take(heads * kGateWords * 4);
   n->M = take(heads * kTriangle * 3 * kOperand * 2);
   n->P = take(heads * kTriangle * 3 * kOperand * 2);
+  n->K = take(columns);
+  n->Q = take(columns);  // (the gradient takes no rows of queries, and has their transposes there)
+  n->Qt = n->Q;
   n->Kt = take(columns);
   if (backward) {
-    n->Qt = take(columns);
     n->rows = take(heads * kTriangle * 3 * kOperand * 2);
-    n->dS = take(heads * Dk * Dv * 4);
+    n->dS = take(heads * Dk * round_up(Dv, 16) * 4);
     n->Y = take((uint64_t)S * T * H * Dv * 4);
   }
   return APEX_OK;
@@ -1331,7 +1419,7 @@ int delta_sizes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, bo
 Prepared delta_prepared(const DeltaBytes &n, void *workspace)
 {
   char *const p = static_cast<char *>(workspace);
-  return Prepared{reinterpret_cast<uint32_t *>(p + n.gates), reinterpret_cast<__bf16 *>(p + n.M), reinterpret_cast<__bf16 *>(p + n.P), p + n.Kt, p + n.Qt,
+  return Prepared{reinterpret_cast<uint32_t *>(p + n.gates), reinterpret_cast<__bf16 *>(p + n.M), reinterpret_cast<__bf16 *>(p + n.P), p + n.K, p + n.Q, p + n.Kt, p + n.Qt,
                   reinterpret_cast<__bf16 *>(p + n.rows)};
 }
 

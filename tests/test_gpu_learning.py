@@ -230,7 +230,10 @@ def test_delta_state_in_place_and_in_pieces(apex, dtype):
         at += n
     assert at == 300
     c.check(dict(o=torch.cat(o, 1), h_last=state), want, names=("o", "h_last"))
-    check(c.run(apex)["carry"], want["carry"], plain.delta_bound("h_last", want, 40, 50)[:, None], torch.float32, "carry")
+    slices = c.run(apex)["carry"]                                      # [S,chunks,H,4,40,16]: by 16 columns
+    columns = slices.transpose(3, 4).reshape(2, 5, 2, 40, 64)
+    check(columns[..., :50], want["carry"], plain.delta_bound("h_last", want, 40, 50)[:, None], torch.float32, "carry")
+    assert (columns[..., 50:] == 0).all()
 
 
 def test_delta_same_bits(apex):

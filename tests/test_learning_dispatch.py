@@ -63,4 +63,4 @@ result = [clip([]), clip([0, 0]), clip([1]), clip([8192, 8193]), clip([10] * 200
     assert out[0] == out[1] == [["norm", 1]] and out[2] == [["norm", 1], ["scale", 1]] and out[3] == [["norm", 3], ["scale", 3]]
     assert out[4] == [["norm", 96], ["norm", 96], ["norm", 8], ["scale", 96], ["scale", 96], ["scale", 8]]
     assert out[5] == [["norm", 3]] and out[6] == [["norm", 3], ["scale", 3]]
-    assert out[7][0][1] <= 8192 + 2 and out[7][0] == ["norm", out[7][1][1]]
+    assert out[7][0][1] <= 2048 + 2 and out[7][0] == ["norm", out[7][1][1]]
