@@ -690,9 +690,9 @@ int apex_verify_draft(uint32_t B, uint32_t G, uint32_t V, int dtype, const void 
  * any whose exponential is 0 in 32 bits, cuts as an episode's end does) and the strength.  discount [S,T], length [S] as of
  * apex_gated_scan (may be NULL).  h0 [S,H,Dk,Dv] fp32 (NULL: zeros).
  * Outputs: o [S,T,H,Dv] of dtype, 0 for steps past a sequence's length, whose inputs are not looked at; h_last [S,H,Dk,Dv] fp32 =
- * c_{len-1} S_{len-1}, or h0 where len = 0 (may be NULL; may be h0); carry [S, ceil(T / APEX_DELTA_CHUNK), H, ceil(Dv / 16), Dk, 16]
- * fp32 (may be NULL): what passes into step t = c * APEX_DELTA_CHUNK, by 16 columns, zeros beyond Dv, for those t below the length,
- * the others are unspecified.  The gradient asks for it.
+ * c_{len-1} S_{len-1}, or h0 where len = 0 (may be NULL; may be h0); carry [S, ceil(T / APEX_DELTA_CHUNK), H, ceil(Dv / 16),
+ * ceil(Dk / 32), 8, 4, 16] fp32 (may be NULL): what passes into step t = c * APEX_DELTA_CHUNK, row 32 i + j + 8 k and column 16 l + m at
+ * [l, i, j, k, m], zeros beyond Dk and Dv, for those t below the length; the others are unspecified.  The gradient asks for it.
  * With T = 1 this is the step of an actor: state in, state out.
  * (Keys are meant to be of unit length, or no longer, and 0 <= beta <= 2, so that the recurrence does not grow.  Longer sequences
  * are computed in pieces of 64 steps by products of matrices, as sums of products in 32 bits: a NaN or an infinity among the inputs

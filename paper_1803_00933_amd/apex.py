@@ -330,7 +330,7 @@ def verify_draft(target, draft, token, rnd, length=None, out=None, workspace=Non
 
 
 def delta_rule_carry_shape(S, T, H, Dk, Dv):
-    return S, -(-T // DELTA_CHUNK), H, -(-Dv // 16), Dk, 16
+    return S, -(-T // DELTA_CHUNK), H, -(-Dv // 16), -(-Dk // 32), 8, 4, 16
 
 
 def delta_rule_workspace(S, T, H, Dk, Dv, backward=False, device="cuda:0"):

@@ -549,7 +549,7 @@ VERB(verify_draft, [](View target, View draft, View token, View rnd, View length
 struct DeltaSizes {
   int64_t S, T, Hk, H, Dk, Dv, state, slices, gates;
   DeltaSizes(const Heads &q, const Heads &k, const Heads &v)
-      : S(q.n[0]), T(q.n[1]), Hk(q.n[2]), H(v.n[2]), Dk(q.n[3]), Dv(v.n[3]), state(S * H * Dk * Dv), slices(S * H * Dk * ((Dv + 15) / 16 * 16)), gates(S * T * H)
+      : S(q.n[0]), T(q.n[1]), Hk(q.n[2]), H(v.n[2]), Dk(q.n[3]), Dv(v.n[3]), state(S * H * Dk * Dv), slices(S * H * ((Dk + 31) / 32 * 32) * ((Dv + 15) / 16 * 16)), gates(S * T * H)
   {
     require(q.dtype >= 0 && k.dtype == q.dtype && v.dtype == q.dtype, "q, k and v: of one floating type");
     require(k.fits(S, T, Hk, Dk) && v.n[0] == S && v.n[1] == T, "q and k: [S,T,Hk,Dk], v: [S,T,H,Dv]");
@@ -566,7 +566,7 @@ VERB(delta_rule, [](Heads q, Heads k, Heads v, State g, State beta, float scale,
                            g.of(n.gates, "g: fp32 [S,T,H]"), beta.of(n.gates, "beta: fp32 [S,T,H]"), scale,
                            floats(discount, n.S * n.T, "discount: fp32 [S,T]"), ints(length, n.S, "length: int32 [S]"),
                            h0.of(n.state, "h0: fp32 [S,H,Dk,Dv]"), o.p, h_last.of(n.state, "h_last: fp32 [S,H,Dk,Dv]"),
-                           carry.of(chunks * n.slices, "carry: fp32 [S,chunks,H,ceil(Dv/16),Dk,16]"),
+                           carry.of(chunks * n.slices, "carry: fp32, of delta_rule_carry_shape"),
                            workspace.of(p_apex_delta_rule_workspace_bytes, n.S, n.T, n.H, n.Dk, n.Dv, 0), s);
 })
 VERB(delta_rule_backward, [](Heads q, Heads k, Heads v, State g, State beta, float scale, View discount, View length, State carry, Heads d_o,
@@ -580,7 +580,7 @@ VERB(delta_rule_backward, [](Heads q, Heads k, Heads v, State g, State beta, flo
   return p_apex_delta_rule_backward(n.S, n.T, n.Hk, n.H, n.Dk, n.Dv, q.dtype, q.p, q.seq, q.time, k.p, k.seq, k.time, v.p, v.seq, v.time,
                                     g.of(n.gates, "g: fp32 [S,T,H]"), beta.of(n.gates, "beta: fp32 [S,T,H]"), scale,
                                     floats(discount, n.S * n.T, "discount: fp32 [S,T]"), ints(length, n.S, "length: int32 [S]"),
-                                    carry.of(chunks * n.slices, "carry: fp32 [S,chunks,H,ceil(Dv/16),Dk,16]"), d_o.p,
+                                    carry.of(chunks * n.slices, "carry: fp32, of delta_rule_carry_shape"), d_o.p,
                                     dh_last.of(n.state, "dh_last: fp32 [S,H,Dk,Dv]"), dq.p, dq.seq, dq.time, dk.p, dk.seq, dk.time, dv.p,
                                     dv.seq, dv.time, dg.of(n.gates, "dg: fp32 [S,T,H]"), dbeta.of(n.gates, "dbeta: fp32 [S,T,H]"),
                                     dh0.of(n.state, "dh0: fp32 [S,H,Dk,Dv]"),

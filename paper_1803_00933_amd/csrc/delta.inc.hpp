@@ -57,7 +57,7 @@ struct DeltaBack {
   void *dq, *dk, *dv;
   float *dg, *dbeta, *dh0;
   float *dS;  // [S][pieces][H]: of the state behind a piece, by 16 columns
-  float *Y;   // [S][T][H][Dv]
+  float *Y;   // [S][pieces][H][ceil(Dv / 16)][kWave][16]
 };
 
 __device__ __forceinline__ uint32_t delta_length(const DeltaArgs &a, uint32_t s)
@@ -201,6 +201,7 @@ struct Prepared {
   __bf16 *M, *P;     // [heads][kTriangle][3][kOperand]
   void *K, *Q;       // [key heads][4][KS][kOperand] of the inputs' type: keys and queries
   void *Kt, *Qt;     // [key heads][2 KS][2][kOperand]: their transposes
+  void *V;           // [heads][ceil(Dv / 16)][kWave][16]: values, backwards dO, as a wave that has 16 columns takes them
   __bf16 *rows;      // M beside its transpose (for the gradient)
 };
 
@@ -237,19 +238,60 @@ __device__ __forceinline__ Run<T, 8> load_step(const T *piece, uint64_t stride, 
 }
 
 template <typename T, uint32_t KS, bool kBack>
-__global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs a, Prepared w)
+__global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs a, const void *d_o, Prepared w)
 {
   constexpr uint32_t kRaw = KS * 32 + 16 / sizeof(T);  // (rows begin on 16 bytes)
   __shared__ Gates gates;
   __shared__ __align__(16) float L[kPiece * kPieceRow], P[kPiece * kPieceRow];
-  __shared__ float inverse[4][16][17];
-  __shared__ __align__(16) T raw[kBack ? 2 : 1][kPiece][kRaw];
+  __shared__ __align__(16) T raw[kPiece][kRaw];  // (three workgroups a compute unit)
+  const auto inverse = [&](uint32_t block, uint32_t t, uint32_t j) -> float & {  // in the blocks above L's diagonal
+    return L[((block == 3 ? 16 : 0) + t) * kPieceRow + (block == 3 ? 32 : 16 * block + 16) + j];
+  };
   const uint32_t h = blockIdx.x % a.H, piece = blockIdx.x / a.H % a.pieces, s = blockIdx.x / a.H / a.pieces, hk = h / a.share;
   const uint32_t len = delta_length(a, s), t0 = piece * kPiece;
   if (t0 >= len) return;
   const uint32_t have = min(kPiece, len - t0);
   const uint32_t lane = lane_id(), wave = threadIdx.x / kWave, m = lane % 16, q = lane / 16;
   const bool first = h % a.share == 0;  // of those that share a key head
+  {
+    const T *const rows = kBack ? static_cast<const T *>(d_o) + (((uint64_t)s * a.T + t0) * a.H + h) * a.Dv
+                                : static_cast<const T *>(a.v) + s * a.v_seq + t0 * a.v_time + (uint64_t)h * a.Dv;
+    const uint64_t stride = kBack ? (uint64_t)a.H * a.Dv : a.v_time;
+    const uint32_t slices = (a.Dv + 15) / 16;
+    for (uint32_t c0 = 0; c0 < a.Dv; c0 += KS * 32) {
+      const auto load = [&](auto whole) {
+        constexpr uint32_t kEach = kPiece * KS * 4 / kDeltaThreads;
+        Run<T, 8> x[kEach];
+#pragma unroll
+        for (uint32_t n = 0; n < kEach; ++n) {
+          const uint32_t i = n * kDeltaThreads + threadIdx.x;
+          x[n] = load_step<T, decltype(whole)::value>(rows, stride, i / (KS * 4), have, c0 + i % (KS * 4) * 8, a.Dv);
+        }
+#pragma unroll
+        for (uint32_t n = 0; n < kEach; ++n) {
+          const uint32_t i = n * kDeltaThreads + threadIdx.x;
+          *reinterpret_cast<Run<T, 8> *>(&raw[i / (KS * 4)][i % (KS * 4) * 8]) = x[n];
+        }
+      };
+      if (a.Dv % (KS * 32))
+        load(std::false_type());
+      else
+        load(std::true_type());
+      __syncthreads();
+      for (uint32_t i = wave; i < 2 * KS; i += kDeltaWaves) {
+        if (c0 / 16 + i >= slices) break;
+        T *const to = static_cast<T *>(w.V) + (((uint64_t)blockIdx.x * slices + c0 / 16 + i) * kWave + lane) * 16;
+#pragma unroll
+        for (uint32_t n = 0; n < 2; ++n) {
+          Run<T, 8> x;
+#pragma unroll
+          for (uint32_t e = 0; e < 8; ++e) x[e] = raw[tile_row(2 * n + e / 4, q * 4 + e % 4)][i * 16 + m];
+          *reinterpret_cast<Run<T, 8> *>(to + n * 8) = x;
+        }
+      }
+      __syncthreads();
+    }
+  }
   const T *const k_rows = static_cast<const T *>(a.k) + s * a.k_seq + t0 * a.k_time + (uint64_t)hk * a.Dk;
   const T *const q_rows = static_cast<const T *>(a.q) + s * a.q_seq + t0 * a.q_time + (uint64_t)hk * a.Dk;
   Run<T, 8> k_own[KS], q_own[KS];
@@ -265,13 +307,28 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
   else
     load_own(std::false_type());
   if (wave == 0) load_gates(a, s, h, t0, len, gates);
+  const auto put_raw = [&](const Run<T, 8>(&x)[KS]) {
 #pragma unroll
-  for (uint32_t i = 0; i < KS; ++i)
+    for (uint32_t i = 0; i < KS; ++i) *reinterpret_cast<Run<T, 8> *>(&raw[wave * 16 + m][i * 32 + q * 8]) = x[i];
+  };
+  const uint64_t key_head = ((uint64_t)s * a.pieces + piece) * a.Hk + hk;
+  const auto put_columns = [&](void *to_all) {
+    for (uint32_t i = threadIdx.x; i < 2 * KS * 2 * kWave; i += kDeltaThreads) {
+      const uint32_t l = i % kWave, ks = i / kWave % 2, tile = i / kWave / 2, d = tile_row(tile, l % 16), t = ks * 32 + l / 16 * 8;
+      Run<T, 8> x;
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) {
-      raw[0][wave * 16 + m][i * 32 + q * 8 + e] = k_own[i][e];
-      if (kBack) raw[kBack][wave * 16 + m][i * 32 + q * 8 + e] = q_own[i][e];
+      for (uint32_t e = 0; e < 8; ++e) x[e] = raw[t + e][d];
+      *reinterpret_cast<Run<T, 8> *>(static_cast<T *>(to_all) + ((key_head * 2 * KS + tile) * 2 + ks) * kOperand + l * 8) = x;
     }
+  };
+  // this wave's rows as operands: row t is row m of tile r
+  const auto put_rows = [&](void *to_all, const Run<T, 8>(&x)[KS]) {
+    const uint32_t t = wave * 16 + m, r = t / 32 * 2 + t / 4 % 2, row = t / 8 % 4 * 4 + t % 4;
+#pragma unroll
+    for (uint32_t i = 0; i < KS; ++i)
+      *reinterpret_cast<Run<T, 8> *>(static_cast<T *>(to_all) + key_head * (4 * KS * kOperand) + (r * KS + i) * kOperand + (q * 16 + row) * 8) = x[i];
+  };
+  put_raw(k_own);
   __syncthreads();
   for (uint32_t c = 0; c < 4; ++c) {
     Tile kk{}, qk{};
@@ -280,7 +337,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
       for (uint32_t i = 0; i < KS; ++i) {
         Run<T, 8> key;
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) key[e] = raw[0][c * 16 + m][i * 32 + q * 8 + e];
+        for (uint32_t e = 0; e < 8; ++e) key[e] = raw[c * 16 + m][i * 32 + q * 8 + e];
         multiply<3>(kk, operand<T>(k_own[i]), operand<T>(key));
         multiply<3>(qk, operand<T>(q_own[i]), operand<T>(key));
       }
@@ -293,7 +350,13 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
       P[t * kPieceRow + j] = j <= t ? qk[e] * d : 0.0f;
     }
   }
+  if (first) {
+    put_rows(w.K, k_own);
+    put_columns(w.Kt);
+    if (!kBack) put_rows(w.Q, q_own);
+  }
   __syncthreads();
+  if (kBack) put_raw(q_own);
   // (1 + L diag(beta))^-1 of the four blocks on the diagonal: a lane has a column
   if (wave == 0) {
     float x[16];
@@ -302,11 +365,12 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
       x[t] = t == m ? 1.0f : 0.0f;
 #pragma unroll
       for (uint32_t i = 0; i < t; ++i) x[t] -= L[(q * 16 + t) * kPieceRow + q * 16 + i] * x[i];
-      inverse[q][t][m] = x[t];
+      inverse(q, t, m) = x[t];
       x[t] *= gates.beta[q * 16 + t];  // (as the rows below take it)
     }
   }
   __syncthreads();
+  if (kBack && first) put_columns(w.Qt);
   // M, block row by block row: a wave has a column of blocks, in the layout that the next product takes
   Tile M[4];
 #pragma unroll
@@ -326,7 +390,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
         }
       }
 #pragma unroll
-    for (uint32_t e = 0; e < 4; ++e) M[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(inverse[i][m][q * 4 + e], x[e], M[i], 0, 0, 0);
+    for (uint32_t e = 0; e < 4; ++e) M[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(inverse(i, m, q * 4 + e), x[e], M[i], 0, 0, 0);
   }
   __syncthreads();
 #pragma unroll
@@ -351,33 +415,6 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
     for (uint32_t p = 0; p < 3; ++p) *reinterpret_cast<Parts8 *>(to + p * kOperand) = parts.part[p];
   }
   for (uint32_t i = threadIdx.x; i < sizeof(Gates) / 4; i += kDeltaThreads) w.gates[head * kGateWords + i] = reinterpret_cast<const uint32_t *>(&gates)[i];
-  if (first) {
-    const uint64_t key_head = ((uint64_t)s * a.pieces + piece) * a.Hk + hk;
-    for (uint32_t i = threadIdx.x; i < (kBack ? 2 : 1) * 2 * KS * 2 * kWave; i += kDeltaThreads) {
-      const uint32_t l = i % kWave, ks = i / kWave % 2, tile = i / kWave / 2 % (2 * KS), which = i / kWave / 2 / (2 * KS);
-      const uint32_t d = tile_row(tile, l % 16), t = ks * 32 + l / 16 * 8;
-      Run<T, 8> x;
-#pragma unroll
-      for (uint32_t e = 0; e < 8; ++e) x[e] = raw[which][t + e][d];
-      T *const to = static_cast<T *>(which ? w.Qt : w.Kt) + ((key_head * 2 * KS + tile) * 2 + ks) * kOperand + l * 8;
-      *reinterpret_cast<Run<T, 8> *>(to) = x;
-    }
-    // rows: of keys, and forwards of queries, too
-    for (uint32_t i = threadIdx.x; i < 4 * KS * kWave; i += kDeltaThreads) {
-      const uint32_t l = i % kWave, at = (i / kWave % KS) * 32 + l / 16 * 8;
-      Run<T, 8> x;
-#pragma unroll
-      for (uint32_t e = 0; e < 8; ++e) x[e] = raw[0][tile_row(i / kWave / KS, l % 16)][at + e];
-      *reinterpret_cast<Run<T, 8> *>(static_cast<T *>(w.K) + key_head * (4 * KS * kOperand) + i / kWave * kOperand + l * 8) = x;
-    }
-    if (!kBack) {
-#pragma unroll
-      for (uint32_t i = 0; i < KS; ++i) {  // (this wave's rows, in tiles of 16 steps as they follow one another: row t is row m of tile r)
-        const uint32_t t = wave * 16 + m, r = t / 32 * 2 + t / 4 % 2, row = t / 8 % 4 * 4 + t % 4;
-        *reinterpret_cast<Run<T, 8> *>(static_cast<T *>(w.Q) + key_head * (4 * KS * kOperand) + (r * KS + i) * kOperand + (q * 16 + row) * 8) = q_own[i];
-      }
-    }
-  }
 }
 
 // ---- from piece to piece.  A workgroup of two waves has 16 columns of a state, all its rows, and a wave's products need nothing
@@ -388,11 +425,12 @@ struct PiecePlace {
   uint32_t s, h, c0;
   bool none;
 };
-__device__ __forceinline__ PiecePlace piece_place(const DeltaArgs &a)
+template <uint32_t kSlices>
+__device__ __forceinline__ PiecePlace piece_place(const DeltaArgs &a, uint32_t slice)
 {
-  const uint32_t slices = (a.Dv + 15) / 16, heads = a.S * a.H;
-  const uint32_t head = blockIdx.x / (8 * slices) * 8 + blockIdx.x % 8;
-  return PiecePlace{head / a.H, head % a.H, blockIdx.x / 8 % slices * 16, head >= heads};
+  const uint32_t groups = (a.Dv + 16 * kSlices - 1) / (16 * kSlices), heads = a.S * a.H;
+  const uint32_t head = blockIdx.x / (8 * groups) * 8 + blockIdx.x % 8;
+  return PiecePlace{head / a.H, head % a.H, (blockIdx.x / 8 % groups * kSlices + slice) * 16, head >= heads};
 }
 
 // Both waves have arrived, and what they wrote to LDS is there.  Loads from memory stay on their way.
@@ -485,6 +523,23 @@ struct PieceColumn {  // a lane's numbers of tiles of steps: rows of a strided a
     }
   }
   __device__ __forceinline__ Tile tile(uint32_t i) const { return Tile{(float)x[i][0], (float)x[i][1], (float)x[i][2], (float)x[i][3]}; }
+};
+template <typename T>
+struct PieceSlice {  // the same, prepared
+  Run<T, 8> x[2];
+  __device__ __forceinline__ void load(const void *from, uint64_t slice)
+  {
+    const T *const p = static_cast<const T *>(from) + (slice * kWave + lane_id()) * 16;
+#pragma unroll
+    for (uint32_t n = 0; n < 2; ++n) x[n] = *reinterpret_cast<const Run<T, 8> *>(p + n * 8);
+  }
+  __device__ __forceinline__ Tile tile(uint32_t i) const
+  {
+    Tile r;
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) r[e] = element<8, T>(x[i / 2], i % 2 * 4 + e);
+    return r;
+  }
 };
 // f(t, address): every step of a lane's part of tiles of steps that a sequence has, and where its number is.
 template <typename T, typename F>
@@ -602,65 +657,69 @@ __device__ __forceinline__ void store_state(const Tile (&S)[2 * KS], float *to, 
       }
   }
 }
-// States that only these kernels read (the carry and its gradient) lie by 16 columns, [ceil(Dv / 16)][Dk][16]: what a wave reads or
-// writes of them is in one place.  (By rows of Dv, 64 bytes out of every 512 were asked for at a time, which is a quarter of the
+// States that only these kernels read (the carry and its gradient) lie by 16 columns, [ceil(Dv / 16)][rows][16], the rows of every
+// 32 in the order 0, 8, 16, 24, 1, 9 ..: what a wave reads or writes of them with one instruction is 256 bytes in one place.  (By rows of Dv, 64 bytes out of every 512 were asked for at a time, which is a quarter of the
 // channels of an L2 cache: the gradient of 4 x 8192 steps of 16 heads 1.74 ms, by columns XXXX.)
-__device__ __forceinline__ uint64_t slices_size(uint32_t Dk, uint32_t Dv) { return (uint64_t)((Dv + 15) / 16) * Dk * 16; }
+__device__ __forceinline__ uint32_t slice_size(uint32_t Dk) { return (Dk + 31) / 32 * 32 * 16; }
+__device__ __forceinline__ uint64_t slices_size(uint32_t Dk, uint32_t Dv) { return (uint64_t)((Dv + 15) / 16) * slice_size(Dk); }
+__device__ __forceinline__ uint32_t slice_row(uint32_t d) { return d / 32 * 32 + d % 8 * 4 + d / 8 % 4; }
 
 // A state of which the three parts are held: their sum is exact.  Zeros beyond the columns.
 template <uint32_t KS>
 __device__ __forceinline__ void store_slice(const Operand<3> (&S)[KS], float *to, uint32_t Dk, uint32_t slice, bool column)
 {
-  const uint32_t q = lane_id() / 16, m = lane_id() % 16;
-  float *const lane_to = to + (uint64_t)slice * Dk * 16 + (q * 8 * 16 + m);
+  float *const lane_to = to + slice * slice_size(Dk) + lane_id();
 #pragma unroll
-  for (uint32_t s = 0; s < KS; ++s)
+  for (uint32_t s = 0; s < KS; ++s) {
+    if (s * 32 >= Dk) break;
 #pragma unroll
     for (uint32_t e = 0; e < 8; ++e) {
       const float x = ((float)S[s].part[2][e] + (float)S[s].part[1][e]) + (float)S[s].part[0][e];
-      if (Dk == KS * 32 || s * 32 + q * 8 + e < Dk) lane_to[(s * 32 + e) * 16] = column ? x : 0.0f;
+      lane_to[(s * 8 + e) * kWave] = column ? x : 0.0f;  // (rows beyond Dk: zeros, as the keys' are)
     }
+  }
 }
 template <uint32_t KS>
 __device__ __forceinline__ void load_slice(Tile (&S)[2 * KS], const float *from, uint32_t Dk, uint32_t slice)
 {
-  const uint32_t q = lane_id() / 16, m = lane_id() % 16;
-  const float *const lane_from = from + (uint64_t)slice * Dk * 16 + m;
+  const float *const lane_from = from + slice * slice_size(Dk) + lane_id();
 #pragma unroll
   for (uint32_t s = 0; s < KS; ++s)
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) S[2 * s + e / 4][e % 4] = lane_from[min(s * 32 + q * 8 + e, Dk - 1) * 16];  // (keys beyond are 0)
+    for (uint32_t e = 0; e < 8; ++e) S[2 * s + e / 4][e % 4] = s * 32 < Dk ? lane_from[(s * 8 + e) * kWave] : 0.0f;
 }
 
 // What the next piece takes is asked for as soon as this one has taken its own: in the same registers, which a wave has 512 of.
 // (Numbers of 32 bits are twice as many; there a piece's are asked for at its begin.)
-template <typename T, uint32_t KS>
-__global__ __launch_bounds__(2 * kWave) void delta_pieces_kernel(DeltaForward f, Prepared w)
+template <typename T, uint32_t KS, uint32_t kSlices>
+__global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(DeltaForward f, Prepared w)
 {
   constexpr bool kAhead = sizeof(T) == 2;
-  __shared__ __align__(16) __bf16 states[2][KS][3 * kOperand];
-  __shared__ Tile corrections[2][4][kWave];  // U
+  __shared__ __align__(16) __bf16 all_states[kSlices][2][KS][3 * kOperand];
+  __shared__ Tile all_corrections[kSlices][2][4][kWave];  // U
+  const uint32_t slice = threadIdx.x / kWave % kSlices;
+  auto &states = all_states[slice];
+  auto &corrections = all_corrections[slice];
   const DeltaArgs &a = f.n;
-  const PiecePlace place = piece_place(a);
+  const PiecePlace place = piece_place<kSlices>(a, slice);
   if (place.none) return;
   const uint32_t s = place.s, h = place.h, hk = h / a.share, lane = lane_id(), c = place.c0 + lane % 16;
-  const bool column = c < a.Dv, carries = threadIdx.x < kWave;
-  const uint32_t len = delta_length(a, s), pieces = (len + kPiece - 1) / kPiece;
+  const bool column = c < a.Dv, carries = threadIdx.x < kSlices * kWave;
+  const uint32_t len = delta_length(a, s), pieces = (len + kPiece - 1) / kPiece, slices = (a.Dv + 15) / 16;
   const uint64_t state = ((uint64_t)s * a.H + h) * a.Dk * a.Dv;
   const auto head_of = [&](uint32_t piece) { return ((uint64_t)s * a.pieces + piece) * a.H + h; };
   const auto have_of = [&](uint32_t piece) { return min(kPiece, len - piece * kPiece); };
   if (carries) {
-    const T *const v_rows = static_cast<const T *>(a.v) + s * a.v_seq + (uint64_t)h * a.Dv;
     Tile S[2 * KS] = {};
     if (f.h0) load_state<KS>(S, f.h0 + state, a.Dk, a.Dv, place.c0);
     PieceKeys<T, KS> K;
-    PieceColumn<T> V;
+    PieceSlice<T> V;
     PieceTriangle<3> M;
     PieceColumns<T, KS> Kt;
     AllGates gates;
     const auto load_keys = [&](uint32_t piece) {
       K.load(w.K, ((uint64_t)s * a.pieces + piece) * a.Hk + hk);
-      V.load(v_rows + (uint64_t)piece * kPiece * a.v_time, a.v_time, have_of(piece), min(c, a.Dv - 1));
+      V.load(w.V, head_of(piece) * slices + min(place.c0 / 16, slices - 1));
     };
     const auto load_columns = [&](uint32_t piece) {
       Kt.load(w.Kt, ((uint64_t)s * a.pieces + piece) * a.Hk + hk);
@@ -737,7 +796,7 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_kernel(DeltaForward f,
       const Operand<3> U[2] = {operand_of<3>(found[0][lane], found[1][lane]), operand_of<3>(found[2][lane], found[3][lane])};
       P.template times<3, false>(O, U);
       if (kAhead) load(min(piece + 1, pieces - 1));
-      if (f.carry) store_slice<KS>(S, f.carry + head_of(piece) * slices_size(a.Dk, a.Dv), a.Dk, place.c0 / 16, column);
+      if (f.carry && place.c0 < a.Dv) store_slice<KS>(S, f.carry + head_of(piece) * slices_size(a.Dk, a.Dv), a.Dk, place.c0 / 16, column);
       if (column)
         each_step(o + (uint64_t)piece * kPiece * o_row, o_row, have_of(piece), c, [&](uint32_t r, uint32_t e, T *to) { *to = (T)(a.scale * O[r][e]); });
     }
@@ -748,22 +807,26 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_kernel(DeltaForward f,
 
 // The same from the last piece to the first, with dS.  The first wave carries it, the second brings P^T dO and Q^T (c dO) and
 // stores dS, Y and dV.
-template <typename T, uint32_t KS>
-__global__ __launch_bounds__(2 * kWave) void delta_pieces_back_kernel(DeltaBack b, Prepared w)
+template <typename T, uint32_t KS, uint32_t kSlices>
+__global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(DeltaBack b, Prepared w)
 {
   constexpr bool kAhead = sizeof(T) == 2;
   struct Brought {
     Tile o[4][kWave], state[2 * KS][kWave];
   };
-  __shared__ Brought brought[2];
-  __shared__ __align__(16) __bf16 states[2][KS][3 * kOperand];
-  __shared__ Tile found[2][4][kWave];  // Y
+  __shared__ Brought all_brought[kSlices][2];
+  __shared__ __align__(16) __bf16 all_states[kSlices][2][KS][3 * kOperand];
+  __shared__ Tile all_found[kSlices][2][4][kWave];  // Y
+  const uint32_t slice = threadIdx.x / kWave % kSlices;
+  auto &brought = all_brought[slice];
+  auto &states = all_states[slice];
+  auto &found = all_found[slice];
   const DeltaArgs &a = b.n;
-  const PiecePlace place = piece_place(a);
+  const PiecePlace place = piece_place<kSlices>(a, slice);
   if (place.none) return;
   const uint32_t s = place.s, h = place.h, hk = h / a.share, lane = lane_id(), c = place.c0 + lane % 16;
-  const bool column = c < a.Dv, carries = threadIdx.x < kWave;
-  const uint32_t len = delta_length(a, s), pieces = (len + kPiece - 1) / kPiece;
+  const bool column = c < a.Dv, carries = threadIdx.x < kSlices * kWave;
+  const uint32_t len = delta_length(a, s), pieces = (len + kPiece - 1) / kPiece, slices = (a.Dv + 15) / 16;
   const uint64_t state = ((uint64_t)s * a.H + h) * a.Dk * a.Dv;
   const auto head_of = [&](uint32_t piece) { return ((uint64_t)s * a.pieces + piece) * a.H + h; };
   const auto key_head_of = [&](uint32_t piece) { return ((uint64_t)s * a.pieces + piece) * a.Hk + hk; };
@@ -822,29 +885,21 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_back_kernel(DeltaBack 
     }
     if (b.dh0) store_state<KS>(S, b.dh0 + state, a.Dk, a.Dv, place.c0);
   } else {
-    const uint64_t o_row = (uint64_t)a.H * a.Dv;
-    const T *const d_o = static_cast<const T *>(b.d_o) + ((uint64_t)s * a.T * a.H + h) * a.Dv;
-    float *const Y = b.Y + ((uint64_t)s * a.T * a.H + h) * a.Dv;
     T *const dv = static_cast<T *>(b.dv) + s * b.dv_seq + (uint64_t)h * a.Dv;
-    PieceColumn<T> taken;
+    PieceSlice<T> taken;
     PieceTriangle<3> P;
     PieceColumns<T, KS> Qt;
     RowGates begin;
     const auto load = [&](uint32_t piece) {
-      taken.load(d_o + (uint64_t)piece * kPiece * o_row, o_row, have_of(piece), min(c, a.Dv - 1));
+      taken.load(w.V, head_of(piece) * slices + min(place.c0 / 16, slices - 1));
       P.load(w.P, head_of(piece));
       Qt.load(w.Qt, key_head_of(piece));
       begin = row_gates(gates_of(w, head_of(piece)).begin);
     };
     const auto bring = [&](uint32_t piece) {
-      const uint32_t have = have_of(piece);
       Tile dO[4];
 #pragma unroll
-      for (uint32_t r = 0; r < 4; ++r) {
-        dO[r] = taken.tile(r);
-#pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) dO[r][e] = state_row(r, e) < have ? dO[r][e] : 0.0f;
-      }
+      for (uint32_t r = 0; r < 4; ++r) dO[r] = taken.tile(r);  // (zeros behind the sequence's end)
       const Operand<kPartsOf<T>> right[2] = {operand_of<kPartsOf<T>>(dO[0], dO[1]), operand_of<kPartsOf<T>>(dO[2], dO[3])};
       Tile of_o[4] = {};
       P.template times<3, true>(of_o, right);
@@ -869,13 +924,15 @@ __global__ __launch_bounds__(2 * kWave) void delta_pieces_back_kernel(DeltaBack 
       Operand<3> S[KS];
 #pragma unroll
       for (uint32_t i = 0; i < KS; ++i) S[i] = get<3>(states[piece % 2][i]);
-      store_slice<KS>(S, b.dS + head * slices_size(a.Dk, a.Dv), a.Dk, place.c0 / 16, column);
+      if (place.c0 < a.Dv) store_slice<KS>(S, b.dS + head * slices_size(a.Dk, a.Dv), a.Dk, place.c0 / 16, column);
       const RowGates beta = row_gates(gates_of(w, head).beta);
       Tile y[4];
 #pragma unroll
-      for (uint32_t r = 0; r < 4; ++r) y[r] = found[piece % 2][r][lane];
+      for (uint32_t r = 0; r < 4; ++r) {
+        y[r] = found[piece % 2][r][lane];
+        if (place.c0 < a.Dv) *reinterpret_cast<Tile *>(b.Y + ((head * slices + place.c0 / 16) * kWave + lane) * 16 + r * 4) = y[r];
+      }
       if (column) {
-        each_step(Y + (uint64_t)piece * kPiece * o_row, o_row, have, c, [&](uint32_t r, uint32_t e, float *to) { *to = y[r][e]; });
         each_step(dv + (uint64_t)piece * kPiece * b.dv_time, b.dv_time, have, c, [&](uint32_t r, uint32_t e, T *to) { *to = (T)(beta.tile[r][e] * y[r][e]); });
       }
     };
@@ -976,7 +1033,6 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
     const float *const S0 = b.carry + head * slices_size(a.Dk, a.Dv), *const dS = b.dS + head * slices_size(a.Dk, a.Dv);
     const T *const v_rows = static_cast<const T *>(a.v) + s * a.v_seq + t0 * a.v_time + (uint64_t)h * a.Dv;
     const T *const o_rows = static_cast<const T *>(b.d_o) + gates_at * a.Dv + (uint64_t)h * a.Dv;
-    const float *const y_rows = b.Y + gates_at * a.Dv + (uint64_t)h * a.Dv;
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < sizeof(Gates) / 4; i += kGradThreads) reinterpret_cast<uint32_t *>(&x.gates)[i] = w.gates[head * kGateWords + i];
     __syncthreads();
@@ -999,9 +1055,9 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
         __builtin_amdgcn_sched_barrier(0);
         K.load(w.K, key_head, 2);
         PieceColumn<T> V;
-        PieceColumn<float> y;
+        PieceSlice<float> y;
         V.load(v_rows, a.v_time, have, c);
-        y.load(y_rows, o_row, have, c);
+        y.load(b.Y, head * ((a.Dv + 15) / 16) + wave);
 #pragma unroll
         for (uint32_t i = 0; i < KS; ++i)
 #pragma unroll
@@ -1063,9 +1119,9 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
       }
       return r;
     };
-    const uint32_t own_row = min(own_d, a.Dk - 1) * 16 + q % 2 * 8, slices = (a.Dv + 15) / 16;
+    const uint32_t own_row = slice_row(min(own_d, a.Dk - 1)) * 16 + q % 2 * 8, slices = (a.Dv + 15) / 16;
     const auto take = [&](uint32_t c0) {
-      const uint64_t at = (uint64_t)min(c0 / 16 + q / 2, slices - 1) * a.Dk * 16 + own_row;
+      const uint32_t at = min(c0 / 16 + q / 2, slices - 1) * slice_size(a.Dk) + own_row;
       next.start = *reinterpret_cast<const Run<float, 8> *>(S0 + at), next.end = *reinterpret_cast<const Run<float, 8> *>(dS + at);
 #pragma unroll
       for (uint32_t i = 0; i < KS; ++i) next.o[i] = eight(o_rows + min(tile_row(r0 + i, m), have - 1) * o_row, c0 + q * 8);
@@ -1312,13 +1368,13 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_steps_kernel(DeltaForward
 #pragma unroll
     for (uint32_t c = 0; c < C; ++c) v[c] = c0 + c < a.Dv ? (float)v_row[c] : 0.0f;
     if (f.carry && t % kPiece == 0 && c0 < (a.Dv + 15) / 16 * 16) {
-      float *const to = f.carry + (((uint64_t)s * a.pieces + t / kPiece) * a.H + h) * slices_size(a.Dk, a.Dv) + (uint64_t)(c0 / 16) * a.Dk * 16 + c0 % 16;
+      float *const to = f.carry + (((uint64_t)s * a.pieces + t / kPiece) * a.H + h) * slices_size(a.Dk, a.Dv) + (c0 / 16) * slice_size(a.Dk) + c0 % 16;
 #pragma unroll
       for (uint32_t i = 0; i < kStepRows; ++i) {
         Run<float, C> v;
 #pragma unroll
         for (uint32_t c = 0; c < C; ++c) v[c] = passes && c0 + c < a.Dv ? S[i][c] : 0.0f;
-        if (d0 + i < a.Dk) *reinterpret_cast<Run<float, C> *>(to + (d0 + i) * 16) = v;
+        if (d0 + i < (a.Dk + 31) / 32 * 32) *reinterpret_cast<Run<float, C> *>(to + slice_row(d0 + i) * 16) = v;  // (0 beyond Dk)
       }
     }
     const bool in = passes && keep != 0.0f;  // a selection: nothing of what has ended
@@ -1383,7 +1439,7 @@ void with_width(uint32_t Dk, F f)
 }
 
 struct DeltaBytes {
-  uint64_t gates, M, P, K, Q, Kt, Qt, rows, dS, Y, bytes;
+  uint64_t gates, M, P, K, Q, Kt, Qt, V, rows, dS, Y, bytes;
 };
 
 int delta_sizes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, bool backward, DeltaBytes *n)
@@ -1408,10 +1464,11 @@ int delta_sizes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, bo
   n->Q = take(columns);  // (the gradient takes no rows of queries, and has their transposes there)
   n->Qt = n->Q;
   n->Kt = take(columns);
+  n->V = take(heads * blocks_for(Dv, 16) * kWave * 16 * 4);
   if (backward) {
     n->rows = take(heads * kTriangle * 3 * kOperand * 2);
-    n->dS = take(heads * Dk * round_up(Dv, 16) * 4);
-    n->Y = take((uint64_t)S * T * H * Dv * 4);
+    n->dS = take(heads * round_up(Dk, 32) * round_up(Dv, 16) * 4);
+    n->Y = take(heads * blocks_for(Dv, 16) * kWave * 16 * 4);
   }
   return APEX_OK;
 }
@@ -1419,12 +1476,25 @@ int delta_sizes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, bo
 Prepared delta_prepared(const DeltaBytes &n, void *workspace)
 {
   char *const p = static_cast<char *>(workspace);
-  return Prepared{reinterpret_cast<uint32_t *>(p + n.gates), reinterpret_cast<__bf16 *>(p + n.M), reinterpret_cast<__bf16 *>(p + n.P), p + n.K, p + n.Q, p + n.Kt, p + n.Qt,
+  return Prepared{reinterpret_cast<uint32_t *>(p + n.gates), reinterpret_cast<__bf16 *>(p + n.M), reinterpret_cast<__bf16 *>(p + n.P), p + n.K, p + n.Q, p + n.Kt, p + n.Qt, p + n.V,
                   reinterpret_cast<__bf16 *>(p + n.rows)};
 }
 
-// Workgroups of the kernels that go from piece to piece: eight heads' slices of 16 columns at a time.
-uint32_t delta_slices(uint32_t S, uint32_t H, uint32_t Dv) { return blocks_for((uint64_t)S * H, 8) * 8 * blocks_for(Dv, 16); }
+// Workgroups of the kernels that go from piece to piece, of `slices` slices of 16 columns each: eight heads' at a time.
+uint32_t delta_groups(uint32_t S, uint32_t H, uint32_t Dv, uint32_t slices) { return blocks_for((uint64_t)S * H, 8) * 8 * blocks_for(Dv, 16 * slices); }
+
+// f(integral_constant<uint32_t>): slices of a workgroup.
+// Two, which read the same operands at the same time, where a compute unit has two anyway and operands are large (4 x 8192 steps of
+// 16 heads of 128 x 128 684 us by one, 621 by two); else one (1 x 16384 of 8 heads 1131 and 1289, 64 x 96 of 8 heads of 64 x 64 33.7
+// and 36).
+template <uint32_t KS, typename F>
+void with_slices(uint32_t S, uint32_t H, uint32_t Dv, F f)
+{
+  if (KS == 4 && Dv > 16 && (uint64_t)S * H * blocks_for(Dv, 16) > kChipCus)
+    f(std::integral_constant<uint32_t, KS / 2>());
+  else
+    f(std::integral_constant<uint32_t, 1>());
+}
 
 int delta_check(const DeltaArgs &a, int dtype)
 {
@@ -1478,8 +1548,11 @@ int apex_delta_rule(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, uint32_t Dk
     typedef decltype(t) E;
     with_width(Dk, [&](auto width) {
       constexpr uint32_t KS = decltype(width)::value;
-      delta_prepare_kernel<E, KS, false><<<dim3(S * f.n.pieces * H), dim3(kDeltaThreads), 0, stream>>>(f.n, w);
-      delta_pieces_kernel<E, KS><<<dim3(delta_slices(S, H, Dv)), dim3(2 * kWave), 0, stream>>>(f, w);
+      delta_prepare_kernel<E, KS, false><<<dim3(S * f.n.pieces * H), dim3(kDeltaThreads), 0, stream>>>(f.n, nullptr, w);
+      with_slices<KS>(S, H, Dv, [&](auto slices) {
+        constexpr uint32_t kSlices = decltype(slices)::value;
+        delta_pieces_kernel<E, KS, kSlices><<<dim3(delta_groups(S, H, Dv, kSlices)), dim3(2 * kSlices * kWave), 0, stream>>>(f, w);
+      });
     });
   });
   APEX_HIP(hipGetLastError());
@@ -1515,8 +1588,11 @@ int apex_delta_rule_backward(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, ui
     typedef decltype(t) E;
     with_width(Dk, [&](auto width) {
       constexpr uint32_t KS = decltype(width)::value;
-      delta_prepare_kernel<E, KS, true><<<dim3(S * b.n.pieces * H), dim3(kDeltaThreads), 0, stream>>>(b.n, w);
-      delta_pieces_back_kernel<E, KS><<<dim3(delta_slices(S, H, Dv)), dim3(2 * kWave), 0, stream>>>(b, w);
+      delta_prepare_kernel<E, KS, true><<<dim3(S * b.n.pieces * H), dim3(kDeltaThreads), 0, stream>>>(b.n, b.d_o, w);
+      with_slices<KS>(S, H, Dv, [&](auto slices) {
+        constexpr uint32_t kSlices = decltype(slices)::value;
+        delta_pieces_back_kernel<E, KS, kSlices><<<dim3(delta_groups(S, H, Dv, kSlices)), dim3(2 * kSlices * kWave), 0, stream>>>(b, w);
+      });
       if (Dv % 32)
         delta_gradients_kernel<E, KS, false><<<dim3(S * b.n.pieces * Hk), dim3(kGradThreads), 0, stream>>>(b, w);
       else

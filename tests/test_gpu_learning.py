@@ -230,10 +230,10 @@ def test_delta_state_in_place_and_in_pieces(apex, dtype):
         at += n
     assert at == 300
     c.check(dict(o=torch.cat(o, 1), h_last=state), want, names=("o", "h_last"))
-    slices = c.run(apex)["carry"]                                      # [S,chunks,H,4,40,16]: by 16 columns
-    columns = slices.transpose(3, 4).reshape(2, 5, 2, 40, 64)
-    check(columns[..., :50], want["carry"], plain.delta_bound("h_last", want, 40, 50)[:, None], torch.float32, "carry")
-    assert (columns[..., 50:] == 0).all()
+    carry = c.run(apex)["carry"]                                        # [S,chunks,H,4,2,8,4,16]: column / 16, row / 32, row % 8, row / 8 % 4, column % 16
+    states = carry.permute(0, 1, 2, 4, 6, 5, 3, 7).reshape(2, 5, 2, 64, 64)
+    check(states[..., :40, :50], want["carry"], plain.delta_bound("h_last", want, 40, 50)[:, None], torch.float32, "carry")
+    assert (states[..., 40:, :] == 0).all() and (states[..., 50:] == 0).all()
 
 
 def test_delta_same_bits(apex):
