@@ -589,6 +589,7 @@ typedef enum apex_gate {
 #define APEX_MAX_DRAFT 64u            /* G of apex_verify_draft                                      */
 #define APEX_DELTA_CHUNK 64u          /* steps per stored state of apex_delta_rule's carry           */
 #define APEX_DELTA_MAX_WIDTH 128u     /* Dk and Dv of apex_delta_rule                                */
+#define APEX_DELTA_MAX_PIECES 1048576u /* S * ceil(T / APEX_DELTA_CHUNK) * H of apex_delta_rule      */
 #define APEX_MAX_TOKENS 8388608u      /* N of apex_embedding                                         */
 #define APEX_MAX_WIDTH 8192u          /* D of apex_embedding                                         */
 #define APEX_MAX_TENSORS 65536u       /* count of apex_clip_gradients                                */

@@ -329,6 +329,12 @@ def verify_draft(target, draft, token, rnd, length=None, out=None, workspace=Non
     return _call.verify_draft(target, draft, token, rnd, length, out["accepted"], out["token"], workspace, stream), out
 
 
+def _on_current_device(t):
+    """The kernels are launched on the current device."""
+    if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("tensors of the current device only (%d), not of device %d" % (torch._C._cuda_getDevice(), t.get_device()))
+
+
 def delta_rule_carry_shape(S, T, H, Dk, Dv):
     return S, -(-T // DELTA_CHUNK), H, -(-Dv // 16), -(-Dk // 32), 8, 4, 16
 
@@ -346,6 +352,7 @@ def delta_rule(q, k, v, g, beta, discount=None, length=None, h0=None, scale=1.0,
     delta_rule_backward needs."""
     if carry and out is not None and out.get("carry") is None:
         raise ValueError("carry=True, and no place for it in out")
+    _on_current_device(q)
     if out is None or workspace is None:
         (S, T, _, Dk), (_, _, H, Dv) = q.shape, v.shape
         with _made_on(stream):
@@ -365,6 +372,7 @@ def delta_rule_backward(q, k, v, g, beta, do, carry, discount=None, length=None,
     """Gradients of delta_rule from do [S,T,H,Dv] and dh_last fp32 [S,H,Dk,Dv], with the carry it left.
     Returns (rc, out): dq, dk, dv as q, k and v (of any strides where `out` brings them), dg and dbeta fp32 [S,T,H], dh0 fp32
     [S,H,Dk,Dv]."""
+    _on_current_device(q)
     if out is None or workspace is None:
         (S, T, _, Dk), (_, _, H, Dv) = q.shape, v.shape
         with _made_on(stream):
@@ -381,6 +389,7 @@ def delta_rule_backward(q, k, v, g, beta, do, carry, discount=None, length=None,
 def embedding(table, token, scale=1.0, out=None, stream=None):
     """scale * table[token] for a table [V,D] and tokens int32 of any shape; zeros for tokens outside the table.
     Returns (rc, out): out [N,D], N the number of tokens."""
+    _on_current_device(table)
     if out is None:
         with _made_on(stream):
             out = dict(out=torch.empty((token.numel(), table.shape[1]), dtype=table.dtype, device=table.device))
@@ -397,6 +406,7 @@ def embedding_backward(dout, token, V, scale=1.0, add=False, out=None, workspace
     Returns (rc, out): dtable [V,D]."""
     if add and out is None:
         raise ValueError("add=True, and no table to add to in out")
+    _on_current_device(dout)
     if out is None or workspace is None:
         N, D = dout.shape
         with _made_on(stream):
@@ -421,6 +431,8 @@ def clip_gradients(grads, max_norm, out=None, norm=None, workspace=None, stream=
     """The tensors of the list `grads` times min(1, max_norm / norm), norm the one over all their elements, into the tensors of the
     list `out` (laid out alike), or in place.  A norm that is not finite scales nothing.
     Returns (rc, out): norm fp32 [1] and out, the list."""
+    if len(grads):
+        _on_current_device(grads[0])
     if norm is None or workspace is None:
         with _made_on(stream):
             if norm is None:

@@ -138,6 +138,7 @@ struct View {
   void *p = nullptr;
   int64_t n[3] = {0, 0, 0}, stride[3] = {0, 0, 0}, count = 0;
   int dim = 0, dtype = -1;  // apex_dtype, or -1
+  int device = -1;
   bool contiguous = false, is_int = false, is_long = false;
   bool is_none() const { return dim == 0; }  // (a tensor without elements has no address either)
   bool fits(int64_t a, int64_t b) const { return dim == 2 && n[0] == a && n[1] == b; }
@@ -175,6 +176,7 @@ struct From<View> {
       }
     }
     v.count = t.numel();
+    v.device = t.get_device();
     const at::ScalarType s = t.scalar_type();
     v.dtype = s == at::kFloat ? APEX_F32 : s == at::kBFloat16 ? APEX_BF16 : s == at::kHalf ? APEX_F16 : -1;
     v.is_int = s == at::kInt;
@@ -190,6 +192,7 @@ struct Heads {
   int64_t n[4], seq, time;
   int dtype;
   bool contiguous;
+  int device;
   bool fits(int64_t a, int64_t b, int64_t c, int64_t d) const { return n[0] == a && n[1] == b && n[2] == c && n[3] == d; }
 };
 template <>
@@ -206,7 +209,7 @@ struct From<Heads> {
       PyErr_SetString(PyExc_AssertionError, "device tensors [S,T,heads,width] only, the heads of a step side by side");
       throw Failed{};
     }
-    Heads h{t.data_ptr(), {}, t.stride(0), t.stride(1), -1, t.is_contiguous()};
+    Heads h{t.data_ptr(), {}, t.stride(0), t.stride(1), -1, t.is_contiguous(), (int)t.get_device()};
     for (int i = 0; i < 4; ++i) {
       h.n[i] = t.size(i);
       if (h.n[i] > INT32_MAX) {
@@ -225,6 +228,7 @@ struct State {
   float *p = nullptr;
   int64_t count = 0;
   bool none = true;
+  int device = -1;
   float *of(int64_t elements, const char *why) const
   {
     require(none || count == elements, why);
@@ -249,6 +253,7 @@ struct From<State> {
     s.p = static_cast<float *>(t.data_ptr());
     s.count = t.numel();
     s.none = false;
+    s.device = t.get_device();
     return s;
   }
 };
@@ -259,6 +264,7 @@ struct Tensors {
   std::vector<uint64_t> elements;
   std::vector<int> dtype;
   bool none = false;
+  int device = -1;
 };
 template <>
 struct From<Tensors> {
@@ -279,10 +285,11 @@ struct From<Tensors> {
       const at::Tensor &t = THPVariable_Unpack(item);
       const at::ScalarType s = t.scalar_type();
       const int dtype = s == at::kFloat ? APEX_F32 : s == at::kBFloat16 ? APEX_BF16 : s == at::kHalf ? APEX_F16 : -1;
-      if (!t.is_cuda() || !t.is_non_overlapping_and_dense() || dtype < 0) {
-        PyErr_SetString(PyExc_AssertionError, "device, dense tensors of a floating type only");
+      if (!t.is_cuda() || !t.is_non_overlapping_and_dense() || dtype < 0 || (i && t.get_device() != r.device)) {
+        PyErr_SetString(PyExc_AssertionError, "dense tensors of a floating type on one device only");
         throw Failed{};
       }
+      r.device = t.get_device();
       r.p.push_back(t.data_ptr());
       r.elements.push_back((uint64_t)t.numel());
       r.dtype.push_back(dtype);
@@ -295,6 +302,7 @@ struct From<Tensors> {
 struct Space {
   void *p;
   size_t bytes;
+  int device;
   // bytes_of(sizes): what it has to hold; sizes that the library does not take are the call's own to refuse
   template <typename F, typename... A>
   void *of(F bytes_of, A... sizes) const
@@ -306,7 +314,11 @@ struct Space {
 };
 template <>
 struct From<Space> {
-  static Space get(PyObject *o) { return Space{address(o), o != Py_None && THPVariable_Check(o) ? THPVariable_Unpack(o).nbytes() : SIZE_MAX}; }
+  static Space get(PyObject *o)
+  {
+    if (o == Py_None || !THPVariable_Check(o)) return Space{address(o), SIZE_MAX, -1};
+    return Space{address(o), THPVariable_Unpack(o).nbytes(), (int)THPVariable_Unpack(o).get_device()};
+  }
 };
 
 // The address of a contiguous fp32 array of `count` elements, or null where there is none.
@@ -546,6 +558,20 @@ VERB(verify_draft, [](View target, View draft, View token, View rnd, View length
                              workspace.of(p_apex_verify_draft_workspace_bytes, B, vocabulary), s);
 })
 
+// Tensors of one call are on one device (-1: there is none).
+template <typename... A>
+void on_one_device(const A &...a)
+{
+  int first = -1;
+  const auto same = [&](int device) {
+    if (first < 0) first = device;
+    return device < 0 || device == first;
+  };
+  bool all = true;
+  ((all = same(a.device) && all), ...);
+  require(all, "tensors of one device only");
+}
+
 struct DeltaSizes {
   int64_t S, T, Hk, H, Dk, Dv, state, slices, gates;
   DeltaSizes(const Heads &q, const Heads &k, const Heads &v)
@@ -559,6 +585,7 @@ struct DeltaSizes {
 VERB(delta_rule, [](Heads q, Heads k, Heads v, State g, State beta, float scale, View discount, View length, State h0, Heads o, State h_last,
                     State carry, Space workspace, Stream s) {
   const DeltaSizes n(q, k, v);
+  on_one_device(q, k, v, g, beta, discount, length, h0, o, h_last, carry, workspace);
   require(o.dtype == q.dtype && o.fits(n.S, n.T, n.H, n.Dv) && o.contiguous, "o: [S,T,H,Dv], contiguous, of q's type");
   require(!g.none && !beta.none, "g and beta: fp32 [S,T,H]");
   const int64_t chunks = (n.T + APEX_DELTA_CHUNK - 1) / APEX_DELTA_CHUNK;
@@ -572,6 +599,7 @@ VERB(delta_rule, [](Heads q, Heads k, Heads v, State g, State beta, float scale,
 VERB(delta_rule_backward, [](Heads q, Heads k, Heads v, State g, State beta, float scale, View discount, View length, State carry, Heads d_o,
                              State dh_last, Heads dq, Heads dk, Heads dv, State dg, State dbeta, State dh0, Space workspace, Stream s) {
   const DeltaSizes n(q, k, v);
+  on_one_device(q, k, v, g, beta, discount, length, carry, d_o, dh_last, dq, dk, dv, dg, dbeta, dh0, workspace);
   require(d_o.dtype == q.dtype && d_o.fits(n.S, n.T, n.H, n.Dv) && d_o.contiguous, "do: [S,T,H,Dv], contiguous, of q's type");
   require(dq.dtype == q.dtype && dk.dtype == q.dtype && dv.dtype == q.dtype && dq.fits(n.S, n.T, n.Hk, n.Dk) &&
               dk.fits(n.S, n.T, n.Hk, n.Dk) && dv.fits(n.S, n.T, n.H, n.Dv), "dq, dk and dv: as q, k and v");
@@ -587,6 +615,7 @@ VERB(delta_rule_backward, [](Heads q, Heads k, Heads v, State g, State beta, flo
                                     workspace.of(p_apex_delta_rule_workspace_bytes, n.S, n.T, n.H, n.Dk, n.Dv, 1), s);
 })
 VERB(embedding, [](View table, View token, float scale, View out, Stream s) {
+  on_one_device(table, token, out);
   require(table.dim == 2 && table.dtype >= 0 && table.rows(), "table: [V,D] of a floating type, contiguous rows");
   require(!token.is_none() && out.fits(token.count, table.n[1]) && out.dtype == table.dtype && out.rows(),
           "out: [N,D] of the table's type, contiguous rows");
@@ -594,6 +623,7 @@ VERB(embedding, [](View table, View token, float scale, View out, Stream s) {
                           scale, out.p, out.stride[0], s);
 })
 VERB(embedding_backward, [](View dout, View token, float scale, int add, View dtable, Space workspace, Stream s) {
+  on_one_device(dout, token, dtable, workspace);
   require(dtable.dim == 2 && dtable.dtype >= 0 && dtable.rows(), "dtable: [V,D] of a floating type, contiguous rows");
   require(!token.is_none() && dout.fits(token.count, dtable.n[1]) && dout.dtype == dtable.dtype && dout.rows(),
           "dout: [N,D] of the table's type, contiguous rows");
@@ -602,6 +632,7 @@ VERB(embedding_backward, [](View dout, View token, float scale, int add, View dt
                                    workspace.of(p_apex_embedding_backward_workspace_bytes, token.count, dtable.n[0], dtable.n[1]), s);
 })
 VERB(clip_gradients, [](Tensors grad, Tensors out, float max_norm, View norm, Space workspace, Stream s) {
+  on_one_device(grad, out, norm, workspace);
   require(!grad.none && (out.none || (out.elements == grad.elements && out.dtype == grad.dtype)), "out: as the gradients");
   return p_apex_clip_gradients(grad.p.size(), grad.p.data(), out.none ? nullptr : out.p.data(), grad.elements.data(), grad.dtype.data(),
                                max_norm, floats(norm, 1, "norm: fp32 [1]"), workspace.of(p_apex_clip_gradients_workspace_bytes, grad.p.size()), s);

@@ -6,7 +6,7 @@ namespace apex {
 
 constexpr uint32_t kClipThreads = 256, kClipTensors = 96;      // tensors of a launch: their table is an argument of the kernel
 constexpr uint32_t kClipMinPiece = 8192;                       // elements that a workgroup takes, where there are few
-constexpr uint32_t kClipPieces = 2048;                         // pieces at most, beside one more per tensor
+constexpr uint32_t kClipPieces = 4096;                         // pieces at most, beside one more per tensor
 
 struct ClipTensor {
   const void *grad;

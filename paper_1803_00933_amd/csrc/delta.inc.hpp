@@ -1446,9 +1446,9 @@ int delta_sizes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, bo
 {
   if (!S || !T || !H || !Dk || !Dv || T > 0x7fffffffu) return APEX_ERR_INVALID_ARG;
   if (Dk > kDeltaMaxWidth || Dv > kDeltaMaxWidth) return APEX_ERR_TOO_LARGE;
-  // workgroups of 512 threads, fewer than 2^32 threads in all
+  // (no launch has 2^32 threads: eight slices of a head, two waves each)
   uint64_t heads;
-  if (__builtin_mul_overflow((uint64_t)S * blocks_for(T, kPiece), (uint64_t)H, &heads) || heads >= 1u << 23) return APEX_ERR_TOO_LARGE;
+  if (__builtin_mul_overflow((uint64_t)S * blocks_for(T, kPiece), (uint64_t)H, &heads) || heads > APEX_DELTA_MAX_PIECES) return APEX_ERR_TOO_LARGE;
   *n = DeltaBytes{};
   if (!backward && T <= kDeltaSteps) return APEX_OK;
   const auto take = [&](uint64_t bytes) {

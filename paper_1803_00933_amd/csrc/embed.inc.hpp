@@ -6,8 +6,9 @@ namespace apex {
 constexpr uint32_t kEmbedThreads = 256;
 constexpr uint32_t kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr uint32_t kDigitBits = 11, kDigits = 1u << kDigitBits;     // of a pass of the sort at most: two passes for any vocabulary
-constexpr uint32_t kSortAlone = 16384, kSortTile = 4096;            // tokens that one workgroup sorts by itself, and of a tile else
+constexpr uint32_t kSortAlone = 8192, kSortTile = 2048;             // tokens that one workgroup sorts by itself, and of a tile else
 constexpr uint32_t kSlice = 64, kSlice2 = kSlice * kSlice;          // sorted tokens whose rows are summed up ahead, if they are one
+constexpr uint32_t kSlice2From = 16384;                             // ... in two steps from so many tokens on (one launch more: 5 us)
 
 struct EmbedArgs {
   uint32_t N, V, D;
@@ -103,15 +104,20 @@ __global__ __launch_bounds__(kEmbedThreads) void sort_tiles_kernel(SortArgs a)
 
 // Places of a tile's tokens: behind all of smaller digits, those of the same digit in earlier tiles, in earlier waves, and in
 // front of it in its wave, which goes through its part in groups of 64: lanes of the same digit find one another by a ballot per
-// bit.  One pass of the sort; kAlone: with the counts of a single tile.
+// bit.  One pass of the sort; kAlone: with the counts of a single tile, kGroups groups a wave at most.  count[digit][wave] holds what
+// a wave has of a digit, then how many tokens of the tile go in front of those; base, of a digit, what the tile's places begin at.
+// A workgroup that is alone keeps tokens and places in `held` from pass to pass, and writes them out in their order at the end: as
+// scattered words, by one compute unit, 7777 took 32 us.
+struct Held {
+  uint32_t key, index;
+};
 template <bool kAlone>
-__device__ __forceinline__ void sort_pass(const SortArgs &a, uint16_t (*in_wave)[kDigits], uint32_t *base)
+__device__ __forceinline__ void sort_pass(const SortArgs &a, uint16_t *count, uint32_t *base, Held *held, bool second)
 {
   constexpr uint32_t kGroups = (kAlone ? kSortAlone : kSortTile) / kSortThreads;
   __shared__ uint32_t of_wave[kSortWaves];
   const uint32_t digits = 1u << a.bits, lane = lane_id(), wave = threadIdx.x / kWave;
-  for (uint32_t d = threadIdx.x; d < digits * kSortWaves; d += kSortThreads) in_wave[d >> a.bits][d & (digits - 1)] = 0;
-  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < digits * kSortWaves / 2; i += kSortThreads) reinterpret_cast<uint32_t *>(count)[i] = 0;
   // a wave's part: consecutive groups
   const uint32_t tile_begin = kAlone ? 0 : blockIdx.x * a.tile, tile_end = kAlone ? a.N : min(a.N, tile_begin + a.tile);
   const uint32_t groups = ((tile_end - tile_begin) + kSortThreads - 1) / kSortThreads;
@@ -121,24 +127,31 @@ __device__ __forceinline__ void sort_pass(const SortArgs &a, uint16_t (*in_wave)
   for (uint32_t g = 0; g < kGroups; ++g) {
     const uint32_t i = begin + g * kWave;
     if (g < groups && i < tile_end) {
-      key[g] = sort_key(a, i);
-      index[g] = a.key_in ? a.index_in[i] : i;
+      if (kAlone && second) {
+        key[g] = held[i].key, index[g] = held[i].index;
+      } else {
+        key[g] = sort_key(a, i);
+        index[g] = a.key_in ? a.index_in[i] : i;
+      }
     }
   }
+  __syncthreads();
 #pragma unroll
   for (uint32_t g = 0; g < kGroups; ++g) {
     if (g >= groups) continue;  // (for all)
     const bool have = begin + g * kWave < tile_end;
     const uint32_t digit = have ? (key[g] >> a.shift) & (digits - 1) : 0;
-    uint64_t same = __ballot(have);
-    for (uint32_t b = 0; b < a.bits; ++b) {
-      const bool one = (digit >> b) & 1;
-      const uint64_t ones = __ballot(one);
-      same &= one ? ones : ~ones;
+    uint32_t low = 0, high = 0;  // lanes of which a bit differs
+#pragma unroll
+    for (uint32_t b = 0; b < kDigitBits; ++b) {
+      const uint32_t mine = (uint32_t)__builtin_amdgcn_sbfe((int)digit, b, 1);  // all ones, or none
+      const uint64_t ones = __ballot(mine != 0);
+      low |= (uint32_t)ones ^ mine, high |= (uint32_t)(ones >> 32) ^ mine;
     }
+    const uint64_t same = __ballot(have) & ~((uint64_t)high << 32 | low);
     if (have) {
       const uint32_t rank = __builtin_popcountll(same & ((1ull << lane) - 1));
-      volatile uint16_t *const place = &in_wave[wave][digit];  // (other lanes of the wave write it)
+      volatile uint16_t *const place = &count[digit * kSortWaves + wave];  // (other lanes of the wave write it)
       const uint32_t had = *place;
       local[g] = had + rank;
       __builtin_amdgcn_wave_barrier();
@@ -147,62 +160,70 @@ __device__ __forceinline__ void sort_pass(const SortArgs &a, uint16_t (*in_wave)
     __builtin_amdgcn_wave_barrier();
   }
   __syncthreads();
-  // a thread's two digits: their waves one behind the other, and the digits one behind the other
-  uint32_t sum[2] = {0, 0};
-#pragma unroll
-  for (uint32_t i = 0; i < 2; ++i) {
-    const uint32_t d = threadIdx.x * 2 + i;
-    if (d < digits) {
-      uint32_t n = 0;
-      for (uint32_t w = 0; w < kSortWaves; ++w) {
-        const uint32_t c = in_wave[w][d];
-        in_wave[w][d] = (uint16_t)n;
-        n += c;
-      }
-      sum[i] = kAlone ? n : a.total[d];
+  // what is in front, digit by digit and wave by wave: a thread has neighbouring counts
+  const uint32_t each = max(digits * kSortWaves / kSortThreads, 1u), first = threadIdx.x * each;
+  uint32_t sum = 0;
+  if (first < digits * kSortWaves)
+    for (uint32_t i = 0; i < each; ++i) sum += count[first + i];
+  const auto in_front = [&](uint32_t mine) {  // of all threads
+    const uint32_t up_to = (uint32_t)wave_inclusive_scan(mine);
+    if (lane == kWave - 1) of_wave[wave] = up_to;
+    __syncthreads();
+    const uint32_t waves = (uint32_t)wave_inclusive_scan(lane < kSortWaves ? of_wave[lane] : 0);
+    __syncthreads();
+    return up_to - mine + (wave ? (uint32_t)__builtin_amdgcn_readlane((int)waves, (int)__builtin_amdgcn_readfirstlane((int)wave) - 1) : 0);
+  };
+  uint32_t before = in_front(sum);
+  if (first < digits * kSortWaves)
+    for (uint32_t i = 0; i < each; ++i) {
+      const uint32_t c = count[first + i];
+      count[first + i] = (uint16_t)before;
+      before += c;
     }
-  }
-  const uint32_t up_to = (uint32_t)wave_inclusive_scan(sum[0] + sum[1]);
-  if (lane == kWave - 1) of_wave[wave] = up_to;
-  __syncthreads();
-  uint32_t before = up_to - sum[0] - sum[1];
-  for (uint32_t w = 0; w < wave; ++w) before += of_wave[w];
-#pragma unroll
-  for (uint32_t i = 0; i < 2; ++i) {
-    const uint32_t d = threadIdx.x * 2 + i;
-    if (d < digits) base[d] = before + (kAlone ? 0 : a.count[(uint64_t)d * a.tiles + blockIdx.x]);
-    before += sum[i];
+  if (!kAlone) {
+    // (a thread's two digits)
+    const uint32_t d = threadIdx.x * 2;
+    const uint32_t n0 = d < digits ? a.total[d] : 0, n1 = d + 1 < digits ? a.total[d + 1] : 0;
+    const uint32_t front = in_front(n0 + n1);
+    __syncthreads();
+    if (d < digits) base[d] = front + a.count[(uint64_t)d * a.tiles + blockIdx.x] - count[d * kSortWaves];
+    if (d + 1 < digits) base[d + 1] = front + n0 + a.count[(uint64_t)(d + 1) * a.tiles + blockIdx.x] - count[(d + 1) * kSortWaves];
   }
   __syncthreads();
 #pragma unroll
   for (uint32_t g = 0; g < kGroups; ++g) {
     if (g >= groups || begin + g * kWave >= tile_end) continue;
     const uint32_t digit = (key[g] >> a.shift) & (digits - 1);
-    const uint32_t to = base[digit] + in_wave[wave][digit] + local[g];
-    a.key_out[to] = key[g];
-    a.index_out[to] = index[g];
+    const uint32_t to = (kAlone ? 0 : base[digit]) + count[digit * kSortWaves + wave] + local[g];
+    if (kAlone) {
+      held[to] = Held{key[g], index[g]};
+    } else {
+      a.key_out[to] = key[g];
+      a.index_out[to] = index[g];
+    }
   }
 }
 
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a)
 {
-  __shared__ uint16_t in_wave[kSortWaves][kDigits];
+  __shared__ __align__(16) uint16_t count[kDigits * kSortWaves];
   __shared__ uint32_t base[kDigits];
-  sort_pass<false>(a, in_wave, base);
+  sort_pass<false>(a, count, base, nullptr, false);
 }
 
-// Both passes by one workgroup: what the first has written is the second's input (behind a barrier, through memory that no
-// other workgroup looks at).
+// Both passes by one workgroup.
 __global__ __launch_bounds__(kSortThreads) void sort_alone_kernel(SortArgs first, SortArgs second)
 {
-  __shared__ uint16_t in_wave[kSortWaves][kDigits];
-  __shared__ uint32_t base[kDigits];
-  sort_pass<true>(first, in_wave, base);
+  __shared__ __align__(16) uint16_t count[kDigits * kSortWaves];
+  __shared__ Held held[kSortAlone];
+  sort_pass<true>(first, count, nullptr, held, false);
+  __syncthreads();
   if (second.bits) {
-    __threadfence_block();
+    sort_pass<true>(second, count, nullptr, held, true);
     __syncthreads();
-    sort_pass<true>(second, in_wave, base);
   }
+  const SortArgs &last = second.bits ? second : first;
+  for (uint32_t i = threadIdx.x; i < first.N; i += kSortThreads) last.key_out[i] = held[i].key, last.index_out[i] = held[i].index;
 }
 
 struct EmbedBackArgs {
@@ -211,7 +232,7 @@ struct EmbedBackArgs {
   const void *dout;
   const uint32_t *key, *index;    // sorted
   uint32_t *begin, *end;          // [V]: a token's places, where it has any (else whatever was there)
-  float *slice, *slice2;          // sums of slices of 64 and of 4096 that are one token's
+  float *slice, *slice2;          // sums of slices of 64 and of 4096 that are one token's (null: of 64 alone)
   float scale;
   bool add;
   void *dtable;
@@ -232,19 +253,19 @@ __device__ __forceinline__ void add_row(const T *row, uint32_t at, uint32_t D, f
   }
 }
 
-// The rows of places [from, to), in their order, four on their way at once.
-template <typename T, int N>
+// The rows of places [from, to), in their order, kAhead on their way at once.
+template <typename T, int N, uint32_t kAhead>
 __device__ __forceinline__ void add_places(const EmbedBackArgs &a, uint32_t from, uint32_t to, uint32_t at, float (&sum)[N])
 {
   const T *const dout = static_cast<const T *>(a.dout);
   uint32_t i = from;
   if (at + N <= a.D) {
-    for (; i + 4 <= to; i += 4) {
-      Run<T, N> r[4];
+    for (; i + kAhead <= to; i += kAhead) {
+      Run<T, N> r[kAhead];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) r[j] = load_run<T, N>(dout + a.index[i + j] * a.dout_row + at);
+      for (uint32_t j = 0; j < kAhead; ++j) r[j] = load_run<T, N>(dout + a.index[i + j] * a.dout_row + at);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (uint32_t j = 0; j < kAhead; ++j)
 #pragma unroll
         for (int e = 0; e < N; ++e) sum[e] += element<N, T>(r[j], e);
     }
@@ -285,7 +306,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_slices_kernel(EmbedBackAr
   const uint32_t at = (piece * kWave + lane) * N;
   if (at >= a.D) return;
   float sum[N] = {};
-  add_places<T, N>(a, (uint32_t)from, (uint32_t)from + kSlice, at, sum);
+  add_places<T, N, 8>(a, (uint32_t)from, (uint32_t)from + kSlice, at, sum);
   put_sums<N>(a.slice + (uint64_t)s * a.D, at, a.D, sum);
 }
 
@@ -324,16 +345,16 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_rows_kernel(EmbedBackArgs
     const uint32_t end = a.end[v];
     const uint32_t whole = (begin + kSlice - 1) / kSlice * kSlice, last = end / kSlice * kSlice;   // (N stays below 2^31)
     if (whole >= last) {
-      add_places<T, N>(a, begin, end, at, sum);
+      add_places<T, N, 4>(a, begin, end, at, sum);
     } else {
-      add_places<T, N>(a, begin, whole, at, sum);
+      add_places<T, N, 4>(a, begin, whole, at, sum);
       for (uint32_t i = whole; i < last;) {
-        const bool many = i % kSlice2 == 0 && last - i >= kSlice2;
+        const bool many = a.slice2 && i % kSlice2 == 0 && last - i >= kSlice2;
         const float *const from = many ? a.slice2 + (uint64_t)(i / kSlice2) * a.D : a.slice + (uint64_t)(i / kSlice) * a.D;
         add_row<float, N>(from, at, a.D, sum);
         i += many ? kSlice2 : kSlice;
       }
-      add_places<T, N>(a, last, end, at, sum);
+      add_places<T, N, 4>(a, last, end, at, sum);
     }
 #pragma unroll
     for (uint32_t e = 0; e < N; ++e) sum[e] *= a.scale;
@@ -449,14 +470,15 @@ int apex_embedding_backward(uint32_t N, uint32_t V, uint32_t D, int dtype, const
     }
   }
   const EmbedBackArgs a{N, V, D, dout_stride, dtable_stride, dout, sort[passes - 1].key_out, sort[passes - 1].index_out, words(s.begin),
-                        words(s.end), reinterpret_cast<float *>(space + s.slice), reinterpret_cast<float *>(space + s.slice2), scale,
+                        words(s.end), reinterpret_cast<float *>(space + s.slice),
+                        N >= kSlice2From ? reinterpret_cast<float *>(space + s.slice2) : nullptr, scale,
                         add != 0, dtable, (uint64_t)V * D * size > kPastCachesBytes};
   with_type(dtype, [&](auto t) {
     typedef decltype(t) E;
     constexpr uint32_t kWaves = kEmbedThreads / kWave;
     const uint64_t pieces = blocks_for(D, kWave * 16 / sizeof(E));
     embed_slices_kernel<E><<<dim3(blocks_for(blocks_for(N, kSlice) * pieces, kWaves)), dim3(kEmbedThreads), 0, stream>>>(a);
-    if (N >= kSlice2)
+    if (a.slice2)
       embed_slices2_kernel<<<dim3(blocks_for((uint64_t)(N / kSlice2) * blocks_for(D, kWave), kWaves)), dim3(kEmbedThreads), 0, stream>>>(a);
     embed_rows_kernel<E><<<dim3(blocks_for(V * pieces, kWaves)), dim3(kEmbedThreads), 0, stream>>>(a);
   });
