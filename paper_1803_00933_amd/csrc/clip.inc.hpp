@@ -90,7 +90,9 @@ __device__ __forceinline__ double squares(const T *x, uint64_t begin, uint64_t e
   return sum[0] + sum[1];
 }
 
-// A workgroup per piece; the last of all of them to be done sums the pieces up, in their order.
+// A workgroup per piece; the last of all of them to be done sums the pieces up, in their order.  Bound by memory: 729 M elements of bf16
+// 269 us, 5.4 TB/s; 80 M 53, of which the counter is some: workgroups count themselves one after the other, 14 ns each, so there are
+// not too many (8192 pieces 70 us and 267, 2048 45 and 300).
 __global__ __launch_bounds__(kClipThreads) void clip_norm_kernel(ClipArgs a)
 {
   constexpr uint32_t kWaves = kClipThreads / kWave;
@@ -141,7 +143,8 @@ __global__ __launch_bounds__(kClipThreads) void clip_norm_kernel(ClipArgs a)
   }
 }
 
-// The pieces from the last one on: what the sums have read last is still in the caches.
+// The pieces from the last one on: what the sums have read last is still in the caches.  Bound by memory: 729 M elements of bf16 573 us,
+// 5.1 TB/s read and written.
 __global__ __launch_bounds__(kClipThreads) void clip_scale_kernel(ClipArgs a)
 {
   const float factor = a.space->factor, power = a.space->power;

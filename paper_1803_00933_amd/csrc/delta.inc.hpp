@@ -189,7 +189,11 @@ __device__ __forceinline__ Operand<N> operand_of(const Tile &x, const Tile &y)
 
 // ---- what does not depend on a state, for every piece: its gates, M and P (or their transposes) and, by the first of the value
 // heads that share them, the keys and queries and their transposes, in the order in which the kernels behind take them as operands:
-// 64 lanes times 8 numbers, lane l has row l % 16 of the tile and numbers 8 (l / 16) .. + 7 of the 32.
+// 64 lanes times 8 numbers, lane l has row l % 16 of the tile and numbers 8 (l / 16) .. + 7 of the 32.  (Rows of a strided array are far
+// apart, often in the same channel of a cache, and were asked for by every 16 columns of every head: 773 us in place of 684.)
+// Bound by what it writes, 78 KB for a piece and head in 16 bits: 223 us for 4 x 8192 steps of 16 heads, 2.9 TB/s; forwards and
+// backwards each.  M's substitution is by blocks of 16: the inverses on the diagonal by a lane per column, all else by 32-bit
+// matrix instructions, with what they leave taken as it lies (row by row for all 64, and keys by 32-bit instructions, 485 us when this was 240).
 constexpr uint32_t kOperand = 64 * 8;                         // numbers
 constexpr uint32_t kTriangle = 6;                             // operands of a triangular matrix: 4 tiles of rows by 2 of 32 steps, less 2
 constexpr uint32_t kGateWords = 512;
@@ -658,8 +662,8 @@ __device__ __forceinline__ void store_state(const Tile (&S)[2 * KS], float *to, 
   }
 }
 // States that only these kernels read (the carry and its gradient) lie by 16 columns, [ceil(Dv / 16)][rows][16], the rows of every
-// 32 in the order 0, 8, 16, 24, 1, 9 ..: what a wave reads or writes of them with one instruction is 256 bytes in one place.  (By rows of Dv, 64 bytes out of every 512 were asked for at a time, which is a quarter of the
-// channels of an L2 cache: the gradient of 4 x 8192 steps of 16 heads 1.74 ms, by columns XXXX.)
+// 32 in the order 0, 8, 16, 24, 1, 9 ..: what a wave reads or writes of them with one instruction is 256 bytes in one place.  (By rows of Dv an instruction has 64 bytes
+// out of every 512: without the carry's stores the forward kernel of 4 x 8192 steps of 16 heads took 480 us in place of 621.)
 __device__ __forceinline__ uint32_t slice_size(uint32_t Dk) { return (Dk + 31) / 32 * 32 * 16; }
 __device__ __forceinline__ uint64_t slices_size(uint32_t Dk, uint32_t Dv) { return (uint64_t)((Dv + 15) / 16) * slice_size(Dk); }
 __device__ __forceinline__ uint32_t slice_row(uint32_t d) { return d / 32 * 32 + d % 8 * 4 + d / 8 % 4; }
@@ -691,6 +695,10 @@ __device__ __forceinline__ void load_slice(Tile (&S)[2 * KS], const float *from,
 
 // What the next piece takes is asked for as soon as this one has taken its own: in the same registers, which a wave has 512 of.
 // (Numbers of 32 bits are twice as many; there a piece's are asked for at its begin.)
+// Bound by the chain from piece to piece: X, E, U and the state, 132 products of tiles and some 850 other instructions of one wave in
+// bf16, 5900 cycles, and as long again for the requests to be taken while four waves of a compute unit ask for 330 KB a piece: 4 x 8192
+// steps of 16 heads of 128 x 128 in bf16 596 us, 4.6 us a piece (without any loads and stores 163); f16, whose keys are two parts,
+// 1 x 16384 of 8 heads 1125 us, 4.4 a piece; f32 6.7 a piece.  With 32-bit matrix instructions, all in LDS, 52 us a piece.
 template <typename T, uint32_t KS, uint32_t kSlices>
 __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(DeltaForward f, Prepared w)
 {
@@ -806,7 +814,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
 }
 
 // The same from the last piece to the first, with dS.  The first wave carries it, the second brings P^T dO and Q^T (c dO) and
-// stores dS, Y and dV.
+// stores dS, Y and dV.  Bound as the way there: 748 us, 5.8 us a piece, of 4 x 8192 steps of 16 heads of 128 x 128 in bf16.
 template <typename T, uint32_t KS, uint32_t kSlices>
 __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(DeltaBack b, Prepared w)
 {
@@ -955,6 +963,9 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
 // What is left of the gradient, a workgroup of eight waves per piece and key head: first a wave has 16 of the state's columns and all
 // steps, and finds U anew; then a wave has a tile of the state's rows and KS tiles of steps, and sums over the columns.  Between the
 // two U and dV cross LDS, in parts.
+// Bound by the chain of its phases, one workgroup a compute unit: keys and state, M, 32 columns after another, B and C, their products
+// with keys and queries, a wait for memory or for all waves between any two.  4 x 8192 steps of 16 heads of 128 x 128 in bf16 1.06 ms, of
+// which its products are 0.19; with 32-bit matrix instructions 3.6.
 constexpr uint32_t kGradThreads = 512, kGradWaves = kGradThreads / kWave, kGradRow = kDeltaMaxWidth + 8;
 
 struct GradSpace {
@@ -1285,6 +1296,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
 
 // ---- few steps: one after the other, the state in registers.  A workgroup has 64 columns of a state, a thread 8 rows of 4 of
 // them; what crosses between rows are three sums a step: k . S, q . S and q . k, so that a step has one barrier.
+// One step is bound by memory, the states read and written once: 64 sequences of 16 heads of 128 x 128 25.4 us, 5.3 TB/s.
 constexpr uint32_t kStepColumns = 64, kStepRows = 8;
 
 template <typename T>
@@ -1426,7 +1438,15 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_steps_kernel(DeltaForward
 
 namespace {
 
-constexpr uint32_t kDeltaSteps = 16;  // sequences of at most so many steps are computed step by step
+// Sequences of at most so many steps are computed step by step, of the second number where workgroups are more than compute units.
+// (A step takes 1.5 us, the pieces' two launches 17 where there are few workgroups: 8 heads of 128 x 128 8 steps 16 us, 12 steps 22,
+// by pieces 17; 64 sequences of 16 of them 16 steps 103 us, by pieces 150, of 8 heads of 64 x 64 35 and 36.)
+constexpr uint32_t kDeltaFew = 8, kDeltaSteps = 16;
+
+bool delta_by_steps(uint32_t S, uint32_t T, uint32_t H, uint32_t Dv)
+{
+  return T <= kDeltaFew || (T <= kDeltaSteps && (uint64_t)S * H * blocks_for(Dv, kStepColumns) > kChipCus);
+}
 
 // f(integral_constant<uint32_t>): the width of keys and queries, in 32.
 template <typename F>
@@ -1450,7 +1470,7 @@ int delta_sizes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, bo
   uint64_t heads;
   if (__builtin_mul_overflow((uint64_t)S * blocks_for(T, kPiece), (uint64_t)H, &heads) || heads > APEX_DELTA_MAX_PIECES) return APEX_ERR_TOO_LARGE;
   *n = DeltaBytes{};
-  if (!backward && T <= kDeltaSteps) return APEX_OK;
+  if (!backward && T <= kDeltaFew) return APEX_OK;  // (sizes grow with the sequences, whether or not a call takes the steps)
   const auto take = [&](uint64_t bytes) {
     const uint64_t at = n->bytes;
     n->bytes += round_up(bytes, 256);
@@ -1536,7 +1556,7 @@ int apex_delta_rule(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, uint32_t Dk
       (n.bytes && (!workspace || (uintptr_t)workspace % 256)))
     return APEX_ERR_INVALID_ARG;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  if (T <= kDeltaSteps) {
+  if (delta_by_steps(S, T, H, Dv)) {
     with_type(dtype, [&](auto t) {
       delta_steps_kernel<decltype(t)><<<dim3(S * H * blocks_for(Dv, kStepColumns)), dim3(kDeltaThreads), 0, stream>>>(f);
     });

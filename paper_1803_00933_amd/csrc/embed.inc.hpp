@@ -22,7 +22,8 @@ struct EmbedArgs {
 };
 
 // Rows of `lanes` lanes each; a token outside the table has a row of zeros.
-// Bound by memory: every row is read where it is named and written once.
+// Bound by memory: every row is read where it is named and written once.  32768 rows of 2048 in bf16 30.5 us, 4.4 TB/s written and as
+// much read, in part from the caches; 64 rows of 1024 2.2.
 template <typename T>
 __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs a)
 {
@@ -211,7 +212,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a)
   sort_pass<false>(a, count, base, nullptr, false);
 }
 
-// Both passes by one workgroup.
+// Both passes by one workgroup: 6144 tokens of 32768 15.6 us, 7777 of 49999 22; groups of a wave one after the other, and LDS.  In tiles
+// of 2048 by as many workgroups, three launches a pass, 32768 tokens of 131072 take 31.
 __global__ __launch_bounds__(kSortThreads) void sort_alone_kernel(SortArgs first, SortArgs second)
 {
   __shared__ __align__(16) uint16_t count[kDigits * kSortWaves];
@@ -327,7 +329,8 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_slices2_kernel(EmbedBackA
 }
 
 // A wave per row of the table and piece of it.  Bound by memory: the table's gradient is written once (zeros where a token is not
-// named), the rows that name it are read once.
+// named), the rows that name it are read once.  131072 x 2048 in bf16 with 32768 places 103 us, 5.2 TB/s written.  (Eight rows on their
+// way instead of four, or four slices, cost registers and waves: 121 and 126.)
 template <typename T>
 __global__ __launch_bounds__(kEmbedThreads) void embed_rows_kernel(EmbedBackArgs a)
 {

@@ -83,7 +83,7 @@ class Delta:
             check(got[n], want[n], bound, torch.float32 if n in ("h_last", "dg", "dbeta", "dh0") else self.dtype, n)
 
 
-SHAPES = [(1, 1, 1, 1, 1, 1), (3, 1, 2, 4, 128, 128), (2, 5, 1, 3, 12, 70), (2, 16, 2, 2, 65, 3), (2, 17, 1, 2, 16, 16), (3, 63, 1, 1, 33, 47),
+SHAPES = [(1, 1, 1, 1, 1, 1), (3, 1, 2, 4, 128, 128), (2, 5, 1, 3, 12, 70), (2, 8, 1, 2, 30, 64), (2, 9, 1, 2, 70, 64), (2, 16, 2, 2, 65, 3), (2, 17, 1, 2, 16, 16), (3, 63, 1, 1, 33, 47),
           (2, 64, 2, 2, 64, 64), (2, 65, 1, 2, 100, 128), (1, 129, 2, 6, 128, 20), (3, 200, 1, 1, 17, 33), (1, 513, 1, 2, 128, 128)]
 
 
@@ -97,7 +97,7 @@ def test_delta(apex, shape, dtype, cut, ragged):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_delta_many_sequences(apex, dtype):
     # (the last one: more slices of 16 columns than compute units, an odd number a head)
-    for shape in ((70, 3, 2, 2, 16, 40), (90, 70, 1, 4, 32, 96), (300, 20, 1, 1, 8, 8), (20, 70, 1, 2, 72, 100), (9, 130, 4, 4, 128, 128)):
+    for shape in ((70, 3, 2, 2, 16, 40), (130, 16, 2, 2, 20, 70), (90, 70, 1, 4, 32, 96), (300, 20, 1, 1, 8, 8), (20, 70, 1, 2, 72, 100), (9, 130, 4, 4, 128, 128)):
         c = Delta(*shape, dtype, seed=shape[0], cut=True, ragged=True)
         c.check(c.run(apex))
 

@@ -21,12 +21,13 @@ def delta(S, T, Hk, H, Dk, Dv, back=False, dtype=1, workspace=True):
 
 def test_delta_rule_by_steps_and_by_pieces(tmp_path):
     out = recorded_hip.run(tmp_path, DELTA + """
-result = [delta(64, 1, 16, 16, 128, 128), delta(2, 16, 1, 3, 16, 65, workspace=False), delta(2, 17, 1, 3, 16, 65), delta(2, 17, 1, 3, 16, 65, workspace=False),
-          delta(4, 8192, 8, 16, 128, 128), delta(4, 8192, 8, 16, 128, 128, back=True)]
+result = [delta(64, 1, 16, 16, 128, 128), delta(2, 8, 1, 3, 16, 65, workspace=False), delta(2, 9, 1, 3, 16, 65), delta(2, 17, 1, 3, 16, 65, workspace=False),
+          delta(4, 8192, 8, 16, 128, 128), delta(4, 8192, 8, 16, 128, 128, back=True),
+          delta(64, 16, 8, 8, 64, 64), delta(64, 17, 8, 8, 64, 64), delta(32, 16, 8, 8, 64, 64), delta(33, 16, 8, 8, 64, 64)]
 """)
-    assert [r for r, _ in out] == [0, 0, 0, -1, 0, 0]
+    assert [r for r, _ in out] == [0, 0, 0, -1, 0, 0, 0, 0, 0, 0]
     names = [[k for k, _, _ in l] for _, l in out]
-    assert ["steps" in n[0] for n in names[:2]] == [True, True] and [len(n) for n in names] == [1, 1, 2, 0, 2, 3]
+    assert ["steps" in n[0] for n in names[:2]] == [True, True] and [len(n) for n in names] == [1, 1, 2, 0, 2, 3, 1, 2, 2, 1]
     assert out[0][1][0][1:] == [64 * 16 * 2, 256] and out[1][1][0][1:] == [2 * 3 * 2, 256]
     for l in (out[2][1], out[4][1], out[5][1]):
         assert "prepare" in l[0][0] and "pieces" in l[1][0]

@@ -91,7 +91,9 @@ def test_delta_rule_workspace(apex):
         n = C.c_size_t(0)
         assert apex.lib.apex_delta_rule_workspace_bytes(*sizes, C.byref(n)) == apex.OK
         return n.value
-    assert need(5, 1, 3, 8, 8, 0) == need(5, 16, 3, 8, 8, 0) == 0
+    assert need(5, 1, 3, 8, 8, 0) == need(5, 8, 3, 8, 8, 0) == 0
+    # what is enough for larger sizes is enough: also where those are computed step by step
+    assert 0 < need(5, 16, 3, 8, 8, 0) <= need(500, 16, 3, 8, 8, 0) <= need(500, 17, 3, 8, 8, 0)
     assert 0 < need(1, 100, 3, 8, 8, 0) < need(2, 100, 3, 8, 8, 0) < need(2, 200, 3, 8, 8, 0)
     for sizes in ((2, 100, 3, 8, 8), (2, 1, 3, 128, 128)):
         assert need(*sizes, 1) > need(*sizes, 0)
