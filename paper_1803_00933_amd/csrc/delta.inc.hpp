@@ -164,15 +164,15 @@ __device__ __forceinline__ Operand<kPartsOf<T>> operand(const Run<T, 8> &x)
   }
 }
 
-// acc + A B over 32: operands' parts together below the `limit`-th.
-template <uint32_t kLimit, uint32_t NA, uint32_t NB>
+// acc + A B over 32: of the parts' products those that are not below the last bit.
+template <uint32_t NA, uint32_t NB>
 __device__ __forceinline__ void multiply(Tile &acc, const Operand<NA> &a, const Operand<NB> &b)
 {
 #pragma unroll
   for (uint32_t i = 0; i < NA; ++i)
 #pragma unroll
     for (uint32_t j = 0; j < NB; ++j)
-      if (i + j < kLimit) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.part[i], b.part[j], acc, 0, 0, 0);
+      if (i + j < 3) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.part[i], b.part[j], acc, 0, 0, 0);
 }
 
 // Two tiles on top of each other as the right operand of the next product: a lane of group q has rows 8 q .. 8 q + 7 of the 32 if
@@ -342,8 +342,8 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
         Run<T, 8> key;
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e) key[e] = raw[c * 16 + m][i * 32 + q * 8 + e];
-        multiply<3>(kk, operand<T>(k_own[i]), operand<T>(key));
-        multiply<3>(qk, operand<T>(q_own[i]), operand<T>(key));
+        multiply(kk, operand<T>(k_own[i]), operand<T>(key));
+        multiply(qk, operand<T>(q_own[i]), operand<T>(key));
       }
     }
 #pragma unroll
@@ -591,26 +591,25 @@ struct PieceColumns {  // their transposes, prepared
       for (uint32_t s = 0; s < 2; ++s) x[i][s] = *reinterpret_cast<const Run<T, 8> *>(p + (i * 2 + s) * kOperand);
   }
 };
-template <uint32_t N>
 struct PieceTriangle {
-  Operand<N> x[kTriangle];
+  Operand<3> x[kTriangle];
   __device__ __forceinline__ void load(const __bf16 *from, uint64_t head)
   {
     const __bf16 *const p = from + head * (kTriangle * 3 * kOperand) + lane_id() * 8;
 #pragma unroll
     for (uint32_t f = 0; f < kTriangle; ++f)
 #pragma unroll
-      for (uint32_t n = 0; n < N; ++n) x[f].part[n] = *reinterpret_cast<const Parts8 *>(p + (f * 3 + n) * kOperand);
+      for (uint32_t n = 0; n < 3; ++n) x[f].part[n] = *reinterpret_cast<const Parts8 *>(p + (f * 3 + n) * kOperand);
   }
   // acc + the matrix times right, whose operands are its rows 0..31 and 32..63
-  template <uint32_t kLimit, bool kUpper, uint32_t NB>
+  template <bool kUpper, uint32_t NB>
   __device__ __forceinline__ void times(Tile (&acc)[4], const Operand<NB> (&right)[2]) const
   {
 #pragma unroll
     for (uint32_t f = 0; f < kTriangle; ++f) {
       const uint32_t r = kUpper ? (f < 4 ? f / 2 : f - 2) : (f < 2 ? f : 2 + (f - 2) / 2);
       const uint32_t s = kUpper ? (f < 4 ? f % 2 : 1) : (f < 2 ? 0 : (f - 2) % 2);
-      multiply<kLimit>(acc[r], x[f], right[s]);
+      multiply(acc[r], x[f], right[s]);
     }
   }
 };
@@ -722,7 +721,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
     if (f.h0) load_state<KS>(S, f.h0 + state, a.Dk, a.Dv, place.c0);
     PieceKeys<T, KS> K;
     PieceSlice<T> V;
-    PieceTriangle<3> M;
+    PieceTriangle M;
     PieceColumns<T, KS> Kt;
     AllGates gates;
     const auto load_keys = [&](uint32_t piece) {
@@ -743,7 +742,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
         const Operand<3> parts = operand_of<3>(S[2 * i], S[2 * i + 1]);
         put(states[piece % 2][i], parts);
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) multiply<3>(kS[r], operand<T>(K.x[r][i]), parts);
+        for (uint32_t r = 0; r < 4; ++r) multiply(kS[r], operand<T>(K.x[r][i]), parts);
       }
 #pragma unroll
       for (uint32_t r = 0; r < 4; ++r) X[r] = V.tile(r) - passed(kS[r], gates.begin.tile[r]);
@@ -751,7 +750,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
       const Operand<3> bX[2] = {operand_of<3>(scaled(X[0], gates.beta.tile[0]), scaled(X[1], gates.beta.tile[1])),
                                 operand_of<3>(scaled(X[2], gates.beta.tile[2]), scaled(X[3], gates.beta.tile[3]))};
       Tile mX[4] = {}, U[4];
-      M.template times<3, false>(mX, bX);
+      M.times<false>(mX, bX);
       if (kAhead) M.load(w.M, head_of(next));
 #pragma unroll
       for (uint32_t r = 0; r < 4; ++r) U[r] = scaled(X[r] - mX[r], gates.beta.tile[r]);
@@ -763,7 +762,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
       for (uint32_t i = 0; i < 2 * KS; ++i) {
         S[i] = gates.last != 0.0f ? S[i] * gates.last : Tile{};
 #pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) multiply<3>(S[i], operand<T>(Kt.x[i][j]), left[j]);
+        for (uint32_t j = 0; j < 2; ++j) multiply(S[i], operand<T>(Kt.x[i][j]), left[j]);
       }
       if (kAhead) load_columns(next);
       meet();
@@ -779,7 +778,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
     T *const o = static_cast<T *>(f.o) + ((uint64_t)s * a.T * a.H + h) * a.Dv;
     const uint64_t o_row = (uint64_t)a.H * a.Dv;
     PieceKeys<T, KS> Q;
-    PieceTriangle<3> P;
+    PieceTriangle P;
     RowGates begin;
     const auto load = [&](uint32_t piece) {
       Q.load(w.Q, ((uint64_t)s * a.pieces + piece) * a.Hk + hk);
@@ -796,13 +795,13 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
       for (uint32_t i = 0; i < KS; ++i) {
         S[i] = get<3>(states[piece % 2][i]);
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) multiply<3>(O[r], operand<T>(Q.x[r][i]), S[i]);
+        for (uint32_t r = 0; r < 4; ++r) multiply(O[r], operand<T>(Q.x[r][i]), S[i]);
       }
 #pragma unroll
       for (uint32_t r = 0; r < 4; ++r) O[r] = passed(O[r], begin.tile[r]);
       const Tile(&found)[4][kWave] = corrections[piece % 2];
       const Operand<3> U[2] = {operand_of<3>(found[0][lane], found[1][lane]), operand_of<3>(found[2][lane], found[3][lane])};
-      P.template times<3, false>(O, U);
+      P.times<false>(O, U);
       if (kAhead) load(min(piece + 1, pieces - 1));
       if (f.carry && place.c0 < a.Dv) store_slice<KS>(S, f.carry + head_of(piece) * slices_size(a.Dk, a.Dv), a.Dk, place.c0 / 16, column);
       if (column)
@@ -843,7 +842,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
     Tile S[2 * KS] = {};
     if (b.dh_last && (len == 0 || delta_passes(a, s, len - 1))) load_state<KS>(S, b.dh_last + state, a.Dk, a.Dv, place.c0);
     PieceKeys<T, KS> K;
-    PieceTriangle<3> M;
+    PieceTriangle M;
     PieceColumns<T, KS> Kt;
     AllGates gates;
     const auto load_keys = [&](uint32_t piece) { K.load(w.K, key_head_of(piece)); };
@@ -864,7 +863,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
         const Operand<3> parts = operand_of<3>(S[2 * i], S[2 * i + 1]);
         put(states[piece % 2][i], parts);
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) multiply<3>(kS[r], operand<T>(K.x[r][i]), parts);
+        for (uint32_t r = 0; r < 4; ++r) multiply(kS[r], operand<T>(K.x[r][i]), parts);
       }
       if (kAhead) load_keys(next);
       Tile dU[4];
@@ -873,7 +872,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
       const Operand<3> bU[2] = {operand_of<3>(scaled(dU[0], gates.beta.tile[0]), scaled(dU[1], gates.beta.tile[1])),
                                 operand_of<3>(scaled(dU[2], gates.beta.tile[2]), scaled(dU[3], gates.beta.tile[3]))};
       Tile mU[4] = {}, V[4];
-      M.template times<3, true>(mU, bU);
+      M.times<true>(mU, bU);
       if (kAhead) M.load(w.M, head_of(next));
 #pragma unroll
       for (uint32_t r = 0; r < 4; ++r) {
@@ -886,7 +885,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
       for (uint32_t i = 0; i < 2 * KS; ++i) {
         S[i] = (gates.last != 0.0f ? S[i] * gates.last : Tile{}) + brought[piece % 2].state[i][lane];
 #pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) multiply<3>(S[i], operand<T>(Kt.x[i][j]), left[j]);
+        for (uint32_t j = 0; j < 2; ++j) multiply(S[i], operand<T>(Kt.x[i][j]), left[j]);
       }
       if (kAhead) load_columns(next);
       meet();
@@ -895,7 +894,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
   } else {
     T *const dv = static_cast<T *>(b.dv) + s * b.dv_seq + (uint64_t)h * a.Dv;
     PieceSlice<T> taken;
-    PieceTriangle<3> P;
+    PieceTriangle P;
     PieceColumns<T, KS> Qt;
     RowGates begin;
     const auto load = [&](uint32_t piece) {
@@ -910,7 +909,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
       for (uint32_t r = 0; r < 4; ++r) dO[r] = taken.tile(r);  // (zeros behind the sequence's end)
       const Operand<kPartsOf<T>> right[2] = {operand_of<kPartsOf<T>>(dO[0], dO[1]), operand_of<kPartsOf<T>>(dO[2], dO[3])};
       Tile of_o[4] = {};
-      P.template times<3, true>(of_o, right);
+      P.times<true>(of_o, right);
 #pragma unroll
       for (uint32_t r = 0; r < 4; ++r) {
         brought[piece % 2].o[r][lane] = a.scale * of_o[r];
@@ -921,7 +920,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
       for (uint32_t i = 0; i < 2 * KS; ++i) {
         Tile x{};
 #pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) multiply<3>(x, operand<T>(Qt.x[i][j]), left[j]);
+        for (uint32_t j = 0; j < 2; ++j) multiply(x, operand<T>(Qt.x[i][j]), left[j]);
         brought[piece % 2].state[i][lane] = x;
       }
       if (piece) load(piece - 1);
@@ -1061,7 +1060,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
         for (uint32_t i = 0; i < KS; ++i) {
           parts[i] = operand_of<3>(S[2 * i], S[2 * i + 1]);
 #pragma unroll
-          for (uint32_t r = 0; r < 2; ++r) multiply<3>(kS[r], operand<T>(K.x[r][i]), parts[i]);
+          for (uint32_t r = 0; r < 2; ++r) multiply(kS[r], operand<T>(K.x[r][i]), parts[i]);
         }
         __builtin_amdgcn_sched_barrier(0);
         K.load(w.K, key_head, 2);
@@ -1072,9 +1071,9 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
 #pragma unroll
         for (uint32_t i = 0; i < KS; ++i)
 #pragma unroll
-          for (uint32_t r = 0; r < 2; ++r) multiply<3>(kS[2 + r], operand<T>(K.x[r][i]), parts[i]);
+          for (uint32_t r = 0; r < 2; ++r) multiply(kS[2 + r], operand<T>(K.x[r][i]), parts[i]);
         __builtin_amdgcn_sched_barrier(0);
-        PieceTriangle<3> M;
+        PieceTriangle M;
         M.load(w.rows, head);
         const RowGates beta = row_gates(x.gates.beta), begin = row_gates(x.gates.begin);
         Tile X[4], mX[4] = {};
@@ -1082,7 +1081,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
         for (uint32_t r = 0; r < 4; ++r) X[r] = V.tile(r) - passed(kS[r], begin.tile[r]);
         const Operand<3> bX[2] = {operand_of<3>(scaled(X[0], beta.tile[0]), scaled(X[1], beta.tile[1])),
                                   operand_of<3>(scaled(X[2], beta.tile[2]), scaled(X[3], beta.tile[3]))};
-        M.template times<3, false>(mX, bX);
+        M.times<false>(mX, bX);
         if (column < a.Dv) {
 #pragma unroll
           for (uint32_t r = 0; r < 4; ++r) {
@@ -1151,9 +1150,9 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
       }
 #pragma unroll
       for (uint32_t i = 0; i < KS; ++i) {
-        multiply<3>(oS[i], operand<T>(now.o[i]), start);
-        multiply<3>(uS[i], get_parts(x.part[0], (r0 + i) * 16 + m, c), end);
-        multiply<3>(vS[i], get_parts(x.part[1], (r0 + i) * 16 + m, c), start);
+        multiply(oS[i], operand<T>(now.o[i]), start);
+        multiply(uS[i], get_parts(x.part[0], (r0 + i) * 16 + m, c), end);
+        multiply(vS[i], get_parts(x.part[1], (r0 + i) * 16 + m, c), start);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -1179,8 +1178,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
 #pragma unroll
       for (uint32_t n = 0; n < 4; ++n) {
         const Operand<3> u = get_parts(x.part[0], j * 16 + m, n * 32 + q * 8);
-        multiply<3>(B[i], operand<T>(of_tile[i][n]), u);
-        multiply<3>(C[i], get_parts(x.part[1], r * 16 + m, n * 32 + q * 8), u);
+        multiply(B[i], operand<T>(of_tile[i][n]), u);
+        multiply(C[i], get_parts(x.part[1], r * 16 + m, n * 32 + q * 8), u);
       }
     }
     T key_at[KS][4], query_at[KS][4];  // this lane's of the keys and queries, as tiles
@@ -1230,16 +1229,16 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
         if (lower) {
 #pragma unroll
           for (uint32_t e = 0; e < 8; ++e) f[e] = x.B[0][t * kPieceRow + j + e];
-          multiply<3>(oS[i], split<3>(f), key);
+          multiply(oS[i], split<3>(f), key);
         }
         if (upper) {
 #pragma unroll
           for (uint32_t e = 0; e < 8; ++e) f[e] = x.B[0][(j + e) * kPieceRow + t];
-          multiply<3>(dk_all[i], split<3>(f), query);
+          multiply(dk_all[i], split<3>(f), query);
         }
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e) f[e] = -((lower ? x.B[1][t * kPieceRow + j + e] : 0.0f) + (upper ? x.B[1][(j + e) * kPieceRow + t] : 0.0f));
-        multiply<3>(dk_all[i], split<3>(f), key);
+        multiply(dk_all[i], split<3>(f), key);
       }
     }
     at_end = wave_sum(at_end);
