@@ -164,6 +164,18 @@ __device__ __forceinline__ Operand<kPartsOf<T>> operand(const Run<T, 8> &x)
   }
 }
 
+// Eight numbers as prepared operands hold them: as they are, or f16 in its parts, as many bytes as 32 bits.  Parts spare a wave that takes
+// a piece's keys 960 instructions, and are more to ask for; so they are for a few workgroups (1 x 16384 steps of 8 heads of 128 x 128
+// 1.24 ms without, 1.03 with them) and not for many (4 x 4096 of 16 heads 522 us and 558, its gradient 1230 and 1409).
+template <typename T, uint32_t KS, uint32_t kSlices>
+constexpr bool kInParts = std::is_same<T, _Float16>::value && KS == 4 && kSlices == 1;
+template <typename T, bool kParts>
+using Stored = std::conditional_t<kParts, Operand<kPartsOf<T>>, Run<T, 8>>;
+template <typename T>
+__device__ __forceinline__ Operand<kPartsOf<T>> prepared(const Run<T, 8> &x) { return operand<T>(x); }
+template <typename T>
+__device__ __forceinline__ Operand<kPartsOf<T>> prepared(const Operand<kPartsOf<T>> &x) { return x; }
+
 // acc + A B over 32: of the parts' products those that are not below the last bit.
 template <uint32_t NA, uint32_t NB>
 __device__ __forceinline__ void multiply(Tile &acc, const Operand<NA> &a, const Operand<NB> &b)
@@ -203,8 +215,8 @@ static_assert(sizeof(Gates) <= kGateWords * 4);
 struct Prepared {
   uint32_t *gates;   // [heads][kGateWords]: Gates
   __bf16 *M, *P;     // [heads][kTriangle][3][kOperand]
-  void *K, *Q;       // [key heads][4][KS][kOperand] of the inputs' type: keys and queries
-  void *Kt, *Qt;     // [key heads][2 KS][2][kOperand]: their transposes
+  void *K, *Q;       // [key heads][4][KS][kWave] of Stored: keys and queries
+  void *Kt, *Qt;     // [key heads][2 KS][2][kWave] of Stored: their transposes
   void *V;           // [heads][ceil(Dv / 16)][kWave][16]: values, backwards dO, as a wave that has 16 columns takes them
   __bf16 *rows;      // M beside its transpose (for the gradient)
 };
@@ -241,7 +253,7 @@ __device__ __forceinline__ Run<T, 8> load_step(const T *piece, uint64_t stride, 
   return t < have ? r : Run<T, 8>{};
 }
 
-template <typename T, uint32_t KS, bool kBack>
+template <typename T, uint32_t KS, bool kBack, bool kParts>
 __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs a, const void *d_o, Prepared w)
 {
   constexpr uint32_t kRaw = KS * 32 + 16 / sizeof(T);  // (rows begin on 16 bytes)
@@ -316,13 +328,19 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
     for (uint32_t i = 0; i < KS; ++i) *reinterpret_cast<Run<T, 8> *>(&raw[wave * 16 + m][i * 32 + q * 8]) = x[i];
   };
   const uint64_t key_head = ((uint64_t)s * a.pieces + piece) * a.Hk + hk;
+  const auto put_eight = [&](void *to_all, uint64_t at, const Run<T, 8> &x) {
+    if constexpr (kParts)
+      static_cast<Stored<T, true> *>(to_all)[at] = operand<T>(x);
+    else
+      static_cast<Stored<T, false> *>(to_all)[at] = x;
+  };
   const auto put_columns = [&](void *to_all) {
     for (uint32_t i = threadIdx.x; i < 2 * KS * 2 * kWave; i += kDeltaThreads) {
       const uint32_t l = i % kWave, ks = i / kWave % 2, tile = i / kWave / 2, d = tile_row(tile, l % 16), t = ks * 32 + l / 16 * 8;
       Run<T, 8> x;
 #pragma unroll
       for (uint32_t e = 0; e < 8; ++e) x[e] = raw[t + e][d];
-      *reinterpret_cast<Run<T, 8> *>(static_cast<T *>(to_all) + ((key_head * 2 * KS + tile) * 2 + ks) * kOperand + l * 8) = x;
+      put_eight(to_all, ((key_head * 2 * KS + tile) * 2 + ks) * kWave + l, x);
     }
   };
   // this wave's rows as operands: row t is row m of tile r
@@ -330,7 +348,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_prepare_kernel(DeltaArgs 
     const uint32_t t = wave * 16 + m, r = t / 32 * 2 + t / 4 % 2, row = t / 8 % 4 * 4 + t % 4;
 #pragma unroll
     for (uint32_t i = 0; i < KS; ++i)
-      *reinterpret_cast<Run<T, 8> *>(static_cast<T *>(to_all) + key_head * (4 * KS * kOperand) + (r * KS + i) * kOperand + (q * 16 + row) * 8) = x[i];
+      put_eight(to_all, (key_head * 4 * KS + r * KS + i) * kWave + q * 16 + row, x[i]);
   };
   put_raw(k_own);
   __syncthreads();
@@ -567,28 +585,28 @@ __device__ __forceinline__ void each_step(T *piece, uint64_t stride, uint32_t ha
       }
   }
 }
-template <typename T, uint32_t KS, uint32_t kTiles = 4>
+template <typename T, uint32_t KS, bool kParts, uint32_t kTiles = 4>
 struct PieceKeys {  // rows of keys or queries, prepared: tiles of steps from `first` on
-  Run<T, 8> x[kTiles][KS];
+  Stored<T, kParts> x[kTiles][KS];
   __device__ __forceinline__ void load(const void *from, uint64_t key_head, uint32_t first = 0)
   {
-    const T *const p = static_cast<const T *>(from) + (key_head * 4 + first) * KS * kOperand + lane_id() * 8;
+    const Stored<T, kParts> *const p = static_cast<const Stored<T, kParts> *>(from) + (key_head * 4 + first) * KS * kWave + lane_id();
 #pragma unroll
     for (uint32_t i = 0; i < kTiles; ++i)
 #pragma unroll
-      for (uint32_t s = 0; s < KS; ++s) x[i][s] = *reinterpret_cast<const Run<T, 8> *>(p + (i * KS + s) * kOperand);
+      for (uint32_t s = 0; s < KS; ++s) x[i][s] = p[(i * KS + s) * kWave];
   }
 };
-template <typename T, uint32_t KS>
+template <typename T, uint32_t KS, bool kParts>
 struct PieceColumns {  // their transposes, prepared
-  Run<T, 8> x[2 * KS][2];
+  Stored<T, kParts> x[2 * KS][2];
   __device__ __forceinline__ void load(const void *from, uint64_t key_head)
   {
-    const T *const p = static_cast<const T *>(from) + key_head * (2 * KS * 2 * kOperand) + lane_id() * 8;
+    const Stored<T, kParts> *const p = static_cast<const Stored<T, kParts> *>(from) + key_head * (2 * KS * 2 * kWave) + lane_id();
 #pragma unroll
     for (uint32_t i = 0; i < 2 * KS; ++i)
 #pragma unroll
-      for (uint32_t s = 0; s < 2; ++s) x[i][s] = *reinterpret_cast<const Run<T, 8> *>(p + (i * 2 + s) * kOperand);
+      for (uint32_t s = 0; s < 2; ++s) x[i][s] = p[(i * 2 + s) * kWave];
   }
 };
 struct PieceTriangle {
@@ -697,11 +715,11 @@ __device__ __forceinline__ void load_slice(Tile (&S)[2 * KS], const float *from,
 // Bound by the chain from piece to piece: X, E, U and the state, 132 products of tiles and some 850 other instructions of one wave in
 // bf16, 5900 cycles, and as long again for the requests to be taken while four waves of a compute unit ask for 330 KB a piece: 4 x 8192
 // steps of 16 heads of 128 x 128 in bf16 596 us, 4.6 us a piece (without any loads and stores 163); f16, whose keys are two parts,
-// 1 x 16384 of 8 heads 1125 us, 4.4 a piece; f32 6.7 a piece.  With 32-bit matrix instructions, all in LDS, 52 us a piece.
+// 1 x 16384 of 8 heads 914 us, 3.6 a piece (1125, with keys that were cut into parts where they were taken); f32 6.7 a piece.  With 32-bit matrix instructions, all in LDS, 52 us a piece.
 template <typename T, uint32_t KS, uint32_t kSlices>
 __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(DeltaForward f, Prepared w)
 {
-  constexpr bool kAhead = sizeof(T) == 2;
+  constexpr bool kAhead = sizeof(T) == 2, kParts = kInParts<T, KS, kSlices>;
   __shared__ __align__(16) __bf16 all_states[kSlices][2][KS][3 * kOperand];
   __shared__ Tile all_corrections[kSlices][2][4][kWave];  // U
   const uint32_t slice = threadIdx.x / kWave % kSlices;
@@ -719,10 +737,10 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
   if (carries) {
     Tile S[2 * KS] = {};
     if (f.h0) load_state<KS>(S, f.h0 + state, a.Dk, a.Dv, place.c0);
-    PieceKeys<T, KS> K;
+    PieceKeys<T, KS, kParts> K;
     PieceSlice<T> V;
     PieceTriangle M;
-    PieceColumns<T, KS> Kt;
+    PieceColumns<T, KS, kParts> Kt;
     AllGates gates;
     const auto load_keys = [&](uint32_t piece) {
       K.load(w.K, ((uint64_t)s * a.pieces + piece) * a.Hk + hk);
@@ -742,7 +760,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
         const Operand<3> parts = operand_of<3>(S[2 * i], S[2 * i + 1]);
         put(states[piece % 2][i], parts);
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) multiply(kS[r], operand<T>(K.x[r][i]), parts);
+        for (uint32_t r = 0; r < 4; ++r) multiply(kS[r], prepared<T>(K.x[r][i]), parts);
       }
 #pragma unroll
       for (uint32_t r = 0; r < 4; ++r) X[r] = V.tile(r) - passed(kS[r], gates.begin.tile[r]);
@@ -762,7 +780,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
       for (uint32_t i = 0; i < 2 * KS; ++i) {
         S[i] = gates.last != 0.0f ? S[i] * gates.last : Tile{};
 #pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) multiply(S[i], operand<T>(Kt.x[i][j]), left[j]);
+        for (uint32_t j = 0; j < 2; ++j) multiply(S[i], prepared<T>(Kt.x[i][j]), left[j]);
       }
       if (kAhead) load_columns(next);
       meet();
@@ -777,7 +795,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
   } else {
     T *const o = static_cast<T *>(f.o) + ((uint64_t)s * a.T * a.H + h) * a.Dv;
     const uint64_t o_row = (uint64_t)a.H * a.Dv;
-    PieceKeys<T, KS> Q;
+    PieceKeys<T, KS, kParts> Q;
     PieceTriangle P;
     RowGates begin;
     const auto load = [&](uint32_t piece) {
@@ -795,7 +813,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
       for (uint32_t i = 0; i < KS; ++i) {
         S[i] = get<3>(states[piece % 2][i]);
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) multiply(O[r], operand<T>(Q.x[r][i]), S[i]);
+        for (uint32_t r = 0; r < 4; ++r) multiply(O[r], prepared<T>(Q.x[r][i]), S[i]);
       }
 #pragma unroll
       for (uint32_t r = 0; r < 4; ++r) O[r] = passed(O[r], begin.tile[r]);
@@ -841,9 +859,9 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
   if (carries) {
     Tile S[2 * KS] = {};
     if (b.dh_last && (len == 0 || delta_passes(a, s, len - 1))) load_state<KS>(S, b.dh_last + state, a.Dk, a.Dv, place.c0);
-    PieceKeys<T, KS> K;
+    PieceKeys<T, KS, false> K;
     PieceTriangle M;
-    PieceColumns<T, KS> Kt;
+    PieceColumns<T, KS, false> Kt;
     AllGates gates;
     const auto load_keys = [&](uint32_t piece) { K.load(w.K, key_head_of(piece)); };
     const auto load_columns = [&](uint32_t piece) {
@@ -863,7 +881,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
         const Operand<3> parts = operand_of<3>(S[2 * i], S[2 * i + 1]);
         put(states[piece % 2][i], parts);
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) multiply(kS[r], operand<T>(K.x[r][i]), parts);
+        for (uint32_t r = 0; r < 4; ++r) multiply(kS[r], prepared<T>(K.x[r][i]), parts);
       }
       if (kAhead) load_keys(next);
       Tile dU[4];
@@ -885,7 +903,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
       for (uint32_t i = 0; i < 2 * KS; ++i) {
         S[i] = (gates.last != 0.0f ? S[i] * gates.last : Tile{}) + brought[piece % 2].state[i][lane];
 #pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) multiply(S[i], operand<T>(Kt.x[i][j]), left[j]);
+        for (uint32_t j = 0; j < 2; ++j) multiply(S[i], prepared<T>(Kt.x[i][j]), left[j]);
       }
       if (kAhead) load_columns(next);
       meet();
@@ -895,7 +913,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
     T *const dv = static_cast<T *>(b.dv) + s * b.dv_seq + (uint64_t)h * a.Dv;
     PieceSlice<T> taken;
     PieceTriangle P;
-    PieceColumns<T, KS> Qt;
+    PieceColumns<T, KS, false> Qt;
     RowGates begin;
     const auto load = [&](uint32_t piece) {
       taken.load(w.V, head_of(piece) * slices + min(place.c0 / 16, slices - 1));
@@ -920,7 +938,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
       for (uint32_t i = 0; i < 2 * KS; ++i) {
         Tile x{};
 #pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) multiply(x, operand<T>(Qt.x[i][j]), left[j]);
+        for (uint32_t j = 0; j < 2; ++j) multiply(x, prepared<T>(Qt.x[i][j]), left[j]);
         brought[piece % 2].state[i][lane] = x;
       }
       if (piece) load(piece - 1);
@@ -1053,14 +1071,14 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
         Tile kS[4] = {}, S[2 * KS];
         load_slice<KS>(S, S0, a.Dk, wave);
         // (half of the keys at a time, and so on: a wave has 256 registers here)
-        PieceKeys<T, KS, 2> K;
+        PieceKeys<T, KS, false, 2> K;
         K.load(w.K, key_head);
         Operand<3> parts[KS];
 #pragma unroll
         for (uint32_t i = 0; i < KS; ++i) {
           parts[i] = operand_of<3>(S[2 * i], S[2 * i + 1]);
 #pragma unroll
-          for (uint32_t r = 0; r < 2; ++r) multiply(kS[r], operand<T>(K.x[r][i]), parts[i]);
+          for (uint32_t r = 0; r < 2; ++r) multiply(kS[r], prepared<T>(K.x[r][i]), parts[i]);
         }
         __builtin_amdgcn_sched_barrier(0);
         K.load(w.K, key_head, 2);
@@ -1071,7 +1089,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
 #pragma unroll
         for (uint32_t i = 0; i < KS; ++i)
 #pragma unroll
-          for (uint32_t r = 0; r < 2; ++r) multiply(kS[2 + r], operand<T>(K.x[r][i]), parts[i]);
+          for (uint32_t r = 0; r < 2; ++r) multiply(kS[2 + r], prepared<T>(K.x[r][i]), parts[i]);
         __builtin_amdgcn_sched_barrier(0);
         PieceTriangle M;
         M.load(w.rows, head);
@@ -1205,8 +1223,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
       }
     }
     __syncthreads();
-    const T *const kt = static_cast<const T *>(w.Kt) + (key_head * 2 * KS + own) * 2 * kOperand + lane * 8;
-    const T *const qt = static_cast<const T *>(w.Qt) + (key_head * 2 * KS + own) * 2 * kOperand + lane * 8;
+    const Stored<T, false> *const kt = static_cast<const Stored<T, false> *>(w.Kt) + (key_head * 2 * KS + own) * 2 * kWave + lane;
+    const Stored<T, false> *const qt = static_cast<const Stored<T, false> *>(w.Qt) + (key_head * 2 * KS + own) * 2 * kWave + lane;
 #pragma unroll
     for (uint32_t i = 0; i < KS; ++i) {
       const Tile begin = *reinterpret_cast<const Tile *>(&x.gates.begin[state_row(r0 + i, 0)]);
@@ -1219,8 +1237,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
     }
 #pragma unroll
     for (uint32_t ks = 0; ks < 2; ++ks) {
-      const Operand<kPartsOf<T>> key = operand<T>(*reinterpret_cast<const Run<T, 8> *>(kt + ks * kOperand));
-      const Operand<kPartsOf<T>> query = operand<T>(*reinterpret_cast<const Run<T, 8> *>(qt + ks * kOperand));
+      const Operand<kPartsOf<T>> key = prepared<T>(kt[ks * kWave]);
+      const Operand<kPartsOf<T>> query = prepared<T>(qt[ks * kWave]);
 #pragma unroll
       for (uint32_t i = 0; i < KS; ++i) {
         const uint32_t r = r0 + i, t = tile_row(r, m), j = ks * 32 + q * 8;
@@ -1504,7 +1522,7 @@ uint32_t delta_groups(uint32_t S, uint32_t H, uint32_t Dv, uint32_t slices) { re
 
 // f(integral_constant<uint32_t>): slices of a workgroup.
 // Two, which read the same operands at the same time, where a compute unit has two anyway and operands are large (4 x 8192 steps of
-// 16 heads of 128 x 128 684 us by one, 621 by two); else one (1 x 16384 of 8 heads 1131 and 1289, 64 x 96 of 8 heads of 64 x 64 33.7
+// 16 heads of 128 x 128 684 us by one, 621 by two); else one (1 x 16384 of 8 heads, keys of f16 not in parts, 1131 and 1289, 64 x 96 of 8 heads of 64 x 64 33.7
 // and 36).
 template <uint32_t KS, typename F>
 void with_slices(uint32_t S, uint32_t H, uint32_t Dv, F f)
@@ -1567,9 +1585,9 @@ int apex_delta_rule(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, uint32_t Dk
     typedef decltype(t) E;
     with_width(Dk, [&](auto width) {
       constexpr uint32_t KS = decltype(width)::value;
-      delta_prepare_kernel<E, KS, false><<<dim3(S * f.n.pieces * H), dim3(kDeltaThreads), 0, stream>>>(f.n, nullptr, w);
       with_slices<KS>(S, H, Dv, [&](auto slices) {
         constexpr uint32_t kSlices = decltype(slices)::value;
+        delta_prepare_kernel<E, KS, false, kInParts<E, KS, kSlices>><<<dim3(S * f.n.pieces * H), dim3(kDeltaThreads), 0, stream>>>(f.n, nullptr, w);
         delta_pieces_kernel<E, KS, kSlices><<<dim3(delta_groups(S, H, Dv, kSlices)), dim3(2 * kSlices * kWave), 0, stream>>>(f, w);
       });
     });
@@ -1607,7 +1625,7 @@ int apex_delta_rule_backward(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, ui
     typedef decltype(t) E;
     with_width(Dk, [&](auto width) {
       constexpr uint32_t KS = decltype(width)::value;
-      delta_prepare_kernel<E, KS, true><<<dim3(S * b.n.pieces * H), dim3(kDeltaThreads), 0, stream>>>(b.n, b.d_o, w);
+      delta_prepare_kernel<E, KS, true, false><<<dim3(S * b.n.pieces * H), dim3(kDeltaThreads), 0, stream>>>(b.n, b.d_o, w);
       with_slices<KS>(S, H, Dv, [&](auto slices) {
         constexpr uint32_t kSlices = decltype(slices)::value;
         delta_pieces_back_kernel<E, KS, kSlices><<<dim3(delta_groups(S, H, Dv, kSlices)), dim3(2 * kSlices * kWave), 0, stream>>>(b, w);
