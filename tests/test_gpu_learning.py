@@ -102,6 +102,23 @@ def test_delta_many_sequences(apex, dtype):
         c.check(c.run(apex))
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_delta_of_a_sequence_does_not_depend_on_how_many_there_are(apex, dtype):
+    """Many sequences share a workgroup's columns, and f16 keys are held otherwise than for few; every product is the same."""
+    S, T, Hk, H, Dk, Dv = 9, 150, 2, 4, 104, 120  # 9 * 4 * 8 slices of 16 columns: more than compute units
+    d = Delta(S, T, Hk, H, Dk, Dv, dtype, cut=True, ragged=True)
+    every = d.run(apex)
+    for s in (0, 4):
+        part = slice(s, s + 1)
+        one = Delta(1, T, Hk, H, Dk, Dv, dtype)
+        for n in ("q", "k", "v", "do", "g", "beta", "h0", "dh_last", "discount", "length"):
+            setattr(one, n, getattr(d, n)[part])
+        alone = one.run(apex)
+        for n in ("o", "h_last") + BACK:
+            assert torch.equal(alone[n], every[n][part]), (n, s)
+    d.check(every)
+
+
 @pytest.mark.parametrize("strength", [0.0, 1.0, 2.0])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_delta_keys_that_are_nearly_alike(apex, dtype, strength):
