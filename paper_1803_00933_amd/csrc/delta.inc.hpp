@@ -977,24 +977,25 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
   }
 }
 
-// What is left of the gradient, a workgroup of eight waves per piece and key head: first a wave has 16 of the state's columns and all
+// What is left of the gradient, a workgroup of eight waves (narrow states: four) per piece and key head: first a wave has 16 of the state's columns and all
 // steps, and finds U anew; then a wave has a tile of the state's rows and KS tiles of steps, and sums over the columns.  Between the
 // two U and dV cross LDS, in parts.
 // Bound by the chain of its phases, one workgroup a compute unit: keys and state, M, 32 columns after another, B and C, their products
 // with keys and queries, a wait for memory or for all waves between any two.  4 x 8192 steps of 16 heads of 128 x 128 in bf16 1.06 ms, of
 // which its products are 0.19; with 32-bit matrix instructions 3.6.
-constexpr uint32_t kGradThreads = 512, kGradWaves = kGradThreads / kWave, kGradRow = kDeltaMaxWidth + 8;
+constexpr uint32_t kGradWaves = kDeltaMaxWidth / 16, kGradNarrowWaves = 4;
 
+template <uint32_t kWaves>
 struct GradSpace {
+  static constexpr uint32_t kRow = kWaves * 16 + 8;
   Gates gates;
   union alignas(16) {  // (eight at a time: at half the alignment a read of them took eight times as long)
-    __bf16 part[2][3][kPiece][kGradRow];  // U, dV; zeros beyond the state's columns
+    __bf16 part[2][3][kPiece][kRow];  // U, dV; zeros beyond the state's columns
     float B[2][kPiece * kPieceRow];       // B, C
   };
-  alignas(16) float of_g[kGradWaves][kPiece], of_v[kGradWaves][kPiece], of_beta[kGradWaves][kPiece];  // sums over a wave's share
-  double at_end[kGradWaves];
+  alignas(16) float of_g[kWaves][kPiece], of_v[kWaves][kPiece], of_beta[kWaves][kPiece];  // sums over a wave's share
+  double at_end[kWaves];
 };
-static_assert(kDeltaMaxWidth == 16 * kGradWaves);
 
 // The sum over the 16 lanes of a row of a tile, in each of them: rotated by 8, 4, 2 and 1 lanes.
 __device__ __forceinline__ float row_sum(float v)
@@ -1007,7 +1008,8 @@ __device__ __forceinline__ float row_sum(float v)
 
 // A 32-bit number's parts, and eight numbers of a row as an operand.  Row: 16 times the tile of steps, and its row of that (neighbours
 // are 4 banks apart, whatever steps they are).
-__device__ __forceinline__ void put_parts(__bf16 (*part)[kPiece][kGradRow], uint32_t t, uint32_t c, float x)
+template <uint32_t kRow>
+__device__ __forceinline__ void put_parts(__bf16 (*part)[kPiece][kRow], uint32_t t, uint32_t c, float x)
 {
 #pragma unroll
   for (uint32_t p = 0; p < 3; ++p) {
@@ -1016,17 +1018,21 @@ __device__ __forceinline__ void put_parts(__bf16 (*part)[kPiece][kGradRow], uint
     x -= __uint_as_float(bits);
   }
 }
-__device__ __forceinline__ Operand<3> get_parts(const __bf16 (*part)[kPiece][kGradRow], uint32_t t, uint32_t c)
+template <uint32_t kRow>
+__device__ __forceinline__ Operand<3> get_parts(const __bf16 (*part)[kPiece][kRow], uint32_t t, uint32_t c)
 {
   Operand<3> x;
 #pragma unroll
   for (uint32_t p = 0; p < 3; ++p) x.part[p] = *reinterpret_cast<const Parts8 *>(&part[p][t][c]);
   return x;
 }
-template <typename T, uint32_t KS, bool kWhole>
-__global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack b, Prepared w)
+template <typename T, uint32_t KS, uint32_t kWaves, bool kWhole>
+__global__ __launch_bounds__(kWaves * kWave, 2) void delta_gradients_kernel(DeltaBack b, Prepared w)
 {
-  __shared__ __align__(16) GradSpace x;
+  constexpr uint32_t kGradThreads = kWaves * kWave, kWidths = kWaves / 2;  // (32 columns each)
+  constexpr uint32_t kSteps = 8 * KS / kWaves;                             // tiles of steps of a wave
+  static_assert((KS == 2 || KS == 4) && kSteps <= 4);
+  __shared__ __align__(16) GradSpace<kWaves> x;
   const DeltaArgs &a = b.n;
   const uint32_t hk = blockIdx.x % a.Hk, piece = blockIdx.x / a.Hk % a.pieces, s = blockIdx.x / a.Hk / a.pieces;
   const uint32_t lane = lane_id(), wave = threadIdx.x / kWave;
@@ -1050,9 +1056,8 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
   const T *const q_rows = static_cast<const T *>(a.q) + s * a.q_seq + t0 * a.q_time + (uint64_t)hk * a.Dk;
   const uint64_t o_row = (uint64_t)a.H * a.Dv, key_head = ((uint64_t)s * a.pieces + piece) * a.Hk + hk;
   // this wave's tile of the state's rows, and its first tile of steps
-  static_assert(KS == 2 || KS == 4);
-  const uint32_t own = KS == 4 ? wave : wave % 4, r0 = KS == 4 ? 0 : wave / 4 * 2;
-  Tile dq_all[KS] = {}, dk_all[KS] = {};
+  const uint32_t own = wave % (2 * KS), r0 = wave / (2 * KS) * kSteps;
+  Tile dq_all[kSteps] = {}, dk_all[kSteps] = {};
 #pragma unroll 1
   for (uint32_t h = hk * a.share; h < (hk + 1) * a.share; ++h) {
     const uint64_t head = ((uint64_t)s * a.pieces + piece) * a.H + h;
@@ -1128,11 +1133,11 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
       }
     }
     __syncthreads();
-    Tile oS[KS] = {}, uS[KS] = {}, vS[KS] = {};
+    Tile oS[kSteps] = {}, uS[kSteps] = {}, vS[kSteps] = {};
     double at_end = 0.0;
     // what 32 columns take from memory, asked for 32 columns ahead
     struct Taken {
-      Run<T, 8> o[KS];
+      Run<T, 8> o[kSteps];
       Run<float, 8> start, end;
     } next;
     // (clamped: what is fetched beyond the widths meets zeros)
@@ -1152,7 +1157,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
       const uint32_t at = min(c0 / 16 + q / 2, slices - 1) * slice_size(a.Dk) + own_row;
       next.start = *reinterpret_cast<const Run<float, 8> *>(S0 + at), next.end = *reinterpret_cast<const Run<float, 8> *>(dS + at);
 #pragma unroll
-      for (uint32_t i = 0; i < KS; ++i) next.o[i] = eight(o_rows + min(tile_row(r0 + i, m), have - 1) * o_row, c0 + q * 8);
+      for (uint32_t i = 0; i < kSteps; ++i) next.o[i] = eight(o_rows + min(tile_row(r0 + i, m), have - 1) * o_row, c0 + q * 8);
     };
     take(0);
 #pragma unroll 1
@@ -1167,7 +1172,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
         for (uint32_t e = 0; e < 8; ++e) at_end += (double)(x.gates.last * now.start[e]) * now.end[e];
       }
 #pragma unroll
-      for (uint32_t i = 0; i < KS; ++i) {
+      for (uint32_t i = 0; i < kSteps; ++i) {
         multiply(oS[i], operand<T>(now.o[i]), start);
         multiply(uS[i], get_parts(x.part[0], (r0 + i) * 16 + m, c), end);
         multiply(vS[i], get_parts(x.part[1], (r0 + i) * 16 + m, c), start);
@@ -1175,34 +1180,35 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
     }
     __builtin_amdgcn_sched_barrier(0);
     // B and C: of 16 tiles, those four of later columns than rows are left out; a wave has one, four waves another one
-    Tile B[2] = {}, C[2] = {};
+    constexpr uint32_t kRounds = (12 + kWaves - 1) / kWaves;
+    Tile B[kRounds] = {}, C[kRounds] = {};
     const auto tile_of = [&](uint32_t i, uint32_t *r, uint32_t *j) {
-      const uint32_t f = wave + i * kGradWaves;
+      const uint32_t f = wave + i * kWaves;
       *r = f < 4 ? f / 2 : 2 + (f - 4) / 4, *j = f < 4 ? f % 2 : (f - 4) % 4;
       return f < 12;
     };
-    Run<T, 8> of_tile[2][4];
+    Run<T, 8> of_tile[kRounds][kWidths];
 #pragma unroll
-    for (uint32_t i = 0; i < 2; ++i) {
+    for (uint32_t i = 0; i < kRounds; ++i) {
       uint32_t r, j;
       tile_of(i, &r, &j);
 #pragma unroll
-      for (uint32_t n = 0; n < 4; ++n) of_tile[i][n] = eight(o_rows + min(tile_row(min(r, 3u), m), have - 1) * o_row, n * 32 + q * 8);
+      for (uint32_t n = 0; n < kWidths; ++n) of_tile[i][n] = eight(o_rows + min(tile_row(min(r, 3u), m), have - 1) * o_row, n * 32 + q * 8);
     }
 #pragma unroll
-    for (uint32_t i = 0; i < 2; ++i) {
+    for (uint32_t i = 0; i < kRounds; ++i) {
       uint32_t r, j;
       if (!tile_of(i, &r, &j)) continue;
 #pragma unroll
-      for (uint32_t n = 0; n < 4; ++n) {
+      for (uint32_t n = 0; n < kWidths; ++n) {
         const Operand<3> u = get_parts(x.part[0], j * 16 + m, n * 32 + q * 8);
         multiply(B[i], operand<T>(of_tile[i][n]), u);
         multiply(C[i], get_parts(x.part[1], r * 16 + m, n * 32 + q * 8), u);
       }
     }
-    T key_at[KS][4], query_at[KS][4];  // this lane's of the keys and queries, as tiles
+    T key_at[kSteps][4], query_at[kSteps][4];  // this lane's of the keys and queries, as tiles
 #pragma unroll
-    for (uint32_t i = 0; i < KS; ++i)
+    for (uint32_t i = 0; i < kSteps; ++i)
 #pragma unroll
       for (uint32_t e = 0; e < 4; ++e) {
         const uint64_t t = min(state_row(r0 + i, e), have - 1);
@@ -1210,7 +1216,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
       }
     __syncthreads();
 #pragma unroll
-    for (uint32_t i = 0; i < 2; ++i) {
+    for (uint32_t i = 0; i < kRounds; ++i) {
       uint32_t r, j;
       if (!tile_of(i, &r, &j)) continue;
       j = tile_row(j, m);
@@ -1226,7 +1232,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
     const Stored<T, false> *const kt = static_cast<const Stored<T, false> *>(w.Kt) + (key_head * 2 * KS + own) * 2 * kWave + lane;
     const Stored<T, false> *const qt = static_cast<const Stored<T, false> *>(w.Qt) + (key_head * 2 * KS + own) * 2 * kWave + lane;
 #pragma unroll
-    for (uint32_t i = 0; i < KS; ++i) {
+    for (uint32_t i = 0; i < kSteps; ++i) {
       const Tile begin = *reinterpret_cast<const Tile *>(&x.gates.begin[state_row(r0 + i, 0)]);
       const Tile end = *reinterpret_cast<const Tile *>(&x.gates.end[state_row(r0 + i, 0)]);
       oS[i] = a.scale * passed(oS[i], begin);
@@ -1240,7 +1246,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
       const Operand<kPartsOf<T>> key = prepared<T>(kt[ks * kWave]);
       const Operand<kPartsOf<T>> query = prepared<T>(qt[ks * kWave]);
 #pragma unroll
-      for (uint32_t i = 0; i < KS; ++i) {
+      for (uint32_t i = 0; i < kSteps; ++i) {
         const uint32_t r = r0 + i, t = tile_row(r, m), j = ks * 32 + q * 8;
         const bool lower = ks <= r / 2, upper = ks >= r / 2;  // (of the matrix: what lies there is not all zeros)
         float f[8];
@@ -1261,16 +1267,16 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
     }
     at_end = wave_sum(at_end);
     if (lane == 0) x.at_end[wave] = at_end;
-    Tile of_g[KS];
+    Tile of_g[kSteps];
 #pragma unroll
-    for (uint32_t i = 0; i < KS; ++i) {
+    for (uint32_t i = 0; i < kSteps; ++i) {
       dq_all[i] += oS[i];
 #pragma unroll
       for (uint32_t e = 0; e < 4; ++e) of_g[i][e] = row_sum(own_d < a.Dk ? (float)query_at[i][e] * oS[i][e] : 0.0f);
     }
     if (m == 0) {
 #pragma unroll
-      for (uint32_t i = 0; i < KS; ++i) *reinterpret_cast<Tile *>(&x.of_g[own][state_row(r0 + i, 0)]) = of_g[i];
+      for (uint32_t i = 0; i < kSteps; ++i) *reinterpret_cast<Tile *>(&x.of_g[own][state_row(r0 + i, 0)]) = of_g[i];
     }
     __syncthreads();
     if (wave == 0) {
@@ -1279,7 +1285,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
       float beta = 0.0f;
       if (t < have)
         for (uint32_t n = 0; n < 2 * KS; ++n) sum += x.of_g[n][t];
-      for (uint32_t n = 0; n < kGradWaves; ++n) {
+      for (uint32_t n = 0; n < kWaves; ++n) {
         if (t < have) sum -= x.of_v[n][t];
         beta += x.of_beta[n][t];
         to_end += x.at_end[n];
@@ -1301,7 +1307,7 @@ __global__ __launch_bounds__(kGradThreads) void delta_gradients_kernel(DeltaBack
   const uint32_t own_d = tile_row(own, lane % 16);
   if (own_d >= a.Dk) return;
 #pragma unroll
-  for (uint32_t i = 0; i < KS; ++i)
+  for (uint32_t i = 0; i < kSteps; ++i)
 #pragma unroll
     for (uint32_t e = 0; e < 4; ++e) {
       const uint32_t t = state_row(r0 + i, e);
@@ -1533,6 +1539,19 @@ void with_slices(uint32_t S, uint32_t H, uint32_t Dv, F f)
     f(std::integral_constant<uint32_t, 1>());
 }
 
+// f(integral_constant<uint32_t>): waves of a workgroup of the gradient's last kernel.
+// Four for narrow states, a wave per 16 columns and per 16 rows, so that a compute unit has two workgroups, one of which works while the
+// other waits: the gradient of 64 x 96 steps of 8 heads of 64 x 64 in bf16 144 -> 121 us, in f32 186 -> 165, of 4 x 4096 399 -> 339;
+// where there is a workgroup a compute unit or less, 1 x 4096 of 4 heads, 184 as before.
+template <uint32_t KS, typename F>
+void with_waves(uint32_t Dv, F f)
+{
+  if (KS == 2 && Dv <= 16 * kGradNarrowWaves)
+    f(std::integral_constant<uint32_t, KS == 2 ? kGradNarrowWaves : kGradWaves>());
+  else
+    f(std::integral_constant<uint32_t, kGradWaves>());
+}
+
 int delta_check(const DeltaArgs &a, int dtype)
 {
   const uint32_t size = element_size(dtype);
@@ -1630,10 +1649,13 @@ int apex_delta_rule_backward(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, ui
         constexpr uint32_t kSlices = decltype(slices)::value;
         delta_pieces_back_kernel<E, KS, kSlices><<<dim3(delta_groups(S, H, Dv, kSlices)), dim3(2 * kSlices * kWave), 0, stream>>>(b, w);
       });
-      if (Dv % 32)
-        delta_gradients_kernel<E, KS, false><<<dim3(S * b.n.pieces * Hk), dim3(kGradThreads), 0, stream>>>(b, w);
-      else
-        delta_gradients_kernel<E, KS, true><<<dim3(S * b.n.pieces * Hk), dim3(kGradThreads), 0, stream>>>(b, w);
+      with_waves<KS>(Dv, [&](auto waves) {
+        constexpr uint32_t kWaves = decltype(waves)::value;
+        if (Dv % 32)
+          delta_gradients_kernel<E, KS, kWaves, false><<<dim3(S * b.n.pieces * Hk), dim3(kWaves * kWave), 0, stream>>>(b, w);
+        else
+          delta_gradients_kernel<E, KS, kWaves, true><<<dim3(S * b.n.pieces * Hk), dim3(kWaves * kWave), 0, stream>>>(b, w);
+      });
     });
   });
   APEX_HIP(hipGetLastError());
