@@ -978,7 +978,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
 }
 
 // What is left of the gradient, a workgroup of eight waves (narrow states: four) per piece and key head: first a wave has 16 of the state's columns and all
-// steps, and finds U anew; then a wave has a tile of the state's rows and KS tiles of steps, and sums over the columns.  Between the
+// steps, and finds U anew; then a wave has a tile of the state's rows and two or four tiles of steps, and sums over the columns.  Between the
 // two U and dV cross LDS, in parts.
 // Bound by the chain of its phases, one workgroup a compute unit: keys and state, M, 32 columns after another, B and C, their products
 // with keys and queries, a wait for memory or for all waves between any two.  4 x 8192 steps of 16 heads of 128 x 128 in bf16 1.06 ms, of
