@@ -79,6 +79,7 @@ struct alignas(16) Gates {
   float beta[kPiece], begin[kPiece], end[kPiece];  // strength; what is left of the start state, and of the step at the end
   uint32_t cut[kPiece];   // nothing passes into the step
   float last;             // what is left of the start state at the end
+  uint32_t enters;        // the step in front of the piece did not end an episode: the start state is one
 };
 
 // By one wave.
@@ -88,7 +89,7 @@ __device__ __forceinline__ void load_gates(const DeltaArgs &a, uint32_t s, uint3
   const bool have = t < len;
   const uint64_t at = ((uint64_t)s * a.T + t) * a.H + h;
   float g = have ? a.g[at] : 0.0f;
-  const bool cut = have && (delta_cuts(g) || (t > 0 && !delta_passes(a, s, t - 1)));
+  const bool enters = !have || t == 0 || delta_passes(a, s, t - 1), cut = have && (delta_cuts(g) || !enters);
   if (cut) g = 0.0f;
   double sum = (double)g * 1.4426950408889634;
   uint32_t episode = cut;
@@ -105,7 +106,10 @@ __device__ __forceinline__ void load_gates(const DeltaArgs &a, uint32_t s, uint3
   x.begin[lane] = episode == 0 ? exp2_of((float)sum) : 0.0f;
   x.end[lane] = episode == episodes ? exp2_of((float)(all - sum)) : 0.0f;
   x.cut[lane] = cut;
-  if (lane == 0) x.last = episodes == 0 ? exp2_of((float)all) : 0.0f;
+  if (lane == 0) {
+    x.last = episodes == 0 ? exp2_of((float)all) : 0.0f;
+    x.enters = enters;
+  }
 }
 
 // D of a step t and an earlier one.
@@ -685,7 +689,7 @@ __device__ __forceinline__ uint32_t slice_size(uint32_t Dk) { return (Dk + 31) /
 __device__ __forceinline__ uint64_t slices_size(uint32_t Dk, uint32_t Dv) { return (uint64_t)((Dv + 15) / 16) * slice_size(Dk); }
 __device__ __forceinline__ uint32_t slice_row(uint32_t d) { return d / 32 * 32 + d % 8 * 4 + d / 8 % 4; }
 
-// A state of which the three parts are held: their sum is exact.  Zeros beyond the columns.
+// A state of which the three parts are held: their sum is exact.  Zeros where `column` is false.
 template <uint32_t KS>
 __device__ __forceinline__ void store_slice(const Operand<3> (&S)[KS], float *to, uint32_t Dk, uint32_t slice, bool column)
 {
@@ -798,10 +802,12 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
     PieceKeys<T, KS, kParts> Q;
     PieceTriangle P;
     RowGates begin;
+    uint32_t enters = 0;
     const auto load = [&](uint32_t piece) {
       Q.load(w.Q, ((uint64_t)s * a.pieces + piece) * a.Hk + hk);
       P.load(w.P, head_of(piece));
       begin = row_gates(gates_of(w, head_of(piece)).begin);
+      enters = gates_of(w, head_of(piece)).enters;
     };
     if (pieces) load(0);
     for (uint32_t piece = 0; piece < pieces; ++piece) {
@@ -820,8 +826,10 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
       const Tile(&found)[4][kWave] = corrections[piece % 2];
       const Operand<3> U[2] = {operand_of<3>(found[0][lane], found[1][lane]), operand_of<3>(found[2][lane], found[3][lane])};
       P.times<false>(O, U);
+      // (the state is carried as the last step left it: what an episode's end keeps out of the piece is not stored)
+      const bool stored = column && enters;
       if (kAhead) load(min(piece + 1, pieces - 1));
-      if (f.carry && place.c0 < a.Dv) store_slice<KS>(S, f.carry + head_of(piece) * slices_size(a.Dk, a.Dv), a.Dk, place.c0 / 16, column);
+      if (f.carry && place.c0 < a.Dv) store_slice<KS>(S, f.carry + head_of(piece) * slices_size(a.Dk, a.Dv), a.Dk, place.c0 / 16, stored);
       if (column)
         each_step(o + (uint64_t)piece * kPiece * o_row, o_row, have_of(piece), c, [&](uint32_t r, uint32_t e, T *to) { *to = (T)(a.scale * O[r][e]); });
     }
