@@ -698,8 +698,9 @@ int apex_verify_draft(uint32_t B, uint32_t G, uint32_t V, int dtype, const void 
  * (Keys are meant to be of unit length, or no longer, and 0 <= beta <= 2, so that the recurrence does not grow.  Longer sequences
  * are computed in pieces of 64 steps by products of matrices, as sums of products in 32 bits: a NaN or an infinity among the inputs
  * or the state of a head may make all of that head's results of its piece and behind it NaN, whether or not an episode ends there;
- * products whose magnitude passes the range of 32-bit numbers do the same.  Only a state that the first step of a call keeps out, and
- * a gradient that the last one does, have no effect whatever they hold.  Limit: S * ceil(T / 64) * H <= APEX_DELTA_MAX_PIECES.)
+ * products whose magnitude passes the range of 32-bit numbers, and numbers within 2^-9 of its end, do the same.  Only a state that
+ * the first step of a call keeps out, and a gradient that the last one does, have no effect whatever they hold.
+ * Limit: S * ceil(T / 64) * H <= APEX_DELTA_MAX_PIECES.)
  */
 int apex_delta_rule_workspace_bytes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, int backward,
                                     size_t *bytes /*host*/);

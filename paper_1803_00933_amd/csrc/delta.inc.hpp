@@ -120,8 +120,13 @@ __device__ __forceinline__ float decay(const Gates &x, uint32_t t, uint32_t i)
 }
 
 // ---- products.  Matrix instructions take numbers of 8 bits (bf16), 16 times as many as of 32 bits, so a 32-bit number is the sum
-// of three of them (cut off, not rounded: 24 bits in three parts of 8, which is exact), and a product of two is the sum of the six
-// products of parts that are not below its last bit.  Numbers of 16 bits are one part (bf16) or two (f16).
+// of three of them, each what is left rounded to nearest even: of a number in [1, 2) the second is at most 2^-8, the third 2^-17 and a
+// multiple of 2^-23, so the sum is exact.  A product of two numbers is the sum of six products of parts; what the other three
+// come to is at most 2 * 2^-8 * 2^-17 of it, half a unit of its last place, on either side of 0.  (Parts that are cut off instead all
+// have the number's sign, and leave out up to 2^-21, always towards 0.)  Numbers of 16 bits are one part (bf16) or two (f16).  A number
+// within 2^-9 of the largest of 32 bits has an infinite first part.  Beside one part nothing is left out, and parts might be cut off there,
+// which takes half of the conversion's time, but brought nothing (4 x 8192 steps of 16 heads in bf16: the pieces 603 us in place of 595, the
+// gradient's last kernel 1131 of 1140).
 typedef __bf16 Parts8 __attribute__((ext_vector_type(8)));  // one part of 8 numbers: an operand's share of a lane
 
 template <typename T>
@@ -131,6 +136,17 @@ template <uint32_t N>
 struct Operand {
   Parts8 part[N];
 };
+
+// Two numbers' next parts, the first in the low half; x and y are what is left of them.  (Both at once, and taken apart as a word: one by
+// one the compiler converts each twice.)
+__device__ __forceinline__ uint32_t next_parts(float &x, float &y)
+{
+  typedef float Two __attribute__((ext_vector_type(2)));
+  typedef __bf16 TwoParts __attribute__((ext_vector_type(2)));
+  const uint32_t word = __builtin_bit_cast(uint32_t, __builtin_convertvector((Two{x, y}), TwoParts));
+  x -= __uint_as_float(word << 16), y -= __uint_as_float(word & 0xffff0000u);
+  return word;
+}
 
 template <uint32_t N>
 __device__ __forceinline__ Operand<N> split(const float (&x)[8])
@@ -143,12 +159,8 @@ __device__ __forceinline__ Operand<N> split(const float (&x)[8])
   for (uint32_t p = 0; p < N; ++p) {
     uint32_t word[4];
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) word[i] = __builtin_amdgcn_perm(__float_as_uint(left[2 * i + 1]), __float_as_uint(left[2 * i]), 0x07060302);
+    for (uint32_t i = 0; i < 4; ++i) word[i] = next_parts(left[2 * i], left[2 * i + 1]);
     __builtin_memcpy(&r.part[p], word, 16);
-    if (p + 1 < N) {
-#pragma unroll
-      for (uint32_t i = 0; i < 8; ++i) left[i] -= __uint_as_float(__float_as_uint(left[i]) & 0xffff0000u);
-    }
   }
   return r;
 }
@@ -180,7 +192,7 @@ __device__ __forceinline__ Operand<kPartsOf<T>> prepared(const Run<T, 8> &x) { r
 template <typename T>
 __device__ __forceinline__ Operand<kPartsOf<T>> prepared(const Operand<kPartsOf<T>> &x) { return x; }
 
-// acc + A B over 32: of the parts' products those that are not below the last bit.
+// acc + A B over 32: of the parts' products all but second with third and third with third.
 template <uint32_t NA, uint32_t NB>
 __device__ __forceinline__ void multiply(Tile &acc, const Operand<NA> &a, const Operand<NB> &b)
 {
@@ -523,6 +535,10 @@ __device__ __forceinline__ uint32_t anew(uint32_t x)
   return x;
 }
 
+// A product's result in registers that ordinary instructions take, once for all that is computed from it (else the compiler copies a state
+// of a piece twice, 32 instructions of 1070).
+__device__ __forceinline__ void held(Tile &x) { asm("" : "+v"(x)); }
+
 // What the kernels take of a piece, as it is in memory: asked for a piece ahead, made operands when it is used.  Behind a
 // sequence's last step that one is fetched again: its strength there is 0, and so is all that comes of it.
 // `near`: 64 rows apart are less than 2^32 bytes apart, and there are 64: a lane's place is an offset from an address that all share.
@@ -761,6 +777,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
       Tile kS[4] = {}, X[4];
 #pragma unroll
       for (uint32_t i = 0; i < KS; ++i) {
+        held(S[2 * i]), held(S[2 * i + 1]);
         const Operand<3> parts = operand_of<3>(S[2 * i], S[2 * i + 1]);
         put(states[piece % 2][i], parts);
 #pragma unroll
@@ -886,6 +903,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
       Tile kS[4] = {};
 #pragma unroll
       for (uint32_t i = 0; i < KS; ++i) {
+        held(S[2 * i]), held(S[2 * i + 1]);
         const Operand<3> parts = operand_of<3>(S[2 * i], S[2 * i + 1]);
         put(states[piece % 2][i], parts);
 #pragma unroll
@@ -1014,16 +1032,16 @@ __device__ __forceinline__ float row_sum(float v)
   return v + dpp_from<0x121, 0xf>(v, 0.0f);
 }
 
-// A 32-bit number's parts, and eight numbers of a row as an operand.  Row: 16 times the tile of steps, and its row of that (neighbours
-// are 4 banks apart, whatever steps they are).
+// The parts of a number of each of two matrices, and eight numbers of a row as an operand.  Row: 16 times the tile of steps, and its row
+// of that (neighbours are 4 banks apart, whatever steps they are).
 template <uint32_t kRow>
-__device__ __forceinline__ void put_parts(__bf16 (*part)[kPiece][kRow], uint32_t t, uint32_t c, float x)
+__device__ __forceinline__ void put_parts(__bf16 (*part)[3][kPiece][kRow], uint32_t t, uint32_t c, float x, float y)
 {
 #pragma unroll
   for (uint32_t p = 0; p < 3; ++p) {
-    const uint32_t bits = __float_as_uint(x) & 0xffff0000u;
-    part[p][t][c] = __builtin_bit_cast(__bf16, (uint16_t)(bits >> 16));
-    x -= __uint_as_float(bits);
+    const uint32_t word = next_parts(x, y);
+    part[0][p][t][c] = __builtin_bit_cast(__bf16, (uint16_t)word);
+    part[1][p][t][c] = __builtin_bit_cast(__bf16, (uint16_t)(word >> 16));
   }
 }
 template <uint32_t kRow>
@@ -1128,8 +1146,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void delta_gradients_kernel(Delt
       for (uint32_t r = 0; r < 4; ++r)
 #pragma unroll
         for (uint32_t e = 0; e < 4; ++e) {
-          put_parts(x.part[0], r * 16 + q * 4 + e, column, U[r][e]);
-          put_parts(x.part[1], r * 16 + q * 4 + e, column, Y[r][e]);
+          put_parts(x.part, r * 16 + q * 4 + e, column, U[r][e], Y[r][e]);
           of_v[r][e] = row_sum(of_v[r][e]), of_beta[r][e] = row_sum(of_beta[r][e]);
         }
       if (m == 0) {
