@@ -743,9 +743,10 @@ int apex_embedding_backward(uint32_t N, uint32_t V, uint32_t D, int dtype, const
  * Clipping by the norm over `count` tensors: norm = sqrt(the sum of all their elements' squares, in 64 bits),
  *     out_i = grad_i * min(1, max_norm / norm),
  * rounded once.  grad, out, elements, dtype: host arrays, read before the call returns; tensor i has elements[i] contiguous elements
- * (0: it is skipped) of dtype[i] (apex_dtype).  out NULL, or out[i] = grad[i]: in place.  Where the norm is not finite (a NaN or an
- * infinity among the elements) nothing is scaled: out_i = grad_i, and the norm tells.  (A norm beyond the range of 32 bits reads +inf;
- * the tensors are scaled by it all the same, unless one of their elements is none.)  max_norm: above 0, +inf for the norm alone
+ * (0: it is skipped) of dtype[i] (apex_dtype).  out NULL, or out[i] = grad[i]: in place.  No output may lie over another one, or over a
+ * gradient that is not its own: a tensor that is to be scaled is named once (APEX_ERR_INVALID_ARG).  Where the norm is not finite (a NaN
+ * or an infinity among the elements) nothing is scaled: out_i = grad_i, and the norm tells.  (A norm beyond the range of 32 bits reads
+ * +inf; the tensors are scaled by it all the same, unless one of their elements is none.)  max_norm: above 0, +inf for the norm alone
  * (and copies, where out is another array).  norm [1] fp32 (device, may be NULL).
  */
 int apex_clip_gradients_workspace_bytes(uint32_t count, size_t *bytes /*host*/);

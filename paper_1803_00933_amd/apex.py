@@ -429,7 +429,7 @@ def clip_gradients_workspace(grads, device=None):
 
 def clip_gradients(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
     """The tensors of the list `grads` times min(1, max_norm / norm), norm the one over all their elements, into the tensors of the
-    list `out` (laid out alike), or in place.  A norm that is not finite scales nothing.
+    list `out` (laid out alike), or in place; each is named once.  A norm that is not finite scales nothing.
     Returns (rc, out): norm fp32 [1] and out, the list."""
     if len(grads):
         _on_current_device(grads[0])

@@ -1,5 +1,7 @@
 // The norm over many tensors, and the tensors scaled by what keeps it below a limit.  Included by apex_replay.hip (one
 // translation unit).
+#include <memory>
+
 #include "elements.hpp"
 
 namespace apex {
@@ -186,6 +188,35 @@ __global__ __launch_bounds__(kClipThreads) void clip_scale_kernel(ClipArgs a)
 
 }  // namespace apex
 
+namespace {
+
+// No output lies over another one, or over a gradient that is not its own: workgroups read some while others write, and a tensor that is
+// named twice would be scaled once or twice.
+bool clip_apart(uint32_t count, const void *const *grad, void *const *out, const uint64_t *elements, const int *dtype)
+{
+  struct Range {
+    uint64_t begin, end;
+  };
+  const auto range = [&](const void *p, uint32_t i) { return Range{(uintptr_t)p, (uintptr_t)p + elements[i] * element_size(dtype[i])}; };
+  const std::unique_ptr<Range[]> written(new (std::nothrow) Range[count]);
+  if (count && !written) return false;
+  Range *last = written.get();
+  for (uint32_t i = 0; i < count; ++i)
+    if (elements[i]) *last++ = range(out[i], i);
+  std::sort(written.get(), last, [](const Range &a, const Range &b) { return a.begin < b.begin; });
+  for (Range *r = written.get(); r + 1 < last; ++r)
+    if (r->end > r[1].begin) return false;
+  for (uint32_t i = 0; i < count; ++i) {
+    if (!elements[i] || out[i] == grad[i]) continue;
+    const Range read = range(grad[i], i);
+    const Range *const w = std::lower_bound(written.get(), last, read, [](const Range &a, const Range &b) { return a.end <= b.begin; });
+    if (w != last && w->begin < read.end) return false;
+  }
+  return true;
+}
+
+}  // namespace
+
 extern "C" {
 
 int apex_clip_gradients_workspace_bytes(uint32_t count, size_t *bytes)
@@ -213,6 +244,8 @@ int apex_clip_gradients(uint32_t count, const void *const *grad, void *const *ou
     bytes += elements[i] * size;
     in_place = in_place && (!out || out[i] == grad[i]);
   }
+  if (!(in_place && max_norm == __builtin_inff()) && !clip_apart(count, grad, out ? out : const_cast<void *const *>(grad), elements, dtype))
+    return APEX_ERR_INVALID_ARG;
   // pieces of whole rounds of a workgroup, so few that their sums are soon summed up
   const uint64_t piece = std::max<uint64_t>(kClipMinPiece, round_up((total + kClipPieces - 1) / kClipPieces, kClipMinPiece));
   if (piece > 0x7fffffffu) return APEX_ERR_TOO_LARGE;
