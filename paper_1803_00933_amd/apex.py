@@ -427,6 +427,13 @@ def clip_gradients_workspace(grads, device=None):
     return _workspace(lib.apex_clip_gradients_workspace_bytes, device, count)
 
 
+def _laid_out_alike(a, b):
+    """The same sizes, and the same element at every place in memory: the stride of a dimension of one element says nothing."""
+    if a.shape != b.shape:
+        return False
+    return a.stride() == b.stride() or a.numel() == 0 or all(n == 1 or x == y for n, x, y in zip(a.shape, a.stride(), b.stride()))
+
+
 def clip_gradients(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
     """The tensors of the list `grads` times min(1, max_norm / norm), norm the one over all their elements, into the tensors of the
     list `out` (laid out alike), or in place; each is named once.  A norm that is not finite scales nothing.
@@ -439,7 +446,7 @@ def clip_gradients(grads, max_norm, out=None, norm=None, workspace=None, stream=
                 norm = torch.empty(1, dtype=torch.float32, device=grads[0].device if len(grads) else "cuda:0")
             if workspace is None:
                 workspace = clip_gradients_workspace(grads)
-    if out is not None and any(a.stride() != b.stride() for a, b in zip(grads, out)):
+    if out is not None and not all(map(_laid_out_alike, grads, out)):
         raise ValueError("out: laid out as the gradients")
     return _call.clip_gradients(grads, out, max_norm, norm, workspace, stream), dict(norm=norm, out=grads if out is None else out)
 

@@ -1,4 +1,7 @@
 """What the learning step's operators refuse before anything is launched (no GPU)."""
+import pytest
+import torch
+
 import recorded_hip
 
 CLIP = """
@@ -26,3 +29,41 @@ result = bad, good
 """)
     assert out[0] == [[-1, 0]] * 10
     assert [rc for rc, _ in out[1]] == [0] * 8 and [n for _, n in out[1]] == [2, 2, 2, 2, 1, 2, 2, 1]
+
+
+@pytest.fixture(scope="module")
+def apex():
+    from paper_1803_00933_amd import apex
+    return apex
+
+
+def clip_into(apex, grad, out):
+    space = torch.zeros(1)
+    apex.clip_gradients([grad], 1.0, out=[out], norm=space, workspace=space)
+
+
+LAID_OUT = [((1, 8), (8, 1), (1, 1)), ((4, 1, 3), (3, 3, 1), (3, 50, 1)), ((5, 1), (1, 1), (1, 7)), ((1,), (1,), (9,)), ((0, 4), (4, 1), (1, 1))]
+
+
+@pytest.mark.parametrize("sizes,strides,others", LAID_OUT, ids=str)
+def test_clipping_into_tensors_of_the_same_layout(apex, sizes, strides, others):
+    """A dimension of one element has any stride: these go on to the binding, which wants tensors of the GPU."""
+    a, b = (torch.zeros(100).as_strided(sizes, s) for s in (strides, others))
+    for x, y in ((a, b), (b, a)):
+        with pytest.raises(AssertionError, match="dense tensors of a floating type"):
+            clip_into(apex, x, y)
+
+
+@pytest.mark.parametrize("grad,out", [((6,), (1, 6)), ((2, 6), (12,)), ((1, 6), (6, 1)), ((2, 3), (3, 2)), ((4,), (5,))], ids=str)
+def test_clipping_into_tensors_of_other_sizes(apex, grad, out):
+    with pytest.raises(ValueError, match="laid out"):
+        clip_into(apex, torch.zeros(grad), torch.zeros(out))
+    with pytest.raises(ValueError, match="laid out"):
+        clip_into(apex, torch.zeros((3, 4)), torch.zeros((4, 3)).t())
+
+
+def test_clipping_into_another_layout_of_one_stride(apex):
+    """[6,1] and [1,6] in memory with the same strides: sizes count."""
+    x = torch.zeros(50)
+    with pytest.raises(ValueError, match="laid out"):
+        clip_into(apex, x.as_strided((6, 1), (1, 1)), x.as_strided((1, 6), (1, 1)))
