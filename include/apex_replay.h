@@ -695,11 +695,14 @@ int apex_verify_draft(uint32_t B, uint32_t G, uint32_t V, int dtype, const void 
  * ceil(Dk / 32), 8, 4, 16] fp32 (may be NULL): what passes into step t = c * APEX_DELTA_CHUNK, row 32 i + j + 8 k and column 16 l + m at
  * [l, i, j, k, m], zeros beyond Dk and Dv, for those t below the length; the others are unspecified.  The gradient asks for it.
  * With T = 1 this is the step of an actor: state in, state out.
- * (Keys are meant to be of unit length, or no longer, and 0 <= beta <= 2, so that the recurrence does not grow.  Longer sequences
- * are computed in pieces of 64 steps by products of matrices, as sums of products in 32 bits: a NaN or an infinity among the inputs
- * or the state of a head may make all of that head's results of its piece and behind it NaN, whether or not an episode ends there;
- * products whose magnitude passes the range of 32-bit numbers, and numbers within 2^-9 of its end, do the same.  Only a state that
- * the first step of a call keeps out, and a gradient that the last one does, have no effect whatever they hold.
+ * (Keys are meant to be of unit length, or no longer, and 0 <= beta <= 2, so that the recurrence does not grow.  Up to 8 steps, and up
+ * to 16 where S * H * ceil(Dv / 64) > 256, are computed one after the other; what an episode's end or a decay of 0 keeps out has no
+ * effect behind it there, NaN and infinities included.  More steps, and the gradient of any number of them, are computed in pieces of 64
+ * by products of matrices, as sums of products in 32 bits: a NaN or an infinity among the inputs or the state of a head may make all of
+ * that head's results of its piece and behind it NaN, and all of its gradients, whether or not an episode ends there; products whose
+ * magnitude passes the range of 32-bit numbers, and numbers within 2^-9 of its end, do the same.  Only a state that the first step of a
+ * call keeps out, and a gradient that the last one does, have no effect whatever they hold.  So how 9 to 16 steps are rounded, and what a
+ * NaN in them reaches, depends on how many sequences there are; the results of other numbers of steps do not.
  * Limit: S * ceil(T / 64) * H <= APEX_DELTA_MAX_PIECES.)
  */
 int apex_delta_rule_workspace_bytes(uint32_t S, uint32_t T, uint32_t H, uint32_t Dk, uint32_t Dv, int backward,
@@ -731,8 +734,10 @@ int apex_delta_rule_backward(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, ui
 int apex_embedding(uint32_t N, uint32_t V, uint32_t D, int dtype, const void *table, uint64_t table_stride, const int32_t *token,
                    float scale, void *out, uint64_t out_stride, void *hip_stream);
 /*
- * The gradient of its table: dtable[v] = scale * the sum of dout[n] over the n with token[n] = v, in their order, in 32 bits; zeros
- * for a token that is not named.  With add != 0 it is added to what dtable holds (a head that is tied to the table, several batches):
+ * The gradient of its table: dtable[v] = scale * the sum of dout[n] over the n with token[n] = v, in 32 bits; zeros for a token that is
+ * not named.  The terms are added in the order of n, those of 64 (and of 4096, from 16384 tokens on) neighbours among the sorted tokens
+ * by themselves first where all are v's: where these groups begin depends on the other tokens, so that the last bits of a frequent token's
+ * row do, too.  With add != 0 it is added to what dtable holds (a head that is tied to the table, several batches):
  * rows that are not named stay as they are, the others are rounded once more.
  */
 int apex_embedding_backward_workspace_bytes(uint32_t N, uint32_t V, uint32_t D, size_t *bytes /*host*/);

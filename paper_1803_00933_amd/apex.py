@@ -347,7 +347,8 @@ def delta_rule_workspace(S, T, H, Dk, Dv, backward=False, device="cuda:0"):
 def delta_rule(q, k, v, g, beta, discount=None, length=None, h0=None, scale=1.0, carry=False, out=None, workspace=None, stream=None):
     """S_t = exp(g_t) S_{t-1} + k_t u_t^T with u_t = beta_t (v_t - exp(g_t) S_{t-1}^T k_t), o_t = scale S_t^T q_t, over device
     tensors q, k [S,T,Hk,Dk] and v [S,T,H,Dv] (any strides but those within a step), g and beta fp32 [S,T,H]; H / Hk value heads
-    share a query and key head.  discount fp32 [S,T] (0: nothing passes on), length int32 [S], h0 fp32 [S,H,Dk,Dv].
+    share a query and key head.  discount fp32 [S,T] (0: nothing passes on), length int32 [S], h0 fp32 [S,H,Dk,Dv].  Numbers that are
+    not finite, and 9 to 16 steps of few and of many sequences: see the header.
     Returns (rc, out): o [S,T,H,Dv], h_last fp32 [S,H,Dk,Dv], and with carry=True (or a place for it in `out`) what
     delta_rule_backward needs."""
     if carry and out is not None and out.get("carry") is None:
