@@ -387,6 +387,11 @@ def delta_rule_backward(q, k, v, g, beta, do, carry, discount=None, length=None,
                                      out["dg"], out["dbeta"], out.get("dh0"), workspace, stream), out
 
 
+def _in_a_row(token):
+    """Tokens of any shape as the binding takes them, in one to three dimensions."""
+    return token if 1 <= token.dim() <= 3 else token.view(-1)
+
+
 def embedding(table, token, scale=1.0, out=None, stream=None):
     """scale * table[token] for a table [V,D] and tokens int32 of any shape; zeros for tokens outside the table.
     Returns (rc, out): out [N,D], N the number of tokens."""
@@ -394,7 +399,7 @@ def embedding(table, token, scale=1.0, out=None, stream=None):
     if out is None:
         with _made_on(stream):
             out = dict(out=torch.empty((token.numel(), table.shape[1]), dtype=table.dtype, device=table.device))
-    return _call.embedding(table, token, scale, out["out"], stream), out
+    return _call.embedding(table, _in_a_row(token), scale, out["out"], stream), out
 
 
 def embedding_backward_workspace(N, V, D, device="cuda:0"):
@@ -417,7 +422,7 @@ def embedding_backward(dout, token, V, scale=1.0, add=False, out=None, workspace
                 workspace = embedding_backward_workspace(N, V, D, device=dout.device)
     if out["dtable"].shape[0] != V:
         raise ValueError("out['dtable'] has %d rows, not %d" % (out["dtable"].shape[0], V))
-    return _call.embedding_backward(dout, token, scale, int(add), out["dtable"], workspace, stream), out
+    return _call.embedding_backward(dout, _in_a_row(token), scale, int(add), out["dtable"], workspace, stream), out
 
 
 def clip_gradients_workspace(grads, device=None):

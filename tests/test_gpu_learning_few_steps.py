@@ -2,7 +2,6 @@
 import pytest
 import torch
 
-
 from test_gpu_learning import BACK, Delta, apex  # noqa: F401
 
 pytestmark = pytest.mark.gpu
