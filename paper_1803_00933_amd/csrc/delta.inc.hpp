@@ -1650,11 +1650,10 @@ int apex_delta_rule_backward(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, ui
 {
   DeltaBytes n;
   if (const int rc = delta_sizes(S, T, H, Dk, Dv, true, &n)) return rc;
-  char *const space = static_cast<char *>(workspace);
   DeltaBack b{{S, T, Hk, H, Dk, Dv, blocks_for(T, kPiece), Hk ? H / Hk : 0, q_seq_stride, q_time_stride, k_seq_stride, k_time_stride,
                v_seq_stride, v_time_stride, q, k, v, g, beta, scale, discount, length},
               carry, d_o, dh_last, dq_seq_stride, dq_time_stride, dk_seq_stride, dk_time_stride, dv_seq_stride, dv_time_stride, dq, dk, dv, dg,
-              dbeta, dh0, reinterpret_cast<float *>(space + n.dS), reinterpret_cast<float *>(space + n.Y)};
+              dbeta, dh0, nullptr, nullptr};
   if (const int rc = delta_check(b.n, dtype)) return rc;
   const uint32_t size = element_size(dtype);
   if (!carry || !d_o || !dg || !dbeta || !workspace || (uintptr_t)workspace % 256 || (uintptr_t)d_o % size ||
@@ -1665,6 +1664,7 @@ int apex_delta_rule_backward(uint32_t S, uint32_t T, uint32_t Hk, uint32_t H, ui
     return APEX_ERR_INVALID_ARG;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const Prepared w = delta_prepared(n, workspace);
+  b.dS = reinterpret_cast<float *>(static_cast<char *>(workspace) + n.dS), b.Y = reinterpret_cast<float *>(static_cast<char *>(workspace) + n.Y);
   with_type(dtype, [&](auto t) {
     typedef decltype(t) E;
     with_width(Dk, [&](auto width) {

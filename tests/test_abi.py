@@ -215,3 +215,72 @@ print("passed", other[0] > 0)
 """
     r = subprocess.run([sys.executable, "-c", code, so], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "passed True" in r.stdout, (r.returncode, r.stderr[-2000:])
+
+
+def test_learning_operators_check_their_arguments_before_they_use_them():
+    """Every array that is missing or not aligned, every size that is none or too large, one at a time: refused, and nothing computed from
+    an address that is not there."""
+    from paper_1803_00933_amd import apex
+    lib, bad, large = apex.lib, apex.ERR_INVALID_ARG, apex.ERR_TOO_LARGE
+    A = 1 << 20                                         # an address that nothing looks behind
+    S, T, Hk, H, Dk, Dv = 2, 100, 1, 2, 16, 24
+    inputs = [A, T * Hk * Dk, Hk * Dk, A, T * Hk * Dk, Hk * Dk, A, T * H * Dv, H * Dv, A, A, 1.0]
+    forward = [S, T, Hk, H, Dk, Dv, 0] + inputs + [None, None, None, A, None, None, A, None]
+    backward = [S, T, Hk, H, Dk, Dv, 0] + inputs + [None, None, A, A, None] + inputs[:9] + [A, A, None, A, None]
+
+    def refused(entry, args, at, values, want=bad):
+        for v in values:
+            changed = list(args)
+            changed[at] = v
+            assert entry(*changed) == want, (entry.__name__, at, v)
+
+    nan, inf = float("nan"), float("inf")
+    for entry, args, required, optional in ((lib.apex_delta_rule, forward, (7, 10, 13, 16, 17, 22, 25), (19, 20, 21, 23, 24)),
+                                            (lib.apex_delta_rule_backward, backward, (7, 10, 13, 16, 17, 21, 22, 24, 27, 30, 33, 34, 36),
+                                             (19, 20, 23, 35))):
+        for at in required:
+            refused(entry, args, at, (None, A + 1))
+        for at in optional:
+            refused(entry, args, at, (A + 1,))
+        for at in range(6):
+            refused(entry, args, at, (0,))
+        refused(entry, args, 2, (3,))
+        for at in (4, 5):
+            refused(entry, args, at, (129,), large)
+        refused(entry, args, 6, (-1, 3))
+        refused(entry, args, 18, (nan, inf, -inf))
+        refused(entry, args, 8, ((1 << 62) // 2, (1 << 64) - 1))
+        refused(entry, args, 0, (1 << 20,), large)
+        refused(entry, args, 1, (1 << 31,))
+        refused(entry, args, 25 if entry is lib.apex_delta_rule else 36, (A + 128,))
+    for at in (25, 26, 28, 29, 31, 32):                 # rows of the gradients over one another
+        refused(lib.apex_delta_rule_backward, backward, at, (1, 0))
+    N, V, D = 50, 90, 10
+    lookup, back = [N, V, D, 0, A, D, A, 1.0, A, D, None], [N, V, D, 0, A, D, A, 1.0, 0, A, D, A, None]
+    for entry, args, required in ((lib.apex_embedding, lookup, (4, 6, 8)), (lib.apex_embedding_backward, back, (4, 6, 9, 11))):
+        for at in required:
+            refused(entry, args, at, (None, A + 1))
+        for at, limit in ((0, 1 << 23), (1, 1 << 20), (2, 8192)):
+            refused(entry, args, at, (0,))
+            refused(entry, args, at, (limit + 1, (1 << 32) - 1), large)
+        refused(entry, args, 3, (-1, 3))
+        refused(entry, args, 7, (nan, inf, -inf))
+        refused(entry, args, 5, ((1 << 64) - 1,))
+    refused(lib.apex_embedding, lookup, 9, (D - 1, 0))
+    refused(lib.apex_embedding_backward, back, 10, (D - 1, 0))
+    p, n, t = (C.c_void_p * 2)(A, 2 * A), (C.c_uint64 * 2)(10, 20), (C.c_int * 2)(0, 1)
+    clip = [2, p, p, n, t, 1.0, A, A, None]
+    for at in (1, 3, 4, 7):
+        refused(lib.apex_clip_gradients, clip, at, (None,))
+    refused(lib.apex_clip_gradients, clip, 1, ((C.c_void_p * 2)(A, None), (C.c_void_p * 2)(A + 2, 2 * A), (C.c_void_p * 2)(A, 2 * A + 1)))
+    refused(lib.apex_clip_gradients, clip, 2, ((C.c_void_p * 2)(A, None), (C.c_void_p * 2)(A + 2, 2 * A), (C.c_void_p * 2)(A, A)))
+    refused(lib.apex_clip_gradients, clip, 3, ((C.c_uint64 * 2)(1 << 49, 1),), large)
+    refused(lib.apex_clip_gradients, clip, 4, ((C.c_int * 2)(0, 3), (C.c_int * 2)(-1, 0)))
+    refused(lib.apex_clip_gradients, clip, 5, (0.0, -1.0, nan))
+    refused(lib.apex_clip_gradients, clip, 6, (A + 2,))
+    refused(lib.apex_clip_gradients, clip, 7, (A + 128,))
+    refused(lib.apex_clip_gradients, clip, 0, ((1 << 16) + 1,), large)
+    size = C.c_size_t()
+    for entry, sizes in ((lib.apex_delta_rule_workspace_bytes, (S, T, H, Dk, Dv, 1)), (lib.apex_embedding_backward_workspace_bytes, (N, V, D)),
+                         (lib.apex_clip_gradients_workspace_bytes, (2,))):
+        assert entry(*sizes, None) == bad and entry(*sizes, C.byref(size)) == 0 and size.value % 256 == 0 and size.value > 0
