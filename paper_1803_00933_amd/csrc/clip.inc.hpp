@@ -92,9 +92,9 @@ __device__ __forceinline__ double squares(const T *x, uint64_t begin, uint64_t e
   return sum[0] + sum[1];
 }
 
-// A workgroup per piece; the last of all of them to be done sums the pieces up, in their order.  Bound by memory: 729 M elements of bf16
-// 269 us, 5.4 TB/s; 80 M 53, of which the counter is some: workgroups count themselves one after the other, 14 ns each, so there are
-// not too many (8192 pieces 70 us and 267, 2048 45 and 300).
+// A workgroup per piece; the last of all of them to be done sums the pieces up, in their order.  Many elements are bound by memory, 729 M of
+// bf16 270 us, 5.4 TB/s; fewer by the counter, at which workgroups arrive one after the other, 14 ns each: 80 M in 3259 pieces 55 us, 46 of
+// it the counter's.  So there are not too many (8192 pieces 70 us and 267, 2048 45 and 300).
 __global__ __launch_bounds__(kClipThreads) void clip_norm_kernel(ClipArgs a)
 {
   constexpr uint32_t kWaves = kClipThreads / kWave;

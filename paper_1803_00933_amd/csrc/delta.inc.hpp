@@ -219,8 +219,8 @@ __device__ __forceinline__ Operand<N> operand_of(const Tile &x, const Tile &y)
 // heads that share them, the keys and queries and their transposes, in the order in which the kernels behind take them as operands:
 // 64 lanes times 8 numbers, lane l has row l % 16 of the tile and numbers 8 (l / 16) .. + 7 of the 32.  (Rows of a strided array are far
 // apart, often in the same channel of a cache, and were asked for by every 16 columns of every head: 773 us in place of 684.)
-// Bound by what it writes, 78 KB for a piece and head in 16 bits: 223 us for 4 x 8192 steps of 16 heads, 2.9 TB/s; forwards and
-// backwards each.  M's substitution is by blocks of 16: the inverses on the diagonal by a lane per column, all else by 32-bit
+// Bound by what it writes, 78 KB for a piece and head in 16 bits: 216 us for 4 x 8192 steps of 16 heads, 3.0 TB/s, forwards, and 254
+// backwards.  M's substitution is by blocks of 16: the inverses on the diagonal by a lane per column, all else by 32-bit
 // matrix instructions, with what they leave taken as it lies (row by row for all 64, and keys by 32-bit instructions, 485 us when this was 240).
 constexpr uint32_t kOperand = 64 * 8;                         // numbers
 constexpr uint32_t kTriangle = 6;                             // operands of a triangular matrix: 4 tiles of rows by 2 of 32 steps, less 2
@@ -734,8 +734,9 @@ __device__ __forceinline__ void load_slice(Tile (&S)[2 * KS], const float *from,
 // (Numbers of 32 bits are twice as many; there a piece's are asked for at its begin.)
 // Bound by the chain from piece to piece: X, E, U and the state, 132 products of tiles and some 850 other instructions of one wave in
 // bf16, 5900 cycles, and as long again for the requests to be taken while four waves of a compute unit ask for 330 KB a piece: 4 x 8192
-// steps of 16 heads of 128 x 128 in bf16 596 us, 4.6 us a piece (without any loads and stores 163); f16, whose keys are two parts,
-// 1 x 16384 of 8 heads 914 us, 3.6 a piece (1125, with keys that were cut into parts where they were taken); f32 6.7 a piece.  With 32-bit matrix instructions, all in LDS, 52 us a piece.
+// steps of 16 heads of 128 x 128 in bf16 595 us, 4.6 us a piece (without any loads and stores 163); f16, whose keys are two parts,
+// 1 x 16384 of 8 heads 930 us, 3.6 a piece (1125, with keys that were cut into parts where they were taken); f32 6.7 a piece, with 7 registers
+// of wide states in scratch.  With 32-bit matrix instructions, all in LDS, 52 us a piece.
 template <typename T, uint32_t KS, uint32_t kSlices>
 __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(DeltaForward f, Prepared w)
 {
@@ -856,7 +857,7 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_kernel(Delta
 }
 
 // The same from the last piece to the first, with dS.  The first wave carries it, the second brings P^T dO and Q^T (c dO) and
-// stores dS, Y and dV.  Bound as the way there: 748 us, 5.8 us a piece, of 4 x 8192 steps of 16 heads of 128 x 128 in bf16.
+// stores dS, Y and dV.  Bound as the way there: 712 us, 5.6 us a piece, of 4 x 8192 steps of 16 heads of 128 x 128 in bf16.
 template <typename T, uint32_t KS, uint32_t kSlices>
 __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(DeltaBack b, Prepared w)
 {
@@ -1007,8 +1008,9 @@ __global__ __launch_bounds__(2 * kSlices * kWave) void delta_pieces_back_kernel(
 // steps, and finds U anew; then a wave has a tile of the state's rows and two or four tiles of steps, and sums over the columns.  Between the
 // two U and dV cross LDS, in parts.
 // Bound by the chain of its phases, one workgroup a compute unit: keys and state, M, 32 columns after another, B and C, their products
-// with keys and queries, a wait for memory or for all waves between any two.  4 x 8192 steps of 16 heads of 128 x 128 in bf16 1.06 ms, of
-// which its products are 0.19; with 32-bit matrix instructions 3.6.
+// with keys and queries, a wait for memory or for all waves between any two.  4 x 8192 steps of 16 heads of 128 x 128 in bf16 1.08 ms, of
+// which its products are 0.19; with 32-bit matrix instructions 3.6.  A wave has 256 registers, and what does not fit lies in scratch: of 16
+// bits and wide states 3 to 5 numbers a lane, 28 where columns are no multiple of 32 (narrow 0 and 7); of 32 bits 37 and 68 (15 and 48).
 constexpr uint32_t kGradWaves = kDeltaMaxWidth / 16, kGradNarrowWaves = 4;
 
 template <uint32_t kWaves>
@@ -1344,7 +1346,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void delta_gradients_kernel(Delt
 
 // ---- few steps: one after the other, the state in registers.  A workgroup has 64 columns of a state, a thread 8 rows of 4 of
 // them; what crosses between rows are three sums a step: k . S, q . S and q . k, so that a step has one barrier.
-// One step is bound by memory, the states read and written once: 64 sequences of 16 heads of 128 x 128 25.4 us, 5.3 TB/s.
+// One step is bound by memory, the states read and written once: 64 sequences of 16 heads of 128 x 128 30 us, 4.5 TB/s
+// (25.4 on the states of the pass before, which are in the caches in part).
 constexpr uint32_t kStepColumns = 64, kStepRows = 8;
 
 template <typename T>

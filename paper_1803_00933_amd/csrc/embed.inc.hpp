@@ -6,9 +6,15 @@ namespace apex {
 constexpr uint32_t kEmbedThreads = 256;
 constexpr uint32_t kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr uint32_t kDigitBits = 11, kDigits = 1u << kDigitBits;     // of a pass of the sort at most: two passes for any vocabulary
-constexpr uint32_t kSortAlone = 8192, kSortTile = 2048;             // tokens that one workgroup sorts by itself, and of a tile else
+// Tokens that one workgroup sorts by itself, and of a tile else (never one tile of more tokens than the first).  The gradient of V x 64 in
+// bf16, alone and in tiles: 2049 tokens of 2000 14.5 us and 20.3, of 49999 22.4 and 33.7; 8192 of 2000 21.0 and 22.3, of 49999 35.1 and 38.1.
+constexpr uint32_t kSortAlone = 8192, kSortTile = 2048;
+static_assert(kSortTile <= kSortAlone);
 constexpr uint32_t kSlice = 64, kSlice2 = kSlice * kSlice;          // sorted tokens whose rows are summed up ahead, if they are one
-constexpr uint32_t kSlice2From = 16384;                             // ... in two steps from so many tokens on (one launch more: 5 us)
+// ... in two steps from so many tokens on.  The gradient of 32000 x 1024 in bf16, in one step and in two: 8192 tokens 77 us and 47 where all
+// are one token, 72 and 73 where half are, 53.9 and 55.5 where a token is as frequent as one over its rank; 16384 125 and 53, 97 and 88, 59.7
+// and 61.2; 32768 217 and 59, 154 and 107, 78.3 and 80.4.
+constexpr uint32_t kSlice2From = 16384;
 
 struct EmbedArgs {
   uint32_t N, V, D;
@@ -22,8 +28,8 @@ struct EmbedArgs {
 };
 
 // Rows of `lanes` lanes each; a token outside the table has a row of zeros.
-// Bound by memory: every row is read where it is named and written once.  32768 rows of 2048 in bf16 30.5 us, 4.4 TB/s written and as
-// much read, in part from the caches; 64 rows of 1024 2.2.
+// Bound by memory: every row is read where it is named and written once.  32768 rows of 2048 in bf16 42 us, 3.2 TB/s written and as
+// much read, in part from the caches (30.5 on the rows of the pass before); 64 rows of 1024 2.2.
 template <typename T>
 __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs a)
 {
@@ -212,7 +218,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a)
   sort_pass<false>(a, count, base, nullptr, false);
 }
 
-// Both passes by one workgroup: 6144 tokens of 32768 15.6 us, 7777 of 49999 22; groups of a wave one after the other, and LDS.  In tiles
+// Both passes by one workgroup: 6144 tokens of 32768 15.2 us, 7777 of 49999 21; groups of a wave one after the other, and LDS.  In tiles
 // of 2048 by as many workgroups, three launches a pass, 32768 tokens of 131072 take 31.
 __global__ __launch_bounds__(kSortThreads) void sort_alone_kernel(SortArgs first, SortArgs second)
 {
@@ -328,9 +334,10 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_slices2_kernel(EmbedBackA
   a.slice2[(uint64_t)s * a.D + at] = sum;
 }
 
-// A wave per row of the table and piece of it.  Bound by memory: the table's gradient is written once (zeros where a token is not
-// named), the rows that name it are read once.  131072 x 2048 in bf16 with 32768 places 103 us, 5.2 TB/s written.  (Eight rows on their
-// way instead of four, or four slices, cost registers and waves: 121 and 126.)
+// A wave per row of the table and piece of it: the table's gradient is written once (zeros where a token is not named), the rows that name
+// it are read once.  131072 x 2048 in bf16 with 32768 places 190 us, 3.5 TB/s read and written; with none 80, 6.7 TB/s: bound by a named row's
+// loads, which come one behind the other (where it begins, its key, where it ends, its places, their rows).  On the inputs of the pass before
+// 103, and eight rows on their way instead of four, or four slices, which cost registers and waves, 121 and 126.
 template <typename T>
 __global__ __launch_bounds__(kEmbedThreads) void embed_rows_kernel(EmbedBackArgs a)
 {
